@@ -319,6 +319,144 @@ pd_status pd_sample_picard(const pd_schedule* s, const pd_denoiser* d, int32_t p
                            int32_t ndim, float* x_out, pd_sample_stats* stats, pd_workspace* ws,
                            void* stream);
 
+/* ------------------------------------------------------------------ transformer operators
+ * For denoisers that mix positions (a policy over an action sequence, a latent
+ * in patches, a history of observations): the parts of a transformer block
+ * around its matrix products, forward and backward.  Everything is device
+ * memory of the current device, and every call only enqueues kernels on
+ * `stream`: no allocation, no synchronisation, no memset, so calls can be
+ * captured in a HIP graph.  Results do not depend on the launch: no atomics,
+ * the same inputs give the same bits.  Strides count elements, not bytes, may
+ * be any (>= 0), and rows need no alignment beyond their element's; the last
+ * dimension is contiguous.  Outputs must not overlap inputs or each other
+ * except where a call says so.  dtype is PD_F32 or PD_BF16; sums, statistics
+ * and exponentials are float32 and each result is rounded once.
+ * `scratch` is device memory of the caller, 16-byte aligned, of at least the bytes the
+ * matching *_scratch call gives (0: may be NULL); it holds nothing between calls. */
+#define PD_F8E4M3 2            /* OCP e4m3 (no infinities, largest 448), outputs only */
+
+/* Root-mean-square norm with the residual's addition.  Per row of `width`:
+ *   s = x + residual (float32, not rounded),  rstd = 1 / sqrt(mean(s^2) + eps),
+ *   sum = s rounded to dtype,  y = s rstd weight rounded to out_dtype.
+ * out_dtype PD_F8E4M3: the row's consecutive groups of `group` values (the
+ * last may be shorter; group 0 = the whole row) have one scale each,
+ * scale = max|y| / 448, and y holds y / scale.  A group whose scale would be
+ * below 2^-126 is stored as zeros with scale 0; one that holds an infinity or
+ * NaN gets a scale that is not finite.
+ * residual, sum, rstd may be NULL (no addition; not stored).  sum and y may be
+ * x or residual themselves, with the same stride and type.
+ * 1 <= width <= 65536; group 0 or a power of two from 16 to 512.
+ * scale: float [rows][ceil(width / group)]; rstd: float [rows]; weight: float [width].
+ * Backward, with sum and rstd as the forward pass left them, n = sum rstd:
+ *   a = dy weight,  dx = dsum + rstd (a - n mean(a n)),  dweight = sum over rows of dy n.
+ * dx is the gradient of x and of residual alike; dsum (NULL: 0) is the gradient
+ * that reaches `sum` from elsewhere.  dx may be dy or dsum (same stride).
+ * dweight: float [width], or NULL.  Strides: dy as y, dsum as residual, dx as x. */
+typedef struct pd_rmsnorm_desc {
+    int64_t rows;
+    int64_t width;
+    int64_t x_stride, residual_stride, sum_stride, y_stride;   /* from row to row */
+    int32_t dtype;             /* of x, residual, sum (backward: also dy, dsum, dx) */
+    int32_t out_dtype;         /* dtype or PD_F8E4M3 (backward: dtype)               */
+    int32_t group;
+    float eps;                 /* >= 0 */
+} pd_rmsnorm_desc;
+pd_status pd_rmsnorm_forward(const pd_rmsnorm_desc* desc, const void* x, const void* residual,
+                             const float* weight, void* sum, void* y, float* scale, float* rstd,
+                             void* stream);
+pd_status pd_rmsnorm_backward_scratch(const pd_rmsnorm_desc* desc, int64_t* bytes);
+pd_status pd_rmsnorm_backward(const pd_rmsnorm_desc* desc, const void* dy, const void* sum,
+                              const float* weight, const float* rstd, const void* dsum, void* dx,
+                              float* dweight, void* scratch, int64_t scratch_bytes, void* stream);
+
+/* Rotary positions: of each head's first `rotary_dim` dimensions, pair k
+ * (dimensions k and k + rotary_dim/2 with PD_ROTARY_HALF, 2k and 2k + 1 with
+ * PD_ROTARY_INTERLEAVED) turns by position * f_k:
+ *   (a, b) -> (a cos - b sin, a sin + b cos); the other dimensions are copied.
+ * pd_rotary_table fills rows [first, first + rows) of a table of (cos, sin), formed in
+ * double and rounded once: float [rows][rotary_dim/2][2], f_k = base^(-2k/rotary_dim),
+ * changed for contexts longer than the trained original_length by
+ *   PD_ROTARY_LINEAR    f / factor;
+ *   PD_ROTARY_BASE      base -> base factor^(rotary_dim/(rotary_dim-2));
+ *   PD_ROTARY_BY_PARTS  g f + (1-g) f / factor, with g going from 0 to 1 as the
+ *                       turns original_length f/2pi go from turns_low to turns_high.
+ * Both cos and sin are multiplied by magnitude.
+ * pd_rotary_apply turns q and k (k may be NULL) by the table's rows at
+ * positions[b * position_stride + i] (position_stride 0: all sequences share
+ * them; a position outside [0, table_rows) is clamped to it).  backward != 0
+ * turns the other way, which is the gradient's map.  q_out may be q and k_out
+ * may be k, with the same strides. */
+#define PD_ROTARY_HALF 0
+#define PD_ROTARY_INTERLEAVED 1
+#define PD_ROTARY_PLAIN 0
+#define PD_ROTARY_LINEAR 1
+#define PD_ROTARY_BASE 2
+#define PD_ROTARY_BY_PARTS 3
+typedef struct pd_rotary_table_desc {
+    int32_t rotary_dim;        /* even, 2..1024                                  */
+    int32_t scaling;           /* PD_ROTARY_PLAIN, ...                           */
+    double base;               /* > 1                                            */
+    double factor;             /* >= 1; not used by PLAIN                        */
+    double original_length;    /* BY_PARTS: > 0                                  */
+    double turns_low, turns_high;   /* BY_PARTS: 0 <= low < high                 */
+    double magnitude;          /* finite; 1 = none                               */
+} pd_rotary_table_desc;
+pd_status pd_rotary_table(const pd_rotary_table_desc* desc, int64_t first, int64_t rows, float* table,
+                          void* stream);
+typedef struct pd_rotary_desc {
+    int64_t batch, length;
+    int32_t heads_q, heads_k;
+    int32_t head_dim, rotary_dim;      /* head_dim <= 1024, rotary_dim even and <= head_dim */
+    int32_t layout;                    /* PD_ROTARY_HALF or PD_ROTARY_INTERLEAVED */
+    int32_t dtype;
+    int32_t backward;
+    int64_t table_rows;
+    int64_t position_stride;
+    int64_t q_stride[3], k_stride[3], q_out_stride[3], k_out_stride[3];   /* batch, token, head */
+} pd_rotary_desc;
+pd_status pd_rotary_apply(const pd_rotary_desc* desc, const void* q, const void* k,
+                          const int32_t* positions, const float* table, void* q_out, void* k_out,
+                          void* stream);
+
+/* Attention with a sliding window and sinks.  Sequence b has n_b = q_lens[b]
+ * queries and m_b = kv_lens[b] keys (device int32, clamped to [0, q_len] and
+ * [0, kv_len]; NULL: all have q_len, kv_len).  Query i < n_b sits at position
+ * t = m_b - n_b + i, so that the last query is at the last key, and sees key
+ * j < m_b when
+ *   causal:     j <= t and (t - j < window or j < sinks),
+ *   otherwise:  |t - j| < window or j < sinks;   window 0: no limit.
+ * out_i = sum_j p_j v_j, p = softmax of scale q_i k_j over the keys seen;
+ * lse_i = log sum_j exp(scale q_i k_j).  A query that sees no key, and the
+ * rows i >= n_b, have out 0 and lse -inf.  What lies in keys and values that a
+ * query does not see (NaN included) does not reach its row.
+ * Query head h reads key head h / (heads_q / heads_kv).
+ * scale: of the scores, finite.  lse: float [batch][heads_q][q_len], or NULL.
+ * In PD_BF16 the probabilities (and in the backward pass the scores'
+ * gradients) are rounded to bfloat16 as operands of the matrix cores, the
+ * products' sums are float32.
+ * Backward: dq, dk, dv from out, lse (forward) and dout, all keys' gradients
+ * written (0 for those that no query sees).  Sums over a group's query heads
+ * are float32, rounded once.
+ * head_dim 1..128 (more: PD_ERR_UNSUPPORTED); heads_q a multiple of heads_kv. */
+typedef struct pd_attention_desc {
+    int32_t batch, heads_q, heads_kv, head_dim;
+    int32_t q_len, kv_len;
+    int32_t dtype, causal;
+    int32_t window, sinks;
+    float scale;
+    int64_t q_stride[3], k_stride[3], v_stride[3], out_stride[3];           /* batch, token, head */
+    int64_t dq_stride[3], dk_stride[3], dv_stride[3], dout_stride[3];       /* backward only */
+} pd_attention_desc;
+pd_status pd_attention_forward_scratch(const pd_attention_desc* desc, int64_t* bytes);
+pd_status pd_attention_forward(const pd_attention_desc* desc, const void* q, const void* k, const void* v,
+                               const int32_t* q_lens, const int32_t* kv_lens, void* out, float* lse,
+                               void* scratch, int64_t scratch_bytes, void* stream);
+pd_status pd_attention_backward_scratch(const pd_attention_desc* desc, int64_t* bytes);
+pd_status pd_attention_backward(const pd_attention_desc* desc, const void* q, const void* k, const void* v,
+                                const void* out, const float* lse, const void* dout,
+                                const int32_t* q_lens, const int32_t* kv_lens, void* dq, void* dk,
+                                void* dv, void* scratch, int64_t scratch_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -25,6 +25,10 @@ __all__ = [
     "PD_DDPM", "PD_DDIM", "PD_DDIM_HEUN", "PD_DDIM_DPM2M", "PD_STOP_RELAXED", "PD_STOP_PROP2",
     "PD_MODEL_GMM2D", "PD_MODEL_MLP", "PD_MODEL_CONV1X1",
     "PD_F32", "PD_BF16", "EXPORTED_SYMBOLS",
+    "pd_rmsnorm_forward", "pd_rmsnorm_backward", "pd_rotary_table", "pd_rotary_apply",
+    "pd_attention_forward", "pd_attention_backward",
+    "PD_F8E4M3", "PD_ROTARY_HALF", "PD_ROTARY_INTERLEAVED",
+    "PD_ROTARY_PLAIN", "PD_ROTARY_LINEAR", "PD_ROTARY_BASE", "PD_ROTARY_BY_PARTS",
 ]
 
 PD_OK, PD_ERR_INVALID_ARG, PD_ERR_OOM, PD_ERR_DEVICE, PD_ERR_NUMERIC, PD_ERR_UNSUPPORTED = range(6)
@@ -34,7 +38,9 @@ PD_DDPM, PD_DDIM, PD_DDIM_HEUN, PD_DDIM_DPM2M = 0, 1, 2, 3
 PD_STOP_RELAXED, PD_STOP_PROP2 = 0, 1
 STOP_RULES = {"relaxed": PD_STOP_RELAXED, "prop2": PD_STOP_PROP2}
 PD_MODEL_GMM2D, PD_MODEL_MLP, PD_MODEL_CONV1X1 = 0, 1, 2
-PD_F32, PD_BF16 = 0, 1
+PD_F32, PD_BF16, PD_F8E4M3 = 0, 1, 2
+PD_ROTARY_HALF, PD_ROTARY_INTERLEAVED = 0, 1
+PD_ROTARY_PLAIN, PD_ROTARY_LINEAR, PD_ROTARY_BASE, PD_ROTARY_BY_PARTS = 0, 1, 2, 3
 
 EXPORTED_SYMBOLS = [
     "pd_last_error", "pd_version", "pd_init_schedule", "pd_destroy_schedule",
@@ -42,6 +48,10 @@ EXPORTED_SYMBOLS = [
     "pd_denoiser_forward", "pd_denoiser_forward_static",
     "pd_normals", "pd_workspace_create", "pd_workspace_destroy", "pd_sample_sequential",
     "pd_sample_picard",
+    "pd_rmsnorm_forward", "pd_rmsnorm_backward_scratch", "pd_rmsnorm_backward",
+    "pd_rotary_table", "pd_rotary_apply",
+    "pd_attention_forward_scratch", "pd_attention_forward",
+    "pd_attention_backward_scratch", "pd_attention_backward",
 ]
 
 
@@ -72,6 +82,43 @@ class _Stats(ctypes.Structure):
                 ("update_launches", ctypes.c_int32), ("finalize_launches", ctypes.c_int32),
                 ("denoiser_ms", ctypes.c_double), ("update_ms", ctypes.c_double),
                 ("finalize_ms", ctypes.c_double)]
+
+
+_I64x3 = ctypes.c_int64 * 3
+
+
+class _RmsnormDesc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("width", ctypes.c_int64), ("x_stride", ctypes.c_int64),
+                ("residual_stride", ctypes.c_int64), ("sum_stride", ctypes.c_int64),
+                ("y_stride", ctypes.c_int64), ("dtype", ctypes.c_int32),
+                ("out_dtype", ctypes.c_int32), ("group", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+
+class _RotaryTableDesc(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("scaling", ctypes.c_int32),
+                ("base", ctypes.c_double), ("factor", ctypes.c_double),
+                ("original_length", ctypes.c_double), ("turns_low", ctypes.c_double),
+                ("turns_high", ctypes.c_double), ("magnitude", ctypes.c_double)]
+
+
+class _RotaryDesc(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int64), ("length", ctypes.c_int64), ("heads_q", ctypes.c_int32),
+                ("heads_k", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("rotary_dim", ctypes.c_int32), ("layout", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("backward", ctypes.c_int32),
+                ("table_rows", ctypes.c_int64), ("position_stride", ctypes.c_int64),
+                ("q_stride", _I64x3), ("k_stride", _I64x3), ("q_out_stride", _I64x3),
+                ("k_out_stride", _I64x3)]
+
+
+class _AttentionDesc(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("heads_q", ctypes.c_int32), ("heads_kv", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("q_len", ctypes.c_int32), ("kv_len", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("causal", ctypes.c_int32), ("window", ctypes.c_int32),
+                ("sinks", ctypes.c_int32), ("scale", ctypes.c_float), ("q_stride", _I64x3),
+                ("k_stride", _I64x3), ("v_stride", _I64x3), ("out_stride", _I64x3),
+                ("dq_stride", _I64x3), ("dk_stride", _I64x3), ("dv_stride", _I64x3),
+                ("dout_stride", _I64x3)]
 
 
 _LIB: Optional[ctypes.CDLL] = None
@@ -109,6 +156,15 @@ def load() -> ctypes.CDLL:
         "pd_workspace_destroy": ([vp], None),
         "pd_sample_sequential": ([vp, vp, u64, i32, P(i64), i32, vp, P(_Stats), vp, vp], i32),
         "pd_sample_picard": ([vp, vp, i32, f32, u64, i32, P(i64), i32, vp, P(_Stats), vp, vp], i32),
+        "pd_rmsnorm_forward": ([P(_RmsnormDesc)] + [vp] * 8, i32),
+        "pd_rmsnorm_backward_scratch": ([P(_RmsnormDesc), P(i64)], i32),
+        "pd_rmsnorm_backward": ([P(_RmsnormDesc)] + [vp] * 8 + [i64, vp], i32),
+        "pd_rotary_table": ([P(_RotaryTableDesc), i64, i64, vp, vp], i32),
+        "pd_rotary_apply": ([P(_RotaryDesc)] + [vp] * 7, i32),
+        "pd_attention_forward_scratch": ([P(_AttentionDesc), P(i64)], i32),
+        "pd_attention_forward": ([P(_AttentionDesc)] + [vp] * 8 + [i64, vp], i32),
+        "pd_attention_backward_scratch": ([P(_AttentionDesc), P(i64)], i32),
+        "pd_attention_backward": ([P(_AttentionDesc)] + [vp] * 12 + [i64, vp], i32),
     }
     for name, (args, res) in sig.items():
         fn = getattr(L, name)
@@ -325,6 +381,252 @@ def pd_sample_picard(sched: Schedule, den: Denoiser, p: int, tau: float, noise_s
                                    shp, nd, _ptr(x_out), ctypes.byref(st),
                                    workspace.handle if workspace else None, _stream(stream)))
     return _out_stats(st, buf)
+
+
+# ------------------------------------------------------------ transformer operators
+_DTYPES = {torch.float32: PD_F32, torch.bfloat16: PD_BF16}
+
+
+def _dtype(t: torch.Tensor) -> int:
+    d = _DTYPES.get(t.dtype)
+    if d is None:
+        raise ValueError(f"float32 or bfloat16 is needed, got {t.dtype}")
+    return d
+
+
+def _on_gpu(*tensors) -> None:
+    dev = torch.cuda.current_device() if torch.cuda.is_available() else -1
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.device.index != dev):
+            raise ValueError("tensors must be on the current GPU")
+
+
+def _rows_of(t: torch.Tensor, shape, dtype, what: str) -> int:
+    """Elements from row to row of a tensor seen as rows of its last dimension."""
+    if t.dtype != dtype or t.shape != shape:
+        raise ValueError(f"{what} must be {dtype} of shape {tuple(shape)}")
+    if t.is_contiguous():
+        return shape[-1]
+    if t.stride(-1) != 1 and shape[-1] > 1:
+        raise ValueError(f"{what}: the last dimension must be contiguous")
+    if t.dim() != 2:
+        try:
+            t = t.view(-1, shape[-1])
+        except RuntimeError:
+            raise ValueError(f"{what}: rows must lie at one stride") from None
+    return t.stride(0)
+
+
+def _dense(t: Optional[torch.Tensor], shape, dtype, what: str):
+    if t is not None and (t.dtype != dtype or t.shape != shape or not t.is_contiguous()):
+        raise ValueError(f"{what} must be contiguous {dtype} of shape {tuple(shape)}")
+
+
+def _strides(t: torch.Tensor, shape, dtype, what: str):
+    """Strides of a [batch, token, head, dim] tensor."""
+    if t.dtype != dtype or t.shape != shape:
+        raise ValueError(f"{what} must be {dtype} of shape {tuple(shape)}")
+    s = t.stride()
+    if s[3] != 1 and shape[3] > 1:
+        raise ValueError(f"{what}: the last dimension must be contiguous")
+    return _I64x3(s[0], s[1], s[2])
+
+
+def _written(t: torch.Tensor, what: str) -> None:
+    """An output whose elements share memory (an expanded view) has no result."""
+    for n, s in zip(t.shape, t.stride()):
+        if s == 0 and n > 1:
+            raise ValueError(f"{what} is an output and must not be an expanded view")
+
+
+def _scratch(given: Optional[torch.Tensor], need: int, stream):
+    """The caller's scratch, or one from torch's allocator that belongs to the call's stream."""
+    if given is not None:
+        if not given.is_contiguous():
+            raise ValueError("scratch must be contiguous")
+        return given, given.numel() * given.element_size()
+    if not need:
+        return None, 0
+    if stream is None:
+        return torch.empty(need, dtype=torch.uint8, device="cuda"), need
+    s = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream))
+    with torch.cuda.stream(s):
+        return torch.empty(need, dtype=torch.uint8, device="cuda"), need
+
+
+def pd_rmsnorm_forward(x: torch.Tensor, weight: torch.Tensor, y: torch.Tensor,
+                       residual: Optional[torch.Tensor] = None,
+                       sum_out: Optional[torch.Tensor] = None,
+                       scale: Optional[torch.Tensor] = None,
+                       rstd: Optional[torch.Tensor] = None, eps: float = 1e-6, group: int = 0,
+                       stream=None) -> None:
+    """y = norm(x + residual) * weight over the last dimension; y of x's type, or float8_e4m3fn
+    with `scale` [rows, ceil(width / group)] (group 0: one a row).  sum_out: x + residual."""
+    dt, sh = _dtype(x), x.shape
+    _on_gpu(x, weight, y, residual, sum_out, scale, rstd)
+    width = sh[-1] if x.dim() else 0
+    if not width:
+        raise ValueError("x must have a last dimension of at least 1")
+    rows = x.numel() // width
+    f8 = y.dtype == torch.float8_e4m3fn
+    _dense(weight, (width,), torch.float32, "weight")
+    if f8:
+        if scale is None:
+            raise ValueError("an output in 8 bits needs scale")
+        per = -(-width // group) if group > 0 else 1
+        if scale.dtype != torch.float32 or not scale.is_contiguous() or scale.numel() != rows * per:
+            raise ValueError(f"scale must be contiguous float32 of {rows} x {per} elements")
+    if rstd is not None and (rstd.dtype != torch.float32 or not rstd.is_contiguous() or rstd.numel() != rows):
+        raise ValueError(f"rstd must be contiguous float32 of {rows} elements")
+    for t in (y, sum_out):
+        if t is not None:
+            _written(t, "y or sum_out")
+    d = _RmsnormDesc(rows, width, _rows_of(x, sh, x.dtype, "x"),
+                     _rows_of(residual, sh, x.dtype, "residual") if residual is not None else 0,
+                     _rows_of(sum_out, sh, x.dtype, "sum_out") if sum_out is not None else 0,
+                     _rows_of(y, sh, y.dtype if f8 else x.dtype, "y"),
+                     dt, PD_F8E4M3 if f8 else dt, group, eps)
+    _check(load().pd_rmsnorm_forward(ctypes.byref(d), _ptr(x), _ptr(residual), _ptr(weight),
+                                     _ptr(sum_out), _ptr(y), _ptr(scale), _ptr(rstd), _stream(stream)))
+
+
+def pd_rmsnorm_backward(dy: torch.Tensor, sum_in: torch.Tensor, weight: torch.Tensor,
+                        rstd: torch.Tensor, dx: torch.Tensor,
+                        dweight: Optional[torch.Tensor] = None,
+                        dsum: Optional[torch.Tensor] = None,
+                        scratch: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Gradients of pd_rmsnorm_forward from its sum_out (sum_in) and rstd: dx (of x and of
+    residual) and dweight.  dsum: the gradient that reaches sum_out from elsewhere."""
+    dt, sh = _dtype(dy), dy.shape
+    _on_gpu(dy, sum_in, weight, rstd, dx, dweight, dsum, scratch)
+    width = sh[-1] if dy.dim() else 0
+    if not width:
+        raise ValueError("dy must have a last dimension of at least 1")
+    rows = dy.numel() // width
+    _dense(weight, (width,), torch.float32, "weight")
+    _dense(dweight, (width,), torch.float32, "dweight")
+    if rstd.dtype != torch.float32 or not rstd.is_contiguous() or rstd.numel() != rows:
+        raise ValueError(f"rstd must be contiguous float32 of {rows} elements")
+    _written(dx, "dx")
+    d = _RmsnormDesc(rows, width, _rows_of(dx, sh, dy.dtype, "dx"),
+                     _rows_of(dsum, sh, dy.dtype, "dsum") if dsum is not None else 0,
+                     _rows_of(sum_in, sh, dy.dtype, "sum_in"), _rows_of(dy, sh, dy.dtype, "dy"),
+                     dt, dt, 0, 0.0)
+    L, need = load(), ctypes.c_int64(0)
+    if dweight is not None:
+        _check(L.pd_rmsnorm_backward_scratch(ctypes.byref(d), ctypes.byref(need)))
+    buf, have = _scratch(scratch, need.value, stream)
+    _check(L.pd_rmsnorm_backward(ctypes.byref(d), _ptr(dy), _ptr(sum_in), _ptr(weight), _ptr(rstd),
+                                 _ptr(dsum), _ptr(dx), _ptr(dweight), _ptr(buf), have, _stream(stream)))
+
+
+def pd_rotary_table(table: torch.Tensor, base: float = 10000.0, scaling: int = PD_ROTARY_PLAIN,
+                    factor: float = 1.0, original_length: float = 0.0, turns_low: float = 1.0,
+                    turns_high: float = 32.0, magnitude: float = 1.0, first: int = 0,
+                    stream=None) -> None:
+    """Fill table [positions, rotary_dim / 2, 2] with cos and sin from position `first` on."""
+    _on_gpu(table)
+    if table.dtype != torch.float32 or table.dim() != 3 or table.shape[2] != 2 or not table.is_contiguous():
+        raise ValueError("table must be contiguous float32 of shape (positions, rotary_dim / 2, 2)")
+    d = _RotaryTableDesc(2 * table.shape[1], scaling, base, factor, original_length, turns_low,
+                         turns_high, magnitude)
+    _check(load().pd_rotary_table(ctypes.byref(d), first, table.shape[0], _ptr(table), _stream(stream)))
+
+
+_NO_STRIDES = _I64x3(0, 0, 0)
+
+
+def pd_rotary_apply(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Tensor,
+                    table: torch.Tensor, q_out: torch.Tensor, k_out: Optional[torch.Tensor] = None,
+                    layout: int = PD_ROTARY_HALF, backward: bool = False, stream=None) -> None:
+    """Turn q and k [batch, token, head, dim] by the table's rows at positions ([token] or
+    [batch, token], int32); q_out may be q, k_out may be k."""
+    dt = _dtype(q)
+    _on_gpu(q, k, positions, table, q_out, k_out)
+    if q.dim() != 4 or (k is None) != (k_out is None):
+        raise ValueError("q must be (batch, token, head, dim), and k_out goes with k")
+    B, n, H, D = q.shape
+    if table.dtype != torch.float32 or table.dim() != 3 or table.shape[2] != 2 or not table.is_contiguous():
+        raise ValueError("table must be contiguous float32 of shape (positions, rotary_dim / 2, 2)")
+    shape = tuple(positions.shape)
+    if positions.dtype != torch.int32 or shape not in ((n,), (B, n)) or (n > 1 and positions.stride(-1) != 1):
+        raise ValueError("positions must be int32 of shape (token,) or (batch, token), tokens contiguous")
+    K = 0
+    if k is not None:
+        if k.dim() != 4:
+            raise ValueError("k must be (batch, token, head, dim)")
+        K = k.shape[2]
+        _written(k_out, "k_out")
+    _written(q_out, "q_out")
+    ks = (B, n, K, D)
+    d = _RotaryDesc(B, n, H, K, D, 2 * table.shape[1], layout, dt, int(backward), table.shape[0],
+                    positions.stride(0) if len(shape) == 2 else 0,
+                    _strides(q, q.shape, q.dtype, "q"),
+                    _strides(k, ks, q.dtype, "k") if K else _NO_STRIDES,
+                    _strides(q_out, q.shape, q.dtype, "q_out"),
+                    _strides(k_out, ks, q.dtype, "k_out") if K else _NO_STRIDES)
+    _check(load().pd_rotary_apply(ctypes.byref(d), _ptr(q), _ptr(k), _ptr(positions), _ptr(table),
+                                  _ptr(q_out), _ptr(k_out), _stream(stream)))
+
+
+def _attention(q, k, v, out, lse, causal, window, sinks, scale, q_lens, kv_lens):
+    dt = _dtype(q)
+    if q.dim() != 4 or k.dim() != 4:
+        raise ValueError("q and k must be (batch, token, head, dim)")
+    B, n, H, D = q.shape
+    ks = (B, k.shape[1], k.shape[2], D)
+    _written(out, "out")
+    if lse is not None and (lse.dtype != torch.float32 or lse.shape != (B, H, n) or not lse.is_contiguous()):
+        raise ValueError(f"lse must be contiguous float32 of shape {(B, H, n)}")
+    for t, what in ((q_lens, "q_lens"), (kv_lens, "kv_lens")):
+        if t is not None and (t.dtype != torch.int32 or t.shape != (B,) or not t.is_contiguous()):
+            raise ValueError(f"{what} must be contiguous int32 of shape {(B,)}")
+    return _AttentionDesc(B, H, ks[2], D, n, ks[1], dt, int(causal), min(window, 0x7fffffff),
+                          min(sinks, 0x7fffffff), D ** -0.5 if scale is None else scale,
+                          _strides(q, q.shape, q.dtype, "q"), _strides(k, ks, q.dtype, "k"),
+                          _strides(v, ks, q.dtype, "v"), _strides(out, q.shape, q.dtype, "out"))
+
+
+def pd_attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor,
+                         lse: Optional[torch.Tensor] = None, causal: bool = True, window: int = 0,
+                         sinks: int = 0, scale: Optional[float] = None,
+                         q_lens: Optional[torch.Tensor] = None,
+                         kv_lens: Optional[torch.Tensor] = None,
+                         scratch: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Attention of q on k, v, all [batch, token, head, dim] at any strides (a head-major cache is
+    a transposed view); lse float32 [batch, head, token]; scale: default dim ** -0.5."""
+    _on_gpu(q, k, v, out, lse, q_lens, kv_lens, scratch)
+    d = _attention(q, k, v, out, lse, causal, window, sinks, scale, q_lens, kv_lens)
+    L, need = load(), ctypes.c_int64(0)
+    if scratch is None:
+        _check(L.pd_attention_forward_scratch(ctypes.byref(d), ctypes.byref(need)))
+    buf, have = _scratch(scratch, need.value, stream)
+    _check(L.pd_attention_forward(ctypes.byref(d), _ptr(q), _ptr(k), _ptr(v), _ptr(q_lens),
+                                  _ptr(kv_lens), _ptr(out), _ptr(lse), _ptr(buf), have,
+                                  _stream(stream)))
+
+
+def pd_attention_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor,
+                          lse: torch.Tensor, dout: torch.Tensor, dq: torch.Tensor,
+                          dk: torch.Tensor, dv: torch.Tensor, causal: bool = True, window: int = 0,
+                          sinks: int = 0, scale: Optional[float] = None,
+                          q_lens: Optional[torch.Tensor] = None,
+                          kv_lens: Optional[torch.Tensor] = None,
+                          scratch: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Gradients dq, dk, dv of pd_attention_forward, from its out and lse and the gradient dout."""
+    _on_gpu(q, k, v, out, lse, dout, dq, dk, dv, q_lens, kv_lens, scratch)
+    d = _attention(q, k, v, out, lse, causal, window, sinks, scale, q_lens, kv_lens)
+    for t, like, what in ((dq, q, "dq"), (dk, k, "dk"), (dv, v, "dv"), (dout, q, "dout")):
+        if t is not dout:
+            _written(t, what)
+        setattr(d, what + "_stride", _strides(t, like.shape, q.dtype, what))
+    L, need = load(), ctypes.c_int64(0)
+    if scratch is None:
+        _check(L.pd_attention_backward_scratch(ctypes.byref(d), ctypes.byref(need)))
+    buf, have = _scratch(scratch, need.value, stream)
+    _check(L.pd_attention_backward(ctypes.byref(d), _ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(lse),
+                                   _ptr(dout), _ptr(q_lens), _ptr(kv_lens), _ptr(dq), _ptr(dk),
+                                   _ptr(dv), _ptr(buf), have, _stream(stream)))
 
 
 # ------------------------------------------------------------ workload helpers

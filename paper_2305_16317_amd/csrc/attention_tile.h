@@ -1,0 +1,173 @@
+// Tiles, operands and masks shared by the attention kernels (attention.hip,
+// attention_grad.hip).
+//
+// Matrix products run as 32 x 32 tiles.  An operand fragment holds eight values a
+// lane: lane l has row (A) or column (B) l % 32 and, of a step of 16 along the
+// summed dimension, the eight from 8 (l / 32).  bfloat16 takes one 32x32x16
+// instruction a step, float32 eight 32x32x2 ones.  The result's lane has column
+// l % 32 and in register r row tile_row(l, r).
+//
+// So the scores are formed transposed (keys are rows, queries columns): a lane
+// then holds scores of one query, and, read as a fragment, its registers 8c..8c+7
+// are the eight values of step c of the next product's B operand, with the keys in
+// the order tile_row gives.  Sums do not care for the order, so the other operand
+// is read in the same one and probabilities never leave their registers.
+#pragma once
+
+#include "ops.h"
+
+namespace pd {
+namespace attn {
+
+constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
+
+// The hardware's base-2 exponential (1 ulp; results under 2^-126 are 0, which
+// beside the row's largest term, 1, is below float32's rounding).
+__device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// A row's log of its sum, from the largest unscaled score, the scale and the sum of
+// 2^(scores over the largest): the product is rounded as the backward pass rounds
+// a score, so that a row with one large score finds p = 1 there.
+__device__ inline float log_sum(float top, float scale, float total) {
+    return total == 0.f ? -INFINITY : top * scale + log2f(total) * kLn2;
+}
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4_u __attribute__((ext_vector_type(4), aligned(4)));
+typedef bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef bf16x4 bf16x4_u __attribute__((aligned(2)));
+
+template <typename T>
+using Frag = typename Vec8<T>::type;
+
+__device__ inline f32x16 mma(bf16x8 a, bf16x8 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ inline f32x16 mma(f32x8 a, f32x8 b, f32x16 c) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], c, 0, 0, 0);
+    return c;
+}
+__device__ inline int tile_row(int lane, int r) { return 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3); }
+
+// registers 8c..8c+7 of a result as the next product's operand
+template <typename T>
+__device__ inline Frag<T> as_frag(const f32x16& v, int c) {
+    f32x8 f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = v[8 * c + e];
+    return narrow<T>(f);
+}
+
+// A tile of rows in LDS: 16-byte units, those of row r exchanged by swz(r), so
+// that both ways of reading (eight rows at one unit; four rows at two
+// neighbouring units) meet every bank once.
+template <typename T, int DP>
+struct Tile {
+    static constexpr int kPitch = (DP * (int)sizeof(T) + 127) / 128 * 128;   // bytes a row
+    static constexpr int kUnits = DP * (int)sizeof(T) / 16;                  // units a row that hold values
+    static __device__ inline int swz(int row) { return ((row & 3) << 1) | ((row >> 2) & 1); }
+    static __device__ inline int at(int row, int unit) { return row * kPitch + ((unit ^ swz(row)) << 4); }
+    // rows row0 .. row0 + 31 of the tile as a fragment, step c of its 16-wide steps
+    static __device__ inline Frag<T> rows(const char* lds, int row0, int c, int lane) {
+        const int row = row0 + (lane & 31), h = lane >> 5;
+        if constexpr (sizeof(T) == 2) {
+            return *reinterpret_cast<const Frag<T>*>(lds + at(row, 2 * c + h));
+        } else {
+            const f32x4 a = *reinterpret_cast<const f32x4*>(lds + at(row, 4 * c + 2 * h));
+            const f32x4 b = *reinterpret_cast<const f32x4*>(lds + at(row, 4 * c + 2 * h + 1));
+            return Frag<T>{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+        }
+    }
+    // columns 32 dt .. 32 dt + 31 as the rows of a fragment, the tile's rows row0 .. row0
+    // + 15 as its step, in the order of as_frag
+    static __device__ inline Frag<T> cols(const char* lds, int row0, int dt, int lane) {
+        const int h = lane >> 5;
+        if constexpr (sizeof(T) == 2) {
+            // the transposing read: of 16 lanes, 4j .. 4j + 3 point at 16 values of row j, and
+            // lane i receives column i of the four rows
+            const int i = lane & 15, row = row0 + 4 * h + (i >> 2);
+            const int unit = 4 * dt + 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
+            const char* p = lds + at(row, unit) + 8 * (i & 1);
+            typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+            const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p));
+            const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 8 * kPitch));
+            typedef short s16x8 __attribute__((ext_vector_type(8)));
+            return __builtin_bit_cast(Frag<T>, s16x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]});
+        } else {
+            Frag<T> f;
+            const int d = 32 * dt + (lane & 31);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int row = row0 + 8 * (e >> 2) + 4 * h + (e & 3);
+                f[e] = *reinterpret_cast<const float*>(lds + at(row, d >> 2) + 4 * (d & 3));
+            }
+            return f;
+        }
+    }
+    // eight values (chunk c of the row) into the tile
+    static __device__ inline void put(char* lds, int row, int c, Frag<T> v) {
+        if constexpr (sizeof(T) == 2) {
+            *reinterpret_cast<Frag<T>*>(lds + at(row, c)) = v;
+        } else {
+            *reinterpret_cast<f32x4*>(lds + at(row, 2 * c)) = f32x4{v[0], v[1], v[2], v[3]};
+            *reinterpret_cast<f32x4*>(lds + at(row, 2 * c + 1)) = f32x4{v[4], v[5], v[6], v[7]};
+        }
+    }
+};
+
+// Four consecutive values of a result's column to memory, the first n of them.
+__device__ inline void store4(float* p, int n, f32x4 v) {
+    if (n >= 4) {
+        *reinterpret_cast<f32x4_u*>(p) = v;
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+        if (e < n) p[e] = v[e];
+}
+__device__ inline void store4(bf16* p, int n, f32x4 v) {
+    const bf16x4 w = __builtin_convertvector(v, bf16x4);
+    if (n >= 4) {
+        *reinterpret_cast<bf16x4_u*>(p) = w;
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 3; ++e)
+        if (e < n) p[e] = w[e];
+}
+
+// ---------------------------------------------------------------- who sees what
+// One sequence: n queries at t = m - n + i, m keys.
+struct Seq {
+    int n, m;
+};
+__device__ inline Seq sequence(const AttentionArgs& a, int b) {
+    Seq s{a.d.q_len, a.d.kv_len};
+    if (a.q_lens) s.n = min(max(a.q_lens[b], 0), a.d.q_len);
+    if (a.kv_lens) s.m = min(max(a.kv_lens[b], 0), a.d.kv_len);
+    return s;
+}
+// The keys that a query sees: lo <= j < hi, or j < sk.  (The host has made a window
+// that limits nothing 0, so no sum here passes 2^31.)
+struct See {
+    int lo, hi, sk;
+    __device__ inline bool operator()(int j) const { return (j >= lo && j < hi) || j < sk; }
+    __device__ inline bool none() const { return hi <= lo && sk <= 0; }
+};
+__device__ inline See sees(const pd_attention_desc& d, const Seq& s, int i) {
+    if (i >= s.n) return See{0, 0, 0};
+    const int t = s.m - s.n + i;
+    const int end = d.causal ? min(s.m, max(t + 1, 0)) : s.m;     // the last key that order allows
+    if (!d.window) return See{0, end, 0};
+    return See{max(t - d.window + 1, 0), min(end, max(t + d.window, 0)), min(d.sinks, end)};
+}
+// Union over the queries i0 .. i1 (both < s.n).
+__device__ inline See sees_any(const pd_attention_desc& d, const Seq& s, int i0, int i1) {
+    const See a = sees(d, s, i0), b = sees(d, s, i1);
+    return See{a.lo, b.hi, b.sk};
+}
+
+}  // namespace attn
+}  // namespace pd

@@ -1,0 +1,242 @@
+// C entry points of the transformer operators: argument checks on the host,
+// then the launches.  Empty work (no rows, no tokens) is PD_OK with nothing
+// launched, but for gradients that are sums over nothing.
+#include <cmath>
+#include <cstring>
+
+#include "api_guard.h"
+#include "ops.h"
+
+using namespace pd;
+
+namespace {
+
+// Every call checks the device it runs on; the answer for a device is kept.
+void require_gfx950() {
+    static thread_local int known = -1;
+    int dev = 0, n = 0;
+    if (hipGetDeviceCount(&n) != hipSuccess || n <= 0) fail(PD_ERR_DEVICE, "no HIP device is available");
+    PD_HIP(hipGetDevice(&dev));
+    if (dev == known) return;
+    hipDeviceProp_t prop;
+    PD_HIP(hipGetDeviceProperties(&prop, dev));
+    if (std::strncmp(prop.gcnArchName, "gfx950", 6) != 0)
+        fail(PD_ERR_DEVICE, std::string("this library is built for gfx950, device is ") + prop.gcnArchName);
+    known = dev;
+}
+
+void check_dtype(int32_t dtype) { require(dtype == PD_F32 || dtype == PD_BF16, "dtype must be PD_F32 or PD_BF16"); }
+
+void check_scratch(const void* scratch, int64_t have, int64_t need) {
+    if (need == 0) return;
+    require(scratch != nullptr && have >= need, "scratch is smaller than the matching scratch call says");
+    require(reinterpret_cast<uintptr_t>(scratch) % 16 == 0, "scratch must be 16-byte aligned");
+}
+
+// Rows from 0 to count - 1 at a stride must not reach past 2^62 elements, and not
+// overlap where they are written.
+constexpr int64_t kMostStride = (int64_t)1 << 40;
+void check_stride(int64_t s) { require(s >= 0 && s < kMostStride, "a stride is out of range"); }
+
+// ------------------------------------------------------------------ norm
+void check_norm(const pd_rmsnorm_desc& d, bool backward) {
+    check_dtype(d.dtype);
+    require(d.rows >= 0 && d.rows <= (int64_t)1 << 31, "rows out of range");
+    require(d.width >= 1 && d.width <= 65536, "width must be in [1, 65536]");
+    require(d.eps >= 0.f && std::isfinite(d.eps), "eps must be finite and >= 0");
+    for (int64_t s : {d.x_stride, d.residual_stride, d.sum_stride, d.y_stride}) check_stride(s);
+    if (backward) {
+        require(d.out_dtype == d.dtype, "the backward pass takes out_dtype = dtype");
+        require(d.rows <= 1 || d.x_stride >= d.width, "x_stride (of dx) must be >= width");
+        return;
+    }
+    require(d.out_dtype == d.dtype || d.out_dtype == PD_F8E4M3, "out_dtype must be dtype or PD_F8E4M3");
+    require(d.rows <= 1 || d.y_stride >= d.width, "y_stride must be >= width");
+    const int g = d.group;
+    require(g == 0 || (g >= 16 && g <= 512 && (g & (g - 1)) == 0), "group must be 0 or a power of two from 16 to 512");
+}
+
+// ------------------------------------------------------------------ attention
+// The desc as the kernels take it: a window that hides nothing becomes 0, and
+// sinks count up to the keys there are.
+pd_attention_desc check_attention(const pd_attention_desc* p) {
+    require(p != nullptr, "desc must not be NULL");
+    pd_attention_desc d = *p;
+    check_dtype(d.dtype);
+    require(d.batch >= 0 && d.heads_q >= 1 && d.heads_kv >= 1, "batch must be >= 0, heads_q and heads_kv >= 1");
+    require(d.heads_q % d.heads_kv == 0, "heads_q must be a multiple of heads_kv");
+    require(d.head_dim >= 1, "head_dim must be >= 1");
+    require(d.q_len >= 0 && d.kv_len >= 0, "q_len and kv_len must be >= 0");
+    require(d.window >= 0 && d.sinks >= 0, "window and sinks must be >= 0");
+    require(std::isfinite(d.scale), "scale must be finite");
+    for (int i = 0; i < 3; ++i)
+        for (int64_t s : {d.q_stride[i], d.k_stride[i], d.v_stride[i], d.out_stride[i]}) check_stride(s);
+    if (d.head_dim > 128) fail(PD_ERR_UNSUPPORTED, "head_dim above 128 is not implemented");
+    const int64_t rows = (int64_t)d.q_len * (d.heads_q / d.heads_kv);
+    if (rows > (int64_t)1 << 28 || d.kv_len > 1 << 28)
+        fail(PD_ERR_UNSUPPORTED, "more than 2^28 keys, or queries of one key head, are not implemented");
+    if ((int64_t)d.batch * d.heads_kv * ((rows > d.kv_len ? rows : d.kv_len) / 32 + 1) > (int64_t)1 << 30)
+        fail(PD_ERR_UNSUPPORTED, "a grid of more than 2^30 tiles is not implemented");
+    if ((int64_t)d.window >= (int64_t)d.q_len + d.kv_len) d.window = 0;
+    if (d.sinks > d.kv_len) d.sinks = d.kv_len;
+    if (!d.window) d.sinks = 0;
+    return d;
+}
+void check_attention_grad(const pd_attention_desc& d) {
+    for (int i = 0; i < 3; ++i)
+        for (int64_t s : {d.dq_stride[i], d.dk_stride[i], d.dv_stride[i], d.dout_stride[i]}) check_stride(s);
+}
+
+}  // namespace
+
+extern "C" pd_status pd_rmsnorm_forward(const pd_rmsnorm_desc* desc, const void* x, const void* residual,
+                                        const float* weight, void* sum, void* y, float* scale, float* rstd,
+                                        void* stream) {
+    return guard([&] {
+        require(desc != nullptr, "desc must not be NULL");
+        check_norm(*desc, false);
+        if (desc->rows == 0) return;
+        require(x && weight && y, "x, weight and y must not be NULL");
+        require(!sum || desc->rows <= 1 || desc->sum_stride >= desc->width, "sum_stride must be >= width");
+        require(desc->out_dtype != PD_F8E4M3 || scale, "an output in 8 bits needs scale");
+        require_gfx950();
+        launch_rmsnorm(NormArgs{*desc, x, residual, weight, sum, y, scale, rstd}, static_cast<hipStream_t>(stream));
+    });
+}
+
+static int64_t norm_grad_scratch(const pd_rmsnorm_desc& d) {
+    return (int64_t)norm_grad_blocks(d) * d.width * (int64_t)sizeof(float);
+}
+
+extern "C" pd_status pd_rmsnorm_backward_scratch(const pd_rmsnorm_desc* desc, int64_t* bytes) {
+    return guard([&] {
+        require(desc != nullptr && bytes != nullptr, "desc and bytes must not be NULL");
+        check_norm(*desc, true);
+        *bytes = norm_grad_scratch(*desc);
+    });
+}
+
+extern "C" pd_status pd_rmsnorm_backward(const pd_rmsnorm_desc* desc, const void* dy, const void* sum,
+                                         const float* weight, const float* rstd, const void* dsum, void* dx,
+                                         float* dweight, void* scratch, int64_t scratch_bytes, void* stream) {
+    return guard([&] {
+        require(desc != nullptr, "desc must not be NULL");
+        check_norm(*desc, true);
+        if (desc->rows == 0 && !dweight) return;
+        require(weight != nullptr, "weight must not be NULL");
+        require(desc->rows == 0 || (dy && sum && rstd && dx), "dy, sum, rstd and dx must not be NULL");
+        if (dweight) check_scratch(scratch, scratch_bytes, norm_grad_scratch(*desc));
+        require_gfx950();
+        launch_rmsnorm_grad(NormGradArgs{*desc, dy, sum, weight, rstd, dsum, dx, dweight, static_cast<float*>(scratch)},
+                            static_cast<hipStream_t>(stream));
+    });
+}
+
+extern "C" pd_status pd_rotary_table(const pd_rotary_table_desc* desc, int64_t first, int64_t rows, float* table,
+                                     void* stream) {
+    return guard([&] {
+        require(desc != nullptr, "desc must not be NULL");
+        const pd_rotary_table_desc& d = *desc;
+        require(d.rotary_dim >= 2 && d.rotary_dim <= 1024 && d.rotary_dim % 2 == 0, "rotary_dim must be even and in [2, 1024]");
+        require(d.scaling >= PD_ROTARY_PLAIN && d.scaling <= PD_ROTARY_BY_PARTS, "scaling must be a PD_ROTARY_* kind");
+        require(d.base > 1.0 && std::isfinite(d.base), "base must be finite and > 1");
+        require(d.scaling == PD_ROTARY_PLAIN || (d.factor >= 1.0 && std::isfinite(d.factor)), "factor must be finite and >= 1");
+        if (d.scaling == PD_ROTARY_BY_PARTS) {
+            require(d.original_length > 0.0 && std::isfinite(d.original_length), "original_length must be finite and > 0");
+            require(d.turns_low >= 0.0 && d.turns_high > d.turns_low && std::isfinite(d.turns_high),
+                    "turns_low and turns_high must be finite with 0 <= low < high");
+        }
+        require(std::isfinite(d.magnitude), "magnitude must be finite");
+        require(first >= 0 && first <= (int64_t)1 << 40 && rows >= 0 && rows <= (int64_t)1 << 28, "first or rows out of range");
+        if (rows == 0) return;
+        require(table != nullptr, "table must not be NULL");
+        require_gfx950();
+        launch_rotary_table(d, first, rows, table, static_cast<hipStream_t>(stream));
+    });
+}
+
+extern "C" pd_status pd_rotary_apply(const pd_rotary_desc* desc, const void* q, const void* k,
+                                     const int32_t* positions, const float* table, void* q_out, void* k_out,
+                                     void* stream) {
+    return guard([&] {
+        require(desc != nullptr, "desc must not be NULL");
+        pd_rotary_desc d = *desc;
+        check_dtype(d.dtype);
+        require(d.layout == PD_ROTARY_HALF || d.layout == PD_ROTARY_INTERLEAVED,
+                "layout must be PD_ROTARY_HALF or PD_ROTARY_INTERLEAVED");
+        require(d.batch >= 0 && d.length >= 0, "batch and length must be >= 0");
+        if (!k) d.heads_k = 0;
+        require(d.heads_q >= 1 && d.heads_q <= 65536 && d.heads_k >= 0 && d.heads_k <= 65536, "heads out of range");
+        require(d.head_dim >= 2 && d.head_dim <= 1024, "head_dim must be in [2, 1024]");
+        require(d.rotary_dim >= 2 && d.rotary_dim <= d.head_dim && d.rotary_dim % 2 == 0,
+                "rotary_dim must be even and in [2, head_dim]");
+        require(d.position_stride >= 0, "position_stride must be >= 0");
+        for (int i = 0; i < 3; ++i)
+            for (int64_t s : {d.q_stride[i], d.k_stride[i], d.q_out_stride[i], d.k_out_stride[i]}) check_stride(s);
+        require(d.batch <= (int64_t)1 << 31 && d.length <= (int64_t)1 << 31, "batch or length out of range");
+        const int64_t units = d.head_dim / 16 + 2;
+        if (d.batch * d.length > ((int64_t)1 << 38) / (units * (d.heads_q + d.heads_k)))
+            fail(PD_ERR_UNSUPPORTED, "more than 2^42 values in one call are not implemented");
+        if (d.batch == 0 || d.length == 0) return;
+        require(q && positions && table && q_out && (!k || k_out), "NULL device pointer");
+        require(d.table_rows >= 1, "table_rows must be >= 1");
+        require_gfx950();
+        launch_rotary(RotaryArgs{d, q, k, positions, table, q_out, k_out}, static_cast<hipStream_t>(stream));
+    });
+}
+
+extern "C" pd_status pd_attention_forward_scratch(const pd_attention_desc* desc, int64_t* bytes) {
+    return guard([&] {
+        require(bytes != nullptr, "bytes must not be NULL");
+        *bytes = attention_scratch_bytes(check_attention(desc));
+    });
+}
+
+extern "C" pd_status pd_attention_forward(const pd_attention_desc* desc, const void* q, const void* k, const void* v,
+                                          const int32_t* q_lens, const int32_t* kv_lens, void* out, float* lse,
+                                          void* scratch, int64_t scratch_bytes, void* stream) {
+    return guard([&] {
+        const pd_attention_desc d = check_attention(desc);
+        if (d.batch == 0 || d.q_len == 0) return;
+        require(q && out && (d.kv_len == 0 || (k && v)), "NULL device pointer");
+        check_scratch(scratch, scratch_bytes, attention_scratch_bytes(d));
+        require_gfx950();
+        AttentionArgs a{};
+        a.d = d;
+        a.q = q, a.k = k, a.v = v;
+        a.q_lens = q_lens, a.kv_lens = kv_lens;
+        a.out = out, a.lse = lse;
+        a.scratch = static_cast<float*>(scratch);
+        launch_attention(a, static_cast<hipStream_t>(stream));
+    });
+}
+
+extern "C" pd_status pd_attention_backward_scratch(const pd_attention_desc* desc, int64_t* bytes) {
+    return guard([&] {
+        require(bytes != nullptr, "bytes must not be NULL");
+        *bytes = attention_grad_scratch_bytes(check_attention(desc));
+    });
+}
+
+extern "C" pd_status pd_attention_backward(const pd_attention_desc* desc, const void* q, const void* k, const void* v,
+                                           const void* out, const float* lse, const void* dout,
+                                           const int32_t* q_lens, const int32_t* kv_lens, void* dq, void* dk, void* dv,
+                                           void* scratch, int64_t scratch_bytes, void* stream) {
+    return guard([&] {
+        const pd_attention_desc d = check_attention(desc);
+        check_attention_grad(d);
+        if (d.batch == 0 || (d.q_len == 0 && d.kv_len == 0)) return;
+        require(d.q_len == 0 || (q && out && lse && dout && dq), "NULL device pointer");
+        require(d.kv_len == 0 || (k && v && dk && dv), "NULL device pointer");
+        check_scratch(scratch, scratch_bytes, attention_grad_scratch_bytes(d));
+        require_gfx950();
+        AttentionArgs a{};
+        a.d = d;
+        a.q = q, a.k = k, a.v = v;
+        a.q_lens = q_lens, a.kv_lens = kv_lens;
+        a.out = const_cast<void*>(out), a.lse = const_cast<float*>(lse);
+        a.dout = dout, a.dq = dq, a.dk = dk, a.dv = dv;
+        a.scratch = static_cast<float*>(scratch);
+        launch_attention_grad(a, static_cast<hipStream_t>(stream));
+    });
+}

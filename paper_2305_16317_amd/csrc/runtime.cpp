@@ -11,6 +11,7 @@
 #include <string>
 #include <vector>
 
+#include "api_guard.h"
 #include "gmm.h"
 #include "mlp.h"
 #include "pd_internal.h"
@@ -26,34 +27,12 @@ void hip_check(hipError_t e, const char* what) {
     fail(code, std::string(what) + ": " + hipGetErrorString(e));
 }
 
+std::string& last_error() {
+    thread_local std::string msg;
+    return msg;
+}
+
 namespace {
-
-thread_local std::string g_last_error;
-
-template <class F>
-pd_status guard(F&& f) {
-    try {
-        f();
-        g_last_error.clear();
-        return PD_OK;
-    } catch (const Error& e) {
-        g_last_error = e.msg;
-        return e.code;
-    } catch (const std::bad_alloc&) {
-        g_last_error = "host allocation failed";
-        return PD_ERR_OOM;
-    } catch (const std::exception& e) {
-        g_last_error = e.what();
-        return PD_ERR_DEVICE;
-    } catch (...) {
-        g_last_error = "unknown error";
-        return PD_ERR_DEVICE;
-    }
-}
-
-void require(bool ok, const std::string& msg) {
-    if (!ok) fail(PD_ERR_INVALID_ARG, msg);
-}
 
 // Device buffer owned by a handle.
 struct DevBuf {
@@ -322,7 +301,7 @@ extern "C" pd_status pd_schedule_multistep_tables(const pd_schedule* s, float* R
     });
 }
 
-extern "C" const char* pd_last_error(void) { return g_last_error.c_str(); }
+extern "C" const char* pd_last_error(void) { return last_error().c_str(); }
 extern "C" const char* pd_version(void) { return "paradigms-gfx950 0.1"; }
 
 // ============================================================== denoiser
