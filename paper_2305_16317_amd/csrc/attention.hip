@@ -2,13 +2,20 @@
 //
 //   x_ij = scale q_i k_j over the keys that query i sees,  o_i = sum_j e^(x_ij - m_i) v_j / l_i
 //
-// One pass over the keys with a running maximum m and sum l (in base 2: p = 2^(s c
-// - m c), c = scale log2 e, one fused multiply-add and one exponential a score).
-// (The product m c is rounded: a shift of all of a row's terms, without effect
-// while it is small.  Where |m c| passes 1024 the difference (s - m) c is formed
-// instead, exact for the row's largest scores of any size.)
-// A block holds 128 rows, 32 a wave; a row is a query of one of the heads that
-// share a key head, so keys and values are read once for all of them.
+// One pass over the keys with a running reference m and sum l, in base 2: p = 2^(s c
+// - m c), c = scale log2 e, one fused multiply-add and one exponential a score.  m
+// is the row's largest score of some earlier tile: it is raised, and o and l
+// rescaled, only when a score passes it by 2^8 (the terms are float32, and a
+// bfloat16 probability is rounded relative to itself, so nothing is lost below that).
+// The product m c is rounded: a shift of all of a row's terms, without effect while
+// it is small.  Where |m c| passes 1024 the difference (s - m) c is formed instead,
+// exact for the row's largest scores of any size.
+//
+// A row is a query of one of the query heads that share a key head: keys and values
+// are read once for all of them.  Two kernels: blocks of 128 rows that share the key
+// tiles in LDS, and, for at most 32 rows (a token's heads, a short sequence), waves
+// of 32 rows that stream key tiles of their own.  Where there are few blocks the keys
+// are split among several of them, whose results k_attention_join puts together.
 #include "attention_tile.h"
 
 namespace pd {
@@ -16,9 +23,8 @@ namespace {
 
 using namespace attn;
 
-constexpr int kBN = 64;          // keys a tile
 constexpr float kLarge = 1024.f;
-
+constexpr float kSlack = 8.f;        // log2 of what a score may pass its reference by
 
 // The row's result from its visible keys alone, one after the other: for rows
 // whose fast sum is not finite.  There a probability of 0 for a key out of
@@ -65,145 +71,183 @@ __device__ void attend_row(const AttentionArgs& a, const T* q, const T* k, const
     if (lse && lane == 0) *lse = log_sum(top, 1.f, total);
 }
 
+// The 32 rows of a wave (lane: row lane % 32) and what they have summed.
 template <typename T, int DP>
-__global__ __launch_bounds__(256) void k_attention(const AttentionArgs a) {
+struct Rows {
+    static constexpr int kSteps = DP / 16, kDT = DP / 32;
     using Ti = Tile<T, DP>;
-    constexpr int kSteps = DP / 16, kDT = DP / 32;
-    __shared__ __align__(16) char lds_k[kBN * Ti::kPitch];
-    __shared__ __align__(16) char lds_v[kBN * Ti::kPitch];
-    const pd_attention_desc& d = a.d;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
-    const int group = d.heads_q / d.heads_kv;
-    const int b = blockIdx.z, hk = blockIdx.y;
-    const Seq seq = sequence(a, b);
-    const int rows_all = d.q_len * group;
-    const int row0 = blockIdx.x * 128 + wave * 32, row = row0 + (lane & 31);
-    const bool real = row < rows_all;
-    const int qi = real ? row / group : 0, hq = hk * group + row % group;
-    const See see = real ? sees(d, seq, qi) : See{0, 0, 0};
+    Frag<T> q[kSteps];
+    f32x16 o[kDT];           // transposed: the lane's row, columns 32 t + tile_row
+    float top, limit;        // the reference and the score that raises it (unscaled)
+    float mc;                // top c2
+    float total;             // over the keys of this half of the wave
+    float c2;
+    bool large;
 
-    const T* kb = static_cast<const T*>(a.k) + b * d.k_stride[0] + hk * d.k_stride[2];
-    const T* vb = static_cast<const T*>(a.v) + b * d.v_stride[0] + hk * d.v_stride[2];
-    const T* qp = static_cast<const T*>(a.q) + b * d.q_stride[0] + qi * d.q_stride[1] + hq * d.q_stride[2];
-
-    Frag<T> qf[kSteps];
+    __device__ __forceinline__ void start(const pd_attention_desc& d, const T* qp, bool real, int lane) {
+        const int h = lane >> 5;
 #pragma unroll
-    for (int c = 0; c < kSteps; ++c) {
-        const int e = 16 * c + 8 * h;
-        qf[c] = Frag<T>{};
-        if (real && !see.none() && d.scale != 0.f) qf[c] = load8(qp + e, d.head_dim - e);
-        if (d.scale < 0.f) qf[c] = -qf[c];
-    }
-    // the running maximum is one of unscaled scores: c2 > 0 (a scale of 0: zero queries)
-    const float c2 = d.scale == 0.f ? 1.f : fabsf(d.scale) * kLog2e;
-
-    // the block's queries, its keys, and the tiles that hold them
-    const int i0 = blockIdx.x * 128 / group, i1 = min((blockIdx.x * 128 + 127) / group, seq.n - 1);
-    See any{0, 0, 0};
-    if (i0 <= i1) any = sees_any(d, seq, i0, i1);
-    const int sink_tiles = (any.sk + kBN - 1) / kBN;
-    const int first = max(any.lo / kBN, sink_tiles), end = max((any.hi + kBN - 1) / kBN, first);
-    const int tiles = sink_tiles + end - first;
-
-    f32x16 o[kDT];
-#pragma unroll
-    for (int t = 0; t < kDT; ++t) o[t] = f32x16{};
-    float top = -INFINITY, total = 0.f;
-
-    for (int it = 0; it < tiles; ++it) {
-        const int j0 = (it < sink_tiles ? it : first + it - sink_tiles) * kBN;
-        __syncthreads();
-        for (int u = threadIdx.x; u < kBN * (DP / 8); u += 256) {
-            const int r = u / (DP / 8), c = u % (DP / 8), j = j0 + r;
-            Frag<T> kv = {}, vv = {};
-            if (any(j)) {
-                kv = load8(kb + (int64_t)j * d.k_stride[1] + 8 * c, d.head_dim - 8 * c);
-                vv = load8(vb + (int64_t)j * d.v_stride[1] + 8 * c, d.head_dim - 8 * c);
-            }
-            Ti::put(lds_k, r, c, kv);
-            Ti::put(lds_v, r, c, vv);
+        for (int c = 0; c < kSteps; ++c) {
+            const int e = 16 * c + 8 * h;
+            q[c] = Frag<T>{};
+            if (real && d.scale != 0.f) q[c] = load8(qp + e, d.head_dim - e);
+            if (d.scale < 0.f) q[c] = -q[c];
         }
-        __syncthreads();
-        f32x16 s[2];
+        // the reference is one of unscaled scores: c2 > 0 (a scale of 0: zero queries)
+        c2 = d.scale == 0.f ? 1.f : fabsf(d.scale) * kLog2e;
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt) {
+        for (int t = 0; t < kDT; ++t) o[t] = f32x16{};
+        top = limit = -INFINITY;
+        mc = total = 0.f;
+        large = false;
+    }
+
+    // 32 NK keys from j0 on, in LDS; `edge`: some row does not see all of them
+    template <int NK>
+    __device__ __forceinline__ void attend(const char* k, const char* v, int j0, const See& see, bool edge, int lane) {
+        f32x16 s[NK];
+#pragma unroll
+        for (int kt = 0; kt < NK; ++kt) {
             s[kt] = f32x16{};
 #pragma unroll
-            for (int c = 0; c < kSteps; ++c) s[kt] = mma(Ti::rows(lds_k, 32 * kt, c, lane), qf[c], s[kt]);
+            for (int c = 0; c < kSteps; ++c) s[kt] = mma(Ti::rows(k, 32 * kt, c, lane), q[c], s[kt]);
         }
-        float m = top;
+        if (edge) {
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt)
+            for (int kt = 0; kt < NK; ++kt)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                if (!see(j0 + 32 * kt + tile_row(lane, r))) s[kt][r] = -INFINITY;
-                m = fmaxf(m, s[kt][r]);
-            }
-        m = fmaxf(m, __shfl_xor(m, 32));
-        const float mc = m == -INFINITY ? 0.f : m * c2;
-        const bool large = __any(!(fabsf(mc) < kLarge));
-        float keep = exp2_fast(top * c2 - mc);
-        if (large) keep = top == -INFINITY ? 0.f : exp2_fast((top - m) * c2);
-        top = m;
+                for (int r = 0; r < 16; ++r)
+                    if (!see(j0 + 32 * kt + tile_row(lane, r))) s[kt][r] = -INFINITY;
+        }
+        float m = s[0][0];
+#pragma unroll
+        for (int kt = 0; kt < NK; ++kt)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) m = fmaxf(m, s[kt][r]);
+        {
+            const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(m), __float_as_uint(m), false, false);
+            m = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
+        }
+        if (__any(m > limit)) {
+            const float up = fmaxf(m, top);
+            const float keep = up == top ? 1.f : exp2_fast((top - up) * c2);
+            top = up;
+            limit = top + kSlack / c2;
+            mc = top == -INFINITY ? 0.f : top * c2;
+            large = __any(!(fabsf(mc) < kLarge));
+            total *= keep;
+#pragma unroll
+            for (int t = 0; t < kDT; ++t) o[t] *= keep;
+        }
         float sum = 0.f;
         if (large) {
 #pragma unroll
-            for (int kt = 0; kt < 2; ++kt)
+            for (int kt = 0; kt < NK; ++kt)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const float x = s[kt][r];
-                    s[kt][r] = m == -INFINITY || x == -INFINITY ? 0.f : exp2_fast((x - m) * c2);
+                    s[kt][r] = x == -INFINITY ? 0.f : exp2_fast((x - top) * c2);
                     sum += s[kt][r];
                 }
         } else {
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt)
+            for (int kt = 0; kt < NK; ++kt)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                s[kt][r] = exp2_fast(fmaf(s[kt][r], c2, -mc));
-                sum += s[kt][r];
-            }
+                for (int r = 0; r < 16; ++r) {
+                    s[kt][r] = exp2_fast(fmaf(s[kt][r], c2, -mc));
+                    sum += s[kt][r];
+                }
         }
-        total = total * keep + sum + __shfl_xor(sum, 32);
+        total += sum;
 #pragma unroll
-        for (int t = 0; t < kDT; ++t) o[t] *= keep;
-#pragma unroll
-        for (int kt = 0; kt < 2; ++kt)
+        for (int kt = 0; kt < NK; ++kt)
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
                 const Frag<T> p = as_frag<T>(s[kt], c);
 #pragma unroll
-                for (int t = 0; t < kDT; ++t) o[t] = mma(Ti::cols(lds_v, 32 * kt + 16 * c, t, lane), p, o[t]);
+                for (int t = 0; t < kDT; ++t) o[t] = mma(Ti::cols(v, 32 * kt + 16 * c, t, lane), p, o[t]);
             }
     }
 
-    float* lse = a.lse ? a.lse + ((int64_t)b * d.heads_q + hq) * d.q_len + qi : nullptr;
-    T* out = static_cast<T*>(a.out) + b * d.out_stride[0] + qi * d.out_stride[1] + hq * d.out_stride[2];
-    const float inv = total == 0.f ? 0.f : 1.f / total;
-    bool odd = false;
-#pragma unroll
-    for (int t = 0; t < kDT; ++t) {
-        o[t] = total == 0.f ? f32x16{} : o[t] * inv;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) odd = odd || !(fabsf(o[t][r]) < INFINITY);
-    }
-    odd = odd && real;
-    const uint64_t both = __ballot(odd);
-    uint32_t again = (uint32_t)both | (uint32_t)(both >> 32);
-    if (real && !((again >> (lane & 31)) & 1)) {
+    __device__ __forceinline__ void finish() { total += __shfl_xor(total, 32); }
+    // whether a value of the lane's row is not finite
+    __device__ __forceinline__ bool odd() const {
+        bool b = false;
 #pragma unroll
         for (int t = 0; t < kDT; ++t)
 #pragma unroll
+            for (int r = 0; r < 16; ++r) b = b || !(fabsf(o[t][r]) < INFINITY);
+        return b;
+    }
+};
+
+// Where the parts of split rows go: [split][row over batch, query head, query] of
+// (head_dim sums, reference, total).
+struct Parts {
+    float* sums;
+    float* stats;      // [..][2]
+};
+__host__ __device__ inline Parts parts(const pd_attention_desc& d, float* scratch, int splits) {
+    const int64_t rows = (int64_t)d.batch * d.heads_q * d.q_len;
+    return Parts{scratch + (((int64_t)splits * rows * 2 + 3) & ~(int64_t)3), scratch};
+}
+
+// Which wave does what.
+struct Plan {
+    int group, rows;           // rows of a key head: group * q_len
+    int row_tiles;             // of 128 rows, or of 32
+    int splits, split_tiles;   // parts of the key tiles, and the tiles of each
+    int64_t units;             // row tiles over all key heads and sequences
+};
+
+template <typename T, int DP>
+__device__ __forceinline__ void store_rows(const AttentionArgs& a, const Plan& p, Rows<T, DP>& w, const Seq& seq, int b, int hk,
+                                           int row0, int split, const T* kb, const T* vb) {
+    const pd_attention_desc& d = a.d;
+    const int lane = threadIdx.x & 63, h = lane >> 5, row = row0 + (lane & 31);
+    const bool real = row < p.rows;
+    const int qi = real ? row / p.group : 0, hq = hk * p.group + row % p.group;
+    w.finish();
+    if (p.splits > 1) {
+        const Parts to = parts(d, a.scratch, p.splits);
+        const int64_t at = ((int64_t)split * d.batch + b) * d.heads_q * d.q_len + (int64_t)hq * d.q_len + qi;
+        if (!real) return;
+        if (h == 0) {
+            to.stats[2 * at] = w.top;
+            to.stats[2 * at + 1] = w.total;
+        }
+        if (w.total == 0.f) return;            // the join leaves such parts out
+        float* sums = to.sums + at * d.head_dim;
+#pragma unroll
+        for (int t = 0; t < w.kDT; ++t)
+#pragma unroll
             for (int g = 0; g < 4; ++g) {
                 const int e = 32 * t + 8 * g + 4 * h;
-                store4(out + e, d.head_dim - e, f32x4{o[t][4 * g], o[t][4 * g + 1], o[t][4 * g + 2], o[t][4 * g + 3]});
+                store4(sums + e, d.head_dim - e, f32x4{w.o[t][4 * g], w.o[t][4 * g + 1], w.o[t][4 * g + 2], w.o[t][4 * g + 3]});
             }
-        if (lse && h == 0) *lse = log_sum(top, fabsf(d.scale), total);
+        return;
+    }
+    const float inv = 1.f / w.total;
+#pragma unroll
+    for (int t = 0; t < w.kDT; ++t) w.o[t] = w.total == 0.f ? f32x16{} : w.o[t] * inv;
+    const uint64_t both = __ballot(w.odd() && real);
+    uint32_t again = (uint32_t)both | (uint32_t)(both >> 32);
+    if (real && !((again >> (lane & 31)) & 1)) {
+        T* out = static_cast<T*>(a.out) + b * d.out_stride[0] + qi * d.out_stride[1] + hq * d.out_stride[2];
+#pragma unroll
+        for (int t = 0; t < w.kDT; ++t)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int e = 32 * t + 8 * g + 4 * h;
+                store4(out + e, d.head_dim - e, f32x4{w.o[t][4 * g], w.o[t][4 * g + 1], w.o[t][4 * g + 2], w.o[t][4 * g + 3]});
+            }
+        if (a.lse && h == 0)
+            a.lse[((int64_t)b * d.heads_q + hq) * d.q_len + qi] = log_sum(w.top, fabsf(d.scale), w.total);
     }
     while (again) {
-        const int w = __ffs(again) - 1, rr = row0 + w;
+        const int rr = row0 + __ffs(again) - 1;
         again &= again - 1;
-        const int i = rr / group, hh = hk * group + rr % group;
+        const int i = rr / p.group, hh = hk * p.group + rr % p.group;
         attend_row<T>(a, static_cast<const T*>(a.q) + b * d.q_stride[0] + i * d.q_stride[1] + hh * d.q_stride[2], kb, vb,
                       sees(d, seq, i), static_cast<T*>(a.out) + b * d.out_stride[0] + i * d.out_stride[1] + hh * d.out_stride[2],
                       a.lse ? a.lse + ((int64_t)b * d.heads_q + hh) * d.q_len + i : nullptr);
@@ -211,11 +255,243 @@ __global__ __launch_bounds__(256) void k_attention(const AttentionArgs a) {
 }
 
 template <typename T, int DP>
-void attention_t(const AttentionArgs& a, hipStream_t s) {
-    const int group = a.d.heads_q / a.d.heads_kv;
-    const int64_t rows = (int64_t)a.d.q_len * group;
-    hipLaunchKernelGGL((k_attention<T, DP>), dim3((unsigned)((rows + 127) / 128), a.d.heads_kv, a.d.batch), dim3(256), 0, s, a);
+constexpr int keys_per_tile() {
+    return Tile<T, DP>::kPitch <= 256 ? 64 : 32;
+}
+
+// A block: 128 rows of one key head, or one part of their keys.  The next tile of keys
+// and values is copied to LDS while the waves work on the present one.
+template <typename T, int DP, bool COPY>
+__global__ __launch_bounds__(256, 2) void k_attention(const AttentionArgs a, const Plan p) {
+    using Ti = Tile<T, DP>;
+    constexpr int BN = keys_per_tile<T, DP>(), kBytes = BN * Ti::kPitch;
+    using F = Fill<T, DP, BN, 256>;
+    __shared__ __align__(128) char lds[4 * kBytes];       // keys, values; twice
+    const pd_attention_desc& d = a.d;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int split = blockIdx.x % p.splits, unit = blockIdx.x / p.splits;
+    const int tile = p.row_tiles - 1 - unit % p.row_tiles, head = unit / p.row_tiles;     // the longest rows first
+    const int hk = head % d.heads_kv, b = head / d.heads_kv;
+    const Seq seq = sequence(a, b);
+    const int row0 = tile * 128 + wave * 32, row = row0 + (lane & 31);
+    const bool real = row < p.rows;
+    const int qi = real ? row / p.group : 0, hq = hk * p.group + row % p.group;
+    const See see = real ? sees(d, seq, qi) : See{0, 0, 0};
+    const WaveSight sight(see);
+    const T* kb = static_cast<const T*>(a.k) + b * d.k_stride[0] + hk * d.k_stride[2];
+    const T* vb = static_cast<const T*>(a.v) + b * d.v_stride[0] + hk * d.v_stride[2];
+
+    Rows<T, DP> w;
+    w.start(d, static_cast<const T*>(a.q) + b * d.q_stride[0] + qi * d.q_stride[1] + hq * d.q_stride[2], real && !see.none(), lane);
+
+    const int i0 = tile * 128 / p.group, i1 = min((tile * 128 + 127) / p.group, seq.n - 1);
+    const KeyTiles<BN> tiles(i0 <= i1 ? sees_any(d, seq, i0, i1) : See{0, 0, 0});
+    const int it0 = split * p.split_tiles, it1 = min(tiles.count, it0 + p.split_tiles);
+    const int units = d.head_dim * (int)sizeof(T) / 16;
+    auto fetch = [&](int it, int buf) {
+        const int j0 = tiles.start(it);
+        const T* kt = kb + (int64_t)j0 * d.k_stride[1];
+        const T* vt = vb + (int64_t)j0 * d.v_stride[1];
+        char* to = lds + buf * 2 * kBytes;
+        if constexpr (COPY) {
+            if (tiles.whole(j0)) {
+                F::copy(kt, d.k_stride[1], units, to, threadIdx.x, [](int r) { return r; });
+                F::copy(vt, d.v_stride[1], units, to + kBytes, threadIdx.x, [](int r) { return r; });
+            } else {
+                auto from = [&](int r) { return tiles.inside(j0, j0 + r) - j0; };
+                F::copy(kt, d.k_stride[1], units, to, threadIdx.x, from);
+                F::copy(vt, d.v_stride[1], units, to + kBytes, threadIdx.x, from);
+            }
+        } else {
+            auto keep = [&](int r) { return tiles.any(j0 + r); };
+            F::load(kt, d.k_stride[1], d.head_dim, to, threadIdx.x, keep);
+            F::load(vt, d.v_stride[1], d.head_dim, to + kBytes, threadIdx.x, keep);
+        }
+    };
+    if (it0 < it1) fetch(it0, 0);
+    for (int it = it0; it < it1; ++it) {
+        const int buf = (it - it0) & 1, j0 = tiles.start(it);
+        if constexpr (COPY) wait_copies();
+        lds_barrier();                                    // this tile is there, the other buffer is free
+        if (it + 1 < it1) fetch(it + 1, buf ^ 1);
+        if (sight.none(j0, BN)) continue;
+        const char* at = lds + buf * 2 * kBytes;
+        w.template attend<BN / 32>(at, at + kBytes, j0, see, !sight.all(j0, BN), lane);
+    }
+    store_rows(a, p, w, seq, b, hk, row0, split, kb, vb);
+}
+
+// A block of one wave: 32 rows of one key head, or one part of their keys.
+template <typename T, int DP, bool COPY>
+__global__ __launch_bounds__(64) void k_attention_few(const AttentionArgs a, const Plan p) {
+    using Ti = Tile<T, DP>;
+    constexpr int BN = 32, kBytes = BN * Ti::kPitch;
+    using F = Fill<T, DP, BN, 64>;
+    __shared__ __align__(128) char lds[(COPY ? 4 : 2) * kBytes];
+    const pd_attention_desc& d = a.d;
+    const int lane = threadIdx.x;
+    const int split = blockIdx.x % p.splits, head = blockIdx.x / p.splits;   // one row tile a key head
+    const int hk = head % d.heads_kv, b = head / d.heads_kv;
+    const Seq seq = sequence(a, b);
+    const int row = lane & 31;
+    const bool real = row < p.rows;
+    const int qi = real ? row / p.group : 0, hq = hk * p.group + row % p.group;
+    const See see = real ? sees(d, seq, qi) : See{0, 0, 0};
+    const WaveSight sight(see);
+    const T* kb = static_cast<const T*>(a.k) + b * d.k_stride[0] + hk * d.k_stride[2];
+    const T* vb = static_cast<const T*>(a.v) + b * d.v_stride[0] + hk * d.v_stride[2];
+
+    Rows<T, DP> w;
+    w.start(d, static_cast<const T*>(a.q) + b * d.q_stride[0] + qi * d.q_stride[1] + hq * d.q_stride[2], real && !see.none(), lane);
+    const KeyTiles<BN> tiles(seq.n > 0 ? sees_any(d, seq, 0, seq.n - 1) : See{0, 0, 0});
+    const int it0 = split * p.split_tiles, it1 = min(tiles.count, it0 + p.split_tiles);
+    const int units = d.head_dim * (int)sizeof(T) / 16;
+    auto fetch = [&](int it, char* to) {
+        const int j0 = tiles.start(it);
+        const T* kt = kb + (int64_t)j0 * d.k_stride[1];
+        const T* vt = vb + (int64_t)j0 * d.v_stride[1];
+        if constexpr (COPY) {
+            auto from = [&](int r) { return tiles.inside(j0, j0 + r) - j0; };
+            F::copy(kt, d.k_stride[1], units, to, lane, from);
+            F::copy(vt, d.v_stride[1], units, to + kBytes, lane, from);
+        } else {
+            auto keep = [&](int r) { return tiles.any(j0 + r); };
+            F::load(kt, d.k_stride[1], d.head_dim, to, lane, keep);
+            F::load(vt, d.v_stride[1], d.head_dim, to + kBytes, lane, keep);
+        }
+    };
+    if constexpr (COPY) {
+        if (it0 < it1) fetch(it0, lds);
+        for (int it = it0; it < it1; ++it) {
+            const int buf = (it - it0) & 1, j0 = tiles.start(it);
+            // the wave's reads of the other buffer are done (their values were used), so
+            // the next tile may go there; then all copies but the next tile's have landed
+            if (it + 1 < it1) {
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                fetch(it + 1, lds + (buf ^ 1) * 2 * kBytes);
+                asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * F::kCopies) : "memory");
+            } else {
+                wait_copies();
+            }
+            __builtin_amdgcn_wave_barrier();
+            const char* at = lds + buf * 2 * kBytes;
+            w.template attend<1>(at, at + kBytes, j0, see, !sight.all(j0, BN), lane);
+            __builtin_amdgcn_wave_barrier();
+        }
+    } else {
+        for (int it = it0; it < it1; ++it) {
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            fetch(it, lds);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            const int j0 = tiles.start(it);
+            w.template attend<1>(lds, lds + kBytes, j0, see, !sight.all(j0, BN), lane);
+        }
+    }
+    store_rows(a, p, w, seq, b, hk, 0, split, kb, vb);
+}
+
+// A row's parts into its result: one wave a row, lane e has values e and e + 64.
+template <typename T>
+__global__ __launch_bounds__(256) void k_attention_join(const AttentionArgs a, const Plan p) {
+    const pd_attention_desc& d = a.d;
+    const int lane = threadIdx.x & 63;
+    const int64_t rows = (int64_t)d.batch * d.heads_q * d.q_len, row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (row >= rows) return;
+    const int i = (int)(row % d.q_len), hq = (int)(row / d.q_len % d.heads_q), b = (int)(row / d.q_len / d.heads_q);
+    const Parts from = parts(d, a.scratch, p.splits);
+    const float c2 = d.scale == 0.f ? 1.f : fabsf(d.scale) * kLog2e;
+    // the largest reference of a part that has terms (a NaN total counts as one)
+    float top = -INFINITY;
+    for (int s = lane; s < p.splits; s += 64) {
+        const float* st = from.stats + 2 * (s * rows + row);
+        if (st[1] != 0.f) top = fmaxf(top, st[0]);
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+    float total = 0.f, acc[2] = {0.f, 0.f};
+    for (int s = 0; s < p.splits; ++s) {
+        const float* st = from.stats + 2 * (s * rows + row);
+        const float t = st[1];
+        if (t == 0.f) continue;
+        const float f = st[0] == top ? 1.f : exp2_fast((st[0] - top) * c2);
+        const float* sums = from.sums + (s * rows + row) * d.head_dim;
+        total = fmaf(f, t, total);
+        if (lane < d.head_dim) acc[0] = fmaf(f, sums[lane], acc[0]);
+        if (lane + 64 < d.head_dim) acc[1] = fmaf(f, sums[lane + 64], acc[1]);
+    }
+    T* out = static_cast<T*>(a.out) + b * d.out_stride[0] + i * d.out_stride[1] + hq * d.out_stride[2];
+    float* lse = a.lse ? a.lse + row : nullptr;
+    const float inv = total == 0.f ? 0.f : 1.f / total;
+    acc[0] *= inv;
+    acc[1] *= inv;
+    if (__any(!(fabsf(acc[0]) < INFINITY) || !(fabsf(acc[1]) < INFINITY))) {
+        const int hk = hq / p.group;
+        attend_row<T>(a, static_cast<const T*>(a.q) + b * d.q_stride[0] + i * d.q_stride[1] + hq * d.q_stride[2],
+                      static_cast<const T*>(a.k) + b * d.k_stride[0] + hk * d.k_stride[2],
+                      static_cast<const T*>(a.v) + b * d.v_stride[0] + hk * d.v_stride[2], sees(d, sequence(a, b), i), out, lse);
+        return;
+    }
+    if (lane < d.head_dim) out[lane] = (T)acc[0];
+    if (lane + 64 < d.head_dim) out[lane + 64] = (T)acc[1];
+    if (lse && lane == 0) *lse = log_sum(top, fabsf(d.scale), total);
+}
+
+// The most tiles of bn keys that a tile of rows can have to read.
+int64_t most_tiles(const pd_attention_desc& d, int rows_per_tile, int group, int bn) {
+    const int64_t all = ((int64_t)d.kv_len + bn - 1) / bn;
+    if (!d.window) return all;
+    const int64_t queries = (int64_t)(rows_per_tile - 1) / group + 2;
+    const int64_t span = (d.causal ? 1 : 2) * (int64_t)d.window + (queries < d.q_len ? queries : d.q_len);
+    const int64_t some = span / bn + 2 + ((int64_t)d.sinks + bn - 1) / bn;
+    return some < all ? some : all;
+}
+
+bool few_rows(const pd_attention_desc& d) { return (int64_t)d.q_len * (d.heads_q / d.heads_kv) <= 32; }
+
+int bn_of(const pd_attention_desc& d) {
+    const int dp = d.head_dim <= 32 ? 32 : d.head_dim <= 64 ? 64 : d.head_dim <= 96 ? 96 : 128;
+    return d.dtype == PD_BF16 || dp <= 64 ? 64 : 32;
+}
+
+// Splits: enough that the waves (few rows) or blocks fill the chip, and parts of at
+// least four tiles.
+Plan plan(const pd_attention_desc& d) {
+    Plan p{};
+    p.group = d.heads_q / d.heads_kv;
+    p.rows = d.q_len * p.group;
+    const bool few = few_rows(d);
+    p.row_tiles = few ? 1 : (p.rows + 127) / 128;
+    p.units = (int64_t)p.row_tiles * d.heads_kv * d.batch;
+    const int64_t tiles = most_tiles(d, few ? 32 : 128, p.group, few ? 32 : bn_of(d));
+    const int64_t want = few ? 4096 : 512;
+    int64_t splits = p.units >= want / 2 ? 1 : want / p.units;
+    if (few && tiles > 64) splits = splits > tiles / 32 ? splits : tiles / 32;
+    if (splits > tiles / 4) splits = tiles / 4;
+    if (splits < 1) splits = 1;
+    p.split_tiles = (int)((tiles + splits - 1) / splits);
+    p.splits = tiles ? (int)((tiles + p.split_tiles - 1) / p.split_tiles) : 1;
+    return p;
+}
+
+template <typename T, int DP, bool COPY>
+void attention_c(const AttentionArgs& a, hipStream_t s) {
+    const Plan p = plan(a.d);
+    if (few_rows(a.d))
+        hipLaunchKernelGGL((k_attention_few<T, DP, COPY>), dim3((unsigned)(p.units * p.splits)), dim3(64), 0, s, a, p);
+    else
+        hipLaunchKernelGGL((k_attention<T, DP, COPY>), dim3((unsigned)(p.units * p.splits)), dim3(256), 0, s, a, p);
     PD_HIP(hipGetLastError());
+    if (p.splits == 1) return;
+    const int64_t rows = (int64_t)a.d.batch * a.d.heads_q * a.d.q_len;
+    hipLaunchKernelGGL((k_attention_join<T>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a, p);
+    PD_HIP(hipGetLastError());
+}
+template <typename T, int DP>
+void attention_t(const AttentionArgs& a, hipStream_t s) {
+    if (copies_fit(a.k, a.d.k_stride, a.d.head_dim, sizeof(T)) && copies_fit(a.v, a.d.v_stride, a.d.head_dim, sizeof(T)))
+        attention_c<T, DP, true>(a, s);
+    else
+        attention_c<T, DP, false>(a, s);
 }
 template <typename T>
 void attention_dim(const AttentionArgs& a, hipStream_t s) {
@@ -227,7 +503,13 @@ void attention_dim(const AttentionArgs& a, hipStream_t s) {
 
 }  // namespace
 
-int64_t attention_scratch_bytes(const pd_attention_desc&) { return 0; }
+int64_t attention_scratch_bytes(const pd_attention_desc& d) {
+    if (d.batch == 0 || d.q_len == 0) return 0;
+    const Plan p = plan(d);
+    if (p.splits == 1) return 0;
+    const int64_t rows = (int64_t)d.batch * d.heads_q * d.q_len * p.splits;
+    return (((rows * 2 + 3) & ~(int64_t)3) + rows * d.head_dim) * (int64_t)sizeof(float);
+}
 
 void launch_attention(const AttentionArgs& a, hipStream_t s) {
     a.d.dtype == PD_F32 ? attention_dim<float>(a, s) : attention_dim<bf16>(a, s);

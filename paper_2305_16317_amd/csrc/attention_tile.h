@@ -138,6 +138,77 @@ __device__ inline void store4(bf16* p, int n, f32x4 v) {
         if (e < n) p[e] = w[e];
 }
 
+// ---------------------------------------------------------------- memory to LDS
+// One copy of 16 bytes a lane from base + off to LDS at lds + 16 lane, past the
+// registers (M0 = lds).  Inline assembly, so that the compiler's wait counts do not
+// see it (it would wait for the copies before every LDS read): who reads the data
+// waits with wait_copies() and a barrier first.
+__device__ __forceinline__ uint64_t uniform_address(const void* p) {
+    const uint64_t v = (uint64_t)(uintptr_t)p;
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v);
+    const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
+    return ((uint64_t)hi << 32) | lo;
+}
+__device__ __forceinline__ void copy16(uint64_t base, uint32_t off, uint32_t lds) {
+    asm volatile("s_mov_b32 m0, %2\n\t"
+                 "global_load_lds_dwordx4 %0, %1"
+                 :
+                 : "v"(off), "s"(base), "s"(lds)
+                 : "memory", "m0");
+}
+__device__ __forceinline__ void wait_copies() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ uint32_t lds_address(const char* p) {
+    return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p;
+}
+// Barrier for LDS traffic alone: copies and stores to memory may be in flight.
+__device__ __forceinline__ void lds_barrier() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+// Fills a tile of ROWS rows with THREADS threads: row r from the row that `source(r)`
+// names (an offset from `base` in rows).  Copies need rows and their stride aligned
+// to 16 bytes, a head of whole 16-byte units, and ROWS rows within 2^31 bytes;
+// the host says whether that holds (copies_fit).  Units past the head's end repeat
+// its first one: what they meet is zero (queries) or not stored (output columns).
+template <typename T, int DP, int ROWS, int THREADS>
+struct Fill {
+    using Ti = Tile<T, DP>;
+    static constexpr int kRowUnits = Ti::kPitch / 16;
+    static constexpr int kCopies = ROWS * kRowUnits / THREADS;
+    static_assert(ROWS * kRowUnits % THREADS == 0 && THREADS % 64 == 0, "whole copies");
+    template <class Source>
+    static __device__ __forceinline__ void copy(const T* base, int64_t stride, int units, char* lds, int thread, Source source) {
+        const uint64_t from = uniform_address(base);
+        const uint32_t to = __builtin_amdgcn_readfirstlane(lds_address(lds) + (thread & ~63) * 16);
+        const uint32_t step = (uint32_t)stride * (uint32_t)sizeof(T);
+#pragma unroll
+        for (int i = 0; i < kCopies; ++i) {
+            const int at = i * THREADS + thread, row = at / kRowUnits;
+            int unit = (at % kRowUnits) ^ Ti::swz(row);
+            unit = unit < units ? unit : 0;
+            copy16(from, (uint32_t)source(row) * step + unit * 16, to + i * THREADS * 16);
+        }
+    }
+    // the same through registers, any stride and alignment; rows for which `keep` is
+    // false and values past the head's end are 0
+    template <class Keep>
+    static __device__ __forceinline__ void load(const T* base, int64_t stride, int head_dim, char* lds, int thread, Keep keep) {
+        for (int u = thread; u < ROWS * (DP / 8); u += THREADS) {
+            const int row = u / (DP / 8), c = u % (DP / 8);
+            Frag<T> v = {};
+            if (keep(row)) v = load8(base + row * stride + 8 * c, head_dim - 8 * c);
+            Ti::put(lds, row, c, v);
+        }
+    }
+};
+inline bool copies_fit(const void* p, const int64_t* stride, int head_dim, int elem) {
+    for (int i = 0; i < 3; ++i)
+        if (stride[i] * elem % 16) return false;
+    return (uintptr_t)p % 16 == 0 && head_dim * elem % 16 == 0 && stride[1] * elem < (1 << 24);
+}
+
 // ---------------------------------------------------------------- who sees what
 // One sequence: n queries at t = m - n + i, m keys.
 struct Seq {
@@ -168,6 +239,47 @@ __device__ inline See sees_any(const pd_attention_desc& d, const Seq& s, int i0,
     const See a = sees(d, s, i0), b = sees(d, s, i1);
     return See{a.lo, b.hi, b.sk};
 }
+
+// The tiles of BN keys that hold the union `any` of a set of rows: first those of the
+// sinks, then those of the window, each once.
+template <int BN>
+struct KeyTiles {
+    See any;
+    int sinks, first, count;
+    __device__ inline explicit KeyTiles(const See& see) : any(see) {
+        sinks = (any.sk + BN - 1) / BN;
+        first = max(any.lo / BN, sinks);
+        count = sinks + max((any.hi + BN - 1) / BN, first) - first;
+    }
+    __device__ inline int start(int it) const { return (it < sinks ? it : first + it - sinks) * BN; }
+    // every key of the tile at j0 is in the union
+    __device__ inline bool whole(int j0) const { return (j0 >= any.lo && j0 + BN <= any.hi) || j0 + BN <= any.sk; }
+    // a key of the tile at j0 that is in the union: j itself where it is
+    __device__ inline int inside(int j0, int j) const {
+        if (any(j)) return j;
+        const int lo = max(any.lo, j0), hi = min(any.hi, j0 + BN);
+        return lo < hi ? min(max(j, lo), hi - 1) : min(any.sk, j0 + BN) - 1;
+    }
+};
+// What the 64 lanes' rows see between them: the smallest and the largest bounds, so
+// that a tile of keys can be told to be in sight of all rows or of none.
+struct WaveSight {
+    int lo_min, lo_max, hi_min, hi_max, sk_min, sk_max;
+    __device__ inline explicit WaveSight(const See& s) {
+        lo_min = lo_max = s.lo, hi_min = hi_max = s.hi, sk_min = sk_max = s.sk;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            lo_min = min(lo_min, __shfl_xor(lo_min, o)), lo_max = max(lo_max, __shfl_xor(lo_max, o));
+            hi_min = min(hi_min, __shfl_xor(hi_min, o)), hi_max = max(hi_max, __shfl_xor(hi_max, o));
+            sk_min = min(sk_min, __shfl_xor(sk_min, o)), sk_max = max(sk_max, __shfl_xor(sk_max, o));
+        }
+        lo_min = __builtin_amdgcn_readfirstlane(lo_min), lo_max = __builtin_amdgcn_readfirstlane(lo_max);
+        hi_min = __builtin_amdgcn_readfirstlane(hi_min), hi_max = __builtin_amdgcn_readfirstlane(hi_max);
+        sk_min = __builtin_amdgcn_readfirstlane(sk_min), sk_max = __builtin_amdgcn_readfirstlane(sk_max);
+    }
+    __device__ inline bool all(int j0, int n) const { return (j0 >= lo_max && j0 + n <= hi_min) || j0 + n <= sk_min; }
+    __device__ inline bool none(int j0, int n) const { return (j0 >= hi_max || j0 + n <= lo_min) && j0 >= sk_max; }
+};
 
 }  // namespace attn
 }  // namespace pd
