@@ -254,17 +254,12 @@ __device__ __forceinline__ void store_rows(const AttentionArgs& a, const Plan& p
     }
 }
 
-template <typename T, int DP>
-constexpr int keys_per_tile() {
-    return Tile<T, DP>::kPitch <= 256 ? 64 : 32;
-}
-
 // A block: 128 rows of one key head, or one part of their keys.  The next tile of keys
 // and values is copied to LDS while the waves work on the present one.
 template <typename T, int DP, bool COPY>
 __global__ __launch_bounds__(256, 2) void k_attention(const AttentionArgs a, const Plan p) {
     using Ti = Tile<T, DP>;
-    constexpr int BN = keys_per_tile<T, DP>(), kBytes = BN * Ti::kPitch;
+    constexpr int BN = tile_rows<T, DP>(), kBytes = BN * Ti::kPitch;
     using F = Fill<T, DP, BN, 256>;
     __shared__ __align__(128) char lds[4 * kBytes];       // keys, values; twice
     const pd_attention_desc& d = a.d;

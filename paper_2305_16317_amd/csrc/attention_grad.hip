@@ -5,10 +5,11 @@
 //   dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_i ds_ij q_i,  dv_j = sum_i p_ij do_i
 //
 // Two kernels, each summing into its own registers: dq over a block of queries
-// (which also leaves delta for the other), dk and dv over a block of keys and all
+// (which also leaves delta for the other), dk and dv over a block of keys and the
 // query heads that read them.  The scores are formed twice (14 D operations a pair
 // and head in place of 10), and in exchange there is no atomic and no order that
-// varies from run to run.
+// varies from run to run.  Where there are few blocks of keys, their queries are
+// split among several blocks, whose sums k_attention_dkv_join adds.
 #include "attention_tile.h"
 
 namespace pd {
@@ -16,8 +17,6 @@ namespace {
 
 using namespace attn;
 
-constexpr int kBN = 64;          // keys a tile of the dq kernel
-constexpr int kBR = 32;          // rows a tile of the dk, dv kernel
 
 // p = e^(scale s - lse): one fused multiply-add in base 2 while |lse| is under 1024;
 // beyond, where rounding lse log2 e would show, from the difference itself, which
@@ -28,6 +27,13 @@ __device__ inline float probability(bool large, float s, float c2, float lse2, f
     const float x = (s * scale - lse) * kLog2e;
     return exp2_fast(x > 0.f ? 0.f : x);
 }
+
+// Scratch: delta of every row, then the parts of dk and dv, [split][sequence, key
+// head, key][dk, dv].
+__host__ __device__ inline int64_t delta_floats(const pd_attention_desc& d) {
+    return ((int64_t)d.batch * d.heads_q * d.q_len + 3) & ~(int64_t)3;
+}
+__device__ inline float* dkv_parts(const AttentionArgs& a) { return a.scratch + delta_floats(a.d); }
 
 // What the backward kernels read of one (sequence, key head).
 template <typename T>
@@ -124,22 +130,55 @@ __device__ void dkv_row(const AttentionArgs& a, const Views<T>& w, const Seq seq
     }
 }
 
+// blocks of 256 threads a compute unit is to hold: two, where the sums and operands
+// that stay in registers leave room (dq: one sum, two operands; dk, dv: two and two)
 template <typename T, int DP>
-__global__ __launch_bounds__(256) void k_attention_dq(const AttentionArgs a) {
+constexpr int dq_blocks_per_cu() {
+    return sizeof(T) == 2 || DP <= 64 ? 2 : 1;
+}
+template <typename T, int DP>
+constexpr int dkv_blocks_per_cu() {
+    return DP * (int)sizeof(T) <= 128 ? 2 : 1;
+}
+
+template <typename T, int DP, bool COPY>
+__global__ __launch_bounds__(256, (dq_blocks_per_cu<T, DP>())) void k_attention_dq(const AttentionArgs a, int row_tiles) {
     using Ti = Tile<T, DP>;
-    constexpr int kSteps = DP / 16, kDT = DP / 32;
-    __shared__ __align__(16) char lds_k[kBN * Ti::kPitch];
-    __shared__ __align__(16) char lds_v[kBN * Ti::kPitch];
+    constexpr int kSteps = DP / 16, kDT = DP / 32, BN = tile_rows<T, DP>(), kBytes = BN * Ti::kPitch;
+    using F = Fill<T, DP, BN, 256>;
+    __shared__ __align__(128) char lds[4 * kBytes];       // keys, values; twice
     const pd_attention_desc& d = a.d;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
-    const int b = blockIdx.z, hk = blockIdx.y;
+    const int tile = row_tiles - 1 - blockIdx.x % row_tiles, head = blockIdx.x / row_tiles;
+    const int hk = head % d.heads_kv, b = head / d.heads_kv;
     const Seq seq = sequence(a, b);
     const Views<T> w = views<T>(a, b, hk);
     const int rows_all = d.q_len * w.group;
-    const int row0 = blockIdx.x * 128 + wave * 32, row = row0 + (lane & 31);
+    const int row0 = tile * 128 + wave * 32, row = row0 + (lane & 31);
     const bool real = row < rows_all;
     const int qi = real ? row / w.group : 0, g = row % w.group;
     const See see = real ? sees(d, seq, qi) : See{0, 0, 0};
+    const WaveSight sight(see);
+
+    const int i0 = tile * 128 / w.group, i1 = min((tile * 128 + 127) / w.group, seq.n - 1);
+    const KeyTiles<BN> tiles(i0 <= i1 ? sees_any(d, seq, i0, i1) : See{0, 0, 0});
+    const int units = d.head_dim * (int)sizeof(T) / 16;
+    auto fetch = [&](int it, int buf) {
+        const int j0 = tiles.start(it);
+        const T* kt = w.k + (int64_t)j0 * d.k_stride[1];
+        const T* vt = w.v + (int64_t)j0 * d.v_stride[1];
+        char* to = lds + buf * 2 * kBytes;
+        if constexpr (COPY) {
+            auto from = [&](int r) { return tiles.inside(j0, j0 + r) - j0; };
+            F::copy(kt, d.k_stride[1], units, to, threadIdx.x, from);
+            F::copy(vt, d.v_stride[1], units, to + kBytes, threadIdx.x, from);
+        } else {
+            auto keep = [&](int r) { return tiles.any(j0 + r); };
+            F::load(kt, d.k_stride[1], d.head_dim, to, threadIdx.x, keep);
+            F::load(vt, d.v_stride[1], d.head_dim, to + kBytes, threadIdx.x, keep);
+        }
+    };
+    if (tiles.count > 0) fetch(0, 0);
 
     Frag<T> qf[kSteps], gf[kSteps];
     float delta = 0.f;
@@ -162,48 +201,41 @@ __global__ __launch_bounds__(256) void k_attention_dq(const AttentionArgs a) {
     const float lse = see.none() ? 0.f : w.lse[at], lse2 = lse * kLog2e;
     const bool large = __any(!(fabsf(lse) < kLarge));
 
-    const int i0 = blockIdx.x * 128 / w.group, i1 = min((blockIdx.x * 128 + 127) / w.group, seq.n - 1);
-    See any{0, 0, 0};
-    if (i0 <= i1) any = sees_any(d, seq, i0, i1);
-    const int sink_tiles = (any.sk + kBN - 1) / kBN;
-    const int first = max(any.lo / kBN, sink_tiles), end = max((any.hi + kBN - 1) / kBN, first);
-    const int tiles = sink_tiles + end - first;
-
     f32x16 o[kDT];
 #pragma unroll
     for (int t = 0; t < kDT; ++t) o[t] = f32x16{};
-    for (int it = 0; it < tiles; ++it) {
-        const int j0 = (it < sink_tiles ? it : first + it - sink_tiles) * kBN;
-        __syncthreads();
-        for (int u = threadIdx.x; u < kBN * (DP / 8); u += 256) {
-            const int r = u / (DP / 8), c = u % (DP / 8), j = j0 + r;
-            Frag<T> kv = {}, vv = {};
-            if (any(j)) {
-                kv = load8(w.k + (int64_t)j * d.k_stride[1] + 8 * c, d.head_dim - 8 * c);
-                vv = load8(w.v + (int64_t)j * d.v_stride[1] + 8 * c, d.head_dim - 8 * c);
-            }
-            Ti::put(lds_k, r, c, kv);
-            Ti::put(lds_v, r, c, vv);
-        }
-        __syncthreads();
+    for (int it = 0; it < tiles.count; ++it) {
+        const int j0 = tiles.start(it);
+        if constexpr (COPY) wait_copies();
+        lds_barrier();                                    // this tile is there, the other buffer is free
+        if (it + 1 < tiles.count) fetch(it + 1, (it + 1) & 1);
+        if (sight.none(j0, BN)) continue;
+        const bool edge = !sight.all(j0, BN);
+        const char *lk = lds + (it & 1) * 2 * kBytes, *lv = lk + kBytes;
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt) {
+        for (int kt = 0; kt < BN / 32; ++kt) {
             f32x16 s = {}, dp = {};
 #pragma unroll
-            for (int c = 0; c < kSteps; ++c) {
-                s = mma(Ti::rows(lds_k, 32 * kt, c, lane), qf[c], s);
-                dp = mma(Ti::rows(lds_v, 32 * kt, c, lane), gf[c], dp);
-            }
+            for (int c = 0; c < kSteps; ++c) s = mma(Ti::rows(lk, 32 * kt, c, lane), qf[c], s);
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const float p = probability(large, s[r], c2, lse2, d.scale, lse);
-                s[r] = see(j0 + 32 * kt + tile_row(lane, r)) ? p * (dp[r] - delta) : 0.f;
+            for (int c = 0; c < kSteps; ++c) dp = mma(Ti::rows(lv, 32 * kt, c, lane), gf[c], dp);
+            if (large) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[r] = probability(true, s[r], c2, lse2, d.scale, lse) * (dp[r] - delta);
+            } else {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[r] = probability(false, s[r], c2, lse2, d.scale, lse) * (dp[r] - delta);
+            }
+            if (edge) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (!see(j0 + 32 * kt + tile_row(lane, r))) s[r] = 0.f;
             }
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
                 const Frag<T> ds = as_frag<T>(s, c);
 #pragma unroll
-                for (int t = 0; t < kDT; ++t) o[t] = mma(Ti::cols(lds_k, 32 * kt + 16 * c, t, lane), ds, o[t]);
+                for (int t = 0; t < kDT; ++t) o[t] = mma(Ti::cols(lk, 32 * kt + 16 * c, t, lane), ds, o[t]);
             }
         }
     }
@@ -236,22 +268,84 @@ __global__ __launch_bounds__(256) void k_attention_dq(const AttentionArgs a) {
     }
 }
 
-template <typename T, int DP>
-__global__ __launch_bounds__(256) void k_attention_dkv(const AttentionArgs a) {
+// The queries that see key j: lo <= i < hi.
+__device__ inline See seen_by(const pd_attention_desc& d, const Seq& s, int j) {
+    if (j >= s.m) return See{0, 0, 0};
+    const int off = s.m - s.n;                            // t = off + i
+    int lo = 0, hi = s.n;
+    if (d.causal) lo = max(lo, j - off);
+    if (d.window && j >= d.sinks) {
+        hi = min(hi, j + d.window - off);
+        if (!d.causal) lo = max(lo, j - d.window + 1 - off);
+    }
+    return See{lo, max(hi, lo), 0};
+}
+
+// A block: 128 keys of one key head, 32 a wave, and the tiles of queries of the group's
+// heads that see any of them, or one part of these.
+template <typename T, int DP, bool COPY>
+__global__ __launch_bounds__(256, (dkv_blocks_per_cu<T, DP>())) void k_attention_dkv(const AttentionArgs a, int key_tiles,
+                                                                                   int splits) {
     using Ti = Tile<T, DP>;
-    constexpr int kSteps = DP / 16, kDT = DP / 32;
-    __shared__ __align__(16) char lds_q[kBR * Ti::kPitch];
-    __shared__ __align__(16) char lds_g[kBR * Ti::kPitch];
-    __shared__ __align__(16) float lds_lse[kBR], lds_delta[kBR];
-    __shared__ __align__(16) See lds_see[kBR];
-    __shared__ bool lds_large;
+    constexpr int kSteps = DP / 16, kDT = DP / 32, BR = tile_rows<T, DP>(), kBytes = BR * Ti::kPitch;
+    using F = Fill<T, DP, BR, 256>;
+    __shared__ __align__(128) char lds[4 * kBytes];       // queries, output gradients; twice
+    __shared__ __align__(16) float stats[2][3][64];       // lse log2 e, delta, lse
     const pd_attention_desc& d = a.d;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
-    const int b = blockIdx.z, hk = blockIdx.y;
+    const int split = blockIdx.x % splits, unit = blockIdx.x / splits;
+    const int tile = unit % key_tiles, head = unit / key_tiles;
+    const int hk = head % d.heads_kv, b = head / d.heads_kv;
     const Seq seq = sequence(a, b);
     const Views<T> w = views<T>(a, b, hk);
-    const int key0 = blockIdx.x * 128, wkey0 = key0 + wave * 32, key = wkey0 + (lane & 31);
+    const int key0 = tile * 128, wkey0 = key0 + wave * 32, key = wkey0 + (lane & 31);
     const bool live = key < seq.m;
+    const See see = seen_by(d, seq, key);
+    const WaveSight sight(see);
+
+    // the block's queries: from the first that sees its first key (two-sided: its earliest)
+    // to the last that sees its last, or a sink among them
+    const int k1 = min(key0 + 127, seq.m - 1);
+    int first = 0, last = 0;
+    if (key0 < seq.m) {
+        first = min(seen_by(d, seq, key0).lo, seen_by(d, seq, k1).lo);
+        last = max(seen_by(d, seq, key0).hi, seen_by(d, seq, k1).hi);
+    }
+    const int per_head = last > first ? (last - first + BR - 1) / BR : 0, all = per_head * w.group;
+    const int each = (all + splits - 1) / splits, x0 = split * each, x1 = min(all, x0 + each);
+    const int units = d.head_dim * (int)sizeof(T) / 16;
+    float stat = 0.f;
+    auto fetch = [&](int x, int buf) {
+        const int g = x / per_head, i0 = first + (x - g * per_head) * BR;
+        if (threadIdx.x < 2 * BR) {
+            const int i = min(i0 + (int)threadIdx.x % BR, seq.n - 1);
+            stat = (threadIdx.x < BR ? w.lse : w.delta)[(int64_t)g * d.q_len + i];
+        }
+        const T* qt = w.q + (int64_t)i0 * d.q_stride[1] + g * d.q_stride[2];
+        const T* gt = w.dout + (int64_t)i0 * d.dout_stride[1] + g * d.dout_stride[2];
+        char* to = lds + buf * 2 * kBytes;
+        if constexpr (COPY) {
+            auto from = [&](int r) { return min(i0 + r, seq.n - 1) - i0; };
+            F::copy(qt, d.q_stride[1], units, to, threadIdx.x, from);
+            F::copy(gt, d.dout_stride[1], units, to + kBytes, threadIdx.x, from);
+        } else {
+            auto keep = [&](int r) { return i0 + r < seq.n; };
+            F::load(qt, d.q_stride[1], d.head_dim, to, threadIdx.x, keep);
+            F::load(gt, d.dout_stride[1], d.head_dim, to + kBytes, threadIdx.x, keep);
+        }
+    };
+    auto put_stat = [&](int buf) {
+        if (threadIdx.x < BR) {
+            stats[buf][0][threadIdx.x] = stat * kLog2e;
+            stats[buf][2][threadIdx.x] = stat;
+        } else if (threadIdx.x < 2 * BR) {
+            stats[buf][1][threadIdx.x - BR] = stat;
+        }
+    };
+    if (x0 < x1) {
+        fetch(x0, 0);
+        put_stat(0);
+    }
 
     Frag<T> kf[kSteps], vf[kSteps];
 #pragma unroll
@@ -263,87 +357,90 @@ __global__ __launch_bounds__(256) void k_attention_dkv(const AttentionArgs a) {
         kf[c] = load8(w.k + (int64_t)key * d.k_stride[1] + e, d.head_dim - e);
         vf[c] = load8(w.v + (int64_t)key * d.v_stride[1] + e, d.head_dim - e);
     }
-    // the queries that may see a key of the block: first .. last
-    const int k1 = min(key0 + 127, seq.m - 1), off = seq.m - seq.n;      // t = off + i
-    int first = 0, last = key0 < seq.m ? seq.n - 1 : -1;
-    if (d.causal) first = max(first, key0 - off);
-    if (d.window && key0 >= d.sinks) {
-        last = min(last, k1 + d.window - 1 - off);
-        if (!d.causal) first = max(first, key0 - d.window + 1 - off);
-    }
     const float c2 = d.scale * kLog2e;
     f32x16 dk[kDT], dv[kDT];
 #pragma unroll
     for (int t = 0; t < kDT; ++t) dk[t] = dv[t] = f32x16{};
-    const int r_end = (last + 1) * w.group;
-    for (int r0 = first * w.group; r0 < r_end; r0 += kBR) {
-        __syncthreads();
-        for (int u = threadIdx.x; u < kBR * (DP / 8); u += 256) {
-            const int r = u / (DP / 8), c = u % (DP / 8), row = r0 + r;
-            Frag<T> qv = {}, gv = {};
-            if (row < r_end) {
-                const int i = row / w.group, g = row % w.group;
-                if (!sees(d, seq, i).none()) {
-                    qv = load8(w.q + i * d.q_stride[1] + g * d.q_stride[2] + 8 * c, d.head_dim - 8 * c);
-                    gv = load8(w.dout + i * d.dout_stride[1] + g * d.dout_stride[2] + 8 * c, d.head_dim - 8 * c);
+    for (int x = x0; x < x1; ++x) {
+        const int buf = (x - x0) & 1, i0 = first + x % per_head * BR;
+        if constexpr (COPY) wait_copies();
+        lds_barrier();                                    // this tile is there, the other buffer is free
+        if (x + 1 < x1) fetch(x + 1, buf ^ 1);
+        if (!sight.none(i0, BR)) {
+            const bool edge = !sight.all(i0, BR);
+            const char *lq = lds + buf * 2 * kBytes, *lg = lq + kBytes;
+#pragma unroll
+            for (int rt = 0; rt < BR / 32; ++rt) {
+                f32x16 s = {}, dp = {};
+#pragma unroll
+                for (int c = 0; c < kSteps; ++c) s = mma(Ti::rows(lq, 32 * rt, c, lane), kf[c], s);
+#pragma unroll
+                for (int c = 0; c < kSteps; ++c) dp = mma(Ti::rows(lg, 32 * rt, c, lane), vf[c], dp);
+                float l2[16], dl[16];
+                bool large = false;
+#pragma unroll
+                for (int r = 0; r < 16; r += 4) {
+                    const int at = 32 * rt + tile_row(lane, r);
+                    const f32x4 x4 = *reinterpret_cast<const f32x4*>(&stats[buf][0][at]);
+                    const f32x4 y4 = *reinterpret_cast<const f32x4*>(&stats[buf][1][at]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        l2[r + e] = x4[e];
+                        dl[r + e] = y4[e];
+                        large = large || !(fabsf(x4[e]) < kLarge);
+                    }
+                }
+                if (__any(large)) {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        s[r] = probability(true, s[r], c2, l2[r], d.scale, stats[buf][2][32 * rt + tile_row(lane, r)]);
+                } else {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[r] = probability(false, s[r], c2, l2[r], d.scale, 0.f);
+                }
+#pragma unroll
+                for (int r = 0; r < 16; ++r) dp[r] = s[r] * (dp[r] - dl[r]);
+                if (edge) {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (!see(i0 + 32 * rt + tile_row(lane, r))) s[r] = dp[r] = 0.f;
+                }
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    const Frag<T> p = as_frag<T>(s, c), ds = as_frag<T>(dp, c);
+#pragma unroll
+                    for (int t = 0; t < kDT; ++t) {
+                        dv[t] = mma(Ti::cols(lg, 32 * rt + 16 * c, t, lane), p, dv[t]);
+                        dk[t] = mma(Ti::cols(lq, 32 * rt + 16 * c, t, lane), ds, dk[t]);
+                    }
                 }
             }
-            Ti::put(lds_q, r, c, qv);
-            Ti::put(lds_g, r, c, gv);
         }
-        if (threadIdx.x < kBR) {
-            const int row = r0 + threadIdx.x;
-            See see{0, 0, 0};
-            float lse = 0.f, delta = 0.f;
-            if (row < r_end) {
-                const int i = row / w.group, g = row % w.group;
-                see = sees(d, seq, i);
-                if (!see.none()) {
-                    lse = w.lse[(int64_t)g * d.q_len + i];
-                    delta = w.delta[(int64_t)g * d.q_len + i];
-                }
-            }
-            lds_see[threadIdx.x] = see;
-            lds_lse[threadIdx.x] = lse;
-            lds_delta[threadIdx.x] = delta;
-            const uint64_t far = __ballot(!(fabsf(lse) < kLarge));
-            if (threadIdx.x == 0) lds_large = far != 0;
-        }
-        __syncthreads();
-        const bool large = lds_large;
-        f32x16 s = {}, dp = {};
-#pragma unroll
-        for (int c = 0; c < kSteps; ++c) {
-            s = mma(Ti::rows(lds_q, 0, c, lane), kf[c], s);
-            dp = mma(Ti::rows(lds_g, 0, c, lane), vf[c], dp);
-        }
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int row = tile_row(lane, r);
-            const bool seen = live && lds_see[row](key);
-            const float lse = lds_lse[row];
-            const float p = probability(large, s[r], c2, lse * kLog2e, d.scale, lse);
-            s[r] = seen ? p : 0.f;
-            dp[r] = seen ? p * (dp[r] - lds_delta[row]) : 0.f;
-        }
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-            const Frag<T> p = as_frag<T>(s, c), ds = as_frag<T>(dp, c);
-#pragma unroll
-            for (int t = 0; t < kDT; ++t) {
-                dv[t] = mma(Ti::cols(lds_g, 16 * c, t, lane), p, dv[t]);
-                dk[t] = mma(Ti::cols(lds_q, 16 * c, t, lane), ds, dk[t]);
-            }
-        }
+        if (x + 1 < x1) put_stat(buf ^ 1);
     }
 
+#pragma unroll
+    for (int t = 0; t < kDT; ++t) dk[t] *= d.scale;
+    if (splits > 1) {
+        if (key >= d.kv_len) return;
+        const int64_t keys = (int64_t)d.batch * d.heads_kv * d.kv_len, kat = ((int64_t)b * d.heads_kv + hk) * d.kv_len + key;
+        float* to = dkv_parts(a) + (split * keys + kat) * 2 * d.head_dim;
+#pragma unroll
+        for (int t = 0; t < kDT; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int e = 32 * t + 8 * r + 4 * h;
+                store4(to + e, d.head_dim - e, f32x4{dk[t][4 * r], dk[t][4 * r + 1], dk[t][4 * r + 2], dk[t][4 * r + 3]});
+                store4(to + d.head_dim + e, d.head_dim - e,
+                       f32x4{dv[t][4 * r], dv[t][4 * r + 1], dv[t][4 * r + 2], dv[t][4 * r + 3]});
+            }
+        return;
+    }
     bool odd = false;
 #pragma unroll
-    for (int t = 0; t < kDT; ++t) {
-        dk[t] *= d.scale;
+    for (int t = 0; t < kDT; ++t)
 #pragma unroll
         for (int r = 0; r < 16; ++r) odd = odd || !(fabsf(dk[t][r]) < INFINITY) || !(fabsf(dv[t][r]) < INFINITY);
-    }
     T* dkp = static_cast<T*>(a.dk) + b * d.dk_stride[0] + hk * d.dk_stride[2];
     T* dvp = static_cast<T*>(a.dv) + b * d.dv_stride[0] + hk * d.dv_stride[2];
     const uint64_t both = __ballot(odd && live);
@@ -370,18 +467,76 @@ __global__ __launch_bounds__(256) void k_attention_dkv(const AttentionArgs a) {
     }
 }
 
-template <typename T, int DP>
-void attention_grad_t(const AttentionArgs& a, hipStream_t s) {
-    const int64_t rows = (int64_t)a.d.q_len * (a.d.heads_q / a.d.heads_kv);
+// The parts of a key's dk and dv into the result: one wave a key.
+template <typename T>
+__global__ __launch_bounds__(256) void k_attention_dkv_join(const AttentionArgs a, int splits) {
+    const pd_attention_desc& d = a.d;
+    const int lane = threadIdx.x & 63, D = d.head_dim;
+    const int64_t keys = (int64_t)d.batch * d.heads_kv * d.kv_len, kat = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (kat >= keys) return;
+    const int j = (int)(kat % d.kv_len), hk = (int)(kat / d.kv_len % d.heads_kv), b = (int)(kat / d.kv_len / d.heads_kv);
+    const Seq seq = sequence(a, b);
+    const bool live = j < seq.m;
+    float v[4] = {0.f, 0.f, 0.f, 0.f};                    // dk, dv at lane; at lane + 64
+    bool odd = false;
+    if (live)
+        for (int s = 0; s < splits; ++s) {
+            const float* from = dkv_parts(a) + (s * keys + kat) * 2 * D;
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+                if (lane + 64 * half < D) {
+                    v[2 * half] += from[lane + 64 * half];
+                    v[2 * half + 1] += from[D + lane + 64 * half];
+                }
+        }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) odd = odd || !(fabsf(v[i]) < INFINITY);
+    T* dk = static_cast<T*>(a.dk) + b * d.dk_stride[0] + hk * d.dk_stride[2] + j * d.dk_stride[1];
+    T* dv = static_cast<T*>(a.dv) + b * d.dv_stride[0] + hk * d.dv_stride[2] + j * d.dv_stride[1];
+    if (__any(odd)) return dkv_row(a, views<T>(a, b, hk), seq, j, dk, dv);
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
+        if (lane + 64 * half < D) {
+            dk[lane + 64 * half] = (T)v[2 * half];
+            dv[lane + 64 * half] = (T)v[2 * half + 1];
+        }
+}
+
+// Parts of the dk, dv kernel's queries: enough that its blocks fill the chip twice (two
+// fit a compute unit), and of at least four tiles.
+int dkv_splits(const pd_attention_desc& d) {
+    const int64_t blocks = ((int64_t)d.kv_len + 127) / 128 * d.heads_kv * d.batch;
+    const int64_t tiles = ((int64_t)d.q_len + 63) / 64 * (d.heads_q / d.heads_kv);
+    int64_t s = blocks >= 512 ? 1 : (1024 + blocks - 1) / blocks;
+    if (s > tiles / 4) s = tiles / 4;
+    return s < 1 ? 1 : (int)s;
+}
+
+template <typename T, int DP, bool COPY>
+void attention_grad_c(const AttentionArgs& a, hipStream_t s) {
+    const int64_t rows = (int64_t)a.d.q_len * (a.d.heads_q / a.d.heads_kv), heads = (int64_t)a.d.heads_kv * a.d.batch;
+    const int row_tiles = (int)((rows + 127) / 128), key_tiles = (int)(((int64_t)a.d.kv_len + 127) / 128);
     if (rows) {
-        hipLaunchKernelGGL((k_attention_dq<T, DP>), dim3((unsigned)((rows + 127) / 128), a.d.heads_kv, a.d.batch), dim3(256),
-                           0, s, a);
+        hipLaunchKernelGGL((k_attention_dq<T, DP, COPY>), dim3((unsigned)(row_tiles * heads)), dim3(256), 0, s, a, row_tiles);
         PD_HIP(hipGetLastError());
     }
     if (!a.d.kv_len) return;
-    hipLaunchKernelGGL((k_attention_dkv<T, DP>), dim3((unsigned)(((int64_t)a.d.kv_len + 127) / 128), a.d.heads_kv, a.d.batch),
-                       dim3(256), 0, s, a);
+    const int splits = dkv_splits(a.d);
+    hipLaunchKernelGGL((k_attention_dkv<T, DP, COPY>), dim3((unsigned)(key_tiles * heads * splits)), dim3(256), 0, s, a, key_tiles,
+                       splits);
     PD_HIP(hipGetLastError());
+    if (splits == 1) return;
+    hipLaunchKernelGGL((k_attention_dkv_join<T>), dim3((unsigned)((heads * a.d.kv_len + 3) / 4)), dim3(256), 0, s, a, splits);
+    PD_HIP(hipGetLastError());
+}
+template <typename T, int DP>
+void attention_grad_t(const AttentionArgs& a, hipStream_t s) {
+    const pd_attention_desc& d = a.d;
+    if (copies_fit(a.k, d.k_stride, d.head_dim, sizeof(T)) && copies_fit(a.v, d.v_stride, d.head_dim, sizeof(T)) &&
+        copies_fit(a.q, d.q_stride, d.head_dim, sizeof(T)) && copies_fit(a.dout, d.dout_stride, d.head_dim, sizeof(T)))
+        attention_grad_c<T, DP, true>(a, s);
+    else
+        attention_grad_c<T, DP, false>(a, s);
 }
 template <typename T>
 void attention_grad_dim(const AttentionArgs& a, hipStream_t s) {
@@ -394,7 +549,9 @@ void attention_grad_dim(const AttentionArgs& a, hipStream_t s) {
 }  // namespace
 
 int64_t attention_grad_scratch_bytes(const pd_attention_desc& d) {
-    return (int64_t)d.batch * d.heads_q * d.q_len * (int64_t)sizeof(float);      // delta
+    const int splits = dkv_splits(d);
+    const int64_t parts = splits == 1 ? 0 : (int64_t)splits * d.batch * d.heads_kv * d.kv_len * 2 * d.head_dim;
+    return (delta_floats(d) + parts) * (int64_t)sizeof(float);
 }
 
 void launch_attention_grad(const AttentionArgs& a, hipStream_t s) {

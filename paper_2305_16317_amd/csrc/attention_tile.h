@@ -281,5 +281,11 @@ struct WaveSight {
     __device__ inline bool none(int j0, int n) const { return (j0 >= hi_max || j0 + n <= lo_min) && j0 >= sk_max; }
 };
 
+// rows of a shared tile: two buffers of two tiles stay within half a compute unit's LDS
+template <typename T, int DP>
+constexpr int tile_rows() {
+    return Tile<T, DP>::kPitch <= 256 ? 64 : 32;
+}
+
 }  // namespace attn
 }  // namespace pd
