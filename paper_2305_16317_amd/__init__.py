@@ -179,8 +179,14 @@ def _check(code: int) -> None:
         raise PdError(code, load().pd_last_error().decode())
 
 
+# the current stream's handle without a Stream object around it (2.6 us a call less), where torch has it
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream) -> ctypes.c_void_p:
     if stream is None:
+        if _raw_stream is not None:
+            return ctypes.c_void_p(_raw_stream(torch.cuda.current_device()))
         return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
     if isinstance(stream, torch.cuda.Stream):
         return ctypes.c_void_p(stream.cuda_stream)
@@ -394,10 +400,12 @@ def _dtype(t: torch.Tensor) -> int:
     return d
 
 
-def _on_gpu(*tensors) -> None:
-    dev = torch.cuda.current_device() if torch.cuda.is_available() else -1
-    for t in tensors:
-        if t is not None and (not t.is_cuda or t.device.index != dev):
+def _on_gpu(first: torch.Tensor, *others) -> None:
+    dev = first.get_device()                     # -1 on the host
+    if dev < 0 or dev != torch.cuda.current_device():
+        raise ValueError("tensors must be on the current GPU")
+    for t in others:
+        if t is not None and t.get_device() != dev:
             raise ValueError("tensors must be on the current GPU")
 
 
@@ -434,9 +442,9 @@ def _strides(t: torch.Tensor, shape, dtype, what: str):
 
 def _written(t: torch.Tensor, what: str) -> None:
     """An output whose elements share memory (an expanded view) has no result."""
-    for n, s in zip(t.shape, t.stride()):
-        if s == 0 and n > 1:
-            raise ValueError(f"{what} is an output and must not be an expanded view")
+    st = t.stride()
+    if 0 in st and any(s == 0 and n > 1 for n, s in zip(t.shape, st)):
+        raise ValueError(f"{what} is an output and must not be an expanded view")
 
 
 def _scratch(given: Optional[torch.Tensor], need: int, stream):

@@ -198,6 +198,7 @@ struct Plan {
     int row_tiles;             // of 128 rows, or of 32
     int splits, split_tiles;   // parts of the key tiles, and the tiles of each
     int64_t units;             // row tiles over all key heads and sequences
+    int waves;                 // few rows: waves that share a part's tiles
 };
 
 template <typename T, int DP>
@@ -316,15 +317,27 @@ __global__ __launch_bounds__(256, 2) void k_attention(const AttentionArgs a, con
     store_rows(a, p, w, seq, b, hk, row0, split, kb, vb);
 }
 
-// A block of one wave: 32 rows of one key head, or one part of their keys.
-template <typename T, int DP, bool COPY>
-__global__ __launch_bounds__(64) void k_attention_few(const AttentionArgs a, const Plan p) {
+// Waves that share the keys of at most 32 rows, each with two buffers of its own.
+template <typename T, int DP>
+constexpr int few_waves() {
+    return 131072 / (4 * 32 * Tile<T, DP>::kPitch) < 8 ? 131072 / (4 * 32 * Tile<T, DP>::kPitch) : 8;
+}
+
+// A block: 32 rows of one key head, or one part of their keys.  Each of its W waves
+// streams every W-th tile of keys through buffers of its own, with no barrier, and the
+// waves' sums are joined in LDS.
+template <typename T, int DP, bool COPY, int W>
+__global__ __launch_bounds__(64 * W) void k_attention_few(const AttentionArgs a, const Plan p) {
     using Ti = Tile<T, DP>;
-    constexpr int BN = 32, kBytes = BN * Ti::kPitch;
+    constexpr int BN = 32, kBytes = BN * Ti::kPitch, kPart = DP + 4;      // floats of a row's part
     using F = Fill<T, DP, BN, 64>;
-    __shared__ __align__(128) char lds[(COPY ? 4 : 2) * kBytes];
+    static_assert(BN * kPart * 4 <= 4 * kBytes, "a wave's sums fit its buffers");
+    __shared__ __align__(128) char lds_all[W][4 * kBytes];
+    __shared__ float stats[W][2][32];
+    __shared__ int redo[32];
     const pd_attention_desc& d = a.d;
-    const int lane = threadIdx.x;
+    const int lane = threadIdx.x & 63, wave = W == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    char* lds = lds_all[wave];
     const int split = blockIdx.x % p.splits, head = blockIdx.x / p.splits;   // one row tile a key head
     const int hk = head % d.heads_kv, b = head / d.heads_kv;
     const Seq seq = sequence(a, b);
@@ -336,34 +349,40 @@ __global__ __launch_bounds__(64) void k_attention_few(const AttentionArgs a, con
     const T* kb = static_cast<const T*>(a.k) + b * d.k_stride[0] + hk * d.k_stride[2];
     const T* vb = static_cast<const T*>(a.v) + b * d.v_stride[0] + hk * d.v_stride[2];
 
-    Rows<T, DP> w;
-    w.start(d, static_cast<const T*>(a.q) + b * d.q_stride[0] + qi * d.q_stride[1] + hq * d.q_stride[2], real && !see.none(), lane);
     const KeyTiles<BN> tiles(seq.n > 0 ? sees_any(d, seq, 0, seq.n - 1) : See{0, 0, 0});
-    const int it0 = split * p.split_tiles, it1 = min(tiles.count, it0 + p.split_tiles);
+    const int it0 = split * p.split_tiles + wave, it1 = min(tiles.count, split * p.split_tiles + p.split_tiles);
     const int units = d.head_dim * (int)sizeof(T) / 16;
     auto fetch = [&](int it, char* to) {
         const int j0 = tiles.start(it);
         const T* kt = kb + (int64_t)j0 * d.k_stride[1];
         const T* vt = vb + (int64_t)j0 * d.v_stride[1];
         if constexpr (COPY) {
-            auto from = [&](int r) { return tiles.inside(j0, j0 + r) - j0; };
-            F::copy(kt, d.k_stride[1], units, to, lane, from);
-            F::copy(vt, d.v_stride[1], units, to + kBytes, lane, from);
+            if (tiles.whole(j0)) {
+                F::copy(kt, d.k_stride[1], units, to, lane, [](int r) { return r; });
+                F::copy(vt, d.v_stride[1], units, to + kBytes, lane, [](int r) { return r; });
+            } else {
+                auto from = [&](int r) { return tiles.inside(j0, j0 + r) - j0; };
+                F::copy(kt, d.k_stride[1], units, to, lane, from);
+                F::copy(vt, d.v_stride[1], units, to + kBytes, lane, from);
+            }
         } else {
             auto keep = [&](int r) { return tiles.any(j0 + r); };
             F::load(kt, d.k_stride[1], d.head_dim, to, lane, keep);
             F::load(vt, d.v_stride[1], d.head_dim, to + kBytes, lane, keep);
         }
     };
+    if (COPY && it0 < it1) fetch(it0, lds);
+    Rows<T, DP> w;
+    w.start(d, static_cast<const T*>(a.q) + b * d.q_stride[0] + qi * d.q_stride[1] + hq * d.q_stride[2], real && !see.none(), lane);
     if constexpr (COPY) {
-        if (it0 < it1) fetch(it0, lds);
-        for (int it = it0; it < it1; ++it) {
-            const int buf = (it - it0) & 1, j0 = tiles.start(it);
+        int buf = 0;
+        for (int it = it0; it < it1; it += W, buf ^= 1) {
+            const int j0 = tiles.start(it);
             // the wave's reads of the other buffer are done (their values were used), so
             // the next tile may go there; then all copies but the next tile's have landed
-            if (it + 1 < it1) {
+            if (it + W < it1) {
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-                fetch(it + 1, lds + (buf ^ 1) * 2 * kBytes);
+                fetch(it + W, lds + (buf ^ 1) * 2 * kBytes);
                 asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * F::kCopies) : "memory");
             } else {
                 wait_copies();
@@ -374,7 +393,7 @@ __global__ __launch_bounds__(64) void k_attention_few(const AttentionArgs a, con
             __builtin_amdgcn_wave_barrier();
         }
     } else {
-        for (int it = it0; it < it1; ++it) {
+        for (int it = it0; it < it1; it += W) {
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             fetch(it, lds);
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -382,7 +401,77 @@ __global__ __launch_bounds__(64) void k_attention_few(const AttentionArgs a, con
             w.template attend<1>(lds, lds + kBytes, j0, see, !sight.all(j0, BN), lane);
         }
     }
-    store_rows(a, p, w, seq, b, hk, 0, split, kb, vb);
+    if constexpr (W == 1) {
+        store_rows(a, p, w, seq, b, hk, 0, split, kb, vb);
+    } else {
+        w.finish();
+        if (lane < 32) {
+            stats[wave][0][row] = w.top;
+            stats[wave][1][row] = w.total;
+            redo[row] = 0;
+        }
+        __syncthreads();
+        // each wave's sums go to the largest reference of one that has terms
+        float top = -INFINITY, total = 0.f;
+#pragma unroll
+        for (int i = 0; i < W; ++i)
+            if (stats[i][1][row] != 0.f) top = fmaxf(top, stats[i][0][row]);
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            const float t = stats[i][1][row], m = stats[i][0][row];
+            if (t != 0.f) total = fmaf(m == top ? 1.f : exp2_fast((m - top) * w.c2), t, total);
+        }
+        const float f = w.total == 0.f ? 0.f : w.top == top ? 1.f : exp2_fast((w.top - top) * w.c2);
+        float* mine = reinterpret_cast<float*>(lds) + row * kPart;
+#pragma unroll
+        for (int t = 0; t < w.kDT; ++t)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                f32x4 v = {w.o[t][4 * g], w.o[t][4 * g + 1], w.o[t][4 * g + 2], w.o[t][4 * g + 3]};
+                v = w.total == 0.f ? f32x4{} : v * f;
+                *reinterpret_cast<f32x4*>(mine + 32 * t + 8 * g + 4 * (lane >> 5)) = v;
+            }
+        const int64_t rows_all = (int64_t)d.batch * d.heads_q * d.q_len, at = ((int64_t)b * d.heads_q + hq) * d.q_len + qi;
+        const Parts to = parts(d, a.scratch, p.splits);
+        if (wave == 0 && lane < 32 && real) {
+            if (p.splits > 1) {
+                to.stats[2 * (split * rows_all + at)] = top;
+                to.stats[2 * (split * rows_all + at) + 1] = total;
+            } else if (a.lse) {
+                a.lse[at] = log_sum(top, fabsf(d.scale), total);
+            }
+        }
+        if (wave == 0 && lane < 32) stats[0][1][row] = total;      // (read by all above; the barrier below orders it)
+        __syncthreads();
+        for (int u = threadIdx.x; u < p.rows * (DP / 4); u += 64 * W) {
+            const int r = u / (DP / 4), e = u % (DP / 4) * 4;
+            if (e >= d.head_dim) continue;
+            f32x4 v = {};
+#pragma unroll
+            for (int i = 0; i < W; ++i) v += *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(lds_all[i]) + r * kPart + e);
+            const int i = r / p.group, hh = hk * p.group + r % p.group;
+            if (p.splits > 1) {
+                const int64_t ra = ((int64_t)b * d.heads_q + hh) * d.q_len + i;
+                store4(to.sums + (split * rows_all + ra) * d.head_dim + e, d.head_dim - e, v);
+                continue;
+            }
+            const float t = stats[0][1][r];
+            v = t == 0.f ? f32x4{} : v * (1.f / t);
+            store4(static_cast<T*>(a.out) + b * d.out_stride[0] + i * d.out_stride[1] + hh * d.out_stride[2] + e, d.head_dim - e, v);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (!(fabsf(v[k]) < INFINITY)) redo[r] = 1;
+        }
+        if (p.splits > 1) return;
+        __syncthreads();
+        for (int r = wave; r < p.rows; r += W) {
+            if (!redo[r]) continue;
+            const int i = r / p.group, hh = hk * p.group + r % p.group;
+            attend_row<T>(a, static_cast<const T*>(a.q) + b * d.q_stride[0] + i * d.q_stride[1] + hh * d.q_stride[2], kb, vb,
+                          sees(d, seq, i), static_cast<T*>(a.out) + b * d.out_stride[0] + i * d.out_stride[1] + hh * d.out_stride[2],
+                          a.lse ? a.lse + ((int64_t)b * d.heads_q + hh) * d.q_len + i : nullptr);
+        }
+    }
 }
 
 // A row's parts into its result: one wave a row, lane e has values e and e + 64.
@@ -448,8 +537,16 @@ int bn_of(const pd_attention_desc& d) {
     return d.dtype == PD_BF16 || dp <= 64 ? 64 : 32;
 }
 
-// Splits: enough that the waves (few rows) or blocks fill the chip, and parts of at
-// least four tiles.
+int few_waves_of(const pd_attention_desc& d) {
+    const int bytes = d.head_dim <= 32 ? 32 : d.head_dim <= 64 ? 64 : d.head_dim <= 96 ? 96 : 128;
+    const int pitch = (bytes * (d.dtype == PD_BF16 ? 2 : 4) + 127) / 128 * 128, n = 131072 / (4 * 32 * pitch);
+    return n < 8 ? n : 8;
+}
+
+// How the work is cut.  Few rows: one wave a block up to two tiles of keys, else
+// few_waves, and parts of eight tiles a wave where there are more (a long cache).  Else
+// blocks of 128 rows; where they would not fill the chip (two a compute unit), parts of
+// at least four tiles.
 Plan plan(const pd_attention_desc& d) {
     Plan p{};
     p.group = d.heads_q / d.heads_kv;
@@ -458,10 +555,15 @@ Plan plan(const pd_attention_desc& d) {
     p.row_tiles = few ? 1 : (p.rows + 127) / 128;
     p.units = (int64_t)p.row_tiles * d.heads_kv * d.batch;
     const int64_t tiles = most_tiles(d, few ? 32 : 128, p.group, few ? 32 : bn_of(d));
-    const int64_t want = few ? 4096 : 512;
-    int64_t splits = p.units >= want / 2 ? 1 : want / p.units;
-    if (few && tiles > 64) splits = splits > tiles / 32 ? splits : tiles / 32;
-    if (splits > tiles / 4) splits = tiles / 4;
+    int64_t splits;
+    if (few) {
+        p.waves = tiles <= 2 ? 1 : few_waves_of(d);
+        const int64_t per = 8 * p.waves;
+        splits = p.units * p.waves >= 8192 ? 1 : (tiles + per - 1) / per;
+    } else {
+        splits = p.units >= 256 ? 1 : 512 / p.units;
+        if (splits > tiles / 4) splits = tiles / 4;
+    }
     if (splits < 1) splits = 1;
     p.split_tiles = (int)((tiles + splits - 1) / splits);
     p.splits = tiles ? (int)((tiles + p.split_tiles - 1) / p.split_tiles) : 1;
@@ -471,8 +573,12 @@ Plan plan(const pd_attention_desc& d) {
 template <typename T, int DP, bool COPY>
 void attention_c(const AttentionArgs& a, hipStream_t s) {
     const Plan p = plan(a.d);
-    if (few_rows(a.d))
-        hipLaunchKernelGGL((k_attention_few<T, DP, COPY>), dim3((unsigned)(p.units * p.splits)), dim3(64), 0, s, a, p);
+    constexpr int W = few_waves<T, DP>();
+    const dim3 few((unsigned)(p.units * p.splits));
+    if (few_rows(a.d) && p.waves == 1)
+        hipLaunchKernelGGL((k_attention_few<T, DP, COPY, 1>), few, dim3(64), 0, s, a, p);
+    else if (few_rows(a.d))
+        hipLaunchKernelGGL((k_attention_few<T, DP, COPY, W>), few, dim3(64 * W), 0, s, a, p);
     else
         hipLaunchKernelGGL((k_attention<T, DP, COPY>), dim3((unsigned)(p.units * p.splits)), dim3(256), 0, s, a, p);
     PD_HIP(hipGetLastError());

@@ -14,9 +14,8 @@ namespace {
 // Every call checks the device it runs on; the answer for a device is kept.
 void require_gfx950() {
     static thread_local int known = -1;
-    int dev = 0, n = 0;
-    if (hipGetDeviceCount(&n) != hipSuccess || n <= 0) fail(PD_ERR_DEVICE, "no HIP device is available");
-    PD_HIP(hipGetDevice(&dev));
+    int dev = 0;
+    if (hipGetDevice(&dev) != hipSuccess) fail(PD_ERR_DEVICE, "no HIP device is available");
     if (dev == known) return;
     hipDeviceProp_t prop;
     PD_HIP(hipGetDeviceProperties(&prop, dev));
