@@ -71,113 +71,144 @@ __device__ void attend_row(const AttentionArgs& a, const T* q, const T* k, const
     if (lse && lane == 0) *lse = log_sum(top, 1.f, total);
 }
 
-// The 32 rows of a wave (lane: row lane % 32) and what they have summed.
-template <typename T, int DP>
+// The 32 QT rows of a wave (lane: rows 32 t + lane % 32) and what they have summed.
+template <typename T, int DP, int QT>
 struct Rows {
     static constexpr int kSteps = DP / 16, kDT = DP / 32;
     using Ti = Tile<T, DP>;
-    Frag<T> q[kSteps];
-    f32x16 o[kDT];           // transposed: the lane's row, columns 32 t + tile_row
-    float top, limit;        // the reference and the score that raises it (unscaled)
-    float mc;                // top c2
-    float total;             // over the keys of this half of the wave
+    Frag<T> q[QT][kSteps];
+    f32x16 o[QT][kDT];           // transposed: the lane's row, columns 32 t + tile_row
+    float top[QT], limit[QT];    // the reference and the score that raises it (unscaled)
+    float mc[QT];                // top c2
+    float total[QT];             // over the keys of this half of the wave
     float c2;
     bool large;
 
-    __device__ __forceinline__ void start(const pd_attention_desc& d, const T* qp, bool real, int lane) {
+    __device__ __forceinline__ void start(const pd_attention_desc& d) {
+        // the reference is one of unscaled scores: c2 > 0 (a scale of 0: zero queries)
+        c2 = d.scale == 0.f ? 1.f : fabsf(d.scale) * kLog2e;
+        large = false;
+#pragma unroll
+        for (int i = 0; i < QT; ++i) {
+#pragma unroll
+            for (int t = 0; t < kDT; ++t) o[i][t] = f32x16{};
+            top[i] = limit[i] = -INFINITY;
+            mc[i] = total[i] = 0.f;
+        }
+    }
+    __device__ __forceinline__ void load(int i, const pd_attention_desc& d, const T* qp, bool real, int lane) {
         const int h = lane >> 5;
 #pragma unroll
         for (int c = 0; c < kSteps; ++c) {
             const int e = 16 * c + 8 * h;
-            q[c] = Frag<T>{};
-            if (real && d.scale != 0.f) q[c] = load8(qp + e, d.head_dim - e);
-            if (d.scale < 0.f) q[c] = -q[c];
+            q[i][c] = Frag<T>{};
+            if (real && d.scale != 0.f) q[i][c] = load8(qp + e, d.head_dim - e);
+            if (d.scale < 0.f) q[i][c] = -q[i][c];
         }
-        // the reference is one of unscaled scores: c2 > 0 (a scale of 0: zero queries)
-        c2 = d.scale == 0.f ? 1.f : fabsf(d.scale) * kLog2e;
-#pragma unroll
-        for (int t = 0; t < kDT; ++t) o[t] = f32x16{};
-        top = limit = -INFINITY;
-        mc = total = 0.f;
-        large = false;
     }
 
-    // 32 NK keys from j0 on, in LDS; `edge`: some row does not see all of them
+    // 32 NK keys from j0 on, in LDS; `edge`: some row does not see all of them.
+    // `see` is from(lane).
     template <int NK>
-    __device__ __forceinline__ void attend(const char* k, const char* v, int j0, const See& see, bool edge, int lane) {
-        f32x16 s[NK];
+    __device__ __forceinline__ void attend(const char* k, const char* v, int j0, const See (&see)[QT], bool edge, int lane) {
+        f32x16 s[QT][NK];
 #pragma unroll
         for (int kt = 0; kt < NK; ++kt) {
-            s[kt] = f32x16{};
 #pragma unroll
-            for (int c = 0; c < kSteps; ++c) s[kt] = mma(Ti::rows(k, 32 * kt, c, lane), q[c], s[kt]);
+            for (int i = 0; i < QT; ++i) s[i][kt] = f32x16{};
+#pragma unroll
+            for (int c = 0; c < kSteps; ++c) {
+                const Frag<T> f = Ti::rows(k, 32 * kt, c, lane);
+#pragma unroll
+                for (int i = 0; i < QT; ++i) s[i][kt] = mma(f, q[i][c], s[i][kt]);
+            }
         }
         if (edge) {
 #pragma unroll
-            for (int kt = 0; kt < NK; ++kt)
+            for (int i = 0; i < QT; ++i)
 #pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (!see(j0 + 32 * kt + tile_row(lane, r))) s[kt][r] = -INFINITY;
+                for (int kt = 0; kt < NK; ++kt)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (!see[i](j0 + 32 * kt + tile_row(0, r))) s[i][kt][r] = -INFINITY;
         }
-        float m = s[0][0];
+        float m[QT];
+        bool raise = false;
 #pragma unroll
-        for (int kt = 0; kt < NK; ++kt)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) m = fmaxf(m, s[kt][r]);
-        {
-            const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(m), __float_as_uint(m), false, false);
-            m = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
-        }
-        if (__any(m > limit)) {
-            const float up = fmaxf(m, top);
-            const float keep = up == top ? 1.f : exp2_fast((top - up) * c2);
-            top = up;
-            limit = top + kSlack / c2;
-            mc = top == -INFINITY ? 0.f : top * c2;
-            large = __any(!(fabsf(mc) < kLarge));
-            total *= keep;
-#pragma unroll
-            for (int t = 0; t < kDT; ++t) o[t] *= keep;
-        }
-        float sum = 0.f;
-        if (large) {
+        for (int i = 0; i < QT; ++i) {
+            m[i] = s[i][0][0];
 #pragma unroll
             for (int kt = 0; kt < NK; ++kt)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const float x = s[kt][r];
-                    s[kt][r] = x == -INFINITY ? 0.f : exp2_fast((x - top) * c2);
-                    sum += s[kt][r];
-                }
-        } else {
-#pragma unroll
-            for (int kt = 0; kt < NK; ++kt)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    s[kt][r] = exp2_fast(fmaf(s[kt][r], c2, -mc));
-                    sum += s[kt][r];
-                }
+                for (int r = 0; r < 16; ++r) m[i] = fmaxf(m[i], s[i][kt][r]);
+            const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(m[i]), __float_as_uint(m[i]), false, false);
+            m[i] = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1]));
+            raise = raise || m[i] > limit[i];
         }
-        total += sum;
+        if (__any(raise)) {
+            bool far = false;
+#pragma unroll
+            for (int i = 0; i < QT; ++i) {
+                const float up = fmaxf(m[i], top[i]);
+                const float keep = up == top[i] ? 1.f : exp2_fast((top[i] - up) * c2);
+                top[i] = up;
+                limit[i] = up + kSlack / c2;
+                mc[i] = up == -INFINITY ? 0.f : up * c2;
+                far = far || !(fabsf(mc[i]) < kLarge);
+                total[i] *= keep;
+#pragma unroll
+                for (int t = 0; t < kDT; ++t) o[i][t] *= keep;
+            }
+            large = __any(far);
+        }
+#pragma unroll
+        for (int i = 0; i < QT; ++i) {
+            float sum = 0.f;
+            if (large) {
+#pragma unroll
+                for (int kt = 0; kt < NK; ++kt)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const float x = s[i][kt][r];
+                        s[i][kt][r] = x == -INFINITY ? 0.f : exp2_fast((x - top[i]) * c2);
+                        sum += s[i][kt][r];
+                    }
+            } else {
+#pragma unroll
+                for (int kt = 0; kt < NK; ++kt)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        s[i][kt][r] = exp2_fast(fmaf(s[i][kt][r], c2, -mc[i]));
+                        sum += s[i][kt][r];
+                    }
+            }
+            total[i] += sum;
+        }
 #pragma unroll
         for (int kt = 0; kt < NK; ++kt)
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-                const Frag<T> p = as_frag<T>(s[kt], c);
+                Frag<T> p[QT];
 #pragma unroll
-                for (int t = 0; t < kDT; ++t) o[t] = mma(Ti::cols(v, 32 * kt + 16 * c, t, lane), p, o[t]);
+                for (int i = 0; i < QT; ++i) p[i] = as_frag<T>(s[i][kt], c);
+#pragma unroll
+                for (int t = 0; t < kDT; ++t) {
+                    const Frag<T> f = Ti::cols(v, 32 * kt + 16 * c, t, lane);
+#pragma unroll
+                    for (int i = 0; i < QT; ++i) o[i][t] = mma(f, p[i], o[i][t]);
+                }
             }
     }
 
-    __device__ __forceinline__ void finish() { total += __shfl_xor(total, 32); }
+    __device__ __forceinline__ void finish(int i) { total[i] += __shfl_xor(total[i], 32); }
     // whether a value of the lane's row is not finite
-    __device__ __forceinline__ bool odd() const {
-        bool b = false;
+    __device__ __forceinline__ bool odd(int i) const {
+        float x = 0.f;                   // 0 times what is not finite is NaN
 #pragma unroll
         for (int t = 0; t < kDT; ++t)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) b = b || !(fabsf(o[t][r]) < INFINITY);
-        return b;
+            for (int r = 0; r < 16; ++r) x = fmaf(o[i][t][r], 0.f, x);
+        return x != 0.f;
     }
 };
 
@@ -195,43 +226,53 @@ __host__ __device__ inline Parts parts(const pd_attention_desc& d, float* scratc
 // Which wave does what.
 struct Plan {
     int group, rows;           // rows of a key head: group * q_len
-    int row_tiles;             // of 128 rows, or of 32
+    int shift;                 // group = 2^shift, or -1
+    int row_tiles;             // of 128 wave_tiles rows, or of 32
     int splits, split_tiles;   // parts of the key tiles, and the tiles of each
     int64_t units;             // row tiles over all key heads and sequences
     int waves;                 // few rows: waves that share a part's tiles
+    int wave_tiles;            // else: tiles of 32 rows a wave
 };
 
-template <typename T, int DP>
-__device__ __forceinline__ void store_rows(const AttentionArgs& a, const Plan& p, Rows<T, DP>& w, const Seq& seq, int b, int hk,
-                                           int row0, int split, const T* kb, const T* vb) {
+__device__ inline int rows_to_query(const Plan& p, int row) { return p.shift >= 0 ? row >> p.shift : row / p.group; }
+
+// The rows row0 .. row0 + 31, tile x of the wave's.
+template <typename T, int DP, int QT>
+__device__ __forceinline__ void store_rows(const AttentionArgs& a, const Plan& p, Rows<T, DP, QT>& w, int x, const Seq& seq, int b,
+                                           int hk, int row0, int split, const T* kb, const T* vb) {
     const pd_attention_desc& d = a.d;
     const int lane = threadIdx.x & 63, h = lane >> 5, row = row0 + (lane & 31);
     const bool real = row < p.rows;
-    const int qi = real ? row / p.group : 0, hq = hk * p.group + row % p.group;
-    w.finish();
+    const int qi = real ? rows_to_query(p, row) : 0, hq = hk * p.group + (real ? row - qi * p.group : 0);
+    w.finish(x);
     if (p.splits > 1) {
         const Parts to = parts(d, a.scratch, p.splits);
         const int64_t at = ((int64_t)split * d.batch + b) * d.heads_q * d.q_len + (int64_t)hq * d.q_len + qi;
         if (!real) return;
         if (h == 0) {
-            to.stats[2 * at] = w.top;
-            to.stats[2 * at + 1] = w.total;
+            to.stats[2 * at] = w.top[x];
+            to.stats[2 * at + 1] = w.total[x];
         }
-        if (w.total == 0.f) return;            // the join leaves such parts out
+        if (w.total[x] == 0.f) return;            // the join leaves such parts out
         float* sums = to.sums + at * d.head_dim;
 #pragma unroll
         for (int t = 0; t < w.kDT; ++t)
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 const int e = 32 * t + 8 * g + 4 * h;
-                store4(sums + e, d.head_dim - e, f32x4{w.o[t][4 * g], w.o[t][4 * g + 1], w.o[t][4 * g + 2], w.o[t][4 * g + 3]});
+                store4(sums + e, d.head_dim - e, f32x4{w.o[x][t][4 * g], w.o[x][t][4 * g + 1], w.o[x][t][4 * g + 2], w.o[x][t][4 * g + 3]});
             }
         return;
     }
-    const float inv = 1.f / w.total;
+    // a row that sees nothing: 0, also where 0 met a NaN
+    const float inv = w.total[x] == 0.f ? 0.f : 1.f / w.total[x];
 #pragma unroll
-    for (int t = 0; t < w.kDT; ++t) w.o[t] = w.total == 0.f ? f32x16{} : w.o[t] * inv;
-    const uint64_t both = __ballot(w.odd() && real);
+    for (int t = 0; t < w.kDT; ++t) w.o[x][t] *= inv;
+    const bool odd = w.odd(x);
+    if (__any(odd && w.total[x] == 0.f))
+#pragma unroll
+        for (int t = 0; t < w.kDT; ++t) w.o[x][t] = w.total[x] == 0.f ? f32x16{} : w.o[x][t];
+    const uint64_t both = __ballot(odd && w.total[x] != 0.f && real);
     uint32_t again = (uint32_t)both | (uint32_t)(both >> 32);
     if (real && !((again >> (lane & 31)) & 1)) {
         T* out = static_cast<T*>(a.out) + b * d.out_stride[0] + qi * d.out_stride[1] + hq * d.out_stride[2];
@@ -240,10 +281,10 @@ __device__ __forceinline__ void store_rows(const AttentionArgs& a, const Plan& p
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 const int e = 32 * t + 8 * g + 4 * h;
-                store4(out + e, d.head_dim - e, f32x4{w.o[t][4 * g], w.o[t][4 * g + 1], w.o[t][4 * g + 2], w.o[t][4 * g + 3]});
+                store4(out + e, d.head_dim - e, f32x4{w.o[x][t][4 * g], w.o[x][t][4 * g + 1], w.o[x][t][4 * g + 2], w.o[x][t][4 * g + 3]});
             }
         if (a.lse && h == 0)
-            a.lse[((int64_t)b * d.heads_q + hq) * d.q_len + qi] = log_sum(w.top, fabsf(d.scale), w.total);
+            a.lse[((int64_t)b * d.heads_q + hq) * d.q_len + qi] = log_sum(w.top[x], fabsf(d.scale), w.total[x]);
     }
     while (again) {
         const int rr = row0 + __ffs(again) - 1;
@@ -255,35 +296,41 @@ __device__ __forceinline__ void store_rows(const AttentionArgs& a, const Plan& p
     }
 }
 
-// A block: 128 rows of one key head, or one part of their keys.  The next tile of keys
+// 32-row tiles of a wave: two where their sums and operands leave room for two waves a
+// SIMD, since both then read each key and value once from LDS.
+template <typename T, int DP>
+constexpr int wave_tiles() {
+    return sizeof(T) == 2 && DP <= 64 ? 2 : 1;
+}
+
+// A block: 128 QT rows of one key head, or one part of their keys.  The next tile of keys
 // and values is copied to LDS while the waves work on the present one.
-template <typename T, int DP, bool COPY>
+template <typename T, int DP, bool COPY, int QT>
 __global__ __launch_bounds__(256, 2) void k_attention(const AttentionArgs a, const Plan p) {
     using Ti = Tile<T, DP>;
-    constexpr int BN = tile_rows<T, DP>(), kBytes = BN * Ti::kPitch;
+    constexpr int BN = tile_rows<T, DP>(), kBytes = BN * Ti::kPitch, BM = 128 * QT;
     using F = Fill<T, DP, BN, 256>;
     __shared__ __align__(128) char lds[4 * kBytes];       // keys, values; twice
     const pd_attention_desc& d = a.d;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int split = blockIdx.x % p.splits, unit = blockIdx.x / p.splits;
+    const int id = near_blocks(blockIdx.x, gridDim.x);
+    const int split = id % p.splits, unit = id / p.splits;
     const int tile = p.row_tiles - 1 - unit % p.row_tiles, head = unit / p.row_tiles;     // the longest rows first
     const int hk = head % d.heads_kv, b = head / d.heads_kv;
     const Seq seq = sequence(a, b);
-    const int row0 = tile * 128 + wave * 32, row = row0 + (lane & 31);
-    const bool real = row < p.rows;
-    const int qi = real ? row / p.group : 0, hq = hk * p.group + row % p.group;
-    const See see = real ? sees(d, seq, qi) : See{0, 0, 0};
-    const WaveSight sight(see);
+    const int row0 = tile * BM + wave * 32 * QT;
     const T* kb = static_cast<const T*>(a.k) + b * d.k_stride[0] + hk * d.k_stride[2];
     const T* vb = static_cast<const T*>(a.v) + b * d.v_stride[0] + hk * d.v_stride[2];
 
-    Rows<T, DP> w;
-    w.start(d, static_cast<const T*>(a.q) + b * d.q_stride[0] + qi * d.q_stride[1] + hq * d.q_stride[2], real && !see.none(), lane);
-
-    const int i0 = tile * 128 / p.group, i1 = min((tile * 128 + 127) / p.group, seq.n - 1);
+    const int i0 = rows_to_query(p, tile * BM), i1 = min(rows_to_query(p, tile * BM + BM - 1), seq.n - 1);
     const KeyTiles<BN> tiles(i0 <= i1 ? sees_any(d, seq, i0, i1) : See{0, 0, 0});
     const int it0 = split * p.split_tiles, it1 = min(tiles.count, it0 + p.split_tiles);
-    const int units = d.head_dim * (int)sizeof(T) / 16;
+    F fk, fv;
+    if constexpr (COPY) {
+        const int units = d.head_dim * (int)sizeof(T) / 16;
+        fk.plan(d.k_stride[1], units, threadIdx.x);
+        fv.plan(d.v_stride[1], units, threadIdx.x);
+    }
     auto fetch = [&](int it, int buf) {
         const int j0 = tiles.start(it);
         const T* kt = kb + (int64_t)j0 * d.k_stride[1];
@@ -291,12 +338,12 @@ __global__ __launch_bounds__(256, 2) void k_attention(const AttentionArgs a, con
         char* to = lds + buf * 2 * kBytes;
         if constexpr (COPY) {
             if (tiles.whole(j0)) {
-                F::copy(kt, d.k_stride[1], units, to, threadIdx.x, [](int r) { return r; });
-                F::copy(vt, d.v_stride[1], units, to + kBytes, threadIdx.x, [](int r) { return r; });
+                fk.copy(kt, to);
+                fv.copy(vt, to + kBytes);
             } else {
                 auto from = [&](int r) { return tiles.inside(j0, j0 + r) - j0; };
-                F::copy(kt, d.k_stride[1], units, to, threadIdx.x, from);
-                F::copy(vt, d.v_stride[1], units, to + kBytes, threadIdx.x, from);
+                fk.copy_some(kt, d.k_stride[1], to, threadIdx.x, from);
+                fv.copy_some(vt, d.v_stride[1], to + kBytes, threadIdx.x, from);
             }
         } else {
             auto keep = [&](int r) { return tiles.any(j0 + r); };
@@ -305,6 +352,21 @@ __global__ __launch_bounds__(256, 2) void k_attention(const AttentionArgs a, con
         }
     };
     if (it0 < it1) fetch(it0, 0);
+
+    Rows<T, DP, QT> w;
+    w.start(d);
+    See see[QT];
+    const Sight sight = sight_of(d, seq, rows_to_query(p, row0), row0 + 32 * QT <= p.rows ? rows_to_query(p, row0 + 32 * QT - 1) : seq.n);
+#pragma unroll
+    for (int x = 0; x < QT; ++x) {
+        const int row = row0 + 32 * x + (lane & 31);
+        const bool real = row < p.rows;
+        const int qi = real ? rows_to_query(p, row) : 0, hq = hk * p.group + (real ? row - qi * p.group : 0);
+        see[x] = real ? sees(d, seq, qi) : See{0, 0, 0};
+        w.load(x, d, static_cast<const T*>(a.q) + b * d.q_stride[0] + qi * d.q_stride[1] + hq * d.q_stride[2],
+               real && !see[x].none(), lane);
+        see[x] = see[x].from(lane);
+    }
     for (int it = it0; it < it1; ++it) {
         const int buf = (it - it0) & 1, j0 = tiles.start(it);
         if constexpr (COPY) wait_copies();
@@ -314,7 +376,8 @@ __global__ __launch_bounds__(256, 2) void k_attention(const AttentionArgs a, con
         const char* at = lds + buf * 2 * kBytes;
         w.template attend<BN / 32>(at, at + kBytes, j0, see, !sight.all(j0, BN), lane);
     }
-    store_rows(a, p, w, seq, b, hk, row0, split, kb, vb);
+#pragma unroll
+    for (int x = 0; x < QT; ++x) store_rows(a, p, w, x, seq, b, hk, row0 + 32 * x, split, kb, vb);
 }
 
 // Waves that share the keys of at most 32 rows, each with two buffers of its own.
@@ -343,27 +406,32 @@ __global__ __launch_bounds__(64 * W) void k_attention_few(const AttentionArgs a,
     const Seq seq = sequence(a, b);
     const int row = lane & 31;
     const bool real = row < p.rows;
-    const int qi = real ? row / p.group : 0, hq = hk * p.group + row % p.group;
+    const int qi = real ? rows_to_query(p, row) : 0, hq = hk * p.group + (real ? row - qi * p.group : 0);
     const See see = real ? sees(d, seq, qi) : See{0, 0, 0};
-    const WaveSight sight(see);
+    const Sight sight = sight_of(d, seq, 0, p.rows == 32 ? d.q_len - 1 : seq.n);
     const T* kb = static_cast<const T*>(a.k) + b * d.k_stride[0] + hk * d.k_stride[2];
     const T* vb = static_cast<const T*>(a.v) + b * d.v_stride[0] + hk * d.v_stride[2];
 
     const KeyTiles<BN> tiles(seq.n > 0 ? sees_any(d, seq, 0, seq.n - 1) : See{0, 0, 0});
     const int it0 = split * p.split_tiles + wave, it1 = min(tiles.count, split * p.split_tiles + p.split_tiles);
-    const int units = d.head_dim * (int)sizeof(T) / 16;
+    F fk, fv;
+    if constexpr (COPY) {
+        const int units = d.head_dim * (int)sizeof(T) / 16;
+        fk.plan(d.k_stride[1], units, lane);
+        fv.plan(d.v_stride[1], units, lane);
+    }
     auto fetch = [&](int it, char* to) {
         const int j0 = tiles.start(it);
         const T* kt = kb + (int64_t)j0 * d.k_stride[1];
         const T* vt = vb + (int64_t)j0 * d.v_stride[1];
         if constexpr (COPY) {
             if (tiles.whole(j0)) {
-                F::copy(kt, d.k_stride[1], units, to, lane, [](int r) { return r; });
-                F::copy(vt, d.v_stride[1], units, to + kBytes, lane, [](int r) { return r; });
+                fk.copy(kt, to);
+                fv.copy(vt, to + kBytes);
             } else {
                 auto from = [&](int r) { return tiles.inside(j0, j0 + r) - j0; };
-                F::copy(kt, d.k_stride[1], units, to, lane, from);
-                F::copy(vt, d.v_stride[1], units, to + kBytes, lane, from);
+                fk.copy_some(kt, d.k_stride[1], to, lane, from);
+                fv.copy_some(vt, d.v_stride[1], to + kBytes, lane, from);
             }
         } else {
             auto keep = [&](int r) { return tiles.any(j0 + r); };
@@ -372,8 +440,10 @@ __global__ __launch_bounds__(64 * W) void k_attention_few(const AttentionArgs a,
         }
     };
     if (COPY && it0 < it1) fetch(it0, lds);
-    Rows<T, DP> w;
-    w.start(d, static_cast<const T*>(a.q) + b * d.q_stride[0] + qi * d.q_stride[1] + hq * d.q_stride[2], real && !see.none(), lane);
+    Rows<T, DP, 1> w;
+    w.start(d);
+    w.load(0, d, static_cast<const T*>(a.q) + b * d.q_stride[0] + qi * d.q_stride[1] + hq * d.q_stride[2], real && !see.none(), lane);
+    const See sees_from[1] = {see.from(lane)};
     if constexpr (COPY) {
         int buf = 0;
         for (int it = it0; it < it1; it += W, buf ^= 1) {
@@ -389,7 +459,7 @@ __global__ __launch_bounds__(64 * W) void k_attention_few(const AttentionArgs a,
             }
             __builtin_amdgcn_wave_barrier();
             const char* at = lds + buf * 2 * kBytes;
-            w.template attend<1>(at, at + kBytes, j0, see, !sight.all(j0, BN), lane);
+            w.template attend<1>(at, at + kBytes, j0, sees_from, !sight.all(j0, BN), lane);
             __builtin_amdgcn_wave_barrier();
         }
     } else {
@@ -398,16 +468,16 @@ __global__ __launch_bounds__(64 * W) void k_attention_few(const AttentionArgs a,
             fetch(it, lds);
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             const int j0 = tiles.start(it);
-            w.template attend<1>(lds, lds + kBytes, j0, see, !sight.all(j0, BN), lane);
+            w.template attend<1>(lds, lds + kBytes, j0, sees_from, !sight.all(j0, BN), lane);
         }
     }
     if constexpr (W == 1) {
-        store_rows(a, p, w, seq, b, hk, 0, split, kb, vb);
+        store_rows(a, p, w, 0, seq, b, hk, 0, split, kb, vb);
     } else {
-        w.finish();
+        w.finish(0);
         if (lane < 32) {
-            stats[wave][0][row] = w.top;
-            stats[wave][1][row] = w.total;
+            stats[wave][0][row] = w.top[0];
+            stats[wave][1][row] = w.total[0];
             redo[row] = 0;
         }
         __syncthreads();
@@ -421,14 +491,14 @@ __global__ __launch_bounds__(64 * W) void k_attention_few(const AttentionArgs a,
             const float t = stats[i][1][row], m = stats[i][0][row];
             if (t != 0.f) total = fmaf(m == top ? 1.f : exp2_fast((m - top) * w.c2), t, total);
         }
-        const float f = w.total == 0.f ? 0.f : w.top == top ? 1.f : exp2_fast((w.top - top) * w.c2);
+        const float f = w.total[0] == 0.f ? 0.f : w.top[0] == top ? 1.f : exp2_fast((w.top[0] - top) * w.c2);
         float* mine = reinterpret_cast<float*>(lds) + row * kPart;
 #pragma unroll
         for (int t = 0; t < w.kDT; ++t)
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                f32x4 v = {w.o[t][4 * g], w.o[t][4 * g + 1], w.o[t][4 * g + 2], w.o[t][4 * g + 3]};
-                v = w.total == 0.f ? f32x4{} : v * f;
+                f32x4 v = {w.o[0][t][4 * g], w.o[0][t][4 * g + 1], w.o[0][t][4 * g + 2], w.o[0][t][4 * g + 3]};
+                v = w.total[0] == 0.f ? f32x4{} : v * f;
                 *reinterpret_cast<f32x4*>(mine + 32 * t + 8 * g + 4 * (lane >> 5)) = v;
             }
         const int64_t rows_all = (int64_t)d.batch * d.heads_q * d.q_len, at = ((int64_t)b * d.heads_q + hq) * d.q_len + qi;
@@ -532,9 +602,12 @@ int64_t most_tiles(const pd_attention_desc& d, int rows_per_tile, int group, int
 
 bool few_rows(const pd_attention_desc& d) { return (int64_t)d.q_len * (d.heads_q / d.heads_kv) <= 32; }
 
-int bn_of(const pd_attention_desc& d) {
-    const int dp = d.head_dim <= 32 ? 32 : d.head_dim <= 64 ? 64 : d.head_dim <= 96 ? 96 : 128;
-    return d.dtype == PD_BF16 || dp <= 64 ? 64 : 32;
+int bn_of(const pd_attention_desc& d) { return d.dtype == PD_BF16 || d.head_dim <= 64 ? 64 : 32; }
+// 32-row tiles a wave takes: one where two would leave compute units without a block
+int wave_tiles_of(const pd_attention_desc& d) {
+    if (d.dtype != PD_BF16 || d.head_dim > 64) return 1;
+    const int64_t rows = (int64_t)d.q_len * (d.heads_q / d.heads_kv);
+    return (rows + 255) / 256 * d.heads_kv * d.batch >= 512 ? 2 : 1;
 }
 
 int few_waves_of(const pd_attention_desc& d) {
@@ -551,10 +624,13 @@ Plan plan(const pd_attention_desc& d) {
     Plan p{};
     p.group = d.heads_q / d.heads_kv;
     p.rows = d.q_len * p.group;
+    p.shift = p.group & (p.group - 1) ? -1 : __builtin_ctz(p.group);
     const bool few = few_rows(d);
-    p.row_tiles = few ? 1 : (p.rows + 127) / 128;
+    p.wave_tiles = few ? 1 : wave_tiles_of(d);
+    const int bm = 128 * p.wave_tiles;
+    p.row_tiles = few ? 1 : (p.rows + bm - 1) / bm;
     p.units = (int64_t)p.row_tiles * d.heads_kv * d.batch;
-    const int64_t tiles = most_tiles(d, few ? 32 : 128, p.group, few ? 32 : bn_of(d));
+    const int64_t tiles = most_tiles(d, few ? 32 : bm, p.group, few ? 32 : bn_of(d));
     int64_t splits;
     if (few) {
         p.waves = tiles <= 2 ? 1 : few_waves_of(d);
@@ -579,8 +655,10 @@ void attention_c(const AttentionArgs& a, hipStream_t s) {
         hipLaunchKernelGGL((k_attention_few<T, DP, COPY, 1>), few, dim3(64), 0, s, a, p);
     else if (few_rows(a.d))
         hipLaunchKernelGGL((k_attention_few<T, DP, COPY, W>), few, dim3(64 * W), 0, s, a, p);
-    else
-        hipLaunchKernelGGL((k_attention<T, DP, COPY>), dim3((unsigned)(p.units * p.splits)), dim3(256), 0, s, a, p);
+    else if (p.wave_tiles == 1)
+        hipLaunchKernelGGL((k_attention<T, DP, COPY, 1>), dim3((unsigned)(p.units * p.splits)), dim3(256), 0, s, a, p);
+    else if constexpr (wave_tiles<T, DP>() == 2)
+        hipLaunchKernelGGL((k_attention<T, DP, COPY, 2>), dim3((unsigned)(p.units * p.splits)), dim3(256), 0, s, a, p);
     PD_HIP(hipGetLastError());
     if (p.splits == 1) return;
     const int64_t rows = (int64_t)a.d.batch * a.d.heads_q * a.d.q_len;

@@ -149,7 +149,7 @@ __global__ __launch_bounds__(256, (dq_blocks_per_cu<T, DP>())) void k_attention_
     __shared__ __align__(128) char lds[4 * kBytes];       // keys, values; twice
     const pd_attention_desc& d = a.d;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
-    const int tile = row_tiles - 1 - blockIdx.x % row_tiles, head = blockIdx.x / row_tiles;
+    const int id = near_blocks(blockIdx.x, gridDim.x), tile = row_tiles - 1 - id % row_tiles, head = id / row_tiles;
     const int hk = head % d.heads_kv, b = head / d.heads_kv;
     const Seq seq = sequence(a, b);
     const Views<T> w = views<T>(a, b, hk);
@@ -157,21 +157,31 @@ __global__ __launch_bounds__(256, (dq_blocks_per_cu<T, DP>())) void k_attention_
     const int row0 = tile * 128 + wave * 32, row = row0 + (lane & 31);
     const bool real = row < rows_all;
     const int qi = real ? row / w.group : 0, g = row % w.group;
-    const See see = real ? sees(d, seq, qi) : See{0, 0, 0};
-    const WaveSight sight(see);
+    const See see = real ? sees(d, seq, qi) : See{0, 0, 0}, see_from = see.from(lane);
+    const Sight sight = sight_of(d, seq, row0 / w.group, row0 + 32 <= rows_all ? (row0 + 31) / w.group : seq.n);
 
     const int i0 = tile * 128 / w.group, i1 = min((tile * 128 + 127) / w.group, seq.n - 1);
     const KeyTiles<BN> tiles(i0 <= i1 ? sees_any(d, seq, i0, i1) : See{0, 0, 0});
-    const int units = d.head_dim * (int)sizeof(T) / 16;
+    F fk, fv;
+    if constexpr (COPY) {
+        const int units = d.head_dim * (int)sizeof(T) / 16;
+        fk.plan(d.k_stride[1], units, threadIdx.x);
+        fv.plan(d.v_stride[1], units, threadIdx.x);
+    }
     auto fetch = [&](int it, int buf) {
         const int j0 = tiles.start(it);
         const T* kt = w.k + (int64_t)j0 * d.k_stride[1];
         const T* vt = w.v + (int64_t)j0 * d.v_stride[1];
         char* to = lds + buf * 2 * kBytes;
         if constexpr (COPY) {
-            auto from = [&](int r) { return tiles.inside(j0, j0 + r) - j0; };
-            F::copy(kt, d.k_stride[1], units, to, threadIdx.x, from);
-            F::copy(vt, d.v_stride[1], units, to + kBytes, threadIdx.x, from);
+            if (tiles.whole(j0)) {
+                fk.copy(kt, to);
+                fv.copy(vt, to + kBytes);
+            } else {
+                auto from = [&](int r) { return tiles.inside(j0, j0 + r) - j0; };
+                fk.copy_some(kt, d.k_stride[1], to, threadIdx.x, from);
+                fv.copy_some(vt, d.v_stride[1], to + kBytes, threadIdx.x, from);
+            }
         } else {
             auto keep = [&](int r) { return tiles.any(j0 + r); };
             F::load(kt, d.k_stride[1], d.head_dim, to, threadIdx.x, keep);
@@ -229,7 +239,7 @@ __global__ __launch_bounds__(256, (dq_blocks_per_cu<T, DP>())) void k_attention_
             if (edge) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
-                    if (!see(j0 + 32 * kt + tile_row(lane, r))) s[r] = 0.f;
+                    if (!see_from(j0 + 32 * kt + tile_row(0, r))) s[r] = 0.f;
             }
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
@@ -281,6 +291,16 @@ __device__ inline See seen_by(const pd_attention_desc& d, const Seq& s, int j) {
     return See{lo, max(hi, lo), 0};
 }
 
+// The same of the keys j0 .. j1 between them.  The bounds grow with j, but that a sink is
+// seen to the last query: the smallest upper bound is the first key's or the first's
+// after the sinks.
+__device__ inline Sight sight_by(const pd_attention_desc& d, const Seq& s, int j0, int j1) {
+    if (j0 >= s.m) return Sight{0, 0, 0, 0, 0, 0};
+    const int j2 = min(j1, s.m - 1);
+    const See a = seen_by(d, s, j0), b = seen_by(d, s, j2), c = seen_by(d, s, min(max(j0, d.sinks), j2));
+    return Sight{a.lo, b.lo, j1 < s.m ? min(a.hi, c.hi) : 0, max(a.hi, b.hi), 0, 0};
+}
+
 // A block: 128 keys of one key head, 32 a wave, and the tiles of queries of the group's
 // heads that see any of them, or one part of these.
 template <typename T, int DP, bool COPY>
@@ -293,15 +313,15 @@ __global__ __launch_bounds__(256, (dkv_blocks_per_cu<T, DP>())) void k_attention
     __shared__ __align__(16) float stats[2][3][64];       // lse log2 e, delta, lse
     const pd_attention_desc& d = a.d;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
-    const int split = blockIdx.x % splits, unit = blockIdx.x / splits;
+    const int id = near_blocks(blockIdx.x, gridDim.x), split = id % splits, unit = id / splits;
     const int tile = unit % key_tiles, head = unit / key_tiles;
     const int hk = head % d.heads_kv, b = head / d.heads_kv;
     const Seq seq = sequence(a, b);
     const Views<T> w = views<T>(a, b, hk);
     const int key0 = tile * 128, wkey0 = key0 + wave * 32, key = wkey0 + (lane & 31);
     const bool live = key < seq.m;
-    const See see = seen_by(d, seq, key);
-    const WaveSight sight(see);
+    const See see = seen_by(d, seq, key).from(lane);
+    const Sight sight = sight_by(d, seq, wkey0, wkey0 + 31);
 
     // the block's queries: from the first that sees its first key (two-sided: its earliest)
     // to the last that sees its last, or a sink among them
@@ -313,7 +333,12 @@ __global__ __launch_bounds__(256, (dkv_blocks_per_cu<T, DP>())) void k_attention
     }
     const int per_head = last > first ? (last - first + BR - 1) / BR : 0, all = per_head * w.group;
     const int each = (all + splits - 1) / splits, x0 = split * each, x1 = min(all, x0 + each);
-    const int units = d.head_dim * (int)sizeof(T) / 16;
+    F fq, fg;
+    if constexpr (COPY) {
+        const int units = d.head_dim * (int)sizeof(T) / 16;
+        fq.plan(d.q_stride[1], units, threadIdx.x);
+        fg.plan(d.dout_stride[1], units, threadIdx.x);
+    }
     float stat = 0.f;
     auto fetch = [&](int x, int buf) {
         const int g = x / per_head, i0 = first + (x - g * per_head) * BR;
@@ -325,9 +350,14 @@ __global__ __launch_bounds__(256, (dkv_blocks_per_cu<T, DP>())) void k_attention
         const T* gt = w.dout + (int64_t)i0 * d.dout_stride[1] + g * d.dout_stride[2];
         char* to = lds + buf * 2 * kBytes;
         if constexpr (COPY) {
-            auto from = [&](int r) { return min(i0 + r, seq.n - 1) - i0; };
-            F::copy(qt, d.q_stride[1], units, to, threadIdx.x, from);
-            F::copy(gt, d.dout_stride[1], units, to + kBytes, threadIdx.x, from);
+            if (i0 + BR <= seq.n) {
+                fq.copy(qt, to);
+                fg.copy(gt, to + kBytes);
+            } else {
+                auto from = [&](int r) { return min(i0 + r, seq.n - 1) - i0; };
+                fq.copy_some(qt, d.q_stride[1], to, threadIdx.x, from);
+                fg.copy_some(gt, d.dout_stride[1], to + kBytes, threadIdx.x, from);
+            }
         } else {
             auto keep = [&](int r) { return i0 + r < seq.n; };
             F::load(qt, d.q_stride[1], d.head_dim, to, threadIdx.x, keep);
@@ -403,7 +433,7 @@ __global__ __launch_bounds__(256, (dkv_blocks_per_cu<T, DP>())) void k_attention
                 if (edge) {
 #pragma unroll
                     for (int r = 0; r < 16; ++r)
-                        if (!see(i0 + 32 * rt + tile_row(lane, r))) s[r] = dp[r] = 0.f;
+                        if (!see(i0 + 32 * rt + tile_row(0, r))) s[r] = dp[r] = 0.f;
                 }
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {

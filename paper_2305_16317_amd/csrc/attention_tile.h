@@ -60,14 +60,19 @@ __device__ inline Frag<T> as_frag(const f32x16& v, int c) {
     return narrow<T>(f);
 }
 
-// A tile of rows in LDS: 16-byte units, those of row r exchanged by swz(r), so
-// that both ways of reading (eight rows at one unit; four rows at two
-// neighbouring units) meet every bank once.
+// A tile of rows in LDS: 16-byte units, those of row r exchanged by swz(r), so that the
+// 16 units that a cycle reads lie in the 16 places of a 256-byte line: 16 rows at one
+// unit (rows), and four rows at four neighbouring units or, in float32, two rows four
+// apart at eight (cols).  Two rows of 128 bytes share a line.
 template <typename T, int DP>
 struct Tile {
     static constexpr int kPitch = (DP * (int)sizeof(T) + 127) / 128 * 128;   // bytes a row
     static constexpr int kUnits = DP * (int)sizeof(T) / 16;                  // units a row that hold values
-    static __device__ inline int swz(int row) { return ((row & 3) << 1) | ((row >> 2) & 1); }
+    static __device__ inline int swz(int row) {
+        if constexpr (kPitch % 256 != 0) return ((row & 2) << 1) | ((row >> 2) & 3);
+        else if constexpr (sizeof(T) == 2) return ((row & 3) << 2) | ((row >> 2) & 3);
+        else return ((row & 4) << 1) | ((row & 3) << 1) | ((row >> 3) & 1);
+    }
     static __device__ inline int at(int row, int unit) { return row * kPitch + ((unit ^ swz(row)) << 4); }
     // rows row0 .. row0 + 31 of the tile as a fragment, step c of its 16-wide steps
     static __device__ inline Frag<T> rows(const char* lds, int row0, int c, int lane) {
@@ -89,10 +94,9 @@ struct Tile {
             // lane i receives column i of the four rows
             const int i = lane & 15, row = row0 + 4 * h + (i >> 2);
             const int unit = 4 * dt + 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
-            const char* p = lds + at(row, unit) + 8 * (i & 1);
             typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-            const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p));
-            const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 8 * kPitch));
+            const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + at(row, unit) + 8 * (i & 1)));
+            const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + at(row + 8, unit) + 8 * (i & 1)));
             typedef short s16x8 __attribute__((ext_vector_type(8)));
             return __builtin_bit_cast(Frag<T>, s16x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]});
         } else {
@@ -138,6 +142,13 @@ __device__ inline void store4(bf16* p, int n, f32x4 v) {
         if (e < n) p[e] = w[e];
 }
 
+// Consecutive blocks go to the 8 dies of the chip in turn; this numbers them so that
+// each die, with its own L2, has a run of neighbours (blocks that read the same keys).
+__device__ inline int near_blocks(int id, int count) {
+    const int die = id & 7, at = id >> 3, each = count >> 3, more = count & 7;
+    return die * each + min(die, more) + at;
+}
+
 // ---------------------------------------------------------------- memory to LDS
 // One copy of 16 bytes a lane from base + off to LDS at lds + 16 lane, past the
 // registers (M0 = lds).  Inline assembly, so that the compiler's wait counts do not
@@ -167,8 +178,7 @@ __device__ __forceinline__ void lds_barrier() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
-// Fills a tile of ROWS rows with THREADS threads: row r from the row that `source(r)`
-// names (an offset from `base` in rows).  Copies need rows and their stride aligned
+// Fills a tile of ROWS rows with THREADS threads.  Copies need rows and their stride aligned
 // to 16 bytes, a head of whole 16-byte units, and ROWS rows within 2^31 bytes;
 // the host says whether that holds (copies_fit).  Units past the head's end repeat
 // its first one: what they meet is zero (queries) or not stored (output columns).
@@ -178,17 +188,35 @@ struct Fill {
     static constexpr int kRowUnits = Ti::kPitch / 16;
     static constexpr int kCopies = ROWS * kRowUnits / THREADS;
     static_assert(ROWS * kRowUnits % THREADS == 0 && THREADS % 64 == 0, "whole copies");
-    template <class Source>
-    static __device__ __forceinline__ void copy(const T* base, int64_t stride, int units, char* lds, int thread, Source source) {
-        const uint64_t from = uniform_address(base);
-        const uint32_t to = __builtin_amdgcn_readfirstlane(lds_address(lds) + (thread & ~63) * 16);
+    uint32_t off[kCopies];      // of this thread's copies from the tile's first row
+    uint32_t to;                // this wave's part of a tile, from its start
+    __device__ __forceinline__ void plan(int64_t stride, int units, int thread) {
         const uint32_t step = (uint32_t)stride * (uint32_t)sizeof(T);
 #pragma unroll
         for (int i = 0; i < kCopies; ++i) {
             const int at = i * THREADS + thread, row = at / kRowUnits;
-            int unit = (at % kRowUnits) ^ Ti::swz(row);
-            unit = unit < units ? unit : 0;
-            copy16(from, (uint32_t)source(row) * step + unit * 16, to + i * THREADS * 16);
+            const int unit = (at % kRowUnits) ^ Ti::swz(row);
+            off[i] = (uint32_t)row * step + (unit < units ? unit : 0) * 16;
+        }
+        to = __builtin_amdgcn_readfirstlane((thread & ~63) * 16);
+    }
+    // the tile whose first row is at `base`
+    __device__ __forceinline__ void copy(const T* base, const char* lds) const {
+        const uint64_t from = uniform_address(base);
+        const uint32_t at = __builtin_amdgcn_readfirstlane(lds_address(lds) + to);
+#pragma unroll
+        for (int i = 0; i < kCopies; ++i) copy16(from, off[i], at + i * THREADS * 16);
+    }
+    // the same, but its row r from the row that source(r) names
+    template <class Source>
+    __device__ __forceinline__ void copy_some(const T* base, int64_t stride, const char* lds, int thread, Source source) const {
+        const uint64_t from = uniform_address(base);
+        const uint32_t at = __builtin_amdgcn_readfirstlane(lds_address(lds) + to);
+        const uint32_t step = (uint32_t)stride * (uint32_t)sizeof(T);
+#pragma unroll
+        for (int i = 0; i < kCopies; ++i) {
+            const int row = (i * THREADS + thread) / kRowUnits;
+            copy16(from, off[i] + (uint32_t)(source(row) - row) * step, at + i * THREADS * 16);
         }
     }
     // the same through registers, any stride and alignment; rows for which `keep` is
@@ -226,6 +254,12 @@ struct See {
     int lo, hi, sk;
     __device__ inline bool operator()(int j) const { return (j >= lo && j < hi) || j < sk; }
     __device__ inline bool none() const { return hi <= lo && sk <= 0; }
+    // for a lane that asks about tile_row(lane, r) = tile_row(0, r) + 4 (lane / 32): the same with
+    // keys counted from 4 (lane / 32), so that the question is one of a uniform number
+    __device__ inline See from(int lane) const {
+        const int h4 = 4 * (lane >> 5);
+        return See{lo - h4, hi - h4, sk - h4};
+    }
 };
 __device__ inline See sees(const pd_attention_desc& d, const Seq& s, int i) {
     if (i >= s.n) return See{0, 0, 0};
@@ -261,25 +295,20 @@ struct KeyTiles {
         return lo < hi ? min(max(j, lo), hi - 1) : min(any.sk, j0 + BN) - 1;
     }
 };
-// What the 64 lanes' rows see between them: the smallest and the largest bounds, so
-// that a tile of keys can be told to be in sight of all rows or of none.
-struct WaveSight {
+// What a wave's rows see between them: the smallest and the largest bounds, so that a
+// tile of keys can be told to be in sight of all rows or of none.
+struct Sight {
     int lo_min, lo_max, hi_min, hi_max, sk_min, sk_max;
-    __device__ inline explicit WaveSight(const See& s) {
-        lo_min = lo_max = s.lo, hi_min = hi_max = s.hi, sk_min = sk_max = s.sk;
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-            lo_min = min(lo_min, __shfl_xor(lo_min, o)), lo_max = max(lo_max, __shfl_xor(lo_max, o));
-            hi_min = min(hi_min, __shfl_xor(hi_min, o)), hi_max = max(hi_max, __shfl_xor(hi_max, o));
-            sk_min = min(sk_min, __shfl_xor(sk_min, o)), sk_max = max(sk_max, __shfl_xor(sk_max, o));
-        }
-        lo_min = __builtin_amdgcn_readfirstlane(lo_min), lo_max = __builtin_amdgcn_readfirstlane(lo_max);
-        hi_min = __builtin_amdgcn_readfirstlane(hi_min), hi_max = __builtin_amdgcn_readfirstlane(hi_max);
-        sk_min = __builtin_amdgcn_readfirstlane(sk_min), sk_max = __builtin_amdgcn_readfirstlane(sk_max);
-    }
     __device__ inline bool all(int j0, int n) const { return (j0 >= lo_max && j0 + n <= hi_min) || j0 + n <= sk_min; }
     __device__ inline bool none(int j0, int n) const { return (j0 >= hi_max || j0 + n <= lo_min) && j0 >= sk_max; }
 };
+// Of the queries i0 .. i1, whose bounds grow with i; a query past s.n sees nothing.
+__device__ inline Sight sight_of(const pd_attention_desc& d, const Seq& s, int i0, int i1) {
+    if (i0 >= s.n) return Sight{0, 0, 0, 0, 0, 0};
+    const See a = sees(d, s, i0), b = sees(d, s, min(i1, s.n - 1));
+    const bool whole = i1 < s.n;
+    return Sight{a.lo, b.lo, whole ? a.hi : 0, b.hi, whole ? a.sk : 0, b.sk};
+}
 
 // rows of a shared tile: two buffers of two tiles stay within half a compute unit's LDS
 template <typename T, int DP>
