@@ -107,10 +107,11 @@ struct Rows {
         }
     }
 
-    // 32 NK keys from j0 on, in LDS; `edge`: some row does not see all of them.
-    // `see` is from(lane).
+    // 32 NK keys from j0 on, in LDS; `edge`: some row does not see all of them; `half`:
+    // none sees one past the first 16.  `see` is from(lane).
     template <int NK>
-    __device__ __forceinline__ void attend(const char* k, const char* v, int j0, const See (&see)[QT], bool edge, int lane) {
+    __device__ __forceinline__ void attend(const char* k, const char* v, int j0, const See (&see)[QT], bool edge, int lane,
+                                           bool half = false) {
         f32x16 s[QT][NK];
 #pragma unroll
         for (int kt = 0; kt < NK; ++kt) {
@@ -188,6 +189,7 @@ struct Rows {
         for (int kt = 0; kt < NK; ++kt)
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
+                if (c == 1 && half) continue;
                 Frag<T> p[QT];
 #pragma unroll
                 for (int i = 0; i < QT; ++i) p[i] = as_frag<T>(s[i][kt], c);
@@ -395,7 +397,8 @@ __global__ __launch_bounds__(64 * W) void k_attention_few(const AttentionArgs a,
     constexpr int BN = 32, kBytes = BN * Ti::kPitch, kPart = DP + 4;      // floats of a row's part
     using F = Fill<T, DP, BN, 64>;
     static_assert(BN * kPart * 4 <= 4 * kBytes, "a wave's sums fit its buffers");
-    __shared__ __align__(128) char lds_all[W][4 * kBytes];
+    constexpr int kBufs = W == 1 ? 1 : 2;                 // a lone wave has a tile or two: no second buffer
+    __shared__ __align__(128) char lds_all[W][kBufs * 2 * kBytes];
     __shared__ float stats[W][2][32];
     __shared__ int redo[32];
     const pd_attention_desc& d = a.d;
@@ -444,7 +447,19 @@ __global__ __launch_bounds__(64 * W) void k_attention_few(const AttentionArgs a,
     w.start(d);
     w.load(0, d, static_cast<const T*>(a.q) + b * d.q_stride[0] + qi * d.q_stride[1] + hq * d.q_stride[2], real && !see.none(), lane);
     const See sees_from[1] = {see.from(lane)};
-    if constexpr (COPY) {
+    if constexpr (COPY && W == 1) {
+        for (int it = it0; it < it1; ++it) {
+            const int j0 = tiles.start(it);
+            if (it > it0) {
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                fetch(it, lds);
+            }
+            wait_copies();
+            __builtin_amdgcn_wave_barrier();
+            w.template attend<1>(lds, lds + kBytes, j0, sees_from, !sight.all(j0, BN), lane, tiles.any.hi <= j0 + 16 && tiles.any.sk <= j0 + 16);
+            __builtin_amdgcn_wave_barrier();
+        }
+    } else if constexpr (COPY) {
         int buf = 0;
         for (int it = it0; it < it1; it += W, buf ^= 1) {
             const int j0 = tiles.start(it);
@@ -563,16 +578,39 @@ __global__ __launch_bounds__(256) void k_attention_join(const AttentionArgs a, c
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
     float total = 0.f, acc[2] = {0.f, 0.f};
-    for (int s = 0; s < p.splits; ++s) {
-        const float* st = from.stats + 2 * (s * rows + row);
-        const float t = st[1];
-        if (t == 0.f) continue;
-        const float f = st[0] == top ? 1.f : exp2_fast((st[0] - top) * c2);
-        const float* sums = from.sums + (s * rows + row) * d.head_dim;
-        total = fmaf(f, t, total);
-        if (lane < d.head_dim) acc[0] = fmaf(f, sums[lane], acc[0]);
-        if (lane + 64 < d.head_dim) acc[1] = fmaf(f, sums[lane + 64], acc[1]);
+    for (int s0 = 0; s0 < p.splits; s0 += 64) {
+        // lane s: the factor of part s0 + s; then the parts' sums, eight loads at a time
+        float f = 0.f;
+        if (s0 + lane < p.splits) {
+            const float* st = from.stats + 2 * ((s0 + lane) * rows + row);
+            const float t = st[1];
+            if (t != 0.f) {
+                f = st[0] == top ? 1.f : exp2_fast((st[0] - top) * c2);
+                total = fmaf(f, t, total);
+            }
+        }
+        const int count = min(64, p.splits - s0);
+        const uint64_t some = __ballot(f != 0.f);          // (also a NaN)
+        for (int s = 0; s < count; s += 8) {
+            if (!((some >> s) & 255)) continue;
+            float v[8][2];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float* sums = from.sums + (min(s0 + s + k, p.splits - 1) * rows + row) * d.head_dim;
+                v[k][0] = lane < d.head_dim ? sums[lane] : 0.f;
+                v[k][1] = lane + 64 < d.head_dim ? sums[lane + 64] : 0.f;
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float g = __shfl(f, (s + k) & 63);
+                if (!((some >> s >> k) & 1)) continue;      // a part without terms has no sums
+                acc[0] = fmaf(g, v[k][0], acc[0]);
+                acc[1] = fmaf(g, v[k][1], acc[1]);
+            }
+        }
     }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o);
     T* out = static_cast<T*>(a.out) + b * d.out_stride[0] + i * d.out_stride[1] + hq * d.out_stride[2];
     float* lse = a.lse ? a.lse + row : nullptr;
     const float inv = total == 0.f ? 0.f : 1.f / total;

@@ -248,19 +248,25 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_rmsnorm_grad(const No
     }
 }
 
-// dweight[c] = sum over blocks: 32 columns a block, eight lanes down each.
-__global__ __launch_bounds__(256) void k_norm_dweight(const float* partial, int blocks, int width, float* dweight) {
-    __shared__ float part[8][32];
-    const int col = threadIdx.x & 31, sub = threadIdx.x >> 5, c = blockIdx.x * 32 + col;
-    float v = 0.f;
+// dweight[c] = sum over blocks: 16 columns a block and 64 lanes down each, which take
+// every 64th row of the sums, four loads at a time (a chain of loads one after the other
+// took 20 us over 512 x 1001 sums; so, 4 us).
+__global__ __launch_bounds__(1024) void k_norm_dweight(const float* partial, int blocks, int width, float* dweight) {
+    __shared__ float part[64][17];
+    const int col = threadIdx.x & 15, sub = threadIdx.x >> 4, c = blockIdx.x * 16 + col;
+    float v[4] = {0.f, 0.f, 0.f, 0.f};
     if (c < width)
-        for (int b = sub; b < blocks; b += 8) v += partial[(int64_t)b * width + c];
-    part[sub][col] = v;
-    __syncthreads();
-    if (sub || c >= width) return;
+        for (int b = sub; b < blocks; b += 256) {
 #pragma unroll
-    for (int s = 1; s < 8; ++s) v += part[s][col];
-    dweight[c] = v;
+            for (int i = 0; i < 4; ++i)
+                if (b + 64 * i < blocks) v[i] += partial[(int64_t)(b + 64 * i) * width + c];
+        }
+    part[sub][col] = (v[0] + v[1]) + (v[2] + v[3]);
+    __syncthreads();
+    // a wave of the 16 takes one column
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const float sum = wave_sum(part[lane][wave]);
+    if (lane == 0 && blockIdx.x * 16 + wave < width) dweight[blockIdx.x * 16 + wave] = sum;
 }
 
 // lanes and steps of a row by its width
@@ -319,7 +325,7 @@ void launch_rmsnorm_grad(const NormGradArgs& a, hipStream_t s) {
     a.d.dtype == PD_F32 ? rmsnorm_grad_t<float>(a, blocks, s) : rmsnorm_grad_t<bf16>(a, blocks, s);
     PD_HIP(hipGetLastError());
     if (!a.dweight) return;
-    hipLaunchKernelGGL(k_norm_dweight, dim3((unsigned)((a.d.width + 31) / 32)), dim3(256), 0, s, a.partial, blocks,
+    hipLaunchKernelGGL(k_norm_dweight, dim3((unsigned)((a.d.width + 15) / 16)), dim3(1024), 0, s, a.partial, blocks,
                        (int)a.d.width, a.dweight);
     PD_HIP(hipGetLastError());
 }
