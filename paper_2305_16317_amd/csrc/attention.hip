@@ -113,6 +113,7 @@ struct Rows {
     __device__ __forceinline__ void attend(const char* k, const char* v, int j0, const See (&see)[QT], bool edge, int lane,
                                            bool half = false) {
         f32x16 s[QT][NK];
+        __builtin_amdgcn_s_setprio(1);       // matrix instructions go first: the other wave's vector ones fill in
 #pragma unroll
         for (int kt = 0; kt < NK; ++kt) {
 #pragma unroll
@@ -124,6 +125,7 @@ struct Rows {
                 for (int i = 0; i < QT; ++i) s[i][kt] = mma(f, q[i][c], s[i][kt]);
             }
         }
+        __builtin_amdgcn_s_setprio(0);
         if (edge) {
 #pragma unroll
             for (int i = 0; i < QT; ++i)
@@ -185,6 +187,7 @@ struct Rows {
             }
             total[i] += sum;
         }
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int kt = 0; kt < NK; ++kt)
 #pragma unroll
@@ -200,6 +203,7 @@ struct Rows {
                     for (int i = 0; i < QT; ++i) o[i][t] = mma(f, p[i], o[i][t]);
                 }
             }
+        __builtin_amdgcn_s_setprio(0);
     }
 
     __device__ __forceinline__ void finish(int i) { total[i] += __shfl_xor(total[i], 32); }

@@ -173,7 +173,7 @@ extern "C" pd_status pd_rotary_apply(const pd_rotary_desc* desc, const void* q, 
         for (int i = 0; i < 3; ++i)
             for (int64_t s : {d.q_stride[i], d.k_stride[i], d.q_out_stride[i], d.k_out_stride[i]}) check_stride(s);
         require(d.batch <= (int64_t)1 << 31 && d.length <= (int64_t)1 << 31, "batch or length out of range");
-        const int64_t units = d.head_dim / 16 + 2;
+        const int64_t units = d.head_dim / 8 + 2;
         if (d.batch * d.length > ((int64_t)1 << 38) / (units * (d.heads_q + d.heads_k)))
             fail(PD_ERR_UNSUPPORTED, "more than 2^42 values in one call are not implemented");
         if (d.batch == 0 || d.length == 0) return;

@@ -3,9 +3,11 @@
 //   pair k of a head at position p:  (a, b) -> (a c - b s, a s + b c),  (c, s) = table[p][k]
 //
 // Bound by memory (each value read and written once; the table's row is shared
-// by a token's heads).  A lane holds the (cos, sin) of eight pairs in registers
-// and turns those pairs of several heads: two loads and two stores of eight
-// values a head in either layout.  q and k go in one launch.
+// by a token's heads).  A lane holds the (cos, sin) of a unit's pairs in registers and
+// turns that unit in several heads.  A unit is eight pairs with halves (two runs of eight
+// values), four with pairs side by side (one run), and eight values where they are
+// copied: neighbouring lanes load neighbouring 16 bytes of bfloat16.  q and k go in one
+// launch.
 #include "ops.h"
 
 namespace pd {
@@ -34,10 +36,11 @@ __global__ __launch_bounds__(256) void k_rotary_table(const pd_rotary_table_desc
     table[2 * i + 1] = (float)(sn * d.magnitude);
 }
 
-// One lane: unit u of a token (eight pairs while u < pair_units, then sixteen
-// values to copy) in the heads hs, hs + lanes_h, ...; the heads of q, then of k.
+// One lane: unit u of a token (pairs while u < pair_units, then values to copy) in the
+// heads hs, hs + lanes_h, ...; the heads of q, then of k.
 template <typename T, bool HALF>
 __global__ __launch_bounds__(256) void k_rotary(const RotaryArgs a, int units, int pair_units, int lanes_h, int64_t lanes) {
+    constexpr int kPairs = HALF ? 8 : 4;
     const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (id >= lanes) return;
     const int per_token = units * lanes_h;
@@ -47,32 +50,28 @@ __global__ __launch_bounds__(256) void k_rotary(const RotaryArgs a, int units, i
     const int64_t b = token / a.d.length, i = token - b * a.d.length;
     const int R = a.d.rotary_dim, half = R / 2;
     const bool turn = u < pair_units;
-    // first element of the two runs of eight, and how many of each count
-    int e0, e1, n0, n1;
-    f32x8 cs = {}, sn = {};
+    // first element of the run (halves: and of the second), and how many of each count
+    int e0, n0;
+    float cs[kPairs], sn[kPairs];
     if (turn) {
-        const int k0 = u * 8, pairs = half - k0 < 8 ? half - k0 : 8;
+        const int k0 = u * kPairs, pairs = min(half - k0, kPairs);
         e0 = HALF ? k0 : 2 * k0;
-        e1 = HALF ? k0 + half : 2 * k0 + 8;
         n0 = HALF ? pairs : 2 * pairs;
-        n1 = HALF ? pairs : 2 * pairs - 8;
         int64_t pos = a.positions[b * a.d.position_stride + i];
         pos = pos < 0 ? 0 : (pos >= a.d.table_rows ? a.d.table_rows - 1 : pos);
         const float* t = a.table + (pos * half + k0) * 2;
-        const f32x8 lo = load8(t, 2 * pairs), hi = load8(t + 8, 2 * pairs - 8);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            cs[e] = lo[2 * e];
-            sn[e] = lo[2 * e + 1];
-            cs[e + 4] = hi[2 * e];
-            sn[e + 4] = hi[2 * e + 1];
+        for (int r = 0; r < kPairs / 4; ++r) {
+            const f32x8 v = load8(t + 8 * r, 2 * pairs - 8 * r);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                cs[4 * r + e] = v[2 * e];
+                sn[4 * r + e] = a.d.backward ? -v[2 * e + 1] : v[2 * e + 1];
+            }
         }
-        if (a.d.backward) sn = -sn;
     } else {
-        e0 = R + (u - pair_units) * 16;
-        e1 = e0 + 8;
+        e0 = R + (u - pair_units) * 8;
         n0 = a.d.head_dim - e0;
-        n1 = n0 - 8;
     }
     const int heads = a.d.heads_q + a.d.heads_k;
     for (int h = hs; h < heads; h += lanes_h) {
@@ -80,37 +79,40 @@ __global__ __launch_bounds__(256) void k_rotary(const RotaryArgs a, int units, i
         const int hh = is_k ? h - a.d.heads_q : h;
         const int64_t* st = is_k ? a.d.k_stride : a.d.q_stride;
         const int64_t* so = is_k ? a.d.k_out_stride : a.d.q_out_stride;
-        const T* x = static_cast<const T*>(is_k ? a.k : a.q) + b * st[0] + i * st[1] + hh * st[2];
-        T* y = static_cast<T*>(is_k ? a.k_out : a.q_out) + b * so[0] + i * so[1] + hh * so[2];
-        typename Vec8<T>::type p = load8(x + e0, n0), q = {};
-        if (n1 > 0) q = load8(x + e1, n1);
-        if (turn) {
-            const f32x8 v = widen(p), w = widen(q);
-            f32x8 ra, rb;
-            if constexpr (HALF) {
-                ra = v * cs - w * sn;
-                rb = v * sn + w * cs;
-            } else {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    ra[2 * e] = v[2 * e] * cs[e] - v[2 * e + 1] * sn[e];
-                    ra[2 * e + 1] = v[2 * e] * sn[e] + v[2 * e + 1] * cs[e];
-                    rb[2 * e] = w[2 * e] * cs[e + 4] - w[2 * e + 1] * sn[e + 4];
-                    rb[2 * e + 1] = w[2 * e] * sn[e + 4] + w[2 * e + 1] * cs[e + 4];
-                }
-            }
-            p = narrow<T>(ra);
-            q = narrow<T>(rb);
+        const T* x = static_cast<const T*>(is_k ? a.k : a.q) + b * st[0] + i * st[1] + hh * st[2] + e0;
+        T* y = static_cast<T*>(is_k ? a.k_out : a.q_out) + b * so[0] + i * so[1] + hh * so[2] + e0;
+        typename Vec8<T>::type p = load8(x, n0);
+        if (!turn) {
+            store8(y, n0, p);
+            continue;
         }
-        store8(y + e0, n0, p);
-        if (n1 > 0) store8(y + e1, n1, q);
+        const f32x8 v = widen(p);
+        f32x8 ra;
+        if constexpr (HALF) {
+            const f32x8 w = widen(load8(x + half, n0));
+            f32x8 rb;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                ra[e] = v[e] * cs[e] - w[e] * sn[e];
+                rb[e] = v[e] * sn[e] + w[e] * cs[e];
+            }
+            store8(y + half, n0, narrow<T>(rb));
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                ra[2 * e] = v[2 * e] * cs[e] - v[2 * e + 1] * sn[e];
+                ra[2 * e + 1] = v[2 * e] * sn[e] + v[2 * e + 1] * cs[e];
+            }
+        }
+        store8(y, n0, narrow<T>(ra));
     }
 }
 
 template <typename T>
 void rotary_t(const RotaryArgs& a, hipStream_t s) {
     const pd_rotary_desc& d = a.d;
-    const int pair_units = (d.rotary_dim / 2 + 7) / 8, units = pair_units + (d.head_dim - d.rotary_dim + 15) / 16;
+    const int pairs = d.layout == PD_ROTARY_HALF ? 8 : 4;
+    const int pair_units = (d.rotary_dim / 2 + pairs - 1) / pairs, units = pair_units + (d.head_dim - d.rotary_dim + 7) / 8;
     const int heads = d.heads_q + d.heads_k;
     const int64_t tokens = d.batch * d.length;
     // heads a lane: as many as leave 16 waves a compute unit, at most 8
