@@ -214,6 +214,12 @@ __global__ __launch_bounds__(256, (dq_blocks_per_cu<T, DP>())) void k_attention_
     f32x16 o[kDT];
 #pragma unroll
     for (int t = 0; t < kDT; ++t) o[t] = f32x16{};
+    // where the registers allow it the products dout v start from -delta
+    constexpr bool kStart = DP * sizeof(T) <= 128;
+    f32x16 start = {};
+    if constexpr (kStart)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) start[r] = -delta;
     for (int it = 0; it < tiles.count; ++it) {
         const int j0 = tiles.start(it);
         if constexpr (COPY) wait_copies();
@@ -224,29 +230,40 @@ __global__ __launch_bounds__(256, (dq_blocks_per_cu<T, DP>())) void k_attention_
         const char *lk = lds + (it & 1) * 2 * kBytes, *lv = lk + kBytes;
 #pragma unroll
         for (int kt = 0; kt < BN / 32; ++kt) {
-            f32x16 s = {}, dp = {};
-#pragma unroll
-            for (int c = 0; c < kSteps; ++c) s = mma(Ti::rows(lk, 32 * kt, c, lane), qf[c], s);
-#pragma unroll
-            for (int c = 0; c < kSteps; ++c) dp = mma(Ti::rows(lv, 32 * kt, c, lane), gf[c], dp);
+            f32x16 s = {}, dp = start;
+            // the products q k and dout v, then those with the keys' columns, read ahead
+            // (in turn, since a product waits for the last one with the same sum)
+            auto rows = [&](int n) { return Ti::rows(n % 2 ? lv : lk, 32 * kt, n / 2, lane); };
+            Stream<T, 2 * kSteps> rs;
+            rs.begin(rows);
+            rs.run(rows, [&](int n, const Frag<T>& f) {
+                if (n % 2 == 0)
+                    s = mma(f, qf[n / 2], s);
+                else
+                    dp = mma(f, gf[n / 2], dp);
+            });
+            auto cols = [&](int n) { return Ti::cols(lk, 32 * kt + 16 * (n / kDT), n % kDT, lane); };
+            Stream<T, 2 * kDT> cs;
+            cs.begin(cols);
             if (large) {
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[r] = probability(true, s[r], c2, lse2, d.scale, lse) * (dp[r] - delta);
+                for (int r = 0; r < 16; ++r) s[r] = probability(true, s[r], c2, lse2, d.scale, lse);
             } else {
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[r] = probability(false, s[r], c2, lse2, d.scale, lse) * (dp[r] - delta);
+                for (int r = 0; r < 16; ++r) s[r] = probability(false, s[r], c2, lse2, d.scale, lse);
             }
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] *= kStart ? dp[r] : dp[r] - delta;
             if (edge) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
                     if (!see_from(j0 + 32 * kt + tile_row(0, r))) s[r] = 0.f;
             }
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                const Frag<T> ds = as_frag<T>(s, c);
-#pragma unroll
-                for (int t = 0; t < kDT; ++t) o[t] = mma(Ti::cols(lk, 32 * kt + 16 * c, t, lane), ds, o[t]);
-            }
+            Frag<T> ds;
+            cs.run(cols, [&](int n, const Frag<T>& f) {
+                if (n % kDT == 0) ds = as_frag<T>(s, n / kDT);
+                o[n % kDT] = mma(f, ds, o[n % kDT]);
+            });
         }
     }
 
@@ -310,7 +327,8 @@ __global__ __launch_bounds__(256, (dkv_blocks_per_cu<T, DP>())) void k_attention
     constexpr int kSteps = DP / 16, kDT = DP / 32, BR = tile_rows<T, DP>(), kBytes = BR * Ti::kPitch;
     using F = Fill<T, DP, BR, 256>;
     __shared__ __align__(128) char lds[4 * kBytes];       // queries, output gradients; twice
-    __shared__ __align__(16) float stats[2][3][64];       // lse log2 e, delta, lse
+    __shared__ __align__(16) float stats[2][3][64];       // -lse / scale, -delta, lse
+    __shared__ int far[2];                                // whether a row's |lse| is large
     const pd_attention_desc& d = a.d;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
     const int id = near_blocks(blockIdx.x, gridDim.x), split = id % splits, unit = id / splits;
@@ -340,6 +358,7 @@ __global__ __launch_bounds__(256, (dkv_blocks_per_cu<T, DP>())) void k_attention
         fg.plan(d.dout_stride[1], units, threadIdx.x);
     }
     float stat = 0.f;
+    const float over = -1.f / d.scale;
     auto fetch = [&](int x, int buf) {
         const int g = x / per_head, i0 = first + (x - g * per_head) * BR;
         if (threadIdx.x < 2 * BR) {
@@ -365,11 +384,13 @@ __global__ __launch_bounds__(256, (dkv_blocks_per_cu<T, DP>())) void k_attention
         }
     };
     auto put_stat = [&](int buf) {
-        if (threadIdx.x < BR) {
-            stats[buf][0][threadIdx.x] = stat * kLog2e;
+        if (threadIdx.x < BR) {                           // (lanes of the first wave)
+            stats[buf][0][threadIdx.x] = stat * over;
             stats[buf][2][threadIdx.x] = stat;
+            const uint64_t some = __ballot(!(fabsf(stat) < kLarge));
+            if (threadIdx.x == 0) far[buf] = some != 0 || d.scale == 0.f;
         } else if (threadIdx.x < 2 * BR) {
-            stats[buf][1][threadIdx.x - BR] = stat;
+            stats[buf][1][threadIdx.x - BR] = -stat;
         }
     };
     if (x0 < x1) {
@@ -391,59 +412,70 @@ __global__ __launch_bounds__(256, (dkv_blocks_per_cu<T, DP>())) void k_attention
     f32x16 dk[kDT], dv[kDT];
 #pragma unroll
     for (int t = 0; t < kDT; ++t) dk[t] = dv[t] = f32x16{};
-    for (int x = x0; x < x1; ++x) {
-        const int buf = (x - x0) & 1, i0 = first + x % per_head * BR;
+    int pos = per_head ? x0 % per_head : 0;               // the tile's place among its head's
+    for (int x = x0; x < x1; ++x, pos = pos + 1 == per_head ? 0 : pos + 1) {
+        const int buf = (x - x0) & 1, i0 = first + pos * BR;
         if constexpr (COPY) wait_copies();
         lds_barrier();                                    // this tile is there, the other buffer is free
         if (x + 1 < x1) fetch(x + 1, buf ^ 1);
         if (!sight.none(i0, BR)) {
             const bool edge = !sight.all(i0, BR);
             const char *lq = lds + buf * 2 * kBytes, *lg = lq + kBytes;
+            const bool large = __builtin_amdgcn_readfirstlane(far[buf]);
 #pragma unroll
             for (int rt = 0; rt < BR / 32; ++rt) {
-                f32x16 s = {}, dp = {};
-#pragma unroll
-                for (int c = 0; c < kSteps; ++c) s = mma(Ti::rows(lq, 32 * rt, c, lane), kf[c], s);
-#pragma unroll
-                for (int c = 0; c < kSteps; ++c) dp = mma(Ti::rows(lg, 32 * rt, c, lane), vf[c], dp);
-                float l2[16], dl[16];
-                bool large = false;
+                // the products q k start from -lse / scale and the products dout v from -delta,
+                // so that p = 2^(c2 s) and ds = p dp
+                f32x16 s, dp;
 #pragma unroll
                 for (int r = 0; r < 16; r += 4) {
                     const int at = 32 * rt + tile_row(lane, r);
-                    const f32x4 x4 = *reinterpret_cast<const f32x4*>(&stats[buf][0][at]);
-                    const f32x4 y4 = *reinterpret_cast<const f32x4*>(&stats[buf][1][at]);
+                    const f32x4 u = *reinterpret_cast<const f32x4*>(&stats[buf][0][at]);
+                    const f32x4 v = *reinterpret_cast<const f32x4*>(&stats[buf][1][at]);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        l2[r + e] = x4[e];
-                        dl[r + e] = y4[e];
-                        large = large || !(fabsf(x4[e]) < kLarge);
-                    }
+                    for (int e = 0; e < 4; ++e) s[r + e] = u[e], dp[r + e] = v[e];
                 }
-                if (__any(large)) {
+                if (large) s = f32x16{};
+                auto rows = [&](int n) { return Ti::rows(n % 2 ? lg : lq, 32 * rt, n / 2, lane); };
+                Stream<T, 2 * kSteps> rs;
+                rs.begin(rows);
+                rs.run(rows, [&](int n, const Frag<T>& f) {
+                    if (n % 2 == 0)
+                        s = mma(f, kf[n / 2], s);
+                    else
+                        dp = mma(f, vf[n / 2], dp);
+                });
+                // then, 16 rows at a time, dv with the output gradients' columns and dk with the queries'
+                auto cols = [&](int n) {
+                    const int c = n / (2 * kDT), t = n % (2 * kDT);
+                    return t < kDT ? Ti::cols(lg, 32 * rt + 16 * c, t, lane) : Ti::cols(lq, 32 * rt + 16 * c, t - kDT, lane);
+                };
+                Stream<T, 4 * kDT> cs;
+                cs.begin(cols);
+                if (large) {
 #pragma unroll
                     for (int r = 0; r < 16; ++r)
-                        s[r] = probability(true, s[r], c2, l2[r], d.scale, stats[buf][2][32 * rt + tile_row(lane, r)]);
+                        s[r] = probability(true, s[r], 0.f, 0.f, d.scale, stats[buf][2][32 * rt + tile_row(lane, r)]);
                 } else {
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) s[r] = probability(false, s[r], c2, l2[r], d.scale, 0.f);
+                    for (int r = 0; r < 16; ++r) s[r] = exp2_fast(s[r] * c2);
                 }
 #pragma unroll
-                for (int r = 0; r < 16; ++r) dp[r] = s[r] * (dp[r] - dl[r]);
+                for (int r = 0; r < 16; ++r) dp[r] *= s[r];
                 if (edge) {
 #pragma unroll
                     for (int r = 0; r < 16; ++r)
                         if (!see(i0 + 32 * rt + tile_row(0, r))) s[r] = dp[r] = 0.f;
                 }
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    const Frag<T> p = as_frag<T>(s, c), ds = as_frag<T>(dp, c);
-#pragma unroll
-                    for (int t = 0; t < kDT; ++t) {
-                        dv[t] = mma(Ti::cols(lg, 32 * rt + 16 * c, t, lane), p, dv[t]);
-                        dk[t] = mma(Ti::cols(lq, 32 * rt + 16 * c, t, lane), ds, dk[t]);
-                    }
-                }
+                Frag<T> p, ds;
+                cs.run(cols, [&](int n, const Frag<T>& f) {
+                    const int c = n / (2 * kDT), t = n % (2 * kDT);
+                    if (t == 0) p = as_frag<T>(s, c), ds = as_frag<T>(dp, c);
+                    if (t < kDT)
+                        dv[t] = mma(f, p, dv[t]);
+                    else
+                        dk[t - kDT] = mma(f, ds, dk[t - kDT]);
+                });
             }
         }
         if (x + 1 < x1) put_stat(buf ^ 1);
@@ -532,14 +564,20 @@ __global__ __launch_bounds__(256) void k_attention_dkv_join(const AttentionArgs 
         }
 }
 
-// Parts of the dk, dv kernel's queries: enough that its blocks fill the chip twice (two
-// fit a compute unit), and of at least four tiles.
+// Parts of the dk, dv kernel's queries, of at least four tiles: the fewest that keep its
+// blocks at work for nine tenths of the time (512 run at once: 288 blocks in 4 parts
+// are 2.25 rounds of them, in 5 parts 2.8), or the best up to eight.
 int dkv_splits(const pd_attention_desc& d) {
     const int64_t blocks = ((int64_t)d.kv_len + 127) / 128 * d.heads_kv * d.batch;
-    const int64_t tiles = ((int64_t)d.q_len + 63) / 64 * (d.heads_q / d.heads_kv);
-    int64_t s = blocks >= 512 ? 1 : (1024 + blocks - 1) / blocks;
-    if (s > tiles / 4) s = tiles / 4;
-    return s < 1 ? 1 : (int)s;
+    const int64_t most = ((int64_t)d.q_len + 63) / 64 * (d.heads_q / d.heads_kv) / 4;
+    int64_t best = 1;
+    double used = 0.0;
+    for (int64_t s = 1; s <= 8 && (s == 1 || s <= most) && used < 0.9; ++s) {
+        const int64_t n = blocks * s, rounds = (n + 511) / 512;
+        const double u = (double)n / (double)(rounds * 512);
+        if (u > used) best = s, used = u;
+    }
+    return (int)best;
 }
 
 template <typename T, int DP, bool COPY>

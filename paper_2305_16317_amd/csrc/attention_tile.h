@@ -121,6 +121,40 @@ struct Tile {
     }
 };
 
+// Runs COUNT products in order, each with a fragment from LDS: reads go G fragments at a
+// time, a group ahead of the products, so that a group's latency passes behind the
+// products of the one before.  (Left to itself the compiler reads a fragment just
+// before its product and waits about 100 cycles for it, three times the product.)
+template <typename T, int COUNT>
+struct Stream {
+    static constexpr int G = sizeof(T) == 2 ? (COUNT < 4 ? COUNT : 4) : 1, kGroups = (COUNT + G - 1) / G;
+    Frag<T> f[2][G];
+    template <class Read>
+    __device__ __forceinline__ void read(int g, Read& r) {
+#pragma unroll
+        for (int i = 0; i < G; ++i)
+            if (g * G + i < COUNT) f[g & 1][i] = r(g * G + i);
+    }
+    // the first group alone, ahead of other work
+    template <class Read>
+    __device__ __forceinline__ void begin(Read r) {
+        read(0, r);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    template <class Read, class Use>
+    __device__ __forceinline__ void run(Read r, Use use) {
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) {
+            if (g + 1 < kGroups) read(g + 1, r);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < G; ++i)
+                if (g * G + i < COUNT) use(g * G + i, f[g & 1][i]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+};
+
 // Four consecutive values of a result's column to memory, the first n of them.
 __device__ inline void store4(float* p, int n, f32x4 v) {
     if (n >= 4) {
