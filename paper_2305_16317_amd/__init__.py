@@ -583,6 +583,8 @@ def _attention(q, k, v, out, lse, causal, window, sinks, scale, q_lens, kv_lens)
         raise ValueError("q and k must be (batch, token, head, dim)")
     B, n, H, D = q.shape
     ks = (B, k.shape[1], k.shape[2], D)
+    if max(B, n, H, D, ks[1], ks[2]) > 0x7fffffff:
+        raise ValueError("a dimension is longer than 2^31 - 1")
     _written(out, "out")
     if lse is not None and (lse.dtype != torch.float32 or lse.shape != (B, H, n) or not lse.is_contiguous()):
         raise ValueError(f"lse must be contiguous float32 of shape {(B, H, n)}")

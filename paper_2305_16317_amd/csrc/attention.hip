@@ -678,6 +678,7 @@ Plan plan(const pd_attention_desc& d) {
         p.waves = tiles <= 2 ? 1 : few_waves_of(d);
         const int64_t per = 8 * p.waves;
         splits = p.units * p.waves >= 8192 ? 1 : (tiles + per - 1) / per;
+        if (splits > 4096) splits = 4096;
     } else {
         splits = p.units >= 256 ? 1 : 512 / p.units;
         if (splits > tiles / 4) splits = tiles / 4;
@@ -709,7 +710,9 @@ void attention_c(const AttentionArgs& a, hipStream_t s) {
 }
 template <typename T, int DP>
 void attention_t(const AttentionArgs& a, hipStream_t s) {
-    if (copies_fit(a.k, a.d.k_stride, a.d.head_dim, sizeof(T)) && copies_fit(a.v, a.d.v_stride, a.d.head_dim, sizeof(T)))
+    const pd_attention_desc& d = a.d;
+    if (copies_fit(a.k, d.k_stride, d.batch, d.kv_len, d.heads_kv, d.head_dim, sizeof(T)) &&
+        copies_fit(a.v, d.v_stride, d.batch, d.kv_len, d.heads_kv, d.head_dim, sizeof(T)))
         attention_c<T, DP, true>(a, s);
     else
         attention_c<T, DP, false>(a, s);

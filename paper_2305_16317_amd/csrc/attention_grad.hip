@@ -600,8 +600,11 @@ void attention_grad_c(const AttentionArgs& a, hipStream_t s) {
 template <typename T, int DP>
 void attention_grad_t(const AttentionArgs& a, hipStream_t s) {
     const pd_attention_desc& d = a.d;
-    if (copies_fit(a.k, d.k_stride, d.head_dim, sizeof(T)) && copies_fit(a.v, d.v_stride, d.head_dim, sizeof(T)) &&
-        copies_fit(a.q, d.q_stride, d.head_dim, sizeof(T)) && copies_fit(a.dout, d.dout_stride, d.head_dim, sizeof(T)))
+    auto fits = [&](const void* p, const int64_t* stride, int64_t tokens, int64_t heads) {
+        return copies_fit(p, stride, d.batch, tokens, heads, d.head_dim, sizeof(T));
+    };
+    if (fits(a.k, d.k_stride, d.kv_len, d.heads_kv) && fits(a.v, d.v_stride, d.kv_len, d.heads_kv) &&
+        fits(a.q, d.q_stride, d.q_len, d.heads_q) && fits(a.dout, d.dout_stride, d.q_len, d.heads_q))
         attention_grad_c<T, DP, true>(a, s);
     else
         attention_grad_c<T, DP, false>(a, s);

@@ -265,10 +265,11 @@ struct Fill {
         }
     }
 };
-inline bool copies_fit(const void* p, const int64_t* stride, int head_dim, int elem) {
+inline bool copies_fit(const void* p, const int64_t* stride, int64_t batch, int64_t tokens, int64_t heads, int head_dim, int elem) {
+    const int64_t count[3] = {batch, tokens, heads};       // (a stride over one element is never taken)
     for (int i = 0; i < 3; ++i)
-        if (stride[i] * elem % 16) return false;
-    return (uintptr_t)p % 16 == 0 && head_dim * elem % 16 == 0 && stride[1] * elem < (1 << 24);
+        if (count[i] > 1 && stride[i] * elem % 16) return false;
+    return (uintptr_t)p % 16 == 0 && head_dim * elem % 16 == 0 && (tokens <= 1 || stride[1] * elem < (1 << 24));
 }
 
 // ---------------------------------------------------------------- who sees what

@@ -305,13 +305,28 @@ void rmsnorm_grad_t(const NormGradArgs& a, int blocks, hipStream_t s) {
 
 }  // namespace
 
-void launch_rmsnorm(const NormArgs& a, hipStream_t s) {
-    const bool f8 = a.d.out_dtype == PD_F8E4M3;
-    if (a.d.dtype == PD_F32)
-        f8 ? rmsnorm_t<float, true>(a, s) : rmsnorm_t<float, false>(a, s);
-    else
-        f8 ? rmsnorm_t<bf16, true>(a, s) : rmsnorm_t<bf16, false>(a, s);
-    PD_HIP(hipGetLastError());
+// A launch holds fewer than 2^32 threads: 2^21 rows (of up to 1024 lanes) at a time.
+constexpr int64_t kLaunchRows = (int64_t)1 << 21;
+
+void launch_rmsnorm(const NormArgs& all, hipStream_t s) {
+    const bool f8 = all.d.out_dtype == PD_F8E4M3;
+    const int64_t elem = all.d.dtype == PD_F32 ? 4 : 2;
+    const int64_t scales = all.d.group ? (all.d.width + all.d.group - 1) / all.d.group : 1;
+    for (int64_t r0 = 0; r0 < all.d.rows; r0 += kLaunchRows) {
+        NormArgs a = all;
+        a.d.rows = all.d.rows - r0 < kLaunchRows ? all.d.rows - r0 : kLaunchRows;
+        a.x = static_cast<const char*>(a.x) + r0 * a.d.x_stride * elem;
+        if (a.residual) a.residual = static_cast<const char*>(a.residual) + r0 * a.d.residual_stride * elem;
+        if (a.sum) a.sum = static_cast<char*>(a.sum) + r0 * a.d.sum_stride * elem;
+        a.y = static_cast<char*>(a.y) + r0 * a.d.y_stride * (f8 ? 1 : elem);
+        if (a.scale) a.scale += r0 * scales;
+        if (a.rstd) a.rstd += r0;
+        if (a.d.dtype == PD_F32)
+            f8 ? rmsnorm_t<float, true>(a, s) : rmsnorm_t<float, false>(a, s);
+        else
+            f8 ? rmsnorm_t<bf16, true>(a, s) : rmsnorm_t<bf16, false>(a, s);
+        PD_HIP(hipGetLastError());
+    }
 }
 
 int norm_grad_blocks(const pd_rmsnorm_desc& d) {

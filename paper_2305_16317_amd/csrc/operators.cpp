@@ -74,8 +74,10 @@ pd_attention_desc check_attention(const pd_attention_desc* p) {
     const int64_t rows = (int64_t)d.q_len * (d.heads_q / d.heads_kv);
     if (rows > (int64_t)1 << 28 || d.kv_len > 1 << 28)
         fail(PD_ERR_UNSUPPORTED, "more than 2^28 keys, or queries of one key head, are not implemented");
-    if ((int64_t)d.batch * d.heads_kv * ((rows > d.kv_len ? rows : d.kv_len) / 32 + 1) > (int64_t)1 << 30)
-        fail(PD_ERR_UNSUPPORTED, "a grid of more than 2^30 tiles is not implemented");
+    // a launch holds fewer than 2^32 threads, 512 a block
+    const int64_t longest = rows > d.kv_len ? rows : d.kv_len;
+    if ((int64_t)d.batch * d.heads_kv > ((int64_t)1 << 22) / (longest / 128 + 1))
+        fail(PD_ERR_UNSUPPORTED, "more than 2^22 tiles of 128 queries or keys are not implemented");
     if ((int64_t)d.window >= (int64_t)d.q_len + d.kv_len) d.window = 0;
     if (d.sinks > d.kv_len) d.sinks = d.kv_len;
     if (!d.window) d.sinks = 0;
@@ -147,6 +149,8 @@ extern "C" pd_status pd_rotary_table(const pd_rotary_table_desc* desc, int64_t f
         }
         require(std::isfinite(d.magnitude), "magnitude must be finite");
         require(first >= 0 && first <= (int64_t)1 << 40 && rows >= 0 && rows <= (int64_t)1 << 28, "first or rows out of range");
+        if (rows > ((int64_t)1 << 31) / (d.rotary_dim / 2))
+            fail(PD_ERR_UNSUPPORTED, "a table of more than 2^31 pairs is not implemented");
         if (rows == 0) return;
         require(table != nullptr, "table must not be NULL");
         require_gfx950();
@@ -173,9 +177,10 @@ extern "C" pd_status pd_rotary_apply(const pd_rotary_desc* desc, const void* q, 
         for (int i = 0; i < 3; ++i)
             for (int64_t s : {d.q_stride[i], d.k_stride[i], d.q_out_stride[i], d.k_out_stride[i]}) check_stride(s);
         require(d.batch <= (int64_t)1 << 31 && d.length <= (int64_t)1 << 31, "batch or length out of range");
-        const int64_t units = d.head_dim / 8 + 2;
-        if (d.batch * d.length > ((int64_t)1 << 38) / (units * (d.heads_q + d.heads_k)))
-            fail(PD_ERR_UNSUPPORTED, "more than 2^42 values in one call are not implemented");
+        // a launch holds fewer than 2^32 threads (at least a unit of 8 values of 8 heads each)
+        const int64_t units = d.head_dim / 8 + 2, heads8 = ((int64_t)d.heads_q + d.heads_k + 7) / 8;
+        if (d.length && d.batch > ((int64_t)1 << 31) / (units * heads8) / d.length)
+            fail(PD_ERR_UNSUPPORTED, "so many tokens in one call are not implemented");
         if (d.batch == 0 || d.length == 0) return;
         require(q && positions && table && q_out && (!k || k_out), "NULL device pointer");
         require(d.table_rows >= 1, "table_rows must be >= 1");

@@ -166,6 +166,19 @@ def test_norm_strides_and_in_place(dtype):
     _close(dy.view(6, 33), rx, TOL[dtype])
 
 
+def test_norm_of_more_rows_than_a_launch_holds():
+    rows = (1 << 21) + 3
+    x, w = _rand((rows, 8), BF16, 25), _rand((8,), F32, 26)
+    y = torch.empty((rows, 8), device="cuda", dtype=torch.float8_e4m3fn)
+    scale, rstd, h = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda"), torch.empty_like(x)
+    pd.pd_rmsnorm_forward(x, w, y, residual=x, sum_out=h, scale=scale, rstd=rstd)
+    for part in (slice(0, 5), slice(rows - 5, rows)):
+        s, yr, rr = ot.rmsnorm(_np(x[part]), _np(x[part]), _np(w), 1e-6)
+        _close(h[part], s, TOL[BF16])
+        _close(rstd[part], rr, 2e-6)
+        _close(scale[part, None], ot.quantise(yr, 0)[1], 2e-6)
+
+
 def test_norm_refuses_what_it_cannot_read():
     x, w = torch.zeros((4, 8), device="cuda"), torch.ones(8, device="cuda")
     for bad in (lambda: pd.pd_rmsnorm_forward(x.t(), torch.ones(4, device="cuda"), torch.empty((8, 4), device="cuda")),
@@ -329,6 +342,15 @@ def test_attention_forward(case, dtype):
 def test_attention_layouts(n, m, D, layout, dtype):
     q, k, v, _ = _att_inputs(2, n, m, 4, 2, D, dtype, 5, layout)
     _forward(q, k, v, True, 60, 4, None, None, None, TOL[dtype], layout)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_attention_strides_over_single_elements(dtype):
+    """One sequence, one key head: their strides may be anything (here odd)."""
+    q, k, v, g = _att_inputs(1, 40, 90, 4, 1, 64, dtype, 6)
+    k, v = (x.contiguous().as_strided(x.shape, (13, 64, 7, 1)) for x in (k, v))
+    _forward(q, k, v, True, 30, 2, None, None, None, TOL[dtype])
+    _backward(q, k, v, g, True, 30, 2, None, None, None, TOL_GRAD[dtype])
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])

@@ -128,6 +128,13 @@ def test_rotary_table_refusals(kw, msg):
     assert _status("pd_rotary_table", ctypes.byref(_table()), 0, 0, None, None)[0] == pd.PD_OK
 
 
+def test_launches_past_2_32_threads_are_refused():
+    code, _ = _status("pd_rotary_table", ctypes.byref(_table(rotary_dim=128)), 0, 2**27, P, None)
+    assert code == pd.PD_ERR_UNSUPPORTED
+    for kw in (dict(batch=2**31, length=2**20), dict(batch=2**20, length=2**12, heads_q=64, head_dim=128, rotary_dim=64)):
+        assert _status("pd_rotary_apply", ctypes.byref(_rotary(**kw)), *[P] * 6, None)[0] == pd.PD_ERR_UNSUPPORTED
+
+
 def _rotary(**kw):
     st = pd._I64x3(64, 32, 8)
     d = dict(batch=2, length=3, heads_q=4, heads_k=2, head_dim=8, rotary_dim=8, layout=0, dtype=pd.PD_F32, backward=0,
