@@ -12,6 +12,7 @@ from __future__ import annotations
 import ctypes
 import dataclasses
 import os
+import struct
 from typing import Dict, List, Optional, Sequence
 
 import numpy as np
@@ -121,6 +122,11 @@ class _AttentionDesc(ctypes.Structure):
                 ("dout_stride", _I64x3)]
 
 
+# the same three as bytes: the calls pack them (a Structure with its arrays takes 2 us more)
+_RMSNORM_BYTES = struct.Struct("6q3if")
+_ROTARY_BYTES = struct.Struct("2q7i14q")
+_ATTENTION_BYTES = struct.Struct("10if24q")
+
 _LIB: Optional[ctypes.CDLL] = None
 
 
@@ -156,15 +162,15 @@ def load() -> ctypes.CDLL:
         "pd_workspace_destroy": ([vp], None),
         "pd_sample_sequential": ([vp, vp, u64, i32, P(i64), i32, vp, P(_Stats), vp, vp], i32),
         "pd_sample_picard": ([vp, vp, i32, f32, u64, i32, P(i64), i32, vp, P(_Stats), vp, vp], i32),
-        "pd_rmsnorm_forward": ([P(_RmsnormDesc)] + [vp] * 8, i32),
-        "pd_rmsnorm_backward_scratch": ([P(_RmsnormDesc), P(i64)], i32),
-        "pd_rmsnorm_backward": ([P(_RmsnormDesc)] + [vp] * 8 + [i64, vp], i32),
+        "pd_rmsnorm_forward": ([vp] + [vp] * 8, i32),
+        "pd_rmsnorm_backward_scratch": ([vp, P(i64)], i32),
+        "pd_rmsnorm_backward": ([vp] + [vp] * 8 + [i64, vp], i32),
         "pd_rotary_table": ([P(_RotaryTableDesc), i64, i64, vp, vp], i32),
-        "pd_rotary_apply": ([P(_RotaryDesc)] + [vp] * 7, i32),
-        "pd_attention_forward_scratch": ([P(_AttentionDesc), P(i64)], i32),
-        "pd_attention_forward": ([P(_AttentionDesc)] + [vp] * 8 + [i64, vp], i32),
-        "pd_attention_backward_scratch": ([P(_AttentionDesc), P(i64)], i32),
-        "pd_attention_backward": ([P(_AttentionDesc)] + [vp] * 12 + [i64, vp], i32),
+        "pd_rotary_apply": ([vp] + [vp] * 7, i32),
+        "pd_attention_forward_scratch": ([vp, P(i64)], i32),
+        "pd_attention_forward": ([vp] + [vp] * 8 + [i64, vp], i32),
+        "pd_attention_backward_scratch": ([vp, P(i64)], i32),
+        "pd_attention_backward": ([vp] + [vp] * 12 + [i64, vp], i32),
     }
     for name, (args, res) in sig.items():
         fn = getattr(L, name)
@@ -393,6 +399,13 @@ def pd_sample_picard(sched: Schedule, den: Denoiser, p: int, tau: float, noise_s
 _DTYPES = {torch.float32: PD_F32, torch.bfloat16: PD_BF16}
 
 
+def _pack(layout: struct.Struct, *values) -> bytes:
+    try:
+        return layout.pack(*values)
+    except (struct.error, OverflowError) as e:
+        raise ValueError(f"an argument does not fit its type: {e}") from None
+
+
 def _dtype(t: torch.Tensor) -> int:
     d = _DTYPES.get(t.dtype)
     if d is None:
@@ -437,7 +450,7 @@ def _strides(t: torch.Tensor, shape, dtype, what: str):
     s = t.stride()
     if s[3] != 1 and shape[3] > 1:
         raise ValueError(f"{what}: the last dimension must be contiguous")
-    return _I64x3(s[0], s[1], s[2])
+    return s[:3]
 
 
 def _written(t: torch.Tensor, what: str) -> None:
@@ -489,12 +502,12 @@ def pd_rmsnorm_forward(x: torch.Tensor, weight: torch.Tensor, y: torch.Tensor,
     for t in (y, sum_out):
         if t is not None:
             _written(t, "y or sum_out")
-    d = _RmsnormDesc(rows, width, _rows_of(x, sh, x.dtype, "x"),
+    d = _pack(_RMSNORM_BYTES, rows, width, _rows_of(x, sh, x.dtype, "x"),
                      _rows_of(residual, sh, x.dtype, "residual") if residual is not None else 0,
                      _rows_of(sum_out, sh, x.dtype, "sum_out") if sum_out is not None else 0,
                      _rows_of(y, sh, y.dtype if f8 else x.dtype, "y"),
                      dt, PD_F8E4M3 if f8 else dt, group, eps)
-    _check(load().pd_rmsnorm_forward(ctypes.byref(d), _ptr(x), _ptr(residual), _ptr(weight),
+    _check(load().pd_rmsnorm_forward(d, _ptr(x), _ptr(residual), _ptr(weight),
                                      _ptr(sum_out), _ptr(y), _ptr(scale), _ptr(rstd), _stream(stream)))
 
 
@@ -516,15 +529,15 @@ def pd_rmsnorm_backward(dy: torch.Tensor, sum_in: torch.Tensor, weight: torch.Te
     if rstd.dtype != torch.float32 or not rstd.is_contiguous() or rstd.numel() != rows:
         raise ValueError(f"rstd must be contiguous float32 of {rows} elements")
     _written(dx, "dx")
-    d = _RmsnormDesc(rows, width, _rows_of(dx, sh, dy.dtype, "dx"),
+    d = _pack(_RMSNORM_BYTES, rows, width, _rows_of(dx, sh, dy.dtype, "dx"),
                      _rows_of(dsum, sh, dy.dtype, "dsum") if dsum is not None else 0,
                      _rows_of(sum_in, sh, dy.dtype, "sum_in"), _rows_of(dy, sh, dy.dtype, "dy"),
                      dt, dt, 0, 0.0)
     L, need = load(), ctypes.c_int64(0)
     if dweight is not None:
-        _check(L.pd_rmsnorm_backward_scratch(ctypes.byref(d), ctypes.byref(need)))
+        _check(L.pd_rmsnorm_backward_scratch(d, ctypes.byref(need)))
     buf, have = _scratch(scratch, need.value, stream)
-    _check(L.pd_rmsnorm_backward(ctypes.byref(d), _ptr(dy), _ptr(sum_in), _ptr(weight), _ptr(rstd),
+    _check(L.pd_rmsnorm_backward(d, _ptr(dy), _ptr(sum_in), _ptr(weight), _ptr(rstd),
                                  _ptr(dsum), _ptr(dx), _ptr(dweight), _ptr(buf), have, _stream(stream)))
 
 
@@ -541,7 +554,7 @@ def pd_rotary_table(table: torch.Tensor, base: float = 10000.0, scaling: int = P
     _check(load().pd_rotary_table(ctypes.byref(d), first, table.shape[0], _ptr(table), _stream(stream)))
 
 
-_NO_STRIDES = _I64x3(0, 0, 0)
+_NO_STRIDES = (0, 0, 0)
 
 
 def pd_rotary_apply(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Tensor,
@@ -567,17 +580,17 @@ def pd_rotary_apply(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch
         _written(k_out, "k_out")
     _written(q_out, "q_out")
     ks = (B, n, K, D)
-    d = _RotaryDesc(B, n, H, K, D, 2 * table.shape[1], layout, dt, int(backward), table.shape[0],
-                    positions.stride(0) if len(shape) == 2 else 0,
-                    _strides(q, q.shape, q.dtype, "q"),
-                    _strides(k, ks, q.dtype, "k") if K else _NO_STRIDES,
-                    _strides(q_out, q.shape, q.dtype, "q_out"),
-                    _strides(k_out, ks, q.dtype, "k_out") if K else _NO_STRIDES)
-    _check(load().pd_rotary_apply(ctypes.byref(d), _ptr(q), _ptr(k), _ptr(positions), _ptr(table),
-                                  _ptr(q_out), _ptr(k_out), _stream(stream)))
+    d = _pack(_ROTARY_BYTES, B, n, H, K, D, 2 * table.shape[1], layout, dt, bool(backward), table.shape[0],
+                           positions.stride(0) if len(shape) == 2 else 0,
+                           *_strides(q, q.shape, q.dtype, "q"),
+                           *(_strides(k, ks, q.dtype, "k") if K else _NO_STRIDES),
+                           *_strides(q_out, q.shape, q.dtype, "q_out"),
+                           *(_strides(k_out, ks, q.dtype, "k_out") if K else _NO_STRIDES))
+    _check(load().pd_rotary_apply(d, _ptr(q), _ptr(k), _ptr(positions), _ptr(table), _ptr(q_out),
+                                  _ptr(k_out), _stream(stream)))
 
 
-def _attention(q, k, v, out, lse, causal, window, sinks, scale, q_lens, kv_lens):
+def _attention(q, k, v, out, lse, causal, window, sinks, scale, q_lens, kv_lens, grads=_NO_STRIDES * 4):
     dt = _dtype(q)
     if q.dim() != 4 or k.dim() != 4:
         raise ValueError("q and k must be (batch, token, head, dim)")
@@ -591,10 +604,11 @@ def _attention(q, k, v, out, lse, causal, window, sinks, scale, q_lens, kv_lens)
     for t, what in ((q_lens, "q_lens"), (kv_lens, "kv_lens")):
         if t is not None and (t.dtype != torch.int32 or t.shape != (B,) or not t.is_contiguous()):
             raise ValueError(f"{what} must be contiguous int32 of shape {(B,)}")
-    return _AttentionDesc(B, H, ks[2], D, n, ks[1], dt, int(causal), min(window, 0x7fffffff),
-                          min(sinks, 0x7fffffff), D ** -0.5 if scale is None else scale,
-                          _strides(q, q.shape, q.dtype, "q"), _strides(k, ks, q.dtype, "k"),
-                          _strides(v, ks, q.dtype, "v"), _strides(out, q.shape, q.dtype, "out"))
+    sh, t = q.shape, q.dtype
+    return _pack(
+        _ATTENTION_BYTES, B, H, ks[2], D, n, ks[1], dt, bool(causal), min(window, 0x7fffffff), min(sinks, 0x7fffffff),
+        D ** -0.5 if scale is None else scale, *_strides(q, sh, t, "q"), *_strides(k, ks, t, "k"),
+        *_strides(v, ks, t, "v"), *_strides(out, sh, t, "out"), *grads)
 
 
 def pd_attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor,
@@ -609,9 +623,9 @@ def pd_attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out:
     d = _attention(q, k, v, out, lse, causal, window, sinks, scale, q_lens, kv_lens)
     L, need = load(), ctypes.c_int64(0)
     if scratch is None:
-        _check(L.pd_attention_forward_scratch(ctypes.byref(d), ctypes.byref(need)))
+        _check(L.pd_attention_forward_scratch(d, ctypes.byref(need)))
     buf, have = _scratch(scratch, need.value, stream)
-    _check(L.pd_attention_forward(ctypes.byref(d), _ptr(q), _ptr(k), _ptr(v), _ptr(q_lens),
+    _check(L.pd_attention_forward(d, _ptr(q), _ptr(k), _ptr(v), _ptr(q_lens),
                                   _ptr(kv_lens), _ptr(out), _ptr(lse), _ptr(buf), have,
                                   _stream(stream)))
 
@@ -625,16 +639,19 @@ def pd_attention_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out
                           scratch: Optional[torch.Tensor] = None, stream=None) -> None:
     """Gradients dq, dk, dv of pd_attention_forward, from its out and lse and the gradient dout."""
     _on_gpu(q, k, v, out, lse, dout, dq, dk, dv, q_lens, kv_lens, scratch)
-    d = _attention(q, k, v, out, lse, causal, window, sinks, scale, q_lens, kv_lens)
-    for t, like, what in ((dq, q, "dq"), (dk, k, "dk"), (dv, v, "dv"), (dout, q, "dout")):
+    if q.dim() != 4 or k.dim() != 4:
+        raise ValueError("q and k must be (batch, token, head, dim)")
+    grads = []
+    for t, like, what in ((dq, q, "dq"), (dk, k, "dk"), (dv, k, "dv"), (dout, q, "dout")):
         if t is not dout:
             _written(t, what)
-        setattr(d, what + "_stride", _strides(t, like.shape, q.dtype, what))
+        grads += _strides(t, like.shape, q.dtype, what)
+    d = _attention(q, k, v, out, lse, causal, window, sinks, scale, q_lens, kv_lens, grads)
     L, need = load(), ctypes.c_int64(0)
     if scratch is None:
-        _check(L.pd_attention_backward_scratch(ctypes.byref(d), ctypes.byref(need)))
+        _check(L.pd_attention_backward_scratch(d, ctypes.byref(need)))
     buf, have = _scratch(scratch, need.value, stream)
-    _check(L.pd_attention_backward(ctypes.byref(d), _ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(lse),
+    _check(L.pd_attention_backward(d, _ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(lse),
                                    _ptr(dout), _ptr(q_lens), _ptr(kv_lens), _ptr(dq), _ptr(dk),
                                    _ptr(dv), _ptr(buf), have, _stream(stream)))
 

@@ -563,6 +563,8 @@ def test_attention_refuses_what_it_cannot_read():
                 lambda: pd.pd_attention_forward(q.transpose(2, 3), k, k, o)):
         with pytest.raises(ValueError):
             bad()
+    with pytest.raises(ValueError):
+        pd.pd_attention_forward(q, k, k, o, scale=1e60)
     for kw in (dict(window=-1), dict(sinks=-2), dict(scale=float("nan"))):
         with pytest.raises(pd.PdError):
             pd.pd_attention_forward(q, k, k, o, **kw)

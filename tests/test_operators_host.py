@@ -201,6 +201,19 @@ def test_attention_null_arguments():
     assert _status("pd_attention_forward", None, *[P] * 8, 0, None)[0] == pd.PD_ERR_INVALID_ARG
 
 
+def test_packed_descriptions_are_laid_out_as_the_structures():
+    for packed, struct in ((pd._RMSNORM_BYTES, pd._RmsnormDesc), (pd._ROTARY_BYTES, pd._RotaryDesc),
+                           (pd._ATTENTION_BYTES, pd._AttentionDesc)):
+        assert packed.size == ctypes.sizeof(struct)
+        n = len(packed.unpack(bytes(packed.size)))
+        d = struct.from_buffer_copy(packed.pack(*range(1, n + 1)))
+        flat = []
+        for name, kind in struct._fields_:
+            v = getattr(d, name)
+            flat += list(v) if hasattr(v, "__len__") else [v]
+        assert flat == list(range(1, n + 1))
+
+
 # ------------------------------------------------------------------ refusals of the binding
 def test_binding_refuses_cpu_tensors_and_wrong_types():
     x = torch.zeros(2, 8)
