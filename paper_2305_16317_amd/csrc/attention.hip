@@ -72,11 +72,12 @@ __device__ void attend_row(const AttentionArgs& a, const T* q, const T* k, const
 }
 
 // The 32 QT rows of a wave (lane: rows 32 t + lane % 32) and what they have summed.
-template <typename T, int DP, int QT>
+template <class As, int DP, int QT>
 struct Rows {
     static constexpr int kSteps = DP / 16, kDT = DP / 32;
-    using Ti = Tile<T, DP>;
-    Frag<T> q[QT][kSteps];
+    using T = typename As::Type;
+    using Operand = typename As::Operand;
+    Operand q[QT][kSteps];
     f32x16 o[QT][kDT];           // transposed: the lane's row, columns 32 t + tile_row
     float top[QT], limit[QT];    // the reference and the score that raises it (unscaled)
     float mc[QT];                // top c2
@@ -101,9 +102,9 @@ struct Rows {
 #pragma unroll
         for (int c = 0; c < kSteps; ++c) {
             const int e = 16 * c + 8 * h;
-            q[i][c] = Frag<T>{};
-            if (real && d.scale != 0.f) q[i][c] = load8(qp + e, d.head_dim - e);
-            if (d.scale < 0.f) q[i][c] = -q[i][c];
+            f32x8 v = {};
+            if (real && d.scale != 0.f) v = widen(load8(qp + e, d.head_dim - e));
+            q[i][c] = As::make(d.scale < 0.f ? -v : v);
         }
     }
 
@@ -120,7 +121,7 @@ struct Rows {
             for (int i = 0; i < QT; ++i) s[i][kt] = f32x16{};
 #pragma unroll
             for (int c = 0; c < kSteps; ++c) {
-                const Frag<T> f = Ti::rows(k, 32 * kt, c, lane);
+                const Operand f = As::rows(k, 32 * kt, c, lane);
 #pragma unroll
                 for (int i = 0; i < QT; ++i) s[i][kt] = mma(f, q[i][c], s[i][kt]);
             }
@@ -193,12 +194,12 @@ struct Rows {
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
                 if (c == 1 && half) continue;
-                Frag<T> p[QT];
+                Operand p[QT];
 #pragma unroll
-                for (int i = 0; i < QT; ++i) p[i] = as_frag<T>(s[i][kt], c);
+                for (int i = 0; i < QT; ++i) p[i] = As::make(eight(s[i][kt], c));
 #pragma unroll
                 for (int t = 0; t < kDT; ++t) {
-                    const Frag<T> f = Ti::cols(v, 32 * kt + 16 * c, t, lane);
+                    const Operand f = As::cols(v, 32 * kt + 16 * c, t, lane);
 #pragma unroll
                     for (int i = 0; i < QT; ++i) o[i][t] = mma(f, p[i], o[i][t]);
                 }
@@ -243,9 +244,10 @@ struct Plan {
 __device__ inline int rows_to_query(const Plan& p, int row) { return p.shift >= 0 ? row >> p.shift : row / p.group; }
 
 // The rows row0 .. row0 + 31, tile x of the wave's.
-template <typename T, int DP, int QT>
-__device__ __forceinline__ void store_rows(const AttentionArgs& a, const Plan& p, Rows<T, DP, QT>& w, int x, const Seq& seq, int b,
-                                           int hk, int row0, int split, const T* kb, const T* vb) {
+template <class As, int DP, int QT>
+__device__ __forceinline__ void store_rows(const AttentionArgs& a, const Plan& p, Rows<As, DP, QT>& w, int x, const Seq& seq, int b,
+                                           int hk, int row0, int split, const typename As::Type* kb, const typename As::Type* vb) {
+    using T = typename As::Type;
     const pd_attention_desc& d = a.d;
     const int lane = threadIdx.x & 63, h = lane >> 5, row = row0 + (lane & 31);
     const bool real = row < p.rows;
@@ -359,7 +361,7 @@ __global__ __launch_bounds__(256, 2) void k_attention(const AttentionArgs a, con
     };
     if (it0 < it1) fetch(it0, 0);
 
-    Rows<T, DP, QT> w;
+    Rows<AsIs<T, DP>, DP, QT> w;
     w.start(d);
     See see[QT];
     const Sight sight = sight_of(d, seq, rows_to_query(p, row0), row0 + 32 * QT <= p.rows ? rows_to_query(p, row0 + 32 * QT - 1) : seq.n);
@@ -384,6 +386,69 @@ __global__ __launch_bounds__(256, 2) void k_attention(const AttentionArgs a, con
     }
 #pragma unroll
     for (int x = 0; x < QT; ++x) store_rows(a, p, w, x, seq, b, hk, row0 + 32 * x, split, kb, vb);
+}
+
+// The same for float32, in three parts: a tile is read into registers while the one
+// before is worked on, and split on its way to LDS, once for the block's four waves.
+template <int DP>
+__global__ __launch_bounds__(256, (DP <= 96 ? 2 : 1)) void k_attention_parts(const AttentionArgs a, const Plan p) {
+    constexpr int BN = tile_rows<float, DP>(), BM = 128, kUnits = BN * (DP / 8), kEach = (kUnits + 255) / 256;
+    using As = InParts<DP, BN>;
+    __shared__ __align__(128) char lds[2 * As::kBytes];   // keys, values
+    char *lk = lds, *lv = lds + As::kBytes;
+    const pd_attention_desc& d = a.d;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int id = near_blocks(blockIdx.x, gridDim.x);
+    const int part = id % p.splits, unit = id / p.splits;
+    const int tile = p.row_tiles - 1 - unit % p.row_tiles, head = unit / p.row_tiles;     // the longest rows first
+    const int hk = head % d.heads_kv, b = head / d.heads_kv;
+    const Seq seq = sequence(a, b);
+    const int row0 = tile * BM + wave * 32, row = row0 + (lane & 31);
+    const float* kb = static_cast<const float*>(a.k) + b * d.k_stride[0] + hk * d.k_stride[2];
+    const float* vb = static_cast<const float*>(a.v) + b * d.v_stride[0] + hk * d.v_stride[2];
+
+    const int i0 = rows_to_query(p, tile * BM), i1 = min(rows_to_query(p, tile * BM + BM - 1), seq.n - 1);
+    const KeyTiles<BN> tiles(i0 <= i1 ? sees_any(d, seq, i0, i1) : See{0, 0, 0});
+    const int it0 = part * p.split_tiles, it1 = min(tiles.count, it0 + p.split_tiles);
+    f32x8 kr[kEach], vr[kEach];
+    auto fetch = [&](int it) {
+        const int j0 = tiles.start(it);
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int u = i * 256 + threadIdx.x, j = j0 + u / (DP / 8), e = u % (DP / 8) * 8;
+            kr[i] = vr[i] = f32x8{};
+            if (u >= kUnits || !tiles.any(j)) continue;
+            kr[i] = load8(kb + (int64_t)j * d.k_stride[1] + e, d.head_dim - e);
+            vr[i] = load8(vb + (int64_t)j * d.v_stride[1] + e, d.head_dim - e);
+        }
+    };
+    if (it0 < it1) fetch(it0);
+
+    Rows<As, DP, 1> w;
+    w.start(d);
+    const Sight sight = sight_of(d, seq, rows_to_query(p, row0), row0 + 32 <= p.rows ? rows_to_query(p, row0 + 31) : seq.n);
+    const bool real = row < p.rows;
+    const int qi = real ? rows_to_query(p, row) : 0, hq = hk * p.group + (real ? row - qi * p.group : 0);
+    See see[1] = {real ? sees(d, seq, qi) : See{0, 0, 0}};
+    w.load(0, d, static_cast<const float*>(a.q) + b * d.q_stride[0] + qi * d.q_stride[1] + hq * d.q_stride[2],
+           real && !see[0].none(), lane);
+    see[0] = see[0].from(lane);
+    for (int it = it0; it < it1; ++it) {
+        const int j0 = tiles.start(it);
+        lds_barrier();                                    // the tile before has been read
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int u = i * 256 + threadIdx.x;
+            if (u >= kUnits) continue;
+            As::put(lk, u / (DP / 8), u % (DP / 8), kr[i]);
+            As::put(lv, u / (DP / 8), u % (DP / 8), vr[i]);
+        }
+        lds_barrier();                                    // this one is there
+        if (it + 1 < it1) fetch(it + 1);
+        if (sight.none(j0, BN)) continue;
+        w.template attend<BN / 32>(lk, lv, j0, see, !sight.all(j0, BN), lane);
+    }
+    store_rows(a, p, w, 0, seq, b, hk, row0, part, kb, vb);
 }
 
 // Waves that share the keys of at most 32 rows, each with two buffers of its own.
@@ -447,7 +512,7 @@ __global__ __launch_bounds__(64 * W) void k_attention_few(const AttentionArgs a,
         }
     };
     if (COPY && it0 < it1) fetch(it0, lds);
-    Rows<T, DP, 1> w;
+    Rows<AsIs<T, DP>, DP, 1> w;
     w.start(d);
     w.load(0, d, static_cast<const T*>(a.q) + b * d.q_stride[0] + qi * d.q_stride[1] + hq * d.q_stride[2], real && !see.none(), lane);
     const See sees_from[1] = {see.from(lane)};
@@ -698,6 +763,8 @@ void attention_c(const AttentionArgs& a, hipStream_t s) {
         hipLaunchKernelGGL((k_attention_few<T, DP, COPY, 1>), few, dim3(64), 0, s, a, p);
     else if (few_rows(a.d))
         hipLaunchKernelGGL((k_attention_few<T, DP, COPY, W>), few, dim3(64 * W), 0, s, a, p);
+    else if constexpr (sizeof(T) == 4)
+        hipLaunchKernelGGL((k_attention_parts<DP>), dim3((unsigned)(p.units * p.splits)), dim3(256), 0, s, a, p);
     else if (p.wave_tiles == 1)
         hipLaunchKernelGGL((k_attention<T, DP, COPY, 1>), dim3((unsigned)(p.units * p.splits)), dim3(256), 0, s, a, p);
     else if constexpr (wave_tiles<T, DP>() == 2)

@@ -20,12 +20,15 @@ using namespace attn;
 
 // p = e^(scale s - lse): one fused multiply-add in base 2 while |lse| is under 1024;
 // beyond, where rounding lse log2 e would show, from the difference itself, which
-// is not above 0 (a score of 10^8 has a unit in the last place of 8).
+// is not above 0 (a score of 10^8 has a unit in the last place of 8).  Past 2^20 a
+// difference within the rounding of the score's terms counts as none: the forward pass
+// may have summed them in another order.
 constexpr float kLarge = 1024.f;
 __device__ inline float probability(bool large, float s, float c2, float lse2, float scale, float lse) {
     if (!large) return exp2_fast(fmaf(s, c2, -lse2));
-    const float x = (s * scale - lse) * kLog2e;
-    return exp2_fast(x > 0.f ? 0.f : x);
+    const float x = s * scale - lse, size = fabsf(lse);
+    if (x > 0.f || (size > 0x1p20f && fabsf(x) <= 0x1p-17f * size)) return x != x ? x : 1.f;
+    return exp2_fast(x * kLog2e);
 }
 
 // Scratch: delta of every row, then the parts of dk and dv, [split][sequence, key

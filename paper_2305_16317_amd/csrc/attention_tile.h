@@ -52,12 +52,15 @@ __device__ inline f32x16 mma(f32x8 a, f32x8 b, f32x16 c) {
 __device__ inline int tile_row(int lane, int r) { return 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3); }
 
 // registers 8c..8c+7 of a result as the next product's operand
-template <typename T>
-__device__ inline Frag<T> as_frag(const f32x16& v, int c) {
+__device__ inline f32x8 eight(const f32x16& v, int c) {
     f32x8 f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) f[e] = v[8 * c + e];
-    return narrow<T>(f);
+    return f;
+}
+template <typename T>
+__device__ inline Frag<T> as_frag(const f32x16& v, int c) {
+    return narrow<T>(eight(v, c));
 }
 
 // A tile of rows in LDS: 16-byte units, those of row r exchanged by swz(r), so that the
@@ -118,6 +121,68 @@ struct Tile {
             *reinterpret_cast<f32x4*>(lds + at(row, 2 * c)) = f32x4{v[0], v[1], v[2], v[3]};
             *reinterpret_cast<f32x4*>(lds + at(row, 2 * c + 1)) = f32x4{v[4], v[5], v[6], v[7]};
         }
+    }
+};
+
+// ---------------------------------------------------------------- float32 in three parts
+// A float32 value is the sum of three bfloat16 ones (8 bits each; exact but where the
+// last falls under the smallest, for values under 2^-110), and a product of two such
+// values that of six products, what is left out being under 2^-24: 6 x 32 cycles for
+// 16 steps in place of 8 x 64, as accurate as float32's own instructions.  (An
+// infinity splits into infinity and NaN: its rows are formed again from memory.)
+struct Split {
+    bf16x8 h, m, l;
+};
+__device__ __forceinline__ Split split(f32x8 x) {
+    Split s;
+    s.h = narrow<bf16>(x);
+    const f32x8 r = x - widen(s.h);
+    s.m = narrow<bf16>(r);
+    s.l = narrow<bf16>(r - widen(s.m));
+    return s;
+}
+__device__ __forceinline__ f32x16 mma(const Split& a, const Split& b, f32x16 c) {
+    c = mma(a.l, b.h, c);
+    c = mma(a.h, b.l, c);
+    c = mma(a.m, b.m, c);
+    c = mma(a.m, b.h, c);
+    c = mma(a.h, b.m, c);
+    return mma(a.h, b.h, c);
+}
+
+// How a kernel holds its operands: as they are, in tiles that copies fill, or in three
+// parts, in three tiles that are filled through the registers.
+template <typename T, int DP>
+struct AsIs {
+    using Type = T;
+    using Operand = Frag<T>;
+    static constexpr int kPitch = Tile<T, DP>::kPitch;
+    static __device__ __forceinline__ Operand make(f32x8 v) { return narrow<T>(v); }
+    static __device__ __forceinline__ Operand rows(const char* lds, int row0, int c, int lane) {
+        return Tile<T, DP>::rows(lds, row0, c, lane);
+    }
+    static __device__ __forceinline__ Operand cols(const char* lds, int row0, int dt, int lane) {
+        return Tile<T, DP>::cols(lds, row0, dt, lane);
+    }
+};
+template <int DP, int ROWS>
+struct InParts {
+    using Type = float;
+    using Operand = Split;
+    using Ti = Tile<bf16, DP>;
+    static constexpr int kPart = ROWS * Ti::kPitch, kBytes = 3 * kPart;
+    static __device__ __forceinline__ Operand make(f32x8 v) { return split(v); }
+    static __device__ __forceinline__ Operand rows(const char* lds, int row0, int c, int lane) {
+        return Split{Ti::rows(lds, row0, c, lane), Ti::rows(lds + kPart, row0, c, lane), Ti::rows(lds + 2 * kPart, row0, c, lane)};
+    }
+    static __device__ __forceinline__ Operand cols(const char* lds, int row0, int dt, int lane) {
+        return Split{Ti::cols(lds, row0, dt, lane), Ti::cols(lds + kPart, row0, dt, lane), Ti::cols(lds + 2 * kPart, row0, dt, lane)};
+    }
+    static __device__ __forceinline__ void put(char* lds, int row, int c, f32x8 v) {
+        const Split s = split(v);
+        Ti::put(lds, row, c, s.h);
+        Ti::put(lds + kPart, row, c, s.m);
+        Ti::put(lds + 2 * kPart, row, c, s.l);
     }
 };
 

@@ -564,8 +564,8 @@ def test_attention_refuses_what_it_cannot_read():
         with pytest.raises(ValueError):
             bad()
     with pytest.raises(ValueError):
-        pd.pd_attention_forward(q, k, k, o, scale=1e60)
-    for kw in (dict(window=-1), dict(sinks=-2), dict(scale=float("nan"))):
+        pd.pd_attention_forward(q, k, k, o, window=-2**40)
+    for kw in (dict(window=-1), dict(sinks=-2), dict(scale=float("nan")), dict(scale=1e60)):
         with pytest.raises(pd.PdError):
             pd.pd_attention_forward(q, k, k, o, **kw)
     big = torch.zeros((1, 1, 1, 256), device="cuda")
