@@ -431,9 +431,9 @@ pd_status pd_rotary_apply(const pd_rotary_desc* desc, const void* q, const void*
  * query does not see (NaN included) does not reach its row.
  * Query head h reads key head h / (heads_q / heads_kv).
  * scale: of the scores, finite.  lse: float [batch][heads_q][q_len], or NULL.
- * In PD_F32 operands are float32, or in the forward pass of more than 32 rows
- * of a key head the sums of three bfloat16 parts (24 bits; a value under 2^-110
- * keeps fewer) with products to 2^-24.
+ * In PD_F32 operands are the sums of three bfloat16 parts (24 bits; a value under
+ * 2^-110 keeps fewer) with products to 2^-24, or float32 itself where a key head
+ * has at most 32 rows in the forward pass.
  * In PD_BF16 the probabilities (and in the backward pass the scores'
  * gradients) are rounded to bfloat16 as operands of the matrix cores, the
  * products' sums are float32.

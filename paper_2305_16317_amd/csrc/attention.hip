@@ -392,7 +392,7 @@ __global__ __launch_bounds__(256, 2) void k_attention(const AttentionArgs a, con
 // before is worked on, and split on its way to LDS, once for the block's four waves.
 template <int DP>
 __global__ __launch_bounds__(256, (DP <= 96 ? 2 : 1)) void k_attention_parts(const AttentionArgs a, const Plan p) {
-    constexpr int BN = tile_rows<float, DP>(), BM = 128, kUnits = BN * (DP / 8), kEach = (kUnits + 255) / 256;
+    constexpr int BN = tile_rows<float, DP>(), BM = 128;
     using As = InParts<DP, BN>;
     __shared__ __align__(128) char lds[2 * As::kBytes];   // keys, values
     char *lk = lds, *lv = lds + As::kBytes;
@@ -410,17 +410,12 @@ __global__ __launch_bounds__(256, (DP <= 96 ? 2 : 1)) void k_attention_parts(con
     const int i0 = rows_to_query(p, tile * BM), i1 = min(rows_to_query(p, tile * BM + BM - 1), seq.n - 1);
     const KeyTiles<BN> tiles(i0 <= i1 ? sees_any(d, seq, i0, i1) : See{0, 0, 0});
     const int it0 = part * p.split_tiles, it1 = min(tiles.count, it0 + p.split_tiles);
-    f32x8 kr[kEach], vr[kEach];
+    FillParts<DP, BN> fk, fv;
     auto fetch = [&](int it) {
         const int j0 = tiles.start(it);
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const int u = i * 256 + threadIdx.x, j = j0 + u / (DP / 8), e = u % (DP / 8) * 8;
-            kr[i] = vr[i] = f32x8{};
-            if (u >= kUnits || !tiles.any(j)) continue;
-            kr[i] = load8(kb + (int64_t)j * d.k_stride[1] + e, d.head_dim - e);
-            vr[i] = load8(vb + (int64_t)j * d.v_stride[1] + e, d.head_dim - e);
-        }
+        auto keep = [&](int r) { return tiles.any(j0 + r); };
+        fk.fetch(kb + (int64_t)j0 * d.k_stride[1], d.k_stride[1], d.head_dim, keep);
+        fv.fetch(vb + (int64_t)j0 * d.v_stride[1], d.v_stride[1], d.head_dim, keep);
     };
     if (it0 < it1) fetch(it0);
 
@@ -436,13 +431,8 @@ __global__ __launch_bounds__(256, (DP <= 96 ? 2 : 1)) void k_attention_parts(con
     for (int it = it0; it < it1; ++it) {
         const int j0 = tiles.start(it);
         lds_barrier();                                    // the tile before has been read
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const int u = i * 256 + threadIdx.x;
-            if (u >= kUnits) continue;
-            As::put(lk, u / (DP / 8), u % (DP / 8), kr[i]);
-            As::put(lv, u / (DP / 8), u % (DP / 8), vr[i]);
-        }
+        fk.put(lk);
+        fv.put(lv);
         lds_barrier();                                    // this one is there
         if (it + 1 < it1) fetch(it + 1);
         if (sight.none(j0, BN)) continue;

@@ -24,8 +24,11 @@ using namespace attn;
 // difference within the rounding of the score's terms counts as none: the forward pass
 // may have summed them in another order.
 constexpr float kLarge = 1024.f;
+// (float32 takes the difference first, so that neither c2's nor lse log2 e's rounding is
+// multiplied by the score.)
+template <typename T>
 __device__ inline float probability(bool large, float s, float c2, float lse2, float scale, float lse) {
-    if (!large) return exp2_fast(fmaf(s, c2, -lse2));
+    if (!large) return sizeof(T) == 2 ? exp2_fast(fmaf(s, c2, -lse2)) : exp2_fast(fmaf(s, scale, -lse) * kLog2e);
     const float x = s * scale - lse, size = fabsf(lse);
     if (x > 0.f || (size > 0x1p20f && fabsf(x) <= 0x1p-17f * size)) return x != x ? x : 1.f;
     return exp2_fast(x * kLog2e);
@@ -73,7 +76,7 @@ __device__ inline void pair_grad(const AttentionArgs& a, const Views<T>& w, int 
         dp = fmaf((float)go[e], (float)v[e], dp);
     }
     const int64_t at = (int64_t)g * d.q_len + i;
-    *p = probability(true, s, 0.f, 0.f, d.scale, w.lse[at]);
+    *p = probability<T>(true, s, 0.f, 0.f, d.scale, w.lse[at]);
     *ds = *p * (dp - w.delta[at]);
 }
 
@@ -137,19 +140,28 @@ __device__ void dkv_row(const AttentionArgs& a, const Views<T>& w, const Seq seq
 // that stay in registers leave room (dq: one sum, two operands; dk, dv: two and two)
 template <typename T, int DP>
 constexpr int dq_blocks_per_cu() {
-    return sizeof(T) == 2 || DP <= 64 ? 2 : 1;
+    return sizeof(T) == 2 || DP <= 32 ? 2 : 1;
 }
 template <typename T, int DP>
 constexpr int dkv_blocks_per_cu() {
     return DP * (int)sizeof(T) <= 128 ? 2 : 1;
 }
+// float32 operands are held in three parts
+template <typename T, int DP, int ROWS>
+using Held = std::conditional_t<sizeof(T) == 2, AsIs<T, DP>, InParts<DP, ROWS>>;
+template <typename T, int DP, int ROWS>
+constexpr int tile_bytes() {
+    return ROWS * Tile<bf16, DP>::kPitch * (sizeof(T) == 2 ? 1 : 3);
+}
 
 template <typename T, int DP, bool COPY>
 __global__ __launch_bounds__(256, (dq_blocks_per_cu<T, DP>())) void k_attention_dq(const AttentionArgs a, int row_tiles) {
-    using Ti = Tile<T, DP>;
-    constexpr int kSteps = DP / 16, kDT = DP / 32, BN = tile_rows<T, DP>(), kBytes = BN * Ti::kPitch;
-    using F = Fill<T, DP, BN, 256>;
-    __shared__ __align__(128) char lds[4 * kBytes];       // keys, values; twice
+    constexpr bool kParts = sizeof(T) == 4;
+    constexpr int kSteps = DP / 16, kDT = DP / 32, BN = tile_rows<T, DP>(), kBytes = tile_bytes<T, DP, BN>();
+    using As = Held<T, DP, BN>;
+    using Operand = typename As::Operand;
+    using F = std::conditional_t<kParts, FillParts<DP, BN>, Fill<bf16, DP, BN, 256>>;
+    __shared__ __align__(128) char lds[(kParts ? 2 : 4) * kBytes];       // keys, values; twice where copies fill them
     const pd_attention_desc& d = a.d;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
     const int id = near_blocks(blockIdx.x, gridDim.x), tile = row_tiles - 1 - id % row_tiles, head = id / row_tiles;
@@ -166,7 +178,7 @@ __global__ __launch_bounds__(256, (dq_blocks_per_cu<T, DP>())) void k_attention_
     const int i0 = tile * 128 / w.group, i1 = min((tile * 128 + 127) / w.group, seq.n - 1);
     const KeyTiles<BN> tiles(i0 <= i1 ? sees_any(d, seq, i0, i1) : See{0, 0, 0});
     F fk, fv;
-    if constexpr (COPY) {
+    if constexpr (COPY && !kParts) {
         const int units = d.head_dim * (int)sizeof(T) / 16;
         fk.plan(d.k_stride[1], units, threadIdx.x);
         fv.plan(d.v_stride[1], units, threadIdx.x);
@@ -176,7 +188,11 @@ __global__ __launch_bounds__(256, (dq_blocks_per_cu<T, DP>())) void k_attention_
         const T* kt = w.k + (int64_t)j0 * d.k_stride[1];
         const T* vt = w.v + (int64_t)j0 * d.v_stride[1];
         char* to = lds + buf * 2 * kBytes;
-        if constexpr (COPY) {
+        if constexpr (kParts) {
+            auto keep = [&](int r) { return tiles.any(j0 + r); };
+            fk.fetch(kt, d.k_stride[1], d.head_dim, keep);
+            fv.fetch(vt, d.v_stride[1], d.head_dim, keep);
+        } else if constexpr (COPY) {
             if (tiles.whole(j0)) {
                 fk.copy(kt, to);
                 fv.copy(vt, to + kBytes);
@@ -193,17 +209,19 @@ __global__ __launch_bounds__(256, (dq_blocks_per_cu<T, DP>())) void k_attention_
     };
     if (tiles.count > 0) fetch(0, 0);
 
-    Frag<T> qf[kSteps], gf[kSteps];
+    Operand qf[kSteps], gf[kSteps];
     float delta = 0.f;
 #pragma unroll
     for (int c = 0; c < kSteps; ++c) {
         const int e = 16 * c + 8 * h;
-        qf[c] = Frag<T>{};
-        gf[c] = Frag<T>{};
-        if (see.none()) continue;
-        qf[c] = load8(w.q + qi * d.q_stride[1] + g * d.q_stride[2] + e, d.head_dim - e);
-        gf[c] = load8(w.dout + qi * d.dout_stride[1] + g * d.dout_stride[2] + e, d.head_dim - e);
-        const f32x8 x = widen(gf[c]), y = widen(load8(w.out + qi * d.out_stride[1] + g * d.out_stride[2] + e, d.head_dim - e));
+        f32x8 u = {}, x = {}, y = {};
+        if (!see.none()) {
+            u = widen(load8(w.q + qi * d.q_stride[1] + g * d.q_stride[2] + e, d.head_dim - e));
+            x = widen(load8(w.dout + qi * d.dout_stride[1] + g * d.dout_stride[2] + e, d.head_dim - e));
+            y = widen(load8(w.out + qi * d.out_stride[1] + g * d.out_stride[2] + e, d.head_dim - e));
+        }
+        qf[c] = As::make(u);
+        gf[c] = As::make(x);
 #pragma unroll
         for (int f = 0; f < 8; ++f) delta = fmaf(x[f], y[f], delta);
     }
@@ -225,35 +243,41 @@ __global__ __launch_bounds__(256, (dq_blocks_per_cu<T, DP>())) void k_attention_
         for (int r = 0; r < 16; ++r) start[r] = -delta;
     for (int it = 0; it < tiles.count; ++it) {
         const int j0 = tiles.start(it);
-        if constexpr (COPY) wait_copies();
-        lds_barrier();                                    // this tile is there, the other buffer is free
+        const char *lk = lds + (kParts ? 0 : (it & 1) * 2 * kBytes), *lv = lk + kBytes;
+        if constexpr (kParts) {
+            lds_barrier();                                // the tile before has been read
+            fk.put(lds);
+            fv.put(lds + kBytes);
+        } else if constexpr (COPY) {
+            wait_copies();
+        }
+        lds_barrier();                                    // this tile is there, and the other buffer free
         if (it + 1 < tiles.count) fetch(it + 1, (it + 1) & 1);
         if (sight.none(j0, BN)) continue;
         const bool edge = !sight.all(j0, BN);
-        const char *lk = lds + (it & 1) * 2 * kBytes, *lv = lk + kBytes;
 #pragma unroll
         for (int kt = 0; kt < BN / 32; ++kt) {
             f32x16 s = {}, dp = start;
             // the products q k and dout v, then those with the keys' columns, read ahead
             // (in turn, since a product waits for the last one with the same sum)
-            auto rows = [&](int n) { return Ti::rows(n % 2 ? lv : lk, 32 * kt, n / 2, lane); };
-            Stream<T, 2 * kSteps> rs;
+            auto rows = [&](int n) { return As::rows(n % 2 ? lv : lk, 32 * kt, n / 2, lane); };
+            Stream<Operand, 2 * kSteps> rs;
             rs.begin(rows);
-            rs.run(rows, [&](int n, const Frag<T>& f) {
+            rs.run(rows, [&](int n, const Operand& f) {
                 if (n % 2 == 0)
                     s = mma(f, qf[n / 2], s);
                 else
                     dp = mma(f, gf[n / 2], dp);
             });
-            auto cols = [&](int n) { return Ti::cols(lk, 32 * kt + 16 * (n / kDT), n % kDT, lane); };
-            Stream<T, 2 * kDT> cs;
+            auto cols = [&](int n) { return As::cols(lk, 32 * kt + 16 * (n / kDT), n % kDT, lane); };
+            Stream<Operand, 2 * kDT> cs;
             cs.begin(cols);
             if (large) {
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[r] = probability(true, s[r], c2, lse2, d.scale, lse);
+                for (int r = 0; r < 16; ++r) s[r] = probability<T>(true, s[r], c2, lse2, d.scale, lse);
             } else {
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[r] = probability(false, s[r], c2, lse2, d.scale, lse);
+                for (int r = 0; r < 16; ++r) s[r] = probability<T>(false, s[r], c2, lse2, d.scale, lse);
             }
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[r] *= kStart ? dp[r] : dp[r] - delta;
@@ -262,9 +286,9 @@ __global__ __launch_bounds__(256, (dq_blocks_per_cu<T, DP>())) void k_attention_
                 for (int r = 0; r < 16; ++r)
                     if (!see_from(j0 + 32 * kt + tile_row(0, r))) s[r] = 0.f;
             }
-            Frag<T> ds;
-            cs.run(cols, [&](int n, const Frag<T>& f) {
-                if (n % kDT == 0) ds = as_frag<T>(s, n / kDT);
+            Operand ds;
+            cs.run(cols, [&](int n, const Operand& f) {
+                if (n % kDT == 0) ds = As::make(eight(s, n / kDT));
                 o[n % kDT] = mma(f, ds, o[n % kDT]);
             });
         }
@@ -326,11 +350,13 @@ __device__ inline Sight sight_by(const pd_attention_desc& d, const Seq& s, int j
 template <typename T, int DP, bool COPY>
 __global__ __launch_bounds__(256, (dkv_blocks_per_cu<T, DP>())) void k_attention_dkv(const AttentionArgs a, int key_tiles,
                                                                                    int splits) {
-    using Ti = Tile<T, DP>;
-    constexpr int kSteps = DP / 16, kDT = DP / 32, BR = tile_rows<T, DP>(), kBytes = BR * Ti::kPitch;
-    using F = Fill<T, DP, BR, 256>;
-    __shared__ __align__(128) char lds[4 * kBytes];       // queries, output gradients; twice
-    __shared__ __align__(16) float stats[2][3][64];       // -lse / scale, -delta, lse
+    constexpr bool kParts = sizeof(T) == 4;
+    constexpr int kSteps = DP / 16, kDT = DP / 32, BR = tile_rows<T, DP>(), kBytes = tile_bytes<T, DP, BR>();
+    using As = Held<T, DP, BR>;
+    using Operand = typename As::Operand;
+    using F = std::conditional_t<kParts, FillParts<DP, BR>, Fill<bf16, DP, BR, 256>>;
+    __shared__ __align__(128) char lds[(kParts ? 2 : 4) * kBytes];       // queries, output gradients; twice where copies fill them
+    __shared__ __align__(16) float stats[2][3][64];       // -lse / scale (float32: lse), -delta, lse
     __shared__ int far[2];                                // whether a row's |lse| is large
     const pd_attention_desc& d = a.d;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
@@ -355,7 +381,7 @@ __global__ __launch_bounds__(256, (dkv_blocks_per_cu<T, DP>())) void k_attention
     const int per_head = last > first ? (last - first + BR - 1) / BR : 0, all = per_head * w.group;
     const int each = (all + splits - 1) / splits, x0 = split * each, x1 = min(all, x0 + each);
     F fq, fg;
-    if constexpr (COPY) {
+    if constexpr (COPY && !kParts) {
         const int units = d.head_dim * (int)sizeof(T) / 16;
         fq.plan(d.q_stride[1], units, threadIdx.x);
         fg.plan(d.dout_stride[1], units, threadIdx.x);
@@ -371,7 +397,11 @@ __global__ __launch_bounds__(256, (dkv_blocks_per_cu<T, DP>())) void k_attention
         const T* qt = w.q + (int64_t)i0 * d.q_stride[1] + g * d.q_stride[2];
         const T* gt = w.dout + (int64_t)i0 * d.dout_stride[1] + g * d.dout_stride[2];
         char* to = lds + buf * 2 * kBytes;
-        if constexpr (COPY) {
+        if constexpr (kParts) {
+            auto keep = [&](int r) { return i0 + r < seq.n; };
+            fq.fetch(qt, d.q_stride[1], d.head_dim, keep);
+            fg.fetch(gt, d.dout_stride[1], d.head_dim, keep);
+        } else if constexpr (COPY) {
             if (i0 + BR <= seq.n) {
                 fq.copy(qt, to);
                 fg.copy(gt, to + kBytes);
@@ -388,7 +418,7 @@ __global__ __launch_bounds__(256, (dkv_blocks_per_cu<T, DP>())) void k_attention
     };
     auto put_stat = [&](int buf) {
         if (threadIdx.x < BR) {                           // (lanes of the first wave)
-            stats[buf][0][threadIdx.x] = stat * over;
+            stats[buf][0][threadIdx.x] = kParts ? stat : stat * over;
             stats[buf][2][threadIdx.x] = stat;
             const uint64_t some = __ballot(!(fabsf(stat) < kLarge));
             if (threadIdx.x == 0) far[buf] = some != 0 || d.scale == 0.f;
@@ -401,15 +431,17 @@ __global__ __launch_bounds__(256, (dkv_blocks_per_cu<T, DP>())) void k_attention
         put_stat(0);
     }
 
-    Frag<T> kf[kSteps], vf[kSteps];
+    Operand kf[kSteps], vf[kSteps];
 #pragma unroll
     for (int c = 0; c < kSteps; ++c) {
         const int e = 16 * c + 8 * h;
-        kf[c] = Frag<T>{};
-        vf[c] = Frag<T>{};
-        if (!live) continue;
-        kf[c] = load8(w.k + (int64_t)key * d.k_stride[1] + e, d.head_dim - e);
-        vf[c] = load8(w.v + (int64_t)key * d.v_stride[1] + e, d.head_dim - e);
+        f32x8 u = {}, v = {};
+        if (live) {
+            u = widen(load8(w.k + (int64_t)key * d.k_stride[1] + e, d.head_dim - e));
+            v = widen(load8(w.v + (int64_t)key * d.v_stride[1] + e, d.head_dim - e));
+        }
+        kf[c] = As::make(u);
+        vf[c] = As::make(v);
     }
     const float c2 = d.scale * kLog2e;
     f32x16 dk[kDT], dv[kDT];
@@ -418,17 +450,23 @@ __global__ __launch_bounds__(256, (dkv_blocks_per_cu<T, DP>())) void k_attention
     int pos = per_head ? x0 % per_head : 0;               // the tile's place among its head's
     for (int x = x0; x < x1; ++x, pos = pos + 1 == per_head ? 0 : pos + 1) {
         const int buf = (x - x0) & 1, i0 = first + pos * BR;
-        if constexpr (COPY) wait_copies();
-        lds_barrier();                                    // this tile is there, the other buffer is free
+        if constexpr (kParts) {
+            lds_barrier();                                // the tile before has been read
+            fq.put(lds);
+            fg.put(lds + kBytes);
+        } else if constexpr (COPY) {
+            wait_copies();
+        }
+        lds_barrier();                                    // this tile is there, and the other buffer free
         if (x + 1 < x1) fetch(x + 1, buf ^ 1);
         if (!sight.none(i0, BR)) {
             const bool edge = !sight.all(i0, BR);
-            const char *lq = lds + buf * 2 * kBytes, *lg = lq + kBytes;
+            const char *lq = lds + (kParts ? 0 : buf * 2 * kBytes), *lg = lq + kBytes;
             const bool large = __builtin_amdgcn_readfirstlane(far[buf]);
 #pragma unroll
             for (int rt = 0; rt < BR / 32; ++rt) {
-                // the products q k start from -lse / scale and the products dout v from -delta,
-                // so that p = 2^(c2 s) and ds = p dp
+                // the products dout v start from -delta and, in bfloat16, q k from -lse / scale,
+                // so that ds = p dp and p = 2^(c2 s) (float32: see probability)
                 f32x16 s, dp;
 #pragma unroll
                 for (int r = 0; r < 16; r += 4) {
@@ -438,11 +476,12 @@ __global__ __launch_bounds__(256, (dkv_blocks_per_cu<T, DP>())) void k_attention
 #pragma unroll
                     for (int e = 0; e < 4; ++e) s[r + e] = u[e], dp[r + e] = v[e];
                 }
-                if (large) s = f32x16{};
-                auto rows = [&](int n) { return Ti::rows(n % 2 ? lg : lq, 32 * rt, n / 2, lane); };
-                Stream<T, 2 * kSteps> rs;
+                const f32x16 from = s;
+                if (large || kParts) s = f32x16{};
+                auto rows = [&](int n) { return As::rows(n % 2 ? lg : lq, 32 * rt, n / 2, lane); };
+                Stream<Operand, 2 * kSteps> rs;
                 rs.begin(rows);
-                rs.run(rows, [&](int n, const Frag<T>& f) {
+                rs.run(rows, [&](int n, const Operand& f) {
                     if (n % 2 == 0)
                         s = mma(f, kf[n / 2], s);
                     else
@@ -451,14 +490,17 @@ __global__ __launch_bounds__(256, (dkv_blocks_per_cu<T, DP>())) void k_attention
                 // then, 16 rows at a time, dv with the output gradients' columns and dk with the queries'
                 auto cols = [&](int n) {
                     const int c = n / (2 * kDT), t = n % (2 * kDT);
-                    return t < kDT ? Ti::cols(lg, 32 * rt + 16 * c, t, lane) : Ti::cols(lq, 32 * rt + 16 * c, t - kDT, lane);
+                    return t < kDT ? As::cols(lg, 32 * rt + 16 * c, t, lane) : As::cols(lq, 32 * rt + 16 * c, t - kDT, lane);
                 };
-                Stream<T, 4 * kDT> cs;
+                Stream<Operand, 4 * kDT> cs;
                 cs.begin(cols);
                 if (large) {
 #pragma unroll
                     for (int r = 0; r < 16; ++r)
-                        s[r] = probability(true, s[r], 0.f, 0.f, d.scale, stats[buf][2][32 * rt + tile_row(lane, r)]);
+                        s[r] = probability<T>(true, s[r], 0.f, 0.f, d.scale, stats[buf][2][32 * rt + tile_row(lane, r)]);
+                } else if constexpr (kParts) {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[r] = probability<T>(false, s[r], 0.f, 0.f, d.scale, from[r]);
                 } else {
 #pragma unroll
                     for (int r = 0; r < 16; ++r) s[r] = exp2_fast(s[r] * c2);
@@ -470,10 +512,10 @@ __global__ __launch_bounds__(256, (dkv_blocks_per_cu<T, DP>())) void k_attention
                     for (int r = 0; r < 16; ++r)
                         if (!see(i0 + 32 * rt + tile_row(0, r))) s[r] = dp[r] = 0.f;
                 }
-                Frag<T> p, ds;
-                cs.run(cols, [&](int n, const Frag<T>& f) {
+                Operand p, ds;
+                cs.run(cols, [&](int n, const Operand& f) {
                     const int c = n / (2 * kDT), t = n % (2 * kDT);
-                    if (t == 0) p = as_frag<T>(s, c), ds = as_frag<T>(dp, c);
+                    if (t == 0) p = As::make(eight(s, c)), ds = As::make(eight(dp, c));
                     if (t < kDT)
                         dv[t] = mma(f, p, dv[t]);
                     else
@@ -606,7 +648,9 @@ void attention_grad_t(const AttentionArgs& a, hipStream_t s) {
     auto fits = [&](const void* p, const int64_t* stride, int64_t tokens, int64_t heads) {
         return copies_fit(p, stride, d.batch, tokens, heads, d.head_dim, sizeof(T));
     };
-    if (fits(a.k, d.k_stride, d.kv_len, d.heads_kv) && fits(a.v, d.v_stride, d.kv_len, d.heads_kv) &&
+    if constexpr (sizeof(T) == 4)
+        attention_grad_c<T, DP, false>(a, s);
+    else if (fits(a.k, d.k_stride, d.kv_len, d.heads_kv) && fits(a.v, d.v_stride, d.kv_len, d.heads_kv) &&
         fits(a.q, d.q_stride, d.q_len, d.heads_q) && fits(a.dout, d.dout_stride, d.q_len, d.heads_q))
         attention_grad_c<T, DP, true>(a, s);
     else

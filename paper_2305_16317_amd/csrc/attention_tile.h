@@ -156,7 +156,6 @@ template <typename T, int DP>
 struct AsIs {
     using Type = T;
     using Operand = Frag<T>;
-    static constexpr int kPitch = Tile<T, DP>::kPitch;
     static __device__ __forceinline__ Operand make(f32x8 v) { return narrow<T>(v); }
     static __device__ __forceinline__ Operand rows(const char* lds, int row0, int c, int lane) {
         return Tile<T, DP>::rows(lds, row0, c, lane);
@@ -186,14 +185,39 @@ struct InParts {
     }
 };
 
+// Fills a tile in parts: 256 threads read its rows into registers (0 where `keep` is
+// false and past the head's end) and, when the tile's place is free, split them there.
+template <int DP, int ROWS>
+struct FillParts {
+    static constexpr int kUnits = ROWS * (DP / 8), kEach = (kUnits + 255) / 256;
+    f32x8 v[kEach];
+    template <class Keep>
+    __device__ __forceinline__ void fetch(const float* base, int64_t stride, int head_dim, Keep keep) {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int u = i * 256 + threadIdx.x, row = u / (DP / 8), e = u % (DP / 8) * 8;
+            v[i] = f32x8{};
+            if (u < kUnits && keep(row)) v[i] = load8(base + row * stride + e, head_dim - e);
+        }
+    }
+    __device__ __forceinline__ void put(char* lds) const {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int u = i * 256 + threadIdx.x;
+            if (u < kUnits) InParts<DP, ROWS>::put(lds, u / (DP / 8), u % (DP / 8), v[i]);
+        }
+    }
+};
+
 // Runs COUNT products in order, each with a fragment from LDS: reads go G fragments at a
 // time, a group ahead of the products, so that a group's latency passes behind the
 // products of the one before.  (Left to itself the compiler reads a fragment just
 // before its product and waits about 100 cycles for it, three times the product.)
-template <typename T, int COUNT>
+template <class Operand, int COUNT>
 struct Stream {
-    static constexpr int G = sizeof(T) == 2 ? (COUNT < 4 ? COUNT : 4) : 1, kGroups = (COUNT + G - 1) / G;
-    Frag<T> f[2][G];
+    // (four bfloat16 fragments; of three parts, whose product takes six, one)
+    static constexpr int G = sizeof(Operand) > 16 ? 1 : COUNT < 4 ? COUNT : 4, kGroups = (COUNT + G - 1) / G;
+    Operand f[2][G];
     template <class Read>
     __device__ __forceinline__ void read(int g, Read& r) {
 #pragma unroll
