@@ -700,7 +700,8 @@ int64_t most_tiles(const pd_attention_desc& d, int rows_per_tile, int group, int
 bool few_rows(const pd_attention_desc& d) { return (int64_t)d.q_len * (d.heads_q / d.heads_kv) <= 32; }
 
 int bn_of(const pd_attention_desc& d) { return d.dtype == PD_BF16 || d.head_dim <= 64 ? 64 : 32; }
-// 32-row tiles a wave takes: one where two would leave compute units without a block
+// 32-row tiles a wave takes: two where they leave two blocks for each compute unit (a
+// window of 64 latents of 576 tokens: 144 us, with one 148)
 int wave_tiles_of(const pd_attention_desc& d) {
     if (d.dtype != PD_BF16 || d.head_dim > 64) return 1;
     const int64_t rows = (int64_t)d.q_len * (d.heads_q / d.heads_kv);
@@ -713,10 +714,29 @@ int few_waves_of(const pd_attention_desc& d) {
     return n < 8 ? n : 8;
 }
 
-// How the work is cut.  Few rows: one wave a block up to two tiles of keys, else
-// few_waves, and parts of eight tiles a wave where there are more (a long cache).  Else
-// blocks of 128 rows; where they would not fill the chip (two a compute unit), parts of
-// at least four tiles.
+// The fewest parts, from as many as give each of 256 compute units a block, that keep
+// them busy for nine tenths of the rounds it takes, or the best of the next few.
+int64_t fill_units(int64_t blocks) {
+    const int64_t first = blocks < 256 ? 256 / blocks : 1;
+    int64_t best = first;
+    double used = 0.0;
+    for (int64_t s = first; s < first + 5 && used < 0.9; ++s) {
+        const int64_t n = blocks * s, rounds = (n + 255) / 256;
+        const double u = (double)n / (double)(rounds * 256);
+        if (u > used) best = s, used = u;
+    }
+    return best;
+}
+
+// How the work is cut (figures in us).
+// At most 32 rows go to k_attention_few: 16 tokens over long caches 151, one over 1024
+// keys 12, 100 sequences of 16 tokens in float32 13 (in blocks of 128 rows 162, 20, 32).  One
+// wave up to two tiles of keys (the sequences; with four waves 54), else few_waves
+// (the tokens), in parts that give each compute unit a block, of at least eight tiles a
+// wave (16 tokens: 256 blocks 151, 512 163, 1024 175, 2048 178).
+// More rows go in blocks of 128 (two waves' tiles: wave_tiles_of).  Where they would not
+// fill the chip (two a compute unit), parts of at least four tiles (the float32 chunk
+// over ragged caches: 3 parts 62, 4 56, 6 and 7 48, 11 55).
 Plan plan(const pd_attention_desc& d) {
     Plan p{};
     p.group = d.heads_q / d.heads_kv;
@@ -731,9 +751,9 @@ Plan plan(const pd_attention_desc& d) {
     int64_t splits;
     if (few) {
         p.waves = tiles <= 2 ? 1 : few_waves_of(d);
-        const int64_t per = 8 * p.waves;
-        splits = p.units * p.waves >= 8192 ? 1 : (tiles + per - 1) / per;
-        if (splits > 4096) splits = 4096;
+        const int64_t most = (tiles + 8 * p.waves - 1) / (8 * p.waves);
+        splits = p.units > 0 ? fill_units(p.units) : 1;
+        if (splits > most) splits = most;
     } else {
         splits = p.units >= 256 ? 1 : 512 / p.units;
         if (splits > tiles / 4) splits = tiles / 4;
