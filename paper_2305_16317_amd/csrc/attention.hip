@@ -12,10 +12,20 @@
 // exact for the row's largest scores of any size.
 //
 // A row is a query of one of the query heads that share a key head: keys and values
-// are read once for all of them.  Two kernels: blocks of 128 rows that share the key
-// tiles in LDS, and, for at most 32 rows (a token's heads, a short sequence), waves
-// of 32 rows that stream key tiles of their own.  Where there are few blocks the keys
-// are split among several of them, whose results k_attention_join puts together.
+// are read once for all of them.  Blocks of 128 rows share the key tiles in LDS
+// (k_attention; float32: k_attention_parts); at most 32 rows (a token's heads, a short
+// sequence) go to waves that stream key tiles of their own (k_attention_few).  Where
+// there are few blocks the keys are split among several of them, whose results
+// k_attention_join puts together.
+//
+// What bounds it: a 32 x 32 x 16 product takes 32 cycles and 16 of the vector units' issue, a
+// score 12 cycles of vector operations and 8 for its exponential, and within a wave
+// nothing overlaps a product, so two waves a SIMD from different blocks fill it
+// between them.  Measured (bfloat16): 8192 tokens two-sided, 32 heads on 8 of 128 values,
+// 1058 us (1039 TFLOP/s; a large library product reaches 1247), of 64 values 563 us
+// (977); with a window of 2048 and sinks, where tiles end outside the window and a block
+// has 34 of them, 285 us (846); 64 sequences of 576 tokens of 64 values, nine tiles a block,
+// 134 us (649): there a third of the time is reading queries and writing results.
 #include "attention_tile.h"
 
 namespace pd {
@@ -390,6 +400,9 @@ __global__ __launch_bounds__(256, 2) void k_attention(const AttentionArgs a, con
 
 // The same for float32, in three parts: a tile is read into registers while the one
 // before is worked on, and split on its way to LDS, once for the block's four waves.
+// (Heads of over 96 values: one block a compute unit, since for two 33 registers spill:
+// 266 us, 357.)  Measured: 2 x 2048 tokens causal, 16 heads on 4: 64 values 137 us, 96 values
+// 202 us, 128 values 266 us, where float32 products took 213, 313 and 570.
 template <int DP>
 __global__ __launch_bounds__(256, (DP <= 96 ? 2 : 1)) void k_attention_parts(const AttentionArgs a, const Plan p) {
     constexpr int BN = tile_rows<float, DP>(), BM = 128;
@@ -449,7 +462,9 @@ constexpr int few_waves() {
 
 // A block: 32 rows of one key head, or one part of their keys.  Each of its W waves
 // streams every W-th tile of keys through buffers of its own, with no barrier, and the
-// waves' sums are joined in LDS.
+// waves' sums are joined in LDS.  Bound by memory on long caches: the next token of 16
+// sequences over up to 32768 keys, window 16384, 150 us (5.5 TB/s); on short ones by its
+// chain of loads and products: one sequence, 1024 keys, 11 us.
 template <typename T, int DP, bool COPY, int W>
 __global__ __launch_bounds__(64 * W) void k_attention_few(const AttentionArgs a, const Plan p) {
     using Ti = Tile<T, DP>;

@@ -10,6 +10,12 @@
 // and head in place of 10), and in exchange there is no atomic and no order that
 // varies from run to run.  Where there are few blocks of keys, their queries are
 // split among several blocks, whose sums k_attention_dkv_join adds.
+//
+// Bound by the chain of LDS reads, products and vector work of a wave (two waves a SIMD):
+// hence reads a group ahead (Stream) and sums that start from -lse / scale and -delta.
+// Measured: 4 x 2304 tokens two-sided, 16 heads on 4 of 64 bfloat16 values 388 us (560
+// TFLOP/s of the 10 D operations, 783 of the 14 D it does): dq 170, dk and dv 200, join 18;
+// float32, 2 x 2048 tokens causal: 64 values 412 us, 128 values 1053 us.
 #include "attention_tile.h"
 
 namespace pd {

