@@ -473,7 +473,7 @@ __global__ __launch_bounds__(64 * W) void k_attention_few(const AttentionArgs a,
     static_assert(BN * kPart * 4 <= 4 * kBytes, "a wave's sums fit its buffers");
     constexpr int kBufs = W == 1 ? 1 : 2;                 // a lone wave has a tile or two: no second buffer
     __shared__ __align__(128) char lds_all[W][kBufs * 2 * kBytes];
-    __shared__ float stats[W][2][32];
+    __shared__ float stats[W][2][32], totals[32];
     __shared__ int redo[32];
     const pd_attention_desc& d = a.d;
     const int lane = threadIdx.x & 63, wave = W == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -600,7 +600,7 @@ __global__ __launch_bounds__(64 * W) void k_attention_few(const AttentionArgs a,
                 a.lse[at] = log_sum(top, fabsf(d.scale), total);
             }
         }
-        if (wave == 0 && lane < 32) stats[0][1][row] = total;      // (read by all above; the barrier below orders it)
+        if (wave == 0 && lane < 32) totals[row] = total;
         __syncthreads();
         for (int u = threadIdx.x; u < p.rows * (DP / 4); u += 64 * W) {
             const int r = u / (DP / 4), e = u % (DP / 4) * 4;
@@ -614,7 +614,7 @@ __global__ __launch_bounds__(64 * W) void k_attention_few(const AttentionArgs a,
                 store4(to.sums + (split * rows_all + ra) * d.head_dim + e, d.head_dim - e, v);
                 continue;
             }
-            const float t = stats[0][1][r];
+            const float t = totals[r];
             v = t == 0.f ? f32x4{} : v * (1.f / t);
             store4(static_cast<T*>(a.out) + b * d.out_stride[0] + i * d.out_stride[1] + hh * d.out_stride[2] + e, d.head_dim - e, v);
 #pragma unroll
