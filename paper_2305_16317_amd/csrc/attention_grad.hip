@@ -427,7 +427,7 @@ __global__ __launch_bounds__(256, (dkv_blocks_per_cu<T, DP>())) void k_attention
             stats[buf][0][threadIdx.x] = kParts ? stat : stat * over;
             stats[buf][2][threadIdx.x] = stat;
             const uint64_t some = __ballot(!(fabsf(stat) < kLarge));
-            if (threadIdx.x == 0) far[buf] = some != 0 || d.scale == 0.f;
+            if (threadIdx.x == 0) far[buf] = some != 0 || !(fabsf(over) < 0x1p100f);      // (a scale near 0)
         } else if (threadIdx.x < 2 * BR) {
             stats[buf][1][threadIdx.x - BR] = -stat;
         }

@@ -414,6 +414,24 @@ def test_attention_values_of_the_types_ends(dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("scale", [0.0, 1e-39, -1e-30, 1e-10])
+def test_attention_backward_of_scales_near_zero(scale, dtype):
+    """All keys weigh the same, so dv is a mean; dq and dk go with the scale."""
+    q, k, v, g = _att_inputs(1, 40, 60, 4, 2, 64, dtype, 29)
+    out, lse = torch.empty_like(q), torch.empty((1, 4, 40), device="cuda")
+    pd.pd_attention_forward(q, k, v, out, lse=lse, causal=False, scale=scale)
+    dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+    pd.pd_attention_backward(q, k, v, out, lse, g, dq, dk, dv, causal=False, scale=scale)
+    refs = ot.attention_grad(_np(q), _np(k), _np(v), _np(g), scale, False)
+    _close(dv, refs[2], TOL_GRAD[dtype])
+    if abs(scale) > 1e-35:
+        _close(dq, refs[0], TOL_GRAD[dtype])
+        _close(dk, refs[1], TOL_GRAD[dtype])
+    else:                                      # (gradients below the normal numbers)
+        assert float(dq.abs().max()) <= 1e-36 and float(dk.abs().max()) <= 1e-36
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("n,m", [(40, 40), (1, 40)])
 def test_attention_backward_of_scores_near_the_types_end(n, m, dtype):
     """One key takes each row whole (as in the test above): dv is the sum of its rows' dout."""
