@@ -276,15 +276,21 @@ __device__ inline int near_blocks(int id, int count) {
 // One copy of 16 bytes a lane from base + off to LDS at lds + 16 lane, past the
 // registers (M0 = lds).  Inline assembly, so that the compiler's wait counts do not
 // see it (it would wait for the copies before every LDS read): who reads the data
-// waits with wait_copies() and a barrier first.
+// waits with wait_copies() and a barrier first.  The hardware does not wait by itself for
+// what a copy reads: M0 must be a wait state old, an address that a vector instruction
+// (readfirstlane) wrote to scalar registers five.  The compiler sees to that between
+// instructions of its own, but not where one of them is in a string: hence the s_nop.
 __device__ __forceinline__ uint64_t uniform_address(const void* p) {
     const uint64_t v = (uint64_t)(uintptr_t)p;
     const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v);
     const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
-    return ((uint64_t)hi << 32) | lo;
+    uint64_t u = ((uint64_t)hi << 32) | lo;
+    asm("s_nop 4" : "+s"(u));
+    return u;
 }
 __device__ __forceinline__ void copy16(uint64_t base, uint32_t off, uint32_t lds) {
     asm volatile("s_mov_b32 m0, %2\n\t"
+                 "s_nop 0\n\t"
                  "global_load_lds_dwordx4 %0, %1"
                  :
                  : "v"(off), "s"(base), "s"(lds)

@@ -485,16 +485,23 @@ __device__ __forceinline__ SplitB silu_split(const f4& ua, const f4& ub, float c
 // kernel's own LDS reads precisely (with an LDS-DMA in flight it would wait
 // for every outstanding LDS read before each use).  Callers wait for these
 // copies explicitly (s_waitcnt vmcnt(0)) before any wave reads their data.
+// The hardware does not wait by itself for what a copy reads: M0 must be a wait
+// state old, an address that readfirstlane wrote five.  The compiler sees to
+// that between instructions of its own, but not where one of them is in an
+// assembly string: hence the s_nop.
 // The base address is uniform over the wave by construction; readfirstlane
 // puts it in scalar registers, as the instruction needs.
 __device__ __forceinline__ uint64_t uniform_addr(const void* p) {
     const uint64_t v = (uint64_t)(uintptr_t)p;
     const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v);
     const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
-    return ((uint64_t)hi << 32) | lo;
+    uint64_t u = ((uint64_t)hi << 32) | lo;
+    asm("s_nop 4" : "+s"(u));
+    return u;
 }
 __device__ __forceinline__ void dma16(const void* gbase, uint32_t voff, uint32_t lds) {
     asm volatile("s_mov_b32 m0, %2\n\t"
+                 "s_nop 0\n\t"
                  "global_load_lds_dwordx4 %0, %1"
                  :
                  : "v"(voff), "s"(uniform_addr(gbase)), "s"(__builtin_amdgcn_readfirstlane(lds))
@@ -502,6 +509,7 @@ __device__ __forceinline__ void dma16(const void* gbase, uint32_t voff, uint32_t
 }
 __device__ __forceinline__ void dma4(const void* gbase, uint32_t voff, uint32_t lds) {
     asm volatile("s_mov_b32 m0, %2\n\t"
+                 "s_nop 0\n\t"
                  "global_load_lds_dword %0, %1"
                  :
                  : "v"(voff), "s"(uniform_addr(gbase)), "s"(__builtin_amdgcn_readfirstlane(lds))
