@@ -334,6 +334,8 @@ void k_conv_bf16(ConvKernArgs ka) {
 
 // ---------------------------------------------------------------- fp32
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+typedef float f2 __attribute__((ext_vector_type(2)));
 
 // Largest value over the wave, the same in every lane: DPP steps build the
 // maximum of each 16-lane row in every lane of it (pairs, quads, half rows,
@@ -428,15 +430,10 @@ __device__ __forceinline__ SplitR silu_r(const float v0, const float v1, float c
 // stage 2: x0s = fp16(fl(t r)) and x1 = fp16(t r - x0s), two halves each
 __device__ __forceinline__ void split_round(const float v0, const float v1, const SplitR& r,
                                             uint32_t& x0s, uint32_t& x1) {
-    const float h0 = v0 * r.r0, h1 = v1 * r.r1;
-    uint32_t a, b;
-    float d0, d1;
-    asm("v_cvt_pk_f16_f32 %0, %1, %2" : "=v"(a) : "v"(h0), "v"(h1));
-    asm("v_fma_mix_f32 %0, %1, %2, -%3 op_sel_hi:[0,0,1]" : "=v"(d0) : "v"(v0), "v"(r.r0), "v"(a));
-    asm("v_fma_mix_f32 %0, %1, %2, -%3 op_sel:[0,0,1] op_sel_hi:[0,0,1]" : "=v"(d1) : "v"(v1), "v"(r.r1), "v"(a));
-    asm("v_cvt_pk_f16_f32 %0, %1, %2" : "=v"(b) : "v"(d0), "v"(d1));
-    x0s = a;
-    x1 = b;
+    const h2 a = __builtin_convertvector(f2{v0 * r.r0, v1 * r.r1}, h2);
+    const f2 d = {__builtin_fmaf(v0, r.r0, -(float)a[0]), __builtin_fmaf(v1, r.r1, -(float)a[1])};
+    x0s = __builtin_bit_cast(uint32_t, a);
+    x1 = __builtin_bit_cast(uint32_t, __builtin_convertvector(d, h2));
 }
 __device__ __forceinline__ void silu_split_q(const float v0, const float v1, float c,
                                              uint32_t& x0s, uint32_t& x1) {

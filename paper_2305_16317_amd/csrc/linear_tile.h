@@ -85,6 +85,8 @@ __device__ __forceinline__ void lds_barrier() {
 
 typedef float lin_f4 __attribute__((ext_vector_type(4)));
 typedef _Float16 lin_h8 __attribute__((ext_vector_type(8)));
+typedef _Float16 lin_h2 __attribute__((ext_vector_type(2)));
+typedef float lin_f2 __attribute__((ext_vector_type(2)));
 typedef uint32_t lin_u4 __attribute__((ext_vector_type(4)));
 
 // Row tile mt of a hidden buffer of M rows: rows of the tile (the last tile is
@@ -127,15 +129,10 @@ __device__ __forceinline__ SplitX split_row(const lin_f4& a, const lin_f4& b, fl
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
         const float v0 = q < 2 ? a[2 * q] : b[2 * q - 4], v1 = q < 2 ? a[2 * q + 1] : b[2 * q - 3];
-        const float h0 = v0 * S, h1 = v1 * S;                 // exact: a power of two
-        uint32_t u, w;
-        float d0, d1;
-        asm("v_cvt_pk_f16_f32 %0, %1, %2" : "=v"(u) : "v"(h0), "v"(h1));
-        asm("v_fma_mix_f32 %0, %1, %2, -%3 op_sel_hi:[0,0,1]" : "=v"(d0) : "v"(v0), "v"(S), "v"(u));
-        asm("v_fma_mix_f32 %0, %1, %2, -%3 op_sel:[0,0,1] op_sel_hi:[0,0,1]" : "=v"(d1) : "v"(v1), "v"(S), "v"(u));
-        asm("v_cvt_pk_f16_f32 %0, %1, %2" : "=v"(w) : "v"(d0), "v"(d1));
-        p0[q] = u;
-        p1[q] = w;
+        const lin_h2 u = __builtin_convertvector(lin_f2{v0 * S, v1 * S}, lin_h2);     // (exact products: a power of two)
+        const lin_f2 d = {__builtin_fmaf(v0, S, -(float)u[0]), __builtin_fmaf(v1, S, -(float)u[1])};
+        p0[q] = __builtin_bit_cast(uint32_t, u);
+        p1[q] = __builtin_bit_cast(uint32_t, __builtin_convertvector(d, lin_h2));
     }
     SplitX s;
     s.x0 = __builtin_bit_cast(lin_h8, p0);

@@ -1,10 +1,13 @@
-"""Wait states around copies to LDS in the built library.
+"""Wait states in the built library's gfx950 code, which is disassembled.
 
-The hardware does not wait by itself in two places, and the compiler does for instructions of its
-own but not for those in assembly strings: a copy to LDS reads M0, which must have been written at
-least one wait state before, and a memory instruction reads its address from scalar registers that a
-vector instruction must not have written in the five wait states before.  The library's gfx950 code
-is disassembled and every copy to LDS is looked at, along all ways that lead to it."""
+The hardware does not wait by itself in some places, and the compiler does for instructions of its
+own but not for those in assembly strings:
+  a copy to LDS reads M0, which must have been written at least one wait state before;
+  a memory instruction reads its address from scalar registers that a vector instruction must not
+  have written in the five wait states before (every copy to LDS is looked at, along all ways that
+  lead to it);
+  a matrix instruction reads registers that a vector instruction must not have written in the two
+  before, and of a 16x16x32 one the summand's registers must not be written in the three after."""
 import os
 import re
 import shutil
@@ -21,6 +24,13 @@ LINE = re.compile(r"^\t(\S+)\s*(.*?)\s*// ([0-9A-F]+):(.*)$")
 def _scalars(text):
     out = set()
     for lo, hi, one in re.findall(r"\bs(?:\[(\d+):(\d+)\]|(\d+)\b)", text):
+        out |= {int(one)} if one else set(range(int(lo), int(hi) + 1))
+    return out
+
+
+def _vectors(text):
+    out = set()
+    for lo, hi, one in re.findall(r"\bv(?:\[(\d+):(\d+)\]|(\d+)\b)", text):
         out |= {int(one)} if one else set(range(int(lo), int(hi) + 1))
     return out
 
@@ -84,6 +94,26 @@ def _faults(code):
     return sum(is_copy), bad
 
 
+def _matrix_faults(code):
+    """(matrix instructions, pairs of a vector and a matrix instruction too close to each other)."""
+    bad, count = [], 0
+    split = [re.split(r",\s*(?![^\[]*\])", ops) for _, _, ops, _ in code]
+    for i, (address, name, ops, _) in enumerate(code):
+        if not name.startswith("v_mfma"):
+            continue
+        count += 1
+        for way, most, regs in ((-1, 2, _vectors(",".join(split[i][1:]))),
+                                (1, 3 if "16x16x32" in name else 0, _vectors(split[i][3]))):
+            waited, j = 0, i + way
+            while waited < most and 0 <= j < len(code) and not code[j][1].startswith(("s_branch", "s_cbranch")):
+                other = code[j][1]
+                if other.startswith("v_") and not other.startswith(("v_mfma", "v_accvgpr", "v_cmp")) and _vectors(split[j][0]) & regs:
+                    bad.append((hex(address), name, ops, other, code[j][2]))
+                waited += int(code[j][2], 0) + 1 if other == "s_nop" else 1
+                j += way
+    return count, bad
+
+
 def _parse(text):
     return list(_functions("0 <f>:\n" + "\n".join(f"\t{ops} // {4 * i:08X}: 0" for i, ops in enumerate(text))))[0]
 
@@ -97,7 +127,17 @@ def test_the_check_sees_a_missing_wait():
     assert not _faults(_parse(["v_readfirstlane_b32 s6, v3", "s_mov_b32 m0, s2", "s_nop 0", copy]))[1]
 
 
-def test_copies_to_lds_wait_for_what_they_read(tmp_path):
+def test_the_check_sees_a_vector_instruction_too_close_to_a_matrix_one():
+    mfma, cvt = "v_mfma_f32_16x16x32_f16 v[8:11], v[4:7], v[0:3], v[12:15]", "v_cvt_pk_f16_f32 v%d, v20, v21"
+    assert _matrix_faults(_parse([cvt % 3, "s_nop 0", mfma]))[1]
+    assert not _matrix_faults(_parse([cvt % 3, "s_nop 1", mfma]))[1]
+    assert _matrix_faults(_parse([mfma, "s_nop 1", cvt % 12]))[1]
+    assert not _matrix_faults(_parse([mfma, "s_nop 2", cvt % 12]))[1]
+
+
+@pytest.fixture(scope="module")
+def listings(tmp_path_factory):
+    tmp_path = tmp_path_factory.mktemp("code")
     if not os.path.exists(OBJDUMP):
         pytest.skip("no llvm-objdump")
     pd.load()
@@ -105,11 +145,25 @@ def test_copies_to_lds_wait_for_what_they_read(tmp_path):
     subprocess.run([OBJDUMP, "--offloading", str(lib)], check=True, capture_output=True, cwd=tmp_path)
     parts = sorted(p for p in tmp_path.iterdir() if p.name.endswith("gfx950"))
     assert parts
+    return [subprocess.run([OBJDUMP, "-d", "--no-show-raw-insn", str(p)], check=True, capture_output=True, text=True).stdout
+            for p in parts]
+
+
+def test_copies_to_lds_wait_for_what_they_read(listings):
     copies = 0
-    for part in parts:
-        listing = subprocess.run([OBJDUMP, "-d", "--no-show-raw-insn", str(part)], check=True, capture_output=True, text=True).stdout
+    for listing in listings:
         for code in _functions(listing):
             count, bad = _faults(code)
             copies += count
             assert not bad, bad[:3]
     assert copies > 1000          # the attention kernels and the convolutions are among them
+
+
+def test_vector_instructions_keep_their_distance_to_matrix_ones(listings):
+    products = 0
+    for listing in listings:
+        for code in _functions(listing):
+            count, bad = _matrix_faults(code)
+            products += count
+            assert not bad, bad[:3]
+    assert products > 1000
