@@ -483,33 +483,36 @@ __device__ __forceinline__ SplitB silu_split(const f4& ua, const f4& ub, float c
 // for every outstanding LDS read before each use).  Callers wait for these
 // copies explicitly (s_waitcnt vmcnt(0)) before any wave reads their data.
 // The hardware does not wait by itself for what a copy reads: M0 must be a wait
-// state old, an address that readfirstlane wrote five.  The compiler sees to
-// that between instructions of its own, but not where one of them is in an
-// assembly string: hence the s_nop.
-// The base address is uniform over the wave by construction; readfirstlane
-// puts it in scalar registers, as the instruction needs.
-__device__ __forceinline__ uint64_t uniform_addr(const void* p) {
+// state old, an address that a vector instruction wrote to scalar registers
+// five.  The compiler sees to that between instructions of its own, but not
+// where one of them is in an assembly string: hence the s_nop.  The base
+// address is uniform: scalar_addr is for one that scalar instructions form (the
+// readfirstlane in it then goes away), uniform_addr for any.
+__device__ __forceinline__ uint64_t scalar_addr(const void* p) {
     const uint64_t v = (uint64_t)(uintptr_t)p;
     const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v);
     const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
-    uint64_t u = ((uint64_t)hi << 32) | lo;
+    return ((uint64_t)hi << 32) | lo;
+}
+__device__ __forceinline__ uint64_t uniform_addr(const void* p) {
+    uint64_t u = scalar_addr(p);
     asm("s_nop 4" : "+s"(u));
     return u;
 }
-__device__ __forceinline__ void dma16(const void* gbase, uint32_t voff, uint32_t lds) {
+__device__ __forceinline__ void dma16(uint64_t gbase, uint32_t voff, uint32_t lds) {
     asm volatile("s_mov_b32 m0, %2\n\t"
                  "s_nop 0\n\t"
                  "global_load_lds_dwordx4 %0, %1"
                  :
-                 : "v"(voff), "s"(uniform_addr(gbase)), "s"(__builtin_amdgcn_readfirstlane(lds))
+                 : "v"(voff), "s"(gbase), "s"(__builtin_amdgcn_readfirstlane(lds))
                  : "memory", "m0");
 }
-__device__ __forceinline__ void dma4(const void* gbase, uint32_t voff, uint32_t lds) {
+__device__ __forceinline__ void dma4(uint64_t gbase, uint32_t voff, uint32_t lds) {
     asm volatile("s_mov_b32 m0, %2\n\t"
                  "s_nop 0\n\t"
                  "global_load_lds_dword %0, %1"
                  :
-                 : "v"(voff), "s"(uniform_addr(gbase)), "s"(__builtin_amdgcn_readfirstlane(lds))
+                 : "v"(voff), "s"(gbase), "s"(__builtin_amdgcn_readfirstlane(lds))
                  : "memory", "m0");
 }
 template <class T>
@@ -561,7 +564,7 @@ void k_conv_f32s(ConvKernArgs ka) {
         asm volatile("" : "+s"(gb), "+v"(lo));
         const uint32_t base = lds_addr(dst);
         for (int c = wave; c < n_units / 64; c += NW)
-            dma16(gb + (size_t)(off + c * 64) * 16u, lo, base + (uint32_t)c * 1024u);
+            dma16(uniform_addr(gb + (size_t)(off + c * 64) * 16u), lo, base + (uint32_t)c * 1024u);
     };
     auto slab_buf = [&](int buf) -> h8* { return slabs + buf * L::SLAB; };
     // streamed slab s (0 <= s < NS) -> buffer buf, PER_WAVE copies per wave
@@ -578,14 +581,14 @@ void k_conv_f32s(ConvKernArgs ka) {
         for (int i = 0; i < PER_WAVE; ++i) {
             int c = wave + i * NW;
             c = c < L::SLAB / 64 ? c : L::SLAB / 64 - 1;
-            dma16(gb + (size_t)(off + c * 64) * 16u, lo, base + (uint32_t)c * 1024u);
+            dma16(scalar_addr(gb + (size_t)(off + c * 64) * 16u), lo, base + (uint32_t)c * 1024u);
         }
     };
     // this wave's first-layer shift (b1 + e_n, plus Wc c on the guided branch) -> its vector row
     // 16 B per lane while a whole 256 floats remain, then 4 B per lane (lanes
     // past the row re-read its last value into the row's padding)
     auto dma_shift = [&](int n, int br) {
-        const float* row = (br == 0 ? a.shift_u : a.shift_c) + (int64_t)n * W;
+        const uint64_t row = uniform_addr((br == 0 ? a.shift_u : a.shift_c) + (int64_t)n * W);
         const uint32_t base = lds_addr(vec + wave * STRIDE);
         constexpr int N4 = W / 256;
         for (int c = 0; c < N4; ++c) dma16(row, (uint32_t)(c * 256 + lane * 4) * 4u, base + (uint32_t)c * 1024u);
