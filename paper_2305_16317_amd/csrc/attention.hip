@@ -360,8 +360,8 @@ __global__ __launch_bounds__(256, 2) void k_attention(const AttentionArgs a, con
                 fv.copy(vt, to + kBytes);
             } else {
                 auto from = [&](int r) { return tiles.inside(j0, j0 + r) - j0; };
-                fk.copy_some(kt, d.k_stride[1], to, threadIdx.x, from);
-                fv.copy_some(vt, d.v_stride[1], to + kBytes, threadIdx.x, from);
+                fk.copy_some(kt, to, threadIdx.x, from);
+                fv.copy_some(vt, to + kBytes, threadIdx.x, from);
             }
         } else {
             auto keep = [&](int r) { return tiles.any(j0 + r); };
@@ -507,8 +507,8 @@ __global__ __launch_bounds__(64 * W) void k_attention_few(const AttentionArgs a,
                 fv.copy(vt, to + kBytes);
             } else {
                 auto from = [&](int r) { return tiles.inside(j0, j0 + r) - j0; };
-                fk.copy_some(kt, d.k_stride[1], to, lane, from);
-                fv.copy_some(vt, d.v_stride[1], to + kBytes, lane, from);
+                fk.copy_some(kt, to, lane, from);
+                fv.copy_some(vt, to + kBytes, lane, from);
             }
         } else {
             auto keep = [&](int r) { return tiles.any(j0 + r); };

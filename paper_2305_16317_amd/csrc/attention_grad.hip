@@ -5,8 +5,8 @@
 //   dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_i ds_ij q_i,  dv_j = sum_i p_ij do_i
 //
 // Two kernels, each summing into its own registers: dq over a block of queries
-// (which also leaves delta for the other), dk and dv over a block of keys and the
-// query heads that read them.  The scores are formed twice (14 D operations a pair
+// (which also leaves delta, and what rows with large scores take them from, for the
+// other), dk and dv over a block of keys and the query heads that read them.  The scores are formed twice (14 D operations a pair
 // and head in place of 10), and in exchange there is no atomic and no order that
 // varies from run to run.  Where there are few blocks of keys, their queries are
 // split among several blocks, whose sums k_attention_dkv_join adds.
@@ -23,29 +23,37 @@ namespace {
 
 using namespace attn;
 
-
 // p = e^(scale s - lse): one fused multiply-add in base 2 while |lse| is under 1024;
-// beyond, where rounding lse log2 e would show, from the difference itself, which
-// is not above 0 (a score of 10^8 has a unit in the last place of 8).  Past 2^20 a
-// difference within the rounding of the score's terms counts as none: the forward pass
-// may have summed them in another order.
+// beyond, lse log2 e and lse itself are rounded too coarsely (at 2^21 a float32 has steps
+// of 1/4).  There the largest score and the sum over it are formed again, from this
+// pass's own scores, and p = e^(scale s - largest) / sum, both terms rounded alike: a
+// row's probabilities sum to 1 at any size, and equal scores have equal ones.
 constexpr float kLarge = 1024.f;
+__device__ inline bool is_large(float lse) { return !(fabsf(lse) < kLarge); }
 // (float32 takes the difference first, so that neither c2's nor lse log2 e's rounding is
 // multiplied by the score.)
 template <typename T>
-__device__ inline float probability(bool large, float s, float c2, float lse2, float scale, float lse) {
-    if (!large) return sizeof(T) == 2 ? exp2_fast(fmaf(s, c2, -lse2)) : exp2_fast(fmaf(s, scale, -lse) * kLog2e);
-    const float x = s * scale - lse, size = fabsf(lse);
-    if (x > 0.f || (size > 0x1p20f && fabsf(x) <= 0x1p-17f * size)) return x != x ? x : 1.f;
-    return exp2_fast(x * kLog2e);
+__device__ inline float probability(float s, float c2, float lse2, float scale, float lse) {
+    return sizeof(T) == 2 ? exp2_fast(fmaf(s, c2, -lse2)) : exp2_fast(fmaf(s, scale, -lse) * kLog2e);
+}
+// What a row's scores are taken from, and what their exponentials are multiplied by:
+// (lse, 1), or the largest score and 1 / sum.
+struct Base {
+    float from, times;
+};
+__device__ inline float probability(float s, float scale, const Base& b) {
+    const float x = s * scale - b.from;
+    return exp2_fast((x > 0.f ? 0.f : x) * kLog2e) * b.times;     // (rounding aside x <= 0)
+}
+__device__ inline Base base_of(float top, float total) {          // no score above -inf: p = 0
+    return Base{top == -INFINITY ? 0.f : top, total == 0.f ? 0.f : 1.f / total};
 }
 
-// Scratch: delta of every row, then the parts of dk and dv, [split][sequence, key
-// head, key][dk, dv].
-__host__ __device__ inline int64_t delta_floats(const pd_attention_desc& d) {
-    return ((int64_t)d.batch * d.heads_q * d.q_len + 3) & ~(int64_t)3;
-}
-__device__ inline float* dkv_parts(const AttentionArgs& a) { return a.scratch + delta_floats(a.d); }
+// Scratch: delta of every row, the Base of those with a large lse, then the parts of dk
+// and dv, [split][sequence, key head, key][dk, dv].
+__host__ __device__ inline int64_t all_rows(const pd_attention_desc& d) { return (int64_t)d.batch * d.heads_q * d.q_len; }
+__host__ __device__ inline int64_t row_floats(const pd_attention_desc& d) { return (3 * all_rows(d) + 3) & ~(int64_t)3; }
+__device__ inline float* dkv_parts(const AttentionArgs& a) { return a.scratch + row_floats(a.d); }
 
 // What the backward kernels read of one (sequence, key head).
 template <typename T>
@@ -53,6 +61,7 @@ struct Views {
     const T *k, *v;              // of the key head
     const T *q, *out, *dout;     // of the group's first query head
     const float *lse, *delta;    // [group][q_len]
+    const float* bases;          // [group][q_len][2]
     int group;
 };
 template <typename T>
@@ -65,38 +74,119 @@ __device__ inline Views<T> views(const AttentionArgs& a, int b, int hk) {
                     static_cast<const T*>(a.q) + b * d.q_stride[0] + hq * d.q_stride[2],
                     static_cast<const T*>(a.out) + b * d.out_stride[0] + hq * d.out_stride[2],
                     static_cast<const T*>(a.dout) + b * d.dout_stride[0] + hq * d.dout_stride[2],
-                    a.lse + at, a.scratch + at, group};
+                    a.lse + at, a.scratch + at, a.scratch + all_rows(d) + 2 * at, group};
 }
 
-// p and ds of one pair, from memory
+// the base of a row from memory
 template <typename T>
-__device__ inline void pair_grad(const AttentionArgs& a, const Views<T>& w, int i, int g, int j, float* p, float* ds) {
-    const pd_attention_desc& d = a.d;
-    const T* q = w.q + i * d.q_stride[1] + g * d.q_stride[2];
-    const T* go = w.dout + i * d.dout_stride[1] + g * d.dout_stride[2];
-    const T* k = w.k + j * d.k_stride[1];
-    const T* v = w.v + j * d.v_stride[1];
-    float s = 0.f, dp = 0.f;
-    for (int e = 0; e < d.head_dim; ++e) {
-        s = fmaf((float)q[e], (float)k[e], s);
-        dp = fmaf((float)go[e], (float)v[e], dp);
+__device__ inline Base row_base(const Views<T>& w, int64_t at) {
+    const float lse = w.lse[at];
+    return is_large(lse) ? Base{w.bases[2 * at], w.bases[2 * at + 1]} : Base{lse, 1.f};
+}
+
+// float32 operands are held in three parts
+template <typename T, int DP, int ROWS>
+using Held = std::conditional_t<sizeof(T) == 2, AsIs<T, DP>, InParts<DP, ROWS>>;
+
+// The score of each lane's own row `mine` with the wave's `one`, as the matrix cores form it for
+// the kernels (TURNED: the rows are queries), so that it fits a row's base to the bit; where
+// that is not finite (a value in parts: infinity less infinity), the plain sum.
+template <typename T, bool TURNED>
+__device__ float wave_score(const T* mine, const T* one, int D) {
+    using As = Held<T, 32, 32>;
+    const int lane = threadIdx.x & 63, h = lane >> 5;
+    const uint64_t address = (uint64_t)(uintptr_t)mine;
+    float got = 0.f;
+    for (int tile = 0; tile < 2; ++tile) {
+        const int from = 32 * tile + (lane & 31);
+        const uint32_t lo = (uint32_t)__shfl((int)(uint32_t)address, from), hi = (uint32_t)__shfl((int)(uint32_t)(address >> 32), from);
+        const T* row = reinterpret_cast<const T*>((uintptr_t)(((uint64_t)hi << 32) | lo));
+        f32x16 s = {};
+        for (int c = 0; 16 * c < D; ++c) {
+            const int e = 16 * c + 8 * h;
+            f32x8 x = {}, y = {};
+            if (e < D) {
+                x = widen(load8(row + e, D - e));
+                y = widen(load8(one + e, D - e));
+            }
+            if constexpr (TURNED)
+                s = mma_turned(As::make(x), As::make(y), s);
+            else
+                s = mma(As::make(x), As::make(y), s);
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const float a = __shfl(s[r], 0), b = __shfl(s[r], 32);
+            if (lane == 32 * tile + tile_row(0, r)) got = a;
+            if (lane == 32 * tile + tile_row(32, r)) got = b;
+        }
     }
+    if (!(fabsf(got) < INFINITY)) {
+        got = 0.f;
+        for (int e = 0; e < D; ++e) got = fmaf((float)mine[e], (float)one[e], got);
+    }
+    return got;
+}
+
+// p and ds of one pair, its score s given, from memory
+template <typename T>
+__device__ inline void pair_grad(const AttentionArgs& a, const Views<T>& w, int i, int g, int j, float s, float* p, float* ds) {
+    const pd_attention_desc& d = a.d;
+    const T* go = w.dout + i * d.dout_stride[1] + g * d.dout_stride[2];
+    const T* v = w.v + j * d.v_stride[1];
+    float dp = 0.f;
+    for (int e = 0; e < d.head_dim; ++e) dp = fmaf((float)go[e], (float)v[e], dp);
     const int64_t at = (int64_t)g * d.q_len + i;
-    *p = probability<T>(true, s, 0.f, 0.f, d.scale, w.lse[at]);
+    *p = probability(s, d.scale, row_base(w, at));
     *ds = *p * (dp - w.delta[at]);
+}
+
+// The base of a row with a large lse from its visible keys alone, for rows whose fast sums are
+// not finite; the whole wave works on the row.
+template <typename T>
+__device__ void base_row(const AttentionArgs& a, const Views<T>& w, int i, int g, const See see) {
+    const int lane = threadIdx.x & 63;
+    const T* q = w.q + i * a.d.q_stride[1] + g * a.d.q_stride[2];
+    float top = -INFINITY, total = 0.f;
+    for (int part = 0; part < 2; ++part) {
+        const int j0 = part == 0 ? 0 : max(see.lo, see.sk), j1 = part == 0 ? see.sk : see.hi;
+        for (int jb = j0; jb < j1; jb += 64) {
+            const float s = wave_score<T, false>(w.k + min(jb + lane, j1 - 1) * a.d.k_stride[1], q, a.d.head_dim);
+            const float x = jb + lane < j1 ? s * a.d.scale : -INFINITY;
+            const float m = fmaxf(top, x), from = m == -INFINITY ? 0.f : m;
+            total = total * exp2_fast((top - from) * kLog2e) + exp2_fast((x - from) * kLog2e);
+            top = m;
+        }
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+        const float t = __shfl_xor(top, o), u = __shfl_xor(total, o), m = fmaxf(top, t), from = m == -INFINITY ? 0.f : m;
+        total = total * exp2_fast((top - from) * kLog2e) + u * exp2_fast((t - from) * kLog2e);
+        top = m;
+    }
+    const Base b = base_of(top, total);
+    if (lane == 0) {
+        float* to = const_cast<float*>(w.bases) + 2 * ((int64_t)g * a.d.q_len + i);
+        to[0] = b.from;
+        to[1] = b.times;
+    }
+    __threadfence();
 }
 
 // A row of dq from its visible keys alone (see attend_row in attention.hip).
 template <typename T>
 __device__ void dq_row(const AttentionArgs& a, const Views<T>& w, int i, int g, const See see, T* dq) {
     const int lane = threadIdx.x & 63, D = a.d.head_dim;
+    const T* q = w.q + i * a.d.q_stride[1] + g * a.d.q_stride[2];
+    if (is_large(w.lse[(int64_t)g * a.d.q_len + i])) base_row(a, w, i, g, see);
     float acc[2] = {0.f, 0.f};
     for (int part = 0; part < 2; ++part) {
         const int j0 = part == 0 ? 0 : max(see.lo, see.sk), j1 = part == 0 ? see.sk : see.hi;
         for (int jb = j0; jb < j1; jb += 64) {
             const int count = min(64, j1 - jb);
             float p = 0.f, ds = 0.f;
-            if (lane < count) pair_grad(a, w, i, g, jb + lane, &p, &ds);
+            const float s = wave_score<T, false>(w.k + (jb + min(lane, count - 1)) * a.d.k_stride[1], q, D);
+            if (lane < count) pair_grad(a, w, i, g, jb + lane, s, &p, &ds);
             for (int jj = 0; jj < count; ++jj) {
                 const float x = __shfl(ds, jj);
                 const T* k = w.k + (int64_t)(jb + jj) * a.d.k_stride[1];
@@ -118,7 +208,9 @@ __device__ void dkv_row(const AttentionArgs& a, const Views<T>& w, const Seq seq
         const int r = r0 + lane, i = r / w.group, g = r % w.group;
         float p = 0.f, ds = 0.f;
         const bool seen = r < rows && sees(a.d, seq, i)(j);
-        if (seen) pair_grad(a, w, i, g, j, &p, &ds);
+        const int ii = r < rows ? i : 0, gg = r < rows ? g : 0;
+        const float s = wave_score<T, true>(w.q + ii * a.d.q_stride[1] + gg * a.d.q_stride[2], w.k + j * a.d.k_stride[1], D);
+        if (seen) pair_grad(a, w, i, g, j, s, &p, &ds);
         for (uint64_t left = __ballot(seen); left; left &= left - 1) {
             const int l = __ffsll((unsigned long long)left) - 1, rr = r0 + l;
             const float pp = __shfl(p, l), dd = __shfl(ds, l);
@@ -152,12 +244,159 @@ template <typename T, int DP>
 constexpr int dkv_blocks_per_cu() {
     return DP * (int)sizeof(T) <= 128 ? 2 : 1;
 }
-// float32 operands are held in three parts
-template <typename T, int DP, int ROWS>
-using Held = std::conditional_t<sizeof(T) == 2, AsIs<T, DP>, InParts<DP, ROWS>>;
 template <typename T, int DP, int ROWS>
 constexpr int tile_bytes() {
     return ROWS * Tile<bf16, DP>::kPitch * (sizeof(T) == 2 ? 1 : 3);
+}
+
+// A wave's rows of dq: `times` o, and again from memory where that is not finite.
+template <typename T, int DP>
+__device__ __forceinline__ void store_dq(const AttentionArgs& a, const Views<T>& w, const Seq& seq, int b, int hk, int row0, int lane,
+                                         f32x16 (&o)[DP / 32], float times) {
+    constexpr int kDT = DP / 32;
+    const pd_attention_desc& d = a.d;
+    const int h = lane >> 5, row = row0 + (lane & 31);
+    const bool real = row < d.q_len * w.group;
+    const int qi = real ? row / w.group : 0, g = row % w.group;
+    const See see = real ? sees(d, seq, qi) : See{0, 0, 0};
+    T* dq = static_cast<T*>(a.dq) + b * d.dq_stride[0] + hk * w.group * d.dq_stride[2];
+    bool odd = false;
+#pragma unroll
+    for (int t = 0; t < kDT; ++t) {
+        o[t] = see.none() ? f32x16{} : o[t] * times;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) odd = odd || !(fabsf(o[t][r]) < INFINITY);
+    }
+    const uint64_t both = __ballot(odd && real);
+    uint32_t again = (uint32_t)both | (uint32_t)(both >> 32);
+    if (real && !((again >> (lane & 31)) & 1)) {
+        T* to = dq + qi * d.dq_stride[1] + g * d.dq_stride[2];
+#pragma unroll
+        for (int t = 0; t < kDT; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int e = 32 * t + 8 * r + 4 * h;
+                store4(to + e, d.head_dim - e, f32x4{o[t][4 * r], o[t][4 * r + 1], o[t][4 * r + 2], o[t][4 * r + 3]});
+            }
+    }
+    if (again) __threadfence();          // this wave's delta, read back below
+    while (again) {
+        const int rr = row0 + __ffs(again) - 1, i = rr / w.group, gg = rr % w.group;
+        again &= again - 1;
+        dq_row(a, w, i, gg, sees(d, seq, i), dq + i * d.dq_stride[1] + gg * d.dq_stride[2]);
+    }
+}
+
+// The kernel's arguments where they lie.
+typedef const __attribute__((address_space(4))) AttentionArgs* ArgsPtr;
+__device__ __forceinline__ ArgsPtr kernel_arguments() {
+    return (ArgsPtr)__builtin_amdgcn_kernarg_segment_ptr();
+}
+
+// A wave's 32 rows of dq where some have a large lse, once more: from the keys and values in
+// memory, with the largest score so far, the sum over it and dq going along.  (A call, so
+// that it takes no registers of the kernel's loop: within it, 230 us became 290 at 128
+// values.  Where every row is large 4 x 2304 tokens take 1740 us, else 373.)
+template <typename T, int DP>
+__device__ __attribute__((noinline)) void dq_again(ArgsPtr args, int b, int hk, int row0) {
+    constexpr int kSteps = DP / 16, kDT = DP / 32, BN = tile_rows<T, DP>();
+    using As = Held<T, DP, BN>;
+    using Operand = typename As::Operand;
+    const AttentionArgs& a = *(const AttentionArgs*)(ArgsPtr)uniform_address((const void*)args);
+    b = __builtin_amdgcn_readfirstlane(b), hk = __builtin_amdgcn_readfirstlane(hk), row0 = __builtin_amdgcn_readfirstlane(row0);
+    const pd_attention_desc& d = a.d;
+    const int lane = threadIdx.x & 63, h = lane >> 5, row = row0 + (lane & 31);
+    const Seq seq = sequence(a, b);
+    const Views<T> w = views<T>(a, b, hk);
+    const int rows_all = d.q_len * w.group;
+    const bool real = row < rows_all;
+    const int qi = real ? row / w.group : 0, g = row % w.group;
+    const int64_t at = (int64_t)g * d.q_len + qi;
+    const See see = real ? sees(d, seq, qi) : See{0, 0, 0}, see_from = see.from(lane);
+    const int i0 = row0 / w.group, i1 = min((row0 + 31) / w.group, seq.n - 1);
+    const KeyTiles<32> tiles(i0 <= i1 ? sees_any(d, seq, i0, i1) : See{0, 0, 0});
+    const float lse = see.none() ? 0.f : w.lse[at];
+    const bool own = is_large(lse);
+    Operand qf[kSteps], gf[kSteps];
+    float delta = 0.f, top = own ? -INFINITY : lse, total = own ? 0.f : 1.f;
+#pragma unroll
+    for (int c = 0; c < kSteps; ++c) {
+        const int e = 16 * c + 8 * h;
+        f32x8 u = {}, x = {}, y = {};
+        if (!see.none()) {
+            u = widen(load8(w.q + qi * d.q_stride[1] + g * d.q_stride[2] + e, d.head_dim - e));
+            x = widen(load8(w.dout + qi * d.dout_stride[1] + g * d.dout_stride[2] + e, d.head_dim - e));
+            y = widen(load8(w.out + qi * d.out_stride[1] + g * d.out_stride[2] + e, d.head_dim - e));
+        }
+        qf[c] = As::make(u);
+        gf[c] = As::make(x);
+#pragma unroll
+        for (int f = 0; f < 8; ++f) delta = fmaf(x[f], y[f], delta);
+    }
+    delta += __shfl_xor(delta, 32);
+    f32x16 o[kDT];
+#pragma unroll
+    for (int t = 0; t < kDT; ++t) o[t] = f32x16{};
+    for (int it = 0; it < tiles.count; ++it) {
+        const int j0 = tiles.start(it);
+        int dim = __builtin_amdgcn_readfirstlane(d.head_dim);   // (or comparisons with it stay in registers)
+        asm volatile("" : "+s"(dim));
+        auto from = [&](int r) { return (int64_t)tiles.inside(j0, j0 + r); };
+        const T* key = w.k + from(lane & 31) * d.k_stride[1];
+        const T* value = w.v + from(lane & 31) * d.v_stride[1];
+        f32x16 s = {}, dp = {};
+#pragma unroll
+        for (int c = 0; c < kSteps; ++c) {
+            const int e = 16 * c + 8 * h;
+            s = mma(As::make(widen(load8(key + e, dim - e))), qf[c], s);
+            dp = mma(As::make(widen(load8(value + e, dim - e))), gf[c], dp);
+            __builtin_amdgcn_sched_barrier(0);       // (a step's loads at a time)
+        }
+        float m = top;
+        uint32_t seen = 0;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const bool yes = see_from(j0 + tile_row(0, r));
+            seen |= (uint32_t)yes << r;
+            s[r] = yes ? s[r] * d.scale : -INFINITY;
+            m = fmaxf(m, s[r]);
+        }
+        m = own ? fmaxf(m, __shfl_xor(m, 32)) : top;
+        const float keep = m > top ? exp2_fast((top - m) * kLog2e) : 1.f;
+        top = m;
+        float sum = 0.f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const float p = probability(s[r], 1.f, base_of(top, 1.f));
+            sum += p;
+            s[r] = seen >> r & 1 ? p * (dp[r] - delta) : 0.f;
+        }
+        total = own ? total * keep + sum : 1.f;
+#pragma unroll
+        for (int t = 0; t < kDT; ++t) {
+            o[t] *= keep;
+            const int e = 32 * t + (lane & 31);
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                f32x8 x = {};
+#pragma unroll
+                for (int f = 0; f < 8; ++f)
+                    if (e < dim) x[f] = (float)w.k[from(16 * c + 8 * (f >> 2) + 4 * h + (f & 3)) * d.k_stride[1] + e];
+                o[t] = mma(As::make(x), As::make(eight(s, c)), o[t]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+    }
+    Base base = {0.f, 1.f};
+    if (own) {
+        base = base_of(top, total + __shfl_xor(total, 32));
+        if (real && h == 0) {
+            float* to = const_cast<float*>(w.bases) + 2 * at;
+            to[0] = base.from;
+            to[1] = base.times;
+        }
+    }
+    store_dq<T, DP>(a, w, seq, b, hk, row0, lane, o, d.scale * base.times);
 }
 
 template <typename T, int DP, bool COPY>
@@ -166,10 +405,12 @@ __global__ __launch_bounds__(256, (dq_blocks_per_cu<T, DP>())) void k_attention_
     constexpr int kSteps = DP / 16, kDT = DP / 32, BN = tile_rows<T, DP>(), kBytes = tile_bytes<T, DP, BN>();
     using As = Held<T, DP, BN>;
     using Operand = typename As::Operand;
-    using F = std::conditional_t<kParts, FillParts<DP, BN>, Fill<bf16, DP, BN, 256>>;
+    // (one offset: at 128 values the loop else reads offsets back from memory: 2 x 2048 tokens
+    // causal 253 us for 235)
+    using F = std::conditional_t<kParts, FillParts<DP, BN>, Fill<bf16, DP, BN, 256, DP == 128>>;
     __shared__ __align__(128) char lds[(kParts ? 2 : 4) * kBytes];       // keys, values; twice where copies fill them
     const pd_attention_desc& d = a.d;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
     const int id = near_blocks(blockIdx.x, gridDim.x), tile = row_tiles - 1 - id % row_tiles, head = id / row_tiles;
     const int hk = head % d.heads_kv, b = head / d.heads_kv;
     const Seq seq = sequence(a, b);
@@ -204,8 +445,8 @@ __global__ __launch_bounds__(256, (dq_blocks_per_cu<T, DP>())) void k_attention_
                 fv.copy(vt, to + kBytes);
             } else {
                 auto from = [&](int r) { return tiles.inside(j0, j0 + r) - j0; };
-                fk.copy_some(kt, d.k_stride[1], to, threadIdx.x, from);
-                fv.copy_some(vt, d.v_stride[1], to + kBytes, threadIdx.x, from);
+                fk.copy_some(kt, to, threadIdx.x, from);
+                fv.copy_some(vt, to + kBytes, threadIdx.x, from);
             }
         } else {
             auto keep = [&](int r) { return tiles.any(j0 + r); };
@@ -235,9 +476,9 @@ __global__ __launch_bounds__(256, (dq_blocks_per_cu<T, DP>())) void k_attention_
     const int64_t at = (int64_t)g * d.q_len + qi;
     if (real && h == 0) const_cast<float*>(w.delta)[at] = delta;
     const float c2 = d.scale * kLog2e;
-    const float lse = see.none() ? 0.f : w.lse[at], lse2 = lse * kLog2e;
-    const bool large = __any(!(fabsf(lse) < kLarge));
-
+    const float lse = see.none() ? 0.f : w.lse[at];
+    const bool large = __any(is_large(lse));
+    const float from = sizeof(T) == 2 ? lse * kLog2e : lse;
     f32x16 o[kDT];
 #pragma unroll
     for (int t = 0; t < kDT; ++t) o[t] = f32x16{};
@@ -278,13 +519,8 @@ __global__ __launch_bounds__(256, (dq_blocks_per_cu<T, DP>())) void k_attention_
             auto cols = [&](int n) { return As::cols(lk, 32 * kt + 16 * (n / kDT), n % kDT, lane); };
             Stream<Operand, 2 * kDT> cs;
             cs.begin(cols);
-            if (large) {
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[r] = probability<T>(true, s[r], c2, lse2, d.scale, lse);
-            } else {
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s[r] = probability<T>(false, s[r], c2, lse2, d.scale, lse);
-            }
+            for (int r = 0; r < 16; ++r) s[r] = probability<T>(s[r], c2, from, d.scale, from);
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[r] *= kStart ? dp[r] : dp[r] - delta;
             if (edge) {
@@ -300,32 +536,10 @@ __global__ __launch_bounds__(256, (dq_blocks_per_cu<T, DP>())) void k_attention_
         }
     }
 
-    T* dq = static_cast<T*>(a.dq) + b * d.dq_stride[0] + hk * w.group * d.dq_stride[2];
-    bool odd = false;
-#pragma unroll
-    for (int t = 0; t < kDT; ++t) {
-        o[t] = see.none() ? f32x16{} : o[t] * d.scale;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) odd = odd || !(fabsf(o[t][r]) < INFINITY);
-    }
-    const uint64_t both = __ballot(odd && real);
-    uint32_t again = (uint32_t)both | (uint32_t)(both >> 32);
-    if (real && !((again >> (lane & 31)) & 1)) {
-        T* to = dq + qi * d.dq_stride[1] + g * d.dq_stride[2];
-#pragma unroll
-        for (int t = 0; t < kDT; ++t)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int e = 32 * t + 8 * r + 4 * h;
-                store4(to + e, d.head_dim - e, f32x4{o[t][4 * r], o[t][4 * r + 1], o[t][4 * r + 2], o[t][4 * r + 3]});
-            }
-    }
-    if (again) __threadfence();          // this wave's delta, read back below
-    while (again) {
-        const int rr = row0 + __ffs(again) - 1, i = rr / w.group, gg = rr % w.group;
-        again &= again - 1;
-        dq_row(a, w, i, gg, sees(d, seq, i), dq + i * d.dq_stride[1] + gg * d.dq_stride[2]);
-    }
+    if (large)
+        dq_again<T, DP>(kernel_arguments(), b, hk, row0);
+    else
+        store_dq<T, DP>(a, w, seq, b, hk, row0, lane, o, d.scale);
 }
 
 // The queries that see key j: lo <= i < hi.
@@ -362,10 +576,10 @@ __global__ __launch_bounds__(256, (dkv_blocks_per_cu<T, DP>())) void k_attention
     using Operand = typename As::Operand;
     using F = std::conditional_t<kParts, FillParts<DP, BR>, Fill<bf16, DP, BR, 256>>;
     __shared__ __align__(128) char lds[(kParts ? 2 : 4) * kBytes];       // queries, output gradients; twice where copies fill them
-    __shared__ __align__(16) float stats[2][3][64];       // -lse / scale (float32: lse), -delta, lse
+    __shared__ __align__(16) float stats[2][4][64];       // -lse / scale (float32: lse), -delta; where far, the bases
     __shared__ int far[2];                                // whether a row's |lse| is large
     const pd_attention_desc& d = a.d;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, h = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
     const int id = near_blocks(blockIdx.x, gridDim.x), split = id % splits, unit = id / splits;
     const int tile = unit % key_tiles, head = unit / key_tiles;
     const int hk = head % d.heads_kv, b = head / d.heads_kv;
@@ -413,8 +627,8 @@ __global__ __launch_bounds__(256, (dkv_blocks_per_cu<T, DP>())) void k_attention
                 fg.copy(gt, to + kBytes);
             } else {
                 auto from = [&](int r) { return min(i0 + r, seq.n - 1) - i0; };
-                fq.copy_some(qt, d.q_stride[1], to, threadIdx.x, from);
-                fg.copy_some(gt, d.dout_stride[1], to + kBytes, threadIdx.x, from);
+                fq.copy_some(qt, to, threadIdx.x, from);
+                fg.copy_some(gt, to + kBytes, threadIdx.x, from);
             }
         } else {
             auto keep = [&](int r) { return i0 + r < seq.n; };
@@ -422,19 +636,28 @@ __global__ __launch_bounds__(256, (dkv_blocks_per_cu<T, DP>())) void k_attention
             F::load(gt, d.dout_stride[1], d.head_dim, to + kBytes, threadIdx.x, keep);
         }
     };
-    auto put_stat = [&](int buf) {
+    auto put_stat = [&](int x, int buf) {
         if (threadIdx.x < BR) {                           // (lanes of the first wave)
             stats[buf][0][threadIdx.x] = kParts ? stat : stat * over;
-            stats[buf][2][threadIdx.x] = stat;
-            const uint64_t some = __ballot(!(fabsf(stat) < kLarge));
-            if (threadIdx.x == 0) far[buf] = some != 0 || !(fabsf(over) < 0x1p100f);      // (a scale near 0)
+            const bool any = __ballot(is_large(stat)) != 0 || !(fabsf(over) < 0x1p100f);      // (a scale near 0)
+            if (threadIdx.x == 0) far[buf] = any;
+            if (any) {
+                Base base = {stat, 1.f};
+                if (is_large(stat)) {
+                    const int g = x / per_head, i = min(first + (x - g * per_head) * BR + (int)threadIdx.x, seq.n - 1);
+                    const float* from = w.bases + 2 * ((int64_t)g * d.q_len + i);
+                    base = Base{from[0], from[1]};
+                }
+                stats[buf][2][threadIdx.x] = base.from;
+                stats[buf][3][threadIdx.x] = base.times;
+            }
         } else if (threadIdx.x < 2 * BR) {
             stats[buf][1][threadIdx.x - BR] = -stat;
         }
     };
     if (x0 < x1) {
         fetch(x0, 0);
-        put_stat(0);
+        put_stat(x0, 0);
     }
 
     Operand kf[kSteps], vf[kSteps];
@@ -489,7 +712,7 @@ __global__ __launch_bounds__(256, (dkv_blocks_per_cu<T, DP>())) void k_attention
                 rs.begin(rows);
                 rs.run(rows, [&](int n, const Operand& f) {
                     if (n % 2 == 0)
-                        s = mma(f, kf[n / 2], s);
+                        s = mma_turned(f, kf[n / 2], s);
                     else
                         dp = mma(f, vf[n / 2], dp);
                 });
@@ -502,11 +725,16 @@ __global__ __launch_bounds__(256, (dkv_blocks_per_cu<T, DP>())) void k_attention
                 cs.begin(cols);
                 if (large) {
 #pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        s[r] = probability<T>(true, s[r], 0.f, 0.f, d.scale, stats[buf][2][32 * rt + tile_row(lane, r)]);
+                    for (int r = 0; r < 16; r += 4) {
+                        const int at = 32 * rt + tile_row(lane, r);
+                        const f32x4 u = *reinterpret_cast<const f32x4*>(&stats[buf][2][at]);
+                        const f32x4 v = *reinterpret_cast<const f32x4*>(&stats[buf][3][at]);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) s[r + e] = probability(s[r + e], d.scale, Base{u[e], v[e]});
+                    }
                 } else if constexpr (kParts) {
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) s[r] = probability<T>(false, s[r], 0.f, 0.f, d.scale, from[r]);
+                    for (int r = 0; r < 16; ++r) s[r] = probability<T>(s[r], 0.f, 0.f, d.scale, from[r]);
                 } else {
 #pragma unroll
                     for (int r = 0; r < 16; ++r) s[r] = exp2_fast(s[r] * c2);
@@ -529,7 +757,7 @@ __global__ __launch_bounds__(256, (dkv_blocks_per_cu<T, DP>())) void k_attention
                 });
             }
         }
-        if (x + 1 < x1) put_stat(buf ^ 1);
+        if (x + 1 < x1) put_stat(x + 1, buf ^ 1);
     }
 
 #pragma unroll
@@ -675,7 +903,7 @@ void attention_grad_dim(const AttentionArgs& a, hipStream_t s) {
 int64_t attention_grad_scratch_bytes(const pd_attention_desc& d) {
     const int splits = dkv_splits(d);
     const int64_t parts = splits == 1 ? 0 : (int64_t)splits * d.batch * d.heads_kv * d.kv_len * 2 * d.head_dim;
-    return (delta_floats(d) + parts) * (int64_t)sizeof(float);
+    return (row_floats(d) + parts) * (int64_t)sizeof(float);
 }
 
 void launch_attention_grad(const AttentionArgs& a, hipStream_t s) {

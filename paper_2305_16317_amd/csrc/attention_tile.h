@@ -150,6 +150,18 @@ __device__ __forceinline__ f32x16 mma(const Split& a, const Split& b, f32x16 c) 
     return mma(a.h, b.h, c);
 }
 
+// The same with the operands exchanged: the bits that mma(b, a, .) gives at the turned
+// place.
+__device__ __forceinline__ f32x16 mma_turned(const Split& a, const Split& b, f32x16 c) {
+    c = mma(a.h, b.l, c);
+    c = mma(a.l, b.h, c);
+    c = mma(a.m, b.m, c);
+    c = mma(a.h, b.m, c);
+    c = mma(a.m, b.h, c);
+    return mma(a.h, b.h, c);
+}
+__device__ __forceinline__ f32x16 mma_turned(bf16x8 a, bf16x8 b, f32x16 c) { return mma(a, b, c); }
+
 // How a kernel holds its operands: as they are, in tiles that copies fill, or in three
 // parts, in three tiles that are filled through the registers.
 template <typename T, int DP>
@@ -314,18 +326,25 @@ __device__ __forceinline__ void lds_barrier() {
 // (Copies, and the same through registers, which takes any alignment: 8192 tokens with a
 // window 283 and 523 us, backward on latents 385 and 624 us, the next token of 16 sequences
 // 178 and 580 us.)
-template <typename T, int DP, int ROWS, int THREADS>
+template <typename T, int DP, int ROWS, int THREADS, bool ONE = false>
 struct Fill {
     using Ti = Tile<T, DP>;
     static constexpr int kRowUnits = Ti::kPitch / 16;
     static constexpr int kCopies = ROWS * kRowUnits / THREADS;
+    static constexpr int kStep = THREADS / kRowUnits;         // rows from a thread's copy to its next
+    // ONE: one offset a thread instead of one a copy, for a kernel without registers to
+    // spare.  swz repeats every 16 rows: copies that are so far apart differ by rows alone,
+    // which the scalar base can say (two instructions a copy more).
+    static constexpr bool kOne = ONE;
+    static_assert(!ONE || kStep % 16 == 0, "copies at whole periods of swz");
     static_assert(ROWS * kRowUnits % THREADS == 0 && THREADS % 64 == 0, "whole copies");
-    uint32_t off[kCopies];      // of this thread's copies from the tile's first row
-    uint32_t to;                // this wave's part of a tile, from its start
+    uint32_t off[kOne ? 1 : kCopies];      // of this thread's copies from the tile's first row
+    uint32_t step;                         // bytes from row to row
+    uint32_t to;                           // this wave's part of a tile, from its start
     __device__ __forceinline__ void plan(int64_t stride, int units, int thread) {
-        const uint32_t step = (uint32_t)stride * (uint32_t)sizeof(T);
+        step = (uint32_t)stride * (uint32_t)sizeof(T);
 #pragma unroll
-        for (int i = 0; i < kCopies; ++i) {
+        for (int i = 0; i < (kOne ? 1 : kCopies); ++i) {
             const int at = i * THREADS + thread, row = at / kRowUnits;
             const int unit = (at % kRowUnits) ^ Ti::swz(row);
             off[i] = (uint32_t)row * step + (unit < units ? unit : 0) * 16;
@@ -337,18 +356,18 @@ struct Fill {
         const uint64_t from = uniform_address(base);
         const uint32_t at = __builtin_amdgcn_readfirstlane(lds_address(lds) + to);
 #pragma unroll
-        for (int i = 0; i < kCopies; ++i) copy16(from, off[i], at + i * THREADS * 16);
+        for (int i = 0; i < kCopies; ++i)
+            copy16(kOne ? from + (uint32_t)(i * kStep) * step : from, off[kOne ? 0 : i], at + i * THREADS * 16);
     }
     // the same, but its row r from the row that source(r) names
     template <class Source>
-    __device__ __forceinline__ void copy_some(const T* base, int64_t stride, const char* lds, int thread, Source source) const {
+    __device__ __forceinline__ void copy_some(const T* base, const char* lds, int thread, Source source) const {
         const uint64_t from = uniform_address(base);
         const uint32_t at = __builtin_amdgcn_readfirstlane(lds_address(lds) + to);
-        const uint32_t step = (uint32_t)stride * (uint32_t)sizeof(T);
 #pragma unroll
         for (int i = 0; i < kCopies; ++i) {
-            const int row = (i * THREADS + thread) / kRowUnits;
-            copy16(from, off[i] + (uint32_t)(source(row) - row) * step, at + i * THREADS * 16);
+            const int row = (i * THREADS + thread) / kRowUnits, mine = kOne ? thread / kRowUnits : row;
+            copy16(from, off[kOne ? 0 : i] + (uint32_t)(source(row) - mine) * step, at + i * THREADS * 16);
         }
     }
     // the same through registers, any stride and alignment; rows for which `keep` is

@@ -445,6 +445,59 @@ def test_attention_backward_of_scores_near_the_types_end(n, m, dtype):
     _close(dv, ot.attention_grad(_np(q), _np(k), _np(v), _np(g), 0.125, True)[2], TOL_GRAD[dtype])
 
 
+def _grad_bounds(q, k, v, g, out, scale, causal, u):
+    """What roundings can add to dq, dk and dv when each of a pair's terms (p, dout v, dout out and their
+    product) is off by u of the sizes that it is summed from."""
+    q, k, v, g, out = (np.abs(_np(x)) if x is not q and x is not k else _np(x) for x in (q, k, v, g, out))
+    dq, dk, dv = np.zeros(q.shape), np.zeros(k.shape), np.zeros(v.shape)
+    for b, i, h, e, j in ot._each(q, k, None, None, causal, 0, 0):
+        x = scale * (k[b, j, e] @ q[b, i, h])
+        p = np.exp(x - np.max(x))
+        p /= p.sum()
+        ds = u * p * (v[b, j, e] @ g[b, i, h] + out[b, i, h] @ g[b, i, h])
+        dq[b, i, h] = abs(scale) * (ds @ np.abs(k[b, j, e]))
+        dk[b, j, e] += abs(scale) * ds[:, None] * np.abs(q[b, i, h])
+        dv[b, j, e] += u * p[:, None] * g[b, i, h]
+    return dq, dk, dv
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("size", [2.0**12, 2.0**21, -2.0**21])
+@pytest.mark.parametrize("n,m,causal", [(40, 70, False), (1, 40, True), (150, 150, True)])
+def test_attention_backward_of_keys_beside_the_largest(n, m, causal, size, dtype):
+    """Scores of `size` less 0 to 3, whole numbers that every sum forms exactly: equal ones share a row, and
+    keys that lie 1 to 3 lower keep their weight, though the row's lse is no number of float32 there.
+    bfloat16: out, p or ds, and the result are rounded, 2^-9 each; float32: fewer than 512 roundings of 2^-24."""
+    print("near the largest", n, m, causal, size, dtype, flush=True)
+    q, k, v, g = _att_inputs(1, n, m, 2, 1, 64, dtype, 31)
+    q.zero_(), k.zero_()
+    q[..., 0], q[..., 1], k[..., 0] = size, 1.0, 1.0
+    k[..., 1] = -(torch.arange(m, device="cuda") % 4)[None, :, None].to(dtype)
+    refs = ot.attention_grad(_np(q), _np(k), _np(v), _np(g), 1.0, causal)
+    kw = dict(causal=causal, scale=1.0)
+    out, lse = torch.empty_like(q), torch.empty((1, 2, n), device="cuda")
+    grads = [torch.empty_like(x) for x in (q, k, v)]
+    pd.pd_attention_forward(q, k, v, out, lse=lse, **kw)
+    pd.pd_attention_backward(q, k, v, out, lse, g, *grads, **kw)
+    u = 2.0**-8 if dtype == BF16 else 2.0**-15
+    bounds = [b + u * np.abs(r) for b, r in zip(_grad_bounds(q, k, v, g, out, 1.0, causal, u), refs)]
+
+    def check(which, part=slice(None)):
+        off = np.abs(_np(grads[which])[:, part] - refs[which][:, part])
+        assert np.all(off <= bounds[which][:, part]), (("dq", "dk", "dv")[which], np.nanmax(off / (bounds[which][:, part] + 1e-300)))
+    for which in range(3):
+        check(which)
+    if n != m:
+        return
+    # the same beside a NaN: rows that do not see the last key, keys that the first row does not see
+    for x, at, which, clean in ((k, n - 1, 0, slice(0, n - 1)), (q, 0, 1, slice(1, n)), (q, 0, 2, slice(1, n))):
+        kept = x[0, at].clone()
+        x[0, at] = float("nan")
+        pd.pd_attention_backward(q, k, v, out, lse, g, *grads, **kw)
+        x[0, at] = kept
+        check(which, clean)
+
+
 def test_attention_cache_offsets_past_32_bits():
     """A cache whose tokens lie 80 MB apart: the last of 60 is 2.4e9 elements from the first."""
     D, m, step = 64, 60, 40_000_000
