@@ -75,7 +75,7 @@ __device__ void attend_row(const AttentionArgs& a, const T* q, const T* k, const
             }
         }
     }
-    const float inv = 1.f / total;
+    const float inv = total == 0.f ? 0.f : 1.f / total;     // (no score above -inf: 0, as for a row that sees nothing)
     if (lane < D) out[lane] = (T)(acc[0] * inv);
     if (lane + 64 < D) out[lane + 64] = (T)(acc[1] * inv);
     if (lse && lane == 0) *lse = log_sum(top, 1.f, total);

@@ -414,6 +414,22 @@ def test_attention_values_of_the_types_ends(dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,m", [(1, 50), (1, 700), (3, 40), (40, 70), (70, 600)])
+def test_attention_of_scores_that_are_all_minus_infinity(n, m, dtype):
+    """Keys of -inf under queries above 0 weigh nothing, alone as beside others: then there is no sum, as
+    for a row that sees nothing, whatever the type and the way the rows go."""
+    q, k, v, _ = _att_inputs(1, n, m, 2, 1, 64, dtype, 33)
+    q = q.abs() + 0.1
+    k.fill_(-float("inf"))
+    out, lse = torch.full_like(q, 7), torch.full((1, 2, n), 7.0, device="cuda")
+    pd.pd_attention_forward(q, k, v, out, lse=lse, causal=False)
+    assert torch.all(out == 0) and torch.all(lse == -float("inf"))
+    k[0, m // 2] = 0.5                                       # one key with a score: its value alone
+    pd.pd_attention_forward(q, k, v, out, lse=lse, causal=False)
+    _close(out, np.broadcast_to(_np(v[0, m // 2]), out.shape), TOL[dtype])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("scale", [0.0, 1e-39, -1e-30, 1e-10])
 def test_attention_backward_of_scales_near_zero(scale, dtype):
     """All keys weigh the same, so dv is a mean; dq and dk go with the scale."""
