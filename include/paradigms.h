@@ -329,8 +329,9 @@ pd_status pd_sample_picard(const pd_schedule* s, const pd_denoiser* d, int32_t p
  * the same inputs give the same bits.  Strides count elements, not bytes, may
  * be any (>= 0), and rows need no alignment beyond their element's; the last
  * dimension is contiguous.  Outputs must not overlap inputs or each other
- * except where a call says so.  dtype is PD_F32 or PD_BF16; sums, statistics
- * and exponentials are float32 and each result is rounded once.
+ * except where a call says so; one whose own rows share elements is refused.
+ * dtype is PD_F32 or PD_BF16; sums, statistics and exponentials are float32 and
+ * each result is rounded once.
  * `scratch` is device memory of the caller, 16-byte aligned, of at least the bytes the
  * matching *_scratch call gives (0: may be NULL); it holds nothing between calls. */
 #define PD_F8E4M3 2            /* OCP e4m3 (no infinities, largest 448), outputs only */

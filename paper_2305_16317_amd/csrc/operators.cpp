@@ -1,6 +1,7 @@
 // C entry points of the transformer operators: argument checks on the host,
 // then the launches.  Empty work (no rows, no tokens) is PD_OK with nothing
 // launched, but for gradients that are sums over nothing.
+#include <algorithm>
 #include <cmath>
 #include <cstring>
 
@@ -36,6 +37,44 @@ void check_scratch(const void* scratch, int64_t have, int64_t need) {
 // overlap where they are written.
 constexpr int64_t kMostStride = (int64_t)1 << 40;
 void check_stride(int64_t s) { require(s >= 0 && s < kMostStride, "a stride is out of range"); }
+
+// The rows of `row` elements of an output at three strides: none may share an element
+// with another.
+bool rows_apart(const int64_t* stride, int64_t batch, int64_t tokens, int64_t heads, int64_t row) {
+    typedef __int128 wide;                                // (a stride times a count can pass 2^63)
+    struct Axis {
+        int64_t stride, count;
+    } axes[3] = {{stride[0], batch}, {stride[1], tokens}, {stride[2], heads}};
+    std::sort(axes, axes + 3, [](const Axis& a, const Axis& b) { return a.stride < b.stride; });
+    // usually each step passes what the smaller steps cover
+    bool nested = true;
+    wide covered = row;
+    for (const Axis& x : axes) {
+        if (x.count <= 1) continue;
+        if (x.stride < row) return false;
+        nested = nested && x.stride >= covered;
+        covered += (wide)x.stride * (x.count - 1);
+    }
+    if (nested) return true;
+    // else the axes interleave: two rows share an element where some difference of places is
+    // under `row`; the longest axis is solved for, the others are gone through
+    std::sort(axes, axes + 3, [](const Axis& a, const Axis& b) { return a.count < b.count; });
+    const Axis &p = axes[0], &q = axes[1], &l = axes[2];
+    for (int64_t i = 0; i < p.count; ++i)
+        for (int64_t j = i ? 1 - q.count : 0; j < q.count; ++j) {
+            const wide at = (wide)i * p.stride + (wide)j * q.stride;
+            const wide back = -at / l.stride;             // (the nearest of the longest axis: this, or one beside it)
+            for (wide k = back - 1; k <= back + 1; ++k) {
+                if (k <= -(wide)l.count || k >= l.count || (i == 0 && j == 0 && k == 0)) continue;
+                const wide off = at + k * l.stride;
+                if (off < row && -off < row) return false;
+            }
+        }
+    return true;
+}
+void check_apart(const char* what, const int64_t* stride, int64_t batch, int64_t tokens, int64_t heads, int64_t row) {
+    require(rows_apart(stride, batch, tokens, heads, row), std::string(what) + ": rows of an output share elements");
+}
 
 // ------------------------------------------------------------------ norm
 void check_norm(const pd_rmsnorm_desc& d, bool backward) {
@@ -184,6 +223,8 @@ extern "C" pd_status pd_rotary_apply(const pd_rotary_desc* desc, const void* q, 
         if (d.batch == 0 || d.length == 0) return;
         require(q && positions && table && q_out && (!k || k_out), "NULL device pointer");
         require(d.table_rows >= 1, "table_rows must be >= 1");
+        check_apart("q_out", d.q_out_stride, d.batch, d.length, d.heads_q, d.head_dim);
+        if (d.heads_k) check_apart("k_out", d.k_out_stride, d.batch, d.length, d.heads_k, d.head_dim);
         require_gfx950();
         launch_rotary(RotaryArgs{d, q, k, positions, table, q_out, k_out}, static_cast<hipStream_t>(stream));
     });
@@ -203,6 +244,7 @@ extern "C" pd_status pd_attention_forward(const pd_attention_desc* desc, const v
         const pd_attention_desc d = check_attention(desc);
         if (d.batch == 0 || d.q_len == 0) return;
         require(q && out && (d.kv_len == 0 || (k && v)), "NULL device pointer");
+        check_apart("out", d.out_stride, d.batch, d.q_len, d.heads_q, d.head_dim);
         check_scratch(scratch, scratch_bytes, attention_scratch_bytes(d));
         require_gfx950();
         AttentionArgs a{};
@@ -232,6 +274,9 @@ extern "C" pd_status pd_attention_backward(const pd_attention_desc* desc, const 
         if (d.batch == 0 || (d.q_len == 0 && d.kv_len == 0)) return;
         require(d.q_len == 0 || (q && out && lse && dout && dq), "NULL device pointer");
         require(d.kv_len == 0 || (k && v && dk && dv), "NULL device pointer");
+        check_apart("dq", d.dq_stride, d.batch, d.q_len, d.heads_q, d.head_dim);
+        check_apart("dk", d.dk_stride, d.batch, d.kv_len, d.heads_kv, d.head_dim);
+        check_apart("dv", d.dv_stride, d.batch, d.kv_len, d.heads_kv, d.head_dim);
         check_scratch(scratch, scratch_bytes, attention_grad_scratch_bytes(d));
         require_gfx950();
         AttentionArgs a{};

@@ -201,6 +201,43 @@ def test_attention_null_arguments():
     assert _status("pd_attention_forward", None, *[P] * 8, 0, None)[0] == pd.PD_ERR_INVALID_ARG
 
 
+def _share(stride, counts, row):
+    """Whether rows at the strides share an element, by going through them all."""
+    at = sorted(sum(i * s for i, s in zip(ix, stride)) for ix in np.ndindex(*counts))
+    return any(b - a < row for a, b in zip(at, at[1:]))
+
+
+def test_outputs_whose_rows_share_elements_are_refused():
+    """What passes the check is refused by the next: scratch is missing (many keys or a gradient need some)."""
+    r = np.random.default_rng(4)
+    cases = [(640, 64, 16), (64, 128, 16), (16, 32, 160), (0, 64, 16), (640, 0, 16), (640, 64, 15), (640, 60, 16), (100, 64, 16),
+             (48, 32, 16), (40, 64, 24), (2**39, 2**39, 2**39), (2**39, 2**20, 16)]
+    cases += [tuple(8 * r.integers(0, 40, 3)) for _ in range(400)]
+    seen = {True: 0, False: 0}
+    for stride in cases:
+        st = pd._I64x3(*[int(x) for x in stride])
+        for name, counts in (("out", (2, 3, 4)), ("dq", (2, 3, 4)), ("dk", (2, 5, 2)), ("dv", (2, 5, 2))):
+            want = _share(stride, counts, 16)
+            seen[want] += 1
+            d = _att(**{name + "_stride": st}, kv_len=2**20 if name == "out" else 5)
+            if name == "out":
+                code, m = _status("pd_attention_forward", ctypes.byref(d), *[P] * 7, None, 0, None)
+            else:
+                code, m = _status("pd_attention_backward", ctypes.byref(d), *[P] * 11, None, 0, None)
+            assert code == pd.PD_ERR_INVALID_ARG
+            assert ("share elements" in m and name in m) == want and ("scratch" in m) != want, (name, stride, m)
+        counts = (2, 3, 4)
+        d = _rotary(q_out_stride=st, k_out_stride=pd._I64x3(96, 32, 8), table_rows=1)
+        code, m = _status("pd_rotary_apply", ctypes.byref(d), *[P] * 6, None) if _share(stride, counts, 8) else (None, "")
+        assert code in (None, pd.PD_ERR_INVALID_ARG) and (code is None or "q_out" in m)
+    assert min(seen.values()) > 100
+    # single elements of an axis have no stride; what is only read may be shared
+    for kw in (dict(batch=1, out_stride=pd._I64x3(0, 64, 16)), dict(q_len=1, out_stride=pd._I64x3(64, 3, 16)),
+               dict(q_stride=pd._I64x3(0, 0, 0), k_stride=pd._I64x3(0, 0, 16))):
+        code, m = _status("pd_attention_forward", ctypes.byref(_att(kv_len=2**20, **kw)), *[P] * 7, None, 0, None)
+        assert code == pd.PD_ERR_INVALID_ARG and "scratch" in m
+
+
 def test_packed_descriptions_are_laid_out_as_the_structures():
     for packed, struct in ((pd._RMSNORM_BYTES, pd._RmsnormDesc), (pd._ROTARY_BYTES, pd._RotaryDesc),
                            (pd._ATTENTION_BYTES, pd._AttentionDesc)):
