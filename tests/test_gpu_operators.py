@@ -371,6 +371,48 @@ def test_attention_long_two_sided_and_windowed():
     _forward(q, k, v, True, 3000, 100, None, [4900], None, TOL[F32])
 
 
+#                     B   n    m    H   K  D  causal window sinks ragged layout
+MANY_BLOCKS = [
+    (64, 257, 257, 8, 8, 64, False, 0, 0, False, "token"),        # 1024 tiles of 256 rows, the second with one row
+    (64, 257, 300, 8, 8, 64, True, 40, 3, True, "token"),
+    (32, 150, 150, 16, 8, 64, True, 0, 0, True, "head"),          # two query heads to a key head: 300 rows
+    (64, 257, 257, 8, 8, 36, False, 30, 5, True, "odd"),          # through the registers
+    (64, 513, 513, 4, 4, 24, True, 100, 70, False, "token"),
+    (171, 200, 90, 3, 3, 50, True, 0, 0, False, "odd"),           # rows before the first key
+]
+
+
+@pytest.mark.parametrize("case", MANY_BLOCKS)
+def test_attention_of_many_blocks(case):
+    """From 512 tiles of 256 rows on, heads of up to 64 bfloat16 values go two tiles of 32 rows a wave.  The first,
+    two middle and the last sequences are compared, of the others that the rows past their queries are 0."""
+    B, n, m, H, K, D, causal, window, sinks, ragged, layout = case
+    print("many blocks", case, flush=True)
+    assert -(-n * (H // K) // 256) * K * B >= 512 and D <= 64
+    q, k, v, _ = _att_inputs(B, n, m, H, K, D, BF16, 41, layout)
+    ql, kl = ([n - 5 * b % n for b in range(B)], [(m * (B - b)) // B for b in range(B)]) if ragged else ([n] * B, [m] * B)
+    out, lse = torch.full(q.shape, 7.0, device="cuda", dtype=BF16), torch.full((B, H, n), 7.0, device="cuda")
+    pd.pd_attention_forward(q, k, v, out, lse=lse, causal=causal, window=window, sinks=sinks, q_lens=_lens(ql), kv_lens=_lens(kl))
+    for b in (0, B // 2, B // 2 + 1, B - 1):
+        one = slice(b, b + 1)
+        ro, rl = ot.attention(_np(q[one]), _np(k[one]), _np(v[one]), D ** -0.5, causal, window, sinks, ql[one], kl[one])
+        _close(out[one], ro, TOL[BF16], ("out", b))
+        _close(lse[one], rl, 5e-6, ("lse", b))
+    for b in range(B):
+        assert torch.all(out[b, ql[b]:] == 0) and torch.all(lse[b, :, ql[b]:] == -float("inf")), b
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("layout", ["head", "odd"])
+@pytest.mark.parametrize("B,n,H,K,D,window,sinks,lens", [
+    (3, 1, 8, 2, 128, 0, 0, [5000, 37, 0]), (3, 1, 8, 2, 64, 0, 0, [4999, 1, 2500]), (2, 1, 8, 8, 64, 3000, 100, [5000, 4200]),
+    (2, 1, 32, 4, 128, 2100, 7, [5000, 3000]), (1, 4, 16, 2, 80, 0, 0, [5000]), (2, 2, 6, 3, 40, 4000, 40, [5000, 4001])])
+def test_attention_of_few_rows_over_long_caches(B, n, H, K, D, window, sinks, lens, layout, dtype):
+    """A cache in parts, whose results are joined: parts that a window leaves without keys, sequences shorter than a part."""
+    q, k, v, _ = _att_inputs(B, n, 5000, H, K, D, dtype, 43, layout)
+    _forward(q, k, v, True, window, sinks, None, lens, None, TOL[dtype], layout)
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
 @pytest.mark.parametrize("n,m", [(96, 200), (1, 200), (3, 400)])
@@ -461,12 +503,12 @@ def test_attention_backward_of_scores_near_the_types_end(n, m, dtype):
     _close(dv, ot.attention_grad(_np(q), _np(k), _np(v), _np(g), 0.125, True)[2], TOL_GRAD[dtype])
 
 
-def _grad_bounds(q, k, v, g, out, scale, causal, u):
+def _grad_bounds(q, k, v, g, out, scale, causal, u, window=0, sinks=0):
     """What roundings can add to dq, dk and dv when each of a pair's terms (p, dout v, dout out and their
     product) is off by u of the sizes that it is summed from."""
     q, k, v, g, out = (np.abs(_np(x)) if x is not q and x is not k else _np(x) for x in (q, k, v, g, out))
     dq, dk, dv = np.zeros(q.shape), np.zeros(k.shape), np.zeros(v.shape)
-    for b, i, h, e, j in ot._each(q, k, None, None, causal, 0, 0):
+    for b, i, h, e, j in ot._each(q, k, None, None, causal, window, sinks):
         x = scale * (k[b, j, e] @ q[b, i, h])
         p = np.exp(x - np.max(x))
         p /= p.sum()
@@ -579,6 +621,25 @@ def test_attention_backward_of_rows_with_one_key(case, dtype):
     size = float(g.double().abs().max() * v.double().abs().max() * max(q.double().abs().max(), k.double().abs().max())) * D
     for got, ref in ((dq, rq), (dk, rk)):
         assert np.max(np.abs(_np(got) - ref)) <= (2**-9 if dtype == BF16 else 2**-20) * size * H / K
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("case", [c for c in GRAD if c[7] == 1 or c[2] == 1])
+def test_attention_backward_of_rows_with_a_key_or_two_to_their_rounding(case, dtype):
+    """The same rows element by element: where a key has its row alone dq and dk are what the rounding of out
+    leaves of dout v - dout out, far under dout v itself (as in the test of keys beside the largest)."""
+    B, n, m, H, K, D, causal, window, sinks, ql, kl = case
+    q, k, v, g = _att_inputs(B, n, m, H, K, D, dtype, 37)
+    out, lse = torch.empty_like(q), torch.empty((B, H, n), device="cuda")
+    kw = dict(causal=causal, window=window, sinks=sinks)
+    pd.pd_attention_forward(q, k, v, out, lse=lse, **kw)
+    grads = [torch.full(x.shape, 7.0, device="cuda", dtype=dtype) for x in (q, k, v)]
+    pd.pd_attention_backward(q, k, v, out, lse, g, *grads, **kw)
+    u = 2.0**-8 if dtype == BF16 else 2.0**-15
+    refs = ot.attention_grad(_np(q), _np(k), _np(v), _np(g), D ** -0.5, causal, window, sinks)
+    bounds = _grad_bounds(q, k, v, g, out, D ** -0.5, causal, u, window, sinks)
+    for name, got, ref, bound in zip(("dq", "dk", "dv"), grads, refs, bounds):
+        assert np.all(np.abs(_np(got) - ref) <= bound + u * np.abs(ref)), name
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
