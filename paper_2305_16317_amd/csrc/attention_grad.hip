@@ -808,9 +808,10 @@ __global__ __launch_bounds__(256, (dkv_blocks_per_cu<T, DP>())) void k_attention
     }
 }
 
-// The parts of a key's dk and dv into the result: one wave a key.
+// The parts of a key's dk and dv into the result: one wave a key.  (Eight waves a SIMD, or
+// the registers of the path for keys that are not finite leave room for five: 25 us for 21.)
 template <typename T>
-__global__ __launch_bounds__(256) void k_attention_dkv_join(const AttentionArgs a, int splits) {
+__global__ __launch_bounds__(256, 8) void k_attention_dkv_join(const AttentionArgs a, int splits) {
     const pd_attention_desc& d = a.d;
     const int lane = threadIdx.x & 63, D = d.head_dim;
     const int64_t keys = (int64_t)d.batch * d.heads_kv * d.kv_len, kat = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
