@@ -440,7 +440,8 @@ pd_status pd_rotary_apply(const pd_rotary_desc* desc, const void* q, const void*
  * products' sums are float32.
  * Backward: dq, dk, dv from out, lse (forward) and dout, all keys' gradients
  * written (0 for those that no query sees).  Sums over a group's query heads
- * are float32, rounded once.
+ * are float32, rounded once.  From |lse| = 1024 on, where lse has too few bits
+ * to take scores from, a row's largest score and sum are formed again.
  * head_dim 1..128 (more: PD_ERR_UNSUPPORTED); heads_q a multiple of heads_kv. */
 typedef struct pd_attention_desc {
     int32_t batch, heads_q, heads_kv, head_dim;

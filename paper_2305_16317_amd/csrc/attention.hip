@@ -22,10 +22,15 @@
 // score 12 cycles of vector operations and 8 for its exponential, and within a wave
 // nothing overlaps a product, so two waves a SIMD from different blocks fill it
 // between them.  Measured (bfloat16): 8192 tokens two-sided, 32 heads on 8 of 128 values,
-// 1058 us (1039 TFLOP/s; a large library product reaches 1247), of 64 values 563 us
-// (977); with a window of 2048 and sinks, where tiles end outside the window and a block
-// has 34 of them, 285 us (846); 64 sequences of 576 tokens of 64 values, nine tiles a block,
-// 134 us (649): there a third of the time is reading queries and writing results.
+// 1063 us (1034 TFLOP/s; a large library product reaches 1247), of 64 values 567 us
+// (970); with a window of 2048 and sinks, where tiles end outside the window and a block
+// has 34 of them, 277 us (868); 64 sequences of 576 tokens of 64 values, nine tiles a block,
+// 132 us (661): there a third of the time is reading queries and writing results.
+//
+// bfloat16 rounds a probability once more, as the matrix instruction's operand (the sum
+// takes it unrounded): relative to itself, so the result's error is 2.3e-3 where the
+// result's own rounding alone makes 1.7e-3.  Two parts would take half as many products
+// again.
 #include "attention_tile.h"
 
 namespace pd {
@@ -401,8 +406,8 @@ __global__ __launch_bounds__(256, 2) void k_attention(const AttentionArgs a, con
 // The same for float32, in three parts: a tile is read into registers while the one
 // before is worked on, and split on its way to LDS, once for the block's four waves.
 // (Heads of over 96 values: one block a compute unit, since for two 33 registers spill:
-// 266 us, 357.)  Measured: 2 x 2048 tokens causal, 16 heads on 4: 64 values 137 us, 96 values
-// 202 us, 128 values 266 us, where float32 products took 213, 313 and 570.
+// 278 us, 357.)  Measured: 2 x 2048 tokens causal, 16 heads on 4: 64 values 138 us, 96 values
+// 210 us, 128 values 278 us, where float32 products took 213, 313 and 570.
 template <int DP>
 __global__ __launch_bounds__(256, (DP <= 96 ? 2 : 1)) void k_attention_parts(const AttentionArgs a, const Plan p) {
     constexpr int BN = tile_rows<float, DP>(), BM = 128;

@@ -6,16 +6,20 @@
 //
 // Two kernels, each summing into its own registers: dq over a block of queries
 // (which also leaves delta, and what rows with large scores take them from, for the
-// other), dk and dv over a block of keys and the query heads that read them.  The scores are formed twice (14 D operations a pair
-// and head in place of 10), and in exchange there is no atomic and no order that
-// varies from run to run.  Where there are few blocks of keys, their queries are
-// split among several blocks, whose sums k_attention_dkv_join adds.
+// other), dk and dv over a block of keys and the query heads that read them.  The scores
+// are formed twice (14 D operations a pair and head in place of 10), and in exchange there
+// is no atomic and no order that varies from run to run.  Where there are few blocks of
+// keys, their queries are split among several blocks, whose sums k_attention_dkv_join adds.
 //
 // Bound by the chain of LDS reads, products and vector work of a wave (two waves a SIMD):
 // hence reads a group ahead (Stream) and sums that start from -lse / scale and -delta.
-// Measured: 4 x 2304 tokens two-sided, 16 heads on 4 of 64 bfloat16 values 388 us (560
-// TFLOP/s of the 10 D operations, 783 of the 14 D it does): dq 170, dk and dv 200, join 18;
-// float32, 2 x 2048 tokens causal: 64 values 412 us, 128 values 1053 us.
+// Measured: 4 x 2304 tokens two-sided, 16 heads on 4 of 64 bfloat16 values 373 us (583
+// TFLOP/s of the 10 D operations, 816 of the 14 D it does; profiled, at lower clocks: dq
+// 158, dk and dv 217, join 21); float32, 2 x 2048 tokens causal: 64 values 407 us, 128
+// values 970 to 1030.
+//
+// bfloat16 rounds p and ds once more, as operands: errors of 2.4e-3 where the results'
+// own rounding alone makes 1.7e-3.
 #include "attention_tile.h"
 
 namespace pd {
@@ -844,9 +848,12 @@ __global__ __launch_bounds__(256, 8) void k_attention_dkv_join(const AttentionAr
         }
 }
 
-// Parts of the dk, dv kernel's queries, of at least four tiles: the fewest that keep its
-// blocks at work for nine tenths of the time (512 run at once: 288 blocks in 4 parts
-// are 2.25 rounds of them, in 5 parts 2.8), or the best up to eight.
+// Parts of the dk, dv kernel's queries, of at least four tiles where no window leaves some
+// out: the fewest that keep its blocks at work for nine tenths of the time (512 run at
+// once: 288 blocks in 4 parts are 2.25 rounds of them, in 5 parts 2.8), or the best up to
+// eight.  All blocks are cut alike, as suits blocks of like length.  With a window and sinks
+// they are not: the block that holds a sink goes through all queries, the others through
+// 128 and the window (8192 tokens, window 1024, 16 heads on 4: 176 us, with four sinks 682).
 int dkv_splits(const pd_attention_desc& d) {
     const int64_t blocks = ((int64_t)d.kv_len + 127) / 128 * d.heads_kv * d.batch;
     const int64_t most = ((int64_t)d.q_len + 63) / 64 * (d.heads_q / d.heads_kv) / 4;
