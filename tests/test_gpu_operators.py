@@ -503,12 +503,12 @@ def test_attention_backward_of_scores_near_the_types_end(n, m, dtype):
     _close(dv, ot.attention_grad(_np(q), _np(k), _np(v), _np(g), 0.125, True)[2], TOL_GRAD[dtype])
 
 
-def _grad_bounds(q, k, v, g, out, scale, causal, u, window=0, sinks=0):
+def _grad_bounds(q, k, v, g, out, scale, causal, u, window=0, sinks=0, q_lens=None, kv_lens=None):
     """What roundings can add to dq, dk and dv when each of a pair's terms (p, dout v, dout out and their
     product) is off by u of the sizes that it is summed from."""
     q, k, v, g, out = (np.abs(_np(x)) if x is not q and x is not k else _np(x) for x in (q, k, v, g, out))
     dq, dk, dv = np.zeros(q.shape), np.zeros(k.shape), np.zeros(v.shape)
-    for b, i, h, e, j in ot._each(q, k, None, None, causal, window, sinks):
+    for b, i, h, e, j in ot._each(q, k, q_lens, kv_lens, causal, window, sinks):
         x = scale * (k[b, j, e] @ q[b, i, h])
         p = np.exp(x - np.max(x))
         p /= p.sum()
@@ -554,6 +554,35 @@ def test_attention_backward_of_keys_beside_the_largest(n, m, causal, size, dtype
         pd.pd_attention_backward(q, k, v, out, lse, g, *grads, **kw)
         x[0, at] = kept
         check(which, clean)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("size", [2.0**11, 2.0**20])
+@pytest.mark.parametrize("B,n,m,H,K,D,causal,window,sinks,ql,kl,layout", [
+    (2, 70, 90, 6, 2, 128, True, 30, 4, None, [90, 40], "head"), (1, 130, 130, 4, 4, 96, False, 20, 3, None, None, "token"),
+    (3, 33, 65, 2, 1, 20, True, 0, 0, [33, 5, 0], None, "token"), (1, 300, 300, 8, 2, 32, True, 0, 0, None, None, "token"),
+    (2, 40, 200, 4, 1, 36, True, 0, 0, None, [200, 0], "odd"), (1, 1, 400, 8, 1, 128, True, 100, 7, None, None, "head")])
+def test_attention_backward_of_large_scores(B, n, m, H, K, D, causal, window, sinks, ql, kl, layout, size, dtype):
+    """Two rows of three have scores of `size` and a small whole number each, which every sum forms exactly; the third's
+    are small.  Bounds as in the test of keys beside the largest."""
+    print("large scores", B, n, m, H, K, D, causal, window, sinks, size, dtype, flush=True)
+    q, k, v, g = _att_inputs(B, n, m, H, K, D, dtype, 47, layout)
+    r = torch.Generator(device="cuda").manual_seed(48)
+    for x in (q, k):
+        x.copy_(torch.randint(-1, 2, x.shape, device="cuda", generator=r))
+    q[..., 0] = (size * (torch.arange(n, device="cuda") % 3 > 0))[None, :, None].to(dtype)
+    k[..., 0] = 1.0
+    refs = ot.attention_grad(_np(q), _np(k), _np(v), _np(g), 1.0, causal, window, sinks, ql, kl)
+    kw = dict(causal=causal, scale=1.0, window=window, sinks=sinks, q_lens=_lens(ql), kv_lens=_lens(kl))
+    out, lse = torch.empty(q.shape, device="cuda", dtype=dtype), torch.empty((B, H, n), device="cuda")
+    grads = [torch.full(x.shape, 7.0, device="cuda", dtype=dtype) for x in (q, k, v)]
+    pd.pd_attention_forward(q, k, v, out, lse=lse, **kw)
+    pd.pd_attention_backward(q, k, v, out, lse, g, *grads, **kw)
+    u = 2.0**-8 if dtype == BF16 else 2.0**-15
+    bounds = _grad_bounds(q, k, v, g, out, 1.0, causal, u, window, sinks, ql, kl)
+    for name, got, ref, bound in zip(("dq", "dk", "dv"), grads, refs, bounds):
+        off = np.abs(_np(got) - ref)
+        assert np.all(off <= bound + u * np.abs(ref)), (name, np.max(off / (bound + u * np.abs(ref) + 1e-300)))
 
 
 def test_attention_cache_offsets_past_32_bits():
@@ -765,3 +794,34 @@ def test_operators_on_another_stream_and_in_a_graph(n, dtype):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want), i
+
+
+@pytest.mark.parametrize("D,dtype", [(64, BF16), (128, BF16), (128, F32)])
+def test_gradients_in_a_graph(D, dtype):
+    """The backward calls captured and replayed with other gradients, among them rows with large scores."""
+    q, k, v, g = _att_inputs(2, 150, 150, 4, 2, D, dtype, 60)
+    q[:, 100:] *= 4096
+    out, lse = torch.empty_like(q), torch.empty((2, 4, 150), device="cuda")
+    grads = [torch.empty_like(x) for x in (q, k, v)]
+    kw = dict(window=90, sinks=3)
+    pd.pd_attention_forward(q, k, v, out, lse=lse, **kw)
+    assert float(lse.abs().max()) > 2048
+    w, dw, rstd = _rand((4 * D,), F32, 61), torch.empty(4 * D, device="cuda"), _rand((300,), F32, 62).abs()
+    dx = torch.empty((300, 4 * D), device="cuda", dtype=dtype)
+
+    def go():
+        pd.pd_attention_backward(q, k, v, out, lse, g, *grads, **kw)
+        pd.pd_rmsnorm_backward(grads[0].view(300, -1), q.view(300, -1), w, rstd, dx, dw)
+    go()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        go()
+    for i in range(4):
+        g.copy_(_rand(g.shape, dtype, 70 + i))
+        go()
+        want = [x.clone() for x in (*grads, dx, dw)]
+        for x in (*grads, dx, dw):
+            x.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip((*grads, dx, dw), want)), i
