@@ -462,6 +462,143 @@ pd_status pd_attention_backward(const pd_attention_desc* desc, const void* q, co
                                 const int32_t* q_lens, const int32_t* kv_lens, void* dq, void* dk,
                                 void* dv, void* scratch, int64_t scratch_bytes, void* stream);
 
+/* Layer norm with the residual's addition, and a weight and bias for each run of `span`
+ * rows (a sequence whose timestep modulates them; span 0: all rows share one).  Per row of
+ * `width`, with g = row / span:
+ *   s = x + residual (float32, not rounded),  mean = mean(s),
+ *   rstd = 1 / sqrt(mean((s - mean)^2) + eps),  n = (s - mean) rstd,
+ *   sum = s rounded to dtype,  y = n weight_g + bias_g rounded to dtype.
+ * weight, bias: float, row g at g * their stride (0: all runs share one); NULL: ones, zeros.
+ * residual, sum, mean, rstd may be NULL.  sum and y may be x or residual themselves, with
+ * the same stride.  mean, rstd: float [rows].
+ * span divides rows; 1 <= width <= 65536.
+ * Backward, with sum, mean and rstd as the forward pass left them, n = (sum - mean) rstd:
+ *   a = dy weight_g,  dx = dsum + rstd (a - mean(a) - n mean(a n)),
+ *   dweight_g = sum over the run's rows of dy n,  dbias_g = the same of dy.
+ * dx is the gradient of x and of residual alike; dsum (NULL: 0) is the gradient that
+ * reaches `sum` from elsewhere.  dx may be dy or dsum (same stride).  dweight, dbias: float
+ * [rows / span][width] ([width] with span 0; then zeros where there are no rows), or NULL.
+ * Strides: dy as y, dsum as residual, dx as x. */
+typedef struct pd_layernorm_desc {
+    int64_t rows;
+    int64_t width;
+    int64_t span;
+    int64_t x_stride, residual_stride, sum_stride, y_stride;   /* from row to row */
+    int64_t weight_stride, bias_stride;                        /* from run to run */
+    int32_t dtype;
+    float eps;                 /* >= 0 */
+} pd_layernorm_desc;
+pd_status pd_layernorm_forward(const pd_layernorm_desc* desc, const void* x, const void* residual,
+                               const float* weight, const float* bias, void* sum, void* y, float* mean,
+                               float* rstd, void* stream);
+pd_status pd_layernorm_backward_scratch(const pd_layernorm_desc* desc, int64_t* bytes);
+pd_status pd_layernorm_backward(const pd_layernorm_desc* desc, const void* dy, const void* sum,
+                                const float* weight, const float* mean, const float* rstd, const void* dsum,
+                                void* dx, float* dweight, float* dbias, void* scratch, int64_t scratch_bytes,
+                                void* stream);
+
+/* Rotary positions over up to four axes (time, height, width of a video's patches): a
+ * token has a position on each, and pair k of a head turns by that of the axis which it
+ * belongs to, as pd_rotary_apply turns it by the token's one position.  sections[a] pairs
+ * belong to axis a; they add up to rotary_dim / 2.
+ *   PD_AXES_RUNS   axis 0's pairs first, then axis 1's, ...;
+ *   PD_AXES_TURNS  the axes take the next pair in turn, those that have some left.
+ * pd_rotary_axes_table fills rows [first, first + rows) of a table of (cos, sin), float
+ * [rows][rotary_dim/2][2], formed in double and rounded once: row p holds p f_k,
+ *   f_k = scale_a base_a^(-i / sections[a]) for the i-th pair of axis a, or with
+ *   `shared` scale_a base_a^(-k / (rotary_dim/2)), one ladder through all axes.
+ * pd_rotary_axes_apply: positions int32, token i of sequence b on axis a at
+ * b * position_stride[0] + i * position_stride[1] + a * position_stride[2]; one outside
+ * [0, table_rows) is clamped to it.  The rest is as for pd_rotary_apply (whose desc's
+ * position_stride is not used). */
+#define PD_AXES_RUNS 0
+#define PD_AXES_TURNS 1
+typedef struct pd_rotary_axes_table_desc {
+    int32_t rotary_dim;        /* even, 2..1024                                  */
+    int32_t axes;              /* 1..4                                           */
+    int32_t order;             /* PD_AXES_RUNS or PD_AXES_TURNS                  */
+    int32_t shared;
+    int32_t sections[4];       /* >= 0                                           */
+    double base[4];            /* > 1                                            */
+    double scale[4];           /* finite                                         */
+} pd_rotary_axes_table_desc;
+pd_status pd_rotary_axes_table(const pd_rotary_axes_table_desc* desc, int64_t first, int64_t rows, float* table,
+                               void* stream);
+typedef struct pd_rotary_axes_desc {
+    pd_rotary_desc rotary;
+    int32_t axes, order;
+    int32_t sections[4];
+    int64_t position_stride[3];
+} pd_rotary_axes_desc;
+pd_status pd_rotary_axes_apply(const pd_rotary_axes_desc* desc, const void* q, const void* k,
+                               const int32_t* positions, const float* table, void* q_out, void* k_out,
+                               void* stream);
+
+/* Dropout with the residual's addition:
+ *   y = residual + (kept ? x / (1 - p') : 0),  p' = t / 65536, t = floor(65536 p + 1/2).
+ * The mask comes from Philox4x32-10 under the key `seed`: values 8 i .. 8 i + 7 of row r
+ * share the counter (q mod 2^32, q / 2^32, rng_stream, step + 1), q = r ceil(width / 8) + i;
+ * value 8 i + e is kept where the e-th 16 bits of its four words (low halves first) are
+ * not under t.  So it depends on nothing but the seed, the numbers and the place, and the
+ * gradient of x is the same call on dy without a residual.  Rows count from first_row, for
+ * a call on part of them.  step_more (device uint32, or NULL) is added to step: a captured
+ * call draws another mask at each replay when the program counts it up between them.  (The
+ * counters' last word is 0 for pd_normals, and step + 1 is not while the steps are fewer
+ * than 2^32 - 1.)
+ * A dropped value is not read: infinity and NaN give 0 too.  residual may be NULL; y may be
+ * x or residual, with the same stride. */
+typedef struct pd_dropout_desc {
+    int64_t rows, width;       /* width 1..2^31 - 1 */
+    int64_t first_row;         /* >= 0 */
+    int64_t x_stride, residual_stride, y_stride;
+    uint64_t seed;
+    double p;                  /* 0..1 */
+    uint32_t rng_stream, step;
+    int32_t dtype;
+} pd_dropout_desc;
+pd_status pd_dropout_apply(const pd_dropout_desc* desc, const void* x, const void* residual,
+                           const uint32_t* step_more, void* y, void* stream);
+
+/* The gated product of a feed-forward block:
+ *   gate = x w_gate,  up = x w_up,  h = act(gate) up,
+ * x [rows][width], w_gate and w_up [width][hidden] (PD_WEIGHTS_IN_OUT) or [hidden][width]
+ * (PD_WEIGHTS_OUT_IN), all of dtype.  h is formed from the unrounded float32 sums; gate and
+ * up (NULL: not stored) are the same sums rounded to dtype, for the backward pass.
+ *   PD_ACT_SILU g / (1 + e^-g);  PD_ACT_GELU g (1 + erf(g / sqrt 2)) / 2;
+ *   PD_ACT_GELU_TANH g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2;
+ *   PD_ACT_SIGMOID 1 / (1 + e^-g);  PD_ACT_RELU max(g, 0).
+ * Backward, from gate and up as stored and the gradient dh:
+ *   dgate = dh up act'(gate),  dup = dh act(gate),
+ *   dx = dgate w_gate^T + dup w_up^T,  dw_gate = x^T dgate,  dw_up = x^T dup,
+ * dw_gate and dw_up in the weights' layout and type (zeros where there are no rows).  dx, the
+ * pair dw_gate and dw_up, and h (act(gate) up, formed again) may be NULL: not formed.
+ * In PD_F32 operands are the sums of three bfloat16 parts (24 bits; a value under 2^-110
+ * keeps fewer) with products to 2^-24, as in attention; an infinity among them gives NaN.  In
+ * PD_BF16 dgate and dup are rounded to bfloat16 as operands of the matrix cores.  Sums are
+ * float32.  relu'(0) = 0.
+ * 1 <= width, hidden <= 2^20; rows <= 2^24 (more: PD_ERR_UNSUPPORTED). */
+#define PD_ACT_SILU 0
+#define PD_ACT_GELU 1
+#define PD_ACT_GELU_TANH 2
+#define PD_ACT_SIGMOID 3
+#define PD_ACT_RELU 4
+#define PD_WEIGHTS_IN_OUT 0
+#define PD_WEIGHTS_OUT_IN 1
+typedef struct pd_gated_desc {
+    int64_t rows;
+    int32_t width, hidden;
+    int32_t dtype, activation, weight_layout;
+    int64_t x_stride, w_gate_stride, w_up_stride, gate_stride, up_stride, h_stride;   /* from row to row */
+    int64_t dh_stride, dx_stride, dw_gate_stride, dw_up_stride;                       /* backward only */
+} pd_gated_desc;
+pd_status pd_gated_forward_scratch(const pd_gated_desc* desc, int64_t* bytes);
+pd_status pd_gated_forward(const pd_gated_desc* desc, const void* x, const void* w_gate, const void* w_up,
+                           void* gate, void* up, void* h, void* scratch, int64_t scratch_bytes, void* stream);
+pd_status pd_gated_backward_scratch(const pd_gated_desc* desc, int64_t* bytes);
+pd_status pd_gated_backward(const pd_gated_desc* desc, const void* x, const void* w_gate, const void* w_up,
+                            const void* gate, const void* up, const void* dh, void* h, void* dx, void* dw_gate,
+                            void* dw_up, void* scratch, int64_t scratch_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -30,6 +30,11 @@ __all__ = [
     "pd_attention_forward", "pd_attention_backward",
     "PD_F8E4M3", "PD_ROTARY_HALF", "PD_ROTARY_INTERLEAVED",
     "PD_ROTARY_PLAIN", "PD_ROTARY_LINEAR", "PD_ROTARY_BASE", "PD_ROTARY_BY_PARTS",
+    "pd_layernorm_forward", "pd_layernorm_backward", "pd_rotary_axes_table", "pd_rotary_axes_apply",
+    "pd_dropout_apply", "pd_gated_forward", "pd_gated_backward",
+    "PD_AXES_RUNS", "PD_AXES_TURNS",
+    "PD_ACT_SILU", "PD_ACT_GELU", "PD_ACT_GELU_TANH", "PD_ACT_SIGMOID", "PD_ACT_RELU",
+    "PD_WEIGHTS_IN_OUT", "PD_WEIGHTS_OUT_IN",
 ]
 
 PD_OK, PD_ERR_INVALID_ARG, PD_ERR_OOM, PD_ERR_DEVICE, PD_ERR_NUMERIC, PD_ERR_UNSUPPORTED = range(6)
@@ -41,6 +46,9 @@ STOP_RULES = {"relaxed": PD_STOP_RELAXED, "prop2": PD_STOP_PROP2}
 PD_MODEL_GMM2D, PD_MODEL_MLP, PD_MODEL_CONV1X1 = 0, 1, 2
 PD_F32, PD_BF16, PD_F8E4M3 = 0, 1, 2
 PD_ROTARY_HALF, PD_ROTARY_INTERLEAVED = 0, 1
+PD_AXES_RUNS, PD_AXES_TURNS = 0, 1
+PD_ACT_SILU, PD_ACT_GELU, PD_ACT_GELU_TANH, PD_ACT_SIGMOID, PD_ACT_RELU = range(5)
+PD_WEIGHTS_IN_OUT, PD_WEIGHTS_OUT_IN = 0, 1
 PD_ROTARY_PLAIN, PD_ROTARY_LINEAR, PD_ROTARY_BASE, PD_ROTARY_BY_PARTS = 0, 1, 2, 3
 
 EXPORTED_SYMBOLS = [
@@ -53,6 +61,9 @@ EXPORTED_SYMBOLS = [
     "pd_rotary_table", "pd_rotary_apply",
     "pd_attention_forward_scratch", "pd_attention_forward",
     "pd_attention_backward_scratch", "pd_attention_backward",
+    "pd_layernorm_forward", "pd_layernorm_backward_scratch", "pd_layernorm_backward",
+    "pd_rotary_axes_table", "pd_rotary_axes_apply", "pd_dropout_apply",
+    "pd_gated_forward_scratch", "pd_gated_forward", "pd_gated_backward_scratch", "pd_gated_backward",
 ]
 
 
@@ -122,10 +133,52 @@ class _AttentionDesc(ctypes.Structure):
                 ("dout_stride", _I64x3)]
 
 
-# the same three as bytes: the calls pack them (a Structure with its arrays takes 2 us more)
+class _LayernormDesc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("width", ctypes.c_int64), ("span", ctypes.c_int64),
+                ("x_stride", ctypes.c_int64), ("residual_stride", ctypes.c_int64),
+                ("sum_stride", ctypes.c_int64), ("y_stride", ctypes.c_int64),
+                ("weight_stride", ctypes.c_int64), ("bias_stride", ctypes.c_int64),
+                ("dtype", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+
+class _RotaryAxesTableDesc(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("axes", ctypes.c_int32), ("order", ctypes.c_int32),
+                ("shared", ctypes.c_int32), ("sections", ctypes.c_int32 * 4),
+                ("base", ctypes.c_double * 4), ("scale", ctypes.c_double * 4)]
+
+
+class _RotaryAxesDesc(ctypes.Structure):
+    _fields_ = [("rotary", _RotaryDesc), ("axes", ctypes.c_int32), ("order", ctypes.c_int32),
+                ("sections", ctypes.c_int32 * 4), ("position_stride", _I64x3)]
+
+
+class _DropoutDesc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("width", ctypes.c_int64), ("first_row", ctypes.c_int64),
+                ("x_stride", ctypes.c_int64), ("residual_stride", ctypes.c_int64),
+                ("y_stride", ctypes.c_int64), ("seed", ctypes.c_uint64),
+                ("p", ctypes.c_double), ("rng_stream", ctypes.c_uint32), ("step", ctypes.c_uint32),
+                ("dtype", ctypes.c_int32)]
+
+
+class _GatedDesc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("width", ctypes.c_int32), ("hidden", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("activation", ctypes.c_int32),
+                ("weight_layout", ctypes.c_int32), ("x_stride", ctypes.c_int64),
+                ("w_gate_stride", ctypes.c_int64), ("w_up_stride", ctypes.c_int64),
+                ("gate_stride", ctypes.c_int64), ("up_stride", ctypes.c_int64),
+                ("h_stride", ctypes.c_int64), ("dh_stride", ctypes.c_int64),
+                ("dx_stride", ctypes.c_int64), ("dw_gate_stride", ctypes.c_int64),
+                ("dw_up_stride", ctypes.c_int64)]
+
+
+# the operators' descriptions as bytes: the calls pack them (a Structure with its arrays takes 2 us more)
 _RMSNORM_BYTES = struct.Struct("6q3if")
 _ROTARY_BYTES = struct.Struct("2q7i14q")
 _ATTENTION_BYTES = struct.Struct("10if24q")
+_LAYERNORM_BYTES = struct.Struct("9qif")
+_ROTARY_AXES_BYTES = struct.Struct("2q7i14q6i3q")
+_DROPOUT_BYTES = struct.Struct("6qQd2Ii4x")
+_GATED_BYTES = struct.Struct("q5i10q")
 
 _LIB: Optional[ctypes.CDLL] = None
 
@@ -171,6 +224,16 @@ def load() -> ctypes.CDLL:
         "pd_attention_forward": ([vp] + [vp] * 8 + [i64, vp], i32),
         "pd_attention_backward_scratch": ([vp, P(i64)], i32),
         "pd_attention_backward": ([vp] + [vp] * 12 + [i64, vp], i32),
+        "pd_layernorm_forward": ([vp] + [vp] * 9, i32),
+        "pd_layernorm_backward_scratch": ([vp, P(i64)], i32),
+        "pd_layernorm_backward": ([vp] + [vp] * 10 + [i64, vp], i32),
+        "pd_rotary_axes_table": ([P(_RotaryAxesTableDesc), i64, i64, vp, vp], i32),
+        "pd_rotary_axes_apply": ([vp] + [vp] * 7, i32),
+        "pd_dropout_apply": ([vp] + [vp] * 5, i32),
+        "pd_gated_forward_scratch": ([vp, P(i64)], i32),
+        "pd_gated_forward": ([vp] + [vp] * 7 + [i64, vp], i32),
+        "pd_gated_backward_scratch": ([vp, P(i64)], i32),
+        "pd_gated_backward": ([vp] + [vp] * 11 + [i64, vp], i32),
     }
     for name, (args, res) in sig.items():
         fn = getattr(L, name)
@@ -654,6 +717,275 @@ def pd_attention_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out
     _check(L.pd_attention_backward(d, _ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(lse),
                                    _ptr(dout), _ptr(q_lens), _ptr(kv_lens), _ptr(dq), _ptr(dk),
                                    _ptr(dv), _ptr(buf), have, _stream(stream)))
+
+
+def _runs(t: Optional[torch.Tensor], rows: int, width: int, what: str):
+    """(runs, elements from run to run) of a weight (width,) or (runs, width); runs 0: shared."""
+    if t is None:
+        return 0, 0
+    if t.dtype != torch.float32 or t.dim() not in (1, 2) or t.shape[-1] != width or (width > 1 and t.stride(-1) != 1):
+        raise ValueError(f"{what} must be float32 of shape ({width},) or (runs, {width}), its last dimension contiguous")
+    if t.dim() == 1:
+        return 0, 0
+    n = t.shape[0]
+    if n == 0 or rows % n:
+        raise ValueError(f"{what}: {n} runs do not divide {rows} rows")
+    return n, t.stride(0)
+
+
+def _span(rows: int, *runs: int) -> int:
+    """Rows of a run, from how many runs each weight has (0: shared)."""
+    some = {n for n in runs if n}
+    if len(some) > 1:
+        raise ValueError(f"weight and bias must have the same number of runs, got {sorted(some)}")
+    return rows // some.pop() if some else 0
+
+
+def _of_each_row(t: Optional[torch.Tensor], rows: int, what: str) -> None:
+    if t is not None and (t.dtype != torch.float32 or not t.is_contiguous() or t.numel() != rows):
+        raise ValueError(f"{what} must be contiguous float32 of {rows} elements")
+
+
+def pd_layernorm_forward(x: torch.Tensor, y: torch.Tensor, weight: Optional[torch.Tensor] = None,
+                         bias: Optional[torch.Tensor] = None,
+                         residual: Optional[torch.Tensor] = None,
+                         sum_out: Optional[torch.Tensor] = None,
+                         mean: Optional[torch.Tensor] = None,
+                         rstd: Optional[torch.Tensor] = None, eps: float = 1e-6, stream=None) -> None:
+    """y = layer norm of (x + residual) over the last dimension, times weight, plus bias.  weight and
+    bias: float32 (width,), or (runs, width) for as many runs of rows of equal length (a modulated
+    sequence each).  sum_out: x + residual; mean, rstd: of each row."""
+    dt, sh = _dtype(x), x.shape
+    _on_gpu(x, y, weight, bias, residual, sum_out, mean, rstd)
+    width = sh[-1] if x.dim() else 0
+    if not width:
+        raise ValueError("x must have a last dimension of at least 1")
+    rows = x.numel() // width
+    wn, ws = _runs(weight, rows, width, "weight")
+    bn, bs = _runs(bias, rows, width, "bias")
+    _of_each_row(mean, rows, "mean")
+    _of_each_row(rstd, rows, "rstd")
+    _written(y, "y")
+    if sum_out is not None:
+        _written(sum_out, "sum_out")
+    d = _pack(_LAYERNORM_BYTES, rows, width, _span(rows, wn, bn), _rows_of(x, sh, x.dtype, "x"),
+              _rows_of(residual, sh, x.dtype, "residual") if residual is not None else 0,
+              _rows_of(sum_out, sh, x.dtype, "sum_out") if sum_out is not None else 0,
+              _rows_of(y, sh, x.dtype, "y"), ws, bs, dt, eps)
+    _check(load().pd_layernorm_forward(d, _ptr(x), _ptr(residual), _ptr(weight), _ptr(bias), _ptr(sum_out),
+                                       _ptr(y), _ptr(mean), _ptr(rstd), _stream(stream)))
+
+
+def pd_layernorm_backward(dy: torch.Tensor, sum_in: torch.Tensor, mean: torch.Tensor,
+                          rstd: torch.Tensor, dx: torch.Tensor,
+                          weight: Optional[torch.Tensor] = None,
+                          dweight: Optional[torch.Tensor] = None,
+                          dbias: Optional[torch.Tensor] = None,
+                          dsum: Optional[torch.Tensor] = None,
+                          scratch: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Gradients of pd_layernorm_forward from its sum_out (sum_in), mean and rstd: dx (of x and of
+    residual), dweight and dbias (contiguous, (width,) or (runs, width) alike).  dsum: the gradient that
+    reaches sum_out from elsewhere."""
+    dt, sh = _dtype(dy), dy.shape
+    _on_gpu(dy, sum_in, mean, rstd, dx, weight, dweight, dbias, dsum, scratch)
+    width = sh[-1] if dy.dim() else 0
+    if not width:
+        raise ValueError("dy must have a last dimension of at least 1")
+    rows = dy.numel() // width
+    wn, ws = _runs(weight, rows, width, "weight")
+    runs = []
+    for t, what in ((dweight, "dweight"), (dbias, "dbias")):
+        if t is not None:
+            if not t.is_contiguous():
+                raise ValueError(f"{what} must be contiguous")
+            runs.append(_runs(t, rows, width, what)[0])
+    if len(set(runs)) > 1 or (runs and wn and not runs[0]):
+        raise ValueError("dweight and dbias must have the runs of weight")
+    _of_each_row(mean, rows, "mean")
+    _of_each_row(rstd, rows, "rstd")
+    _written(dx, "dx")
+    d = _pack(_LAYERNORM_BYTES, rows, width, _span(rows, wn, *runs), _rows_of(dx, sh, dy.dtype, "dx"),
+              _rows_of(dsum, sh, dy.dtype, "dsum") if dsum is not None else 0,
+              _rows_of(sum_in, sh, dy.dtype, "sum_in"), _rows_of(dy, sh, dy.dtype, "dy"), ws, 0, dt, 0.0)
+    L, need = load(), ctypes.c_int64(0)
+    if scratch is None and runs:
+        _check(L.pd_layernorm_backward_scratch(d, ctypes.byref(need)))
+    buf, have = _scratch(scratch, need.value, stream)
+    _check(L.pd_layernorm_backward(d, _ptr(dy), _ptr(sum_in), _ptr(weight), _ptr(mean), _ptr(rstd), _ptr(dsum),
+                                   _ptr(dx), _ptr(dweight), _ptr(dbias), _ptr(buf), have, _stream(stream)))
+
+
+def _sections(sections: Sequence[int]) -> List[int]:
+    s = [int(v) for v in sections]
+    if not 1 <= len(s) <= 4:
+        raise ValueError("sections must name the pairs of one to four axes")
+    return s
+
+
+def pd_rotary_axes_table(table: torch.Tensor, sections: Sequence[int], base=10000.0, scale=1.0,
+                         order: int = PD_AXES_RUNS, shared: bool = False, first: int = 0,
+                         stream=None) -> None:
+    """Fill table [positions, rotary_dim / 2, 2] with cos and sin from position `first` on, for axes of
+    sections[a] pairs.  base and scale: one for all axes, or one each; shared: one ladder of frequencies
+    through all pairs."""
+    _on_gpu(table)
+    if table.dtype != torch.float32 or table.dim() != 3 or table.shape[2] != 2 or not table.is_contiguous():
+        raise ValueError("table must be contiguous float32 of shape (positions, rotary_dim / 2, 2)")
+    s = _sections(sections)
+
+    def each(v, what):
+        v = [float(v)] * len(s) if isinstance(v, (int, float)) else [float(e) for e in v]
+        if len(v) != len(s):
+            raise ValueError(f"{what} must be one number, or one for each axis")
+        return (ctypes.c_double * 4)(*v)
+    d = _RotaryAxesTableDesc(2 * table.shape[1], len(s), order, int(bool(shared)), (ctypes.c_int32 * 4)(*s),
+                             each(base, "base"), each(scale, "scale"))
+    _check(load().pd_rotary_axes_table(ctypes.byref(d), first, table.shape[0], _ptr(table), _stream(stream)))
+
+
+def pd_rotary_axes_apply(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Tensor,
+                         table: torch.Tensor, sections: Sequence[int], q_out: torch.Tensor,
+                         k_out: Optional[torch.Tensor] = None, layout: int = PD_ROTARY_HALF,
+                         order: int = PD_AXES_RUNS, backward: bool = False, stream=None) -> None:
+    """Turn q and k [batch, token, head, dim], sections[a] pairs of each head by the table's rows at the
+    positions on axis a ([token, axis] or [batch, token, axis], int32, any strides)."""
+    dt = _dtype(q)
+    _on_gpu(q, k, positions, table, q_out, k_out)
+    if q.dim() != 4 or (k is None) != (k_out is None):
+        raise ValueError("q must be (batch, token, head, dim), and k_out goes with k")
+    B, n, H, D = q.shape
+    s = _sections(sections)
+    axes = len(s)
+    if table.dtype != torch.float32 or table.dim() != 3 or table.shape[2] != 2 or not table.is_contiguous():
+        raise ValueError("table must be contiguous float32 of shape (positions, rotary_dim / 2, 2)")
+    shape = tuple(positions.shape)
+    if positions.dtype != torch.int32 or shape not in ((n, axes), (B, n, axes)):
+        raise ValueError("positions must be int32 of shape (token, axis) or (batch, token, axis)")
+    at = positions.stride()
+    if len(at) == 2:
+        at = (0, *at)
+    K = 0
+    if k is not None:
+        if k.dim() != 4:
+            raise ValueError("k must be (batch, token, head, dim)")
+        K = k.shape[2]
+        _written(k_out, "k_out")
+    _written(q_out, "q_out")
+    ks = (B, n, K, D)
+    d = _pack(_ROTARY_AXES_BYTES, B, n, H, K, D, 2 * table.shape[1], layout, dt, bool(backward), table.shape[0], 0,
+              *_strides(q, q.shape, q.dtype, "q"), *(_strides(k, ks, q.dtype, "k") if K else _NO_STRIDES),
+              *_strides(q_out, q.shape, q.dtype, "q_out"),
+              *(_strides(k_out, ks, q.dtype, "k_out") if K else _NO_STRIDES),
+              axes, order, *s, *([0] * (4 - axes)), *at)
+    _check(load().pd_rotary_axes_apply(d, _ptr(q), _ptr(k), _ptr(positions), _ptr(table), _ptr(q_out),
+                                       _ptr(k_out), _stream(stream)))
+
+
+def pd_dropout_apply(x: torch.Tensor, y: torch.Tensor, p: float, seed: int, rng_stream: int = 0,
+                     step: int = 0, step_more: Optional[torch.Tensor] = None,
+                     residual: Optional[torch.Tensor] = None, first_row: int = 0, stream=None) -> None:
+    """y = residual + dropout(x): each value is dropped with probability p (in steps of 2^-16), the others
+    are divided by 1 - p.  The mask follows from seed, rng_stream (which dropout of a model), step and the
+    place alone; dx is the same call on dy.  step_more: an int32 tensor of one element, added to step when
+    the kernel runs.  first_row: number of x's first row, for a call on part of the rows."""
+    dt, sh = _dtype(x), x.shape
+    _on_gpu(x, y, step_more, residual)
+    width = sh[-1] if x.dim() else 0
+    if not width:
+        raise ValueError("x must have a last dimension of at least 1")
+    if step_more is not None and (step_more.dtype != torch.int32 or step_more.numel() != 1):
+        raise ValueError("step_more must be int32 of one element")
+    _written(y, "y")
+    d = _pack(_DROPOUT_BYTES, x.numel() // width, width, first_row, _rows_of(x, sh, x.dtype, "x"),
+              _rows_of(residual, sh, x.dtype, "residual") if residual is not None else 0,
+              _rows_of(y, sh, x.dtype, "y"), seed, p, rng_stream, step, dt)
+    _check(load().pd_dropout_apply(d, _ptr(x), _ptr(residual), _ptr(step_more), _ptr(y), _stream(stream)))
+
+
+def _weight_layout(w_gate: torch.Tensor, w_up: torch.Tensor, width: int, dtype) -> int:
+    """How the weights, seen as (width, hidden), lie: rows or columns contiguous."""
+    if w_gate.dim() != 2 or w_gate.shape[0] != width or w_gate.shape != w_up.shape or 0 in w_gate.shape:
+        raise ValueError(f"w_gate and w_up must be ({width}, hidden) alike")
+    if w_gate.dtype != dtype or w_up.dtype != dtype:
+        raise ValueError(f"w_gate and w_up must be {dtype}")
+    for layout, along in ((PD_WEIGHTS_IN_OUT, 1), (PD_WEIGHTS_OUT_IN, 0)):
+        if all(w.stride(along) == 1 or w.shape[along] == 1 for w in (w_gate, w_up)):
+            return layout
+    raise ValueError("w_gate and w_up must both have contiguous rows, or both contiguous columns")
+
+
+def _weight_stride(w: torch.Tensor, layout: int, shape, dtype, what: str) -> int:
+    if w.dtype != dtype or w.shape != shape:
+        raise ValueError(f"{what} must be {dtype} of shape {tuple(shape)}")
+    along = 1 if layout == PD_WEIGHTS_IN_OUT else 0
+    if w.stride(along) != 1 and shape[along] > 1:
+        raise ValueError(f"{what} must lie as w_gate does")
+    return w.stride(1 - along)
+
+
+def pd_gated_forward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, h: torch.Tensor,
+                     gate: Optional[torch.Tensor] = None, up: Optional[torch.Tensor] = None,
+                     activation: int = PD_ACT_SILU, scratch: Optional[torch.Tensor] = None,
+                     stream=None) -> None:
+    """h = act(x w_gate) * (x w_up) over x's last dimension; w_gate and w_up (width, hidden), rows
+    contiguous or (a linear layer's weight, transposed) columns.  gate, up: the two products, for the
+    backward pass."""
+    dt, sh = _dtype(x), x.shape
+    _on_gpu(x, w_gate, w_up, h, gate, up, scratch)
+    width = sh[-1] if x.dim() else 0
+    if not width:
+        raise ValueError("x must have a last dimension of at least 1")
+    layout = _weight_layout(w_gate, w_up, width, x.dtype)
+    hidden = w_gate.shape[1]
+    hs = (*sh[:-1], hidden)
+    strides = []
+    for t, what in ((gate, "gate"), (up, "up"), (h, "h")):
+        if t is not None:
+            _written(t, what)
+        strides.append(0 if t is None else _rows_of(t, hs, x.dtype, what))
+    d = _pack(_GATED_BYTES, x.numel() // width, width, hidden, dt, activation, layout, _rows_of(x, sh, x.dtype, "x"),
+              _weight_stride(w_gate, layout, w_gate.shape, x.dtype, "w_gate"),
+              _weight_stride(w_up, layout, w_gate.shape, x.dtype, "w_up"), *strides, 0, 0, 0, 0)
+    L, need = load(), ctypes.c_int64(0)
+    if scratch is None:
+        _check(L.pd_gated_forward_scratch(d, ctypes.byref(need)))
+    buf, have = _scratch(scratch, need.value, stream)
+    _check(L.pd_gated_forward(d, _ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(gate), _ptr(up), _ptr(h), _ptr(buf), have,
+                              _stream(stream)))
+
+
+def pd_gated_backward(dh: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor,
+                      gate: torch.Tensor, up: torch.Tensor, dx: Optional[torch.Tensor] = None,
+                      dw_gate: Optional[torch.Tensor] = None, dw_up: Optional[torch.Tensor] = None,
+                      h: Optional[torch.Tensor] = None, activation: int = PD_ACT_SILU,
+                      scratch: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Gradients of pd_gated_forward from its gate and up and the gradient dh: dx, dw_gate and dw_up
+    (laid out as the weights), each if given.  h: act(gate) * up, formed again for the product after it."""
+    dt, sh = _dtype(x), x.shape
+    _on_gpu(dh, x, w_gate, w_up, gate, up, dx, dw_gate, dw_up, h, scratch)
+    width = sh[-1] if x.dim() else 0
+    if not width:
+        raise ValueError("x must have a last dimension of at least 1")
+    if (dw_gate is None) != (dw_up is None):
+        raise ValueError("dw_gate and dw_up come together")
+    layout = _weight_layout(w_gate, w_up, width, x.dtype)
+    ws = w_gate.shape
+    hs = (*sh[:-1], ws[1])
+    for t, what in ((dx, "dx"), (dw_gate, "dw_gate"), (dw_up, "dw_up"), (h, "h")):
+        if t is not None:
+            _written(t, what)
+    of = lambda t, shape, what: 0 if t is None else _rows_of(t, shape, x.dtype, what)  # noqa: E731
+    d = _pack(_GATED_BYTES, x.numel() // width, width, ws[1], dt, activation, layout, _rows_of(x, sh, x.dtype, "x"),
+              _weight_stride(w_gate, layout, ws, x.dtype, "w_gate"), _weight_stride(w_up, layout, ws, x.dtype, "w_up"),
+              of(gate, hs, "gate"), of(up, hs, "up"), of(h, hs, "h"), of(dh, hs, "dh"), of(dx, sh, "dx"),
+              *(0 if t is None else _weight_stride(t, layout, ws, x.dtype, what)
+                for t, what in ((dw_gate, "dw_gate"), (dw_up, "dw_up"))))
+    L, need = load(), ctypes.c_int64(0)
+    if scratch is None and (dx is not None or dw_gate is not None):
+        _check(L.pd_gated_backward_scratch(d, ctypes.byref(need)))
+    buf, have = _scratch(scratch, need.value, stream)
+    _check(L.pd_gated_backward(d, _ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(gate), _ptr(up), _ptr(dh), _ptr(h), _ptr(dx),
+                               _ptr(dw_gate), _ptr(dw_up), _ptr(buf), have, _stream(stream)))
 
 
 # ------------------------------------------------------------ workload helpers

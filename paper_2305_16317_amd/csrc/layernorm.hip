@@ -1,0 +1,403 @@
+// Layer norm with the residual's addition and a weight and bias for each run of rows
+// (a sequence's modulation), forward and backward.
+//
+//   s = x + r,  mu = mean s,  rstd = (mean (s - mu)^2 + eps)^-1/2,  n = (s - mu) rstd
+//   y = n w_g + b_g,  g = row / span
+//   a = dy w_g:  dx = dsum + rstd (a - mean a - n mean(a n)),
+//   dw_g = sum over the rows of g of dy n,  db_g = the same of dy
+//
+// Bound by memory: 4 values move per element each way.  A row stays in registers from
+// its one read to its writes, eight values a lane and step, so the squares are summed
+// around the mean itself and an offset common to the row costs no digits.  Rows up to
+// 2048 values belong to one wave, longer ones to a block of 256 or 1024 lanes.
+#include "ops.h"
+
+namespace pd {
+namespace {
+
+__device__ inline float wave_sum(float v) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+    return v;
+}
+// Sums of two values over the TPR lanes of a row; `slot` holds two values a wave.
+template <int TPR>
+__device__ inline void row_sums(float& u, float& v, float* slot) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+        u += __shfl_xor(u, o);
+        v += __shfl_xor(v, o);
+    }
+    if constexpr (TPR > 64) {
+        __syncthreads();                     // the last use of slot is over
+        if ((threadIdx.x & 63) == 0) {
+            slot[2 * (threadIdx.x >> 6)] = u;
+            slot[2 * (threadIdx.x >> 6) + 1] = v;
+        }
+        __syncthreads();
+        u = slot[0], v = slot[1];
+#pragma unroll
+        for (int w = 1; w < TPR / 64; ++w) {
+            u += slot[2 * w];
+            v += slot[2 * w + 1];
+        }
+    }
+}
+template <int TPR>
+__device__ inline float row_sum(float v, float* slot) {
+    float none = 0.f;
+    row_sums<TPR>(v, none, slot);
+    return v;
+}
+
+// TPR lanes a row, NV steps of eight values a lane.
+template <typename T, int TPR, int NV>
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_layernorm(const LayerNormArgs a) {
+    constexpr int kRows = TPR < 256 ? 256 / TPR : 1;      // rows a block
+    __shared__ float slot[32];
+    const int lane = threadIdx.x % TPR;
+    const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR;
+    if (row >= a.d.rows) return;             // whole waves; with TPR > 64 there is one row a block
+    const int width = (int)a.d.width;
+    const T* x = static_cast<const T*>(a.x) + row * a.d.x_stride;
+    const T* r = a.residual ? static_cast<const T*>(a.residual) + row * a.d.residual_stride : nullptr;
+    f32x8 v[NV];
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = (i * TPR + lane) * 8, n = width - c;
+        v[i] = f32x8{};
+        if (n <= 0) continue;
+        v[i] = widen(load8(x + c, n));
+        if (r) v[i] += widen(load8(r + c, n));
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum += v[i][e];
+    if (a.sum) {
+        T* h = static_cast<T*>(a.sum) + row * a.d.sum_stride;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (i * TPR + lane) * 8, n = width - c;
+            if (n > 0) store8(h + c, n, narrow<T>(v[i]));
+        }
+    }
+    const float mean = row_sum<TPR>(sum, slot) / (float)width;
+    float ss = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int n = width - (i * TPR + lane) * 8;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            v[i][e] -= mean;
+            if (e < n) ss = fmaf(v[i][e], v[i][e], ss);
+        }
+    }
+    const float rstd = 1.f / sqrtf(row_sum<TPR>(ss, slot) / (float)width + a.d.eps);
+    if (lane == 0) {
+        if (a.mean) a.mean[row] = mean;
+        if (a.rstd) a.rstd[row] = rstd;
+    }
+    const int64_t g = (uint32_t)(a.first + row) / (uint32_t)a.d.span;
+    const float* w = a.weight ? a.weight + g * a.d.weight_stride : nullptr;
+    const float* b = a.bias ? a.bias + g * a.d.bias_stride : nullptr;
+    T* y = static_cast<T*>(a.y) + row * a.d.y_stride;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = (i * TPR + lane) * 8, n = width - c;
+        if (n <= 0) continue;
+        f32x8 o = v[i] * rstd;
+        if (w) o = o * load8(w + c, n);
+        if (b) o = o + load8(b + c, n);
+        store8(y + c, n, narrow<T>(o));
+    }
+}
+
+// Backward.  Item i of the grid's loop is part i % parts of run i / parts: its rows are
+// every parts-th of the run.  A lane keeps its columns over all of them, so dw and db are
+// summed in registers, then over the block's rows in LDS, and over the parts by
+// k_layernorm_join: a fixed order.  SUMS false:
+// dx alone.
+template <typename T, int TPR, int NV, bool SUMS>
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_layernorm_grad(const LayerNormGradArgs a) {
+    constexpr int kRows = TPR < 256 ? 256 / TPR : 1;
+    constexpr bool KEEP = TPR < 1024;         // the row stays in registers (else it is read again, from the cache)
+    __shared__ float slot[32];
+    __shared__ float part[SUMS && kRows > 1 ? (kRows - 1) * TPR * NV * 8 : 1];
+    const int lane = threadIdx.x % TPR, sub = threadIdx.x / TPR;
+    const int width = (int)a.d.width;
+    for (int64_t item = blockIdx.x; item < (int64_t)a.groups * a.parts; item += gridDim.x) {
+        const int64_t g = item / a.parts, first = g * a.d.span;
+        const float* weight = a.weight ? a.weight + g * a.d.weight_stride : nullptr;
+        const auto row8 = [&](const T* p, int i) {
+            const int c = (i * TPR + lane) * 8, n = width - c;
+            return n > 0 ? load8(p + c, n) : typename Vec8<T>::type{};
+        };
+        const auto weights = [&](int i) {
+            const int c = (i * TPR + lane) * 8, n = width - c;
+            if (weight && n > 0) return load8(weight + c, n);
+            return f32x8{1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
+        };
+        f32x8 dw[SUMS ? NV : 1], db[SUMS ? NV : 1];
+#pragma unroll
+        for (int i = 0; i < (SUMS ? NV : 1); ++i) dw[i] = db[i] = f32x8{};
+        for (int64_t at = (item - g * a.parts) * kRows + sub; at < a.d.span; at += (int64_t)a.parts * kRows) {
+            const int64_t row = first + at;
+            const T* dy = static_cast<const T*>(a.dy) + row * a.d.y_stride;
+            const T* h = static_cast<const T*>(a.sum) + row * a.d.sum_stride;
+            const T* ds = a.dsum ? static_cast<const T*>(a.dsum) + row * a.d.residual_stride : nullptr;
+            T* dx = static_cast<T*>(a.dx) + row * a.d.x_stride;
+            const float rstd = a.rstd[row], mean = a.mean[row];
+            typename Vec8<T>::type vdy[KEEP ? NV : 1], vh[KEEP ? NV : 1], vds[KEEP ? NV : 1];
+            float dot = 0.f, sum = 0.f;
+            if constexpr (KEEP) {
+#pragma unroll
+                for (int i = 0; i < NV; ++i) {
+                    vdy[i] = row8(dy, i);
+                    vh[i] = row8(h, i);
+                    vds[i] = ds ? row8(ds, i) : typename Vec8<T>::type{};
+                }
+            }
+            // (past the row's end dy is 0, and what it meets a number wherever the row's values are)
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const f32x8 g = widen(KEEP ? vdy[KEEP ? i : 0] : row8(dy, i)), w = weights(i);
+                const f32x8 nn = (widen(KEEP ? vh[KEEP ? i : 0] : row8(h, i)) - mean) * rstd;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    if (SUMS) {
+                        dw[SUMS ? i : 0][e] = fmaf(g[e], nn[e], dw[SUMS ? i : 0][e]);
+                        db[SUMS ? i : 0][e] += g[e];
+                    }
+                    sum = fmaf(g[e], w[e], sum);
+                    dot = fmaf(g[e] * w[e], nn[e], dot);
+                }
+            }
+            row_sums<TPR>(dot, sum, slot);
+            dot /= (float)width;
+            sum /= (float)width;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int c = (i * TPR + lane) * 8, n = width - c;
+                if (n <= 0) continue;
+                const f32x8 g = widen(KEEP ? vdy[KEEP ? i : 0] : row8(dy, i)), w = weights(i);
+                const f32x8 nn = (widen(KEEP ? vh[KEEP ? i : 0] : row8(h, i)) - mean) * rstd;
+                f32x8 o = widen(KEEP ? vds[KEEP ? i : 0] : ds ? row8(ds, i) : typename Vec8<T>::type{});
+#pragma unroll
+                for (int e = 0; e < 8; ++e) o[e] = fmaf(rstd, fmaf(-nn[e], dot, fmaf(g[e], w[e], -sum)), o[e]);
+                store8(dx + c, n, narrow<T>(o));
+            }
+        }
+        if constexpr (SUMS) {
+            // the parts' sums, or with one part the results themselves
+            float* to_w = a.parts == 1 ? a.dweight : a.partial;
+            float* to_b = a.parts == 1 ? a.dbias : a.partial + (int64_t)a.groups * a.parts * width;
+#pragma unroll
+            for (int which = 0; which < 2; ++which) {
+                float* to = which ? to_b : to_w;
+                f32x8* d = which ? db : dw;
+                if (which ? !a.dbias : !a.dweight) continue;
+                if constexpr (kRows > 1) {
+                    __syncthreads();                     // the last use of part is over
+                    if (sub > 0)
+#pragma unroll
+                        for (int i = 0; i < NV; ++i)
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) part[(((sub - 1) * NV + i) * 8 + e) * TPR + lane] = d[i][e];
+                    __syncthreads();
+                    if (sub == 0)
+#pragma unroll
+                        for (int s = 0; s < kRows - 1; ++s)
+#pragma unroll
+                            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) d[i][e] += part[((s * NV + i) * 8 + e) * TPR + lane];
+                }
+                if (sub == 0)
+#pragma unroll
+                    for (int i = 0; i < NV; ++i) {
+                        const int c = (i * TPR + lane) * 8, n = width - c;
+                        if (n > 0) store8(to + item * width + c, n, d[i]);
+                    }
+            }
+        }
+    }
+}
+
+// The gradients of weight and bias alone, for rows too wide to keep their sums in
+// registers: 32 lanes side by side take 256 columns, 8 rows at a time.
+template <typename T>
+__global__ __launch_bounds__(256) void k_layernorm_columns(const LayerNormGradArgs a) {
+    __shared__ float part[7][256][2];
+    const int lane = threadIdx.x & 31, sub = threadIdx.x >> 5;
+    const int width = (int)a.d.width, c = blockIdx.x * 256 + lane * 8, n = width - c;
+    for (int64_t item = blockIdx.y; item < (int64_t)a.groups * a.parts; item += gridDim.y) {
+        const int64_t g = item / a.parts, first = g * a.d.span;
+        f32x8 dw = {}, db = {};
+        if (n > 0)
+            for (int64_t at = (item - g * a.parts) * 8 + sub; at < a.d.span; at += (int64_t)a.parts * 8) {
+                const int64_t row = first + at;
+                const f32x8 dy = widen(load8(static_cast<const T*>(a.dy) + row * a.d.y_stride + c, n));
+                const f32x8 nn = (widen(load8(static_cast<const T*>(a.sum) + row * a.d.sum_stride + c, n)) - a.mean[row]) * a.rstd[row];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) dw[e] = fmaf(dy[e], nn[e], dw[e]);
+                db += dy;
+            }
+        __syncthreads();                     // the last use of part is over
+        if (sub > 0)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                part[sub - 1][e * 32 + lane][0] = dw[e];
+                part[sub - 1][e * 32 + lane][1] = db[e];
+            }
+        __syncthreads();
+        if (sub == 0 && n > 0) {
+#pragma unroll
+            for (int s = 0; s < 7; ++s)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    dw[e] += part[s][e * 32 + lane][0];
+                    db[e] += part[s][e * 32 + lane][1];
+                }
+            float* to_w = a.parts == 1 ? a.dweight : a.partial;
+            float* to_b = a.parts == 1 ? a.dbias : a.partial + (int64_t)a.groups * a.parts * width;
+            if (a.dweight) store8(to_w + item * width + c, n, dw);
+            if (a.dbias) store8(to_b + item * width + c, n, db);
+        }
+    }
+}
+
+// The sums over a run's parts: 16 columns a block and 64 lanes down each, which take
+// every 64th part.  Grid row 2 g is run g's weight, 2 g + 1 its bias.
+__global__ __launch_bounds__(1024) void k_layernorm_join(const LayerNormGradArgs a) {
+    __shared__ float part[64][17];
+    const int col = threadIdx.x & 15, sub = threadIdx.x >> 4, c = blockIdx.x * 16 + col, width = (int)a.d.width;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    for (int64_t at = blockIdx.y; at < 2 * (int64_t)a.groups; at += gridDim.y) {
+        const int64_t g = at >> 1;
+        float* to = (at & 1) ? a.dbias : a.dweight;
+        if (!to) continue;
+        const float* from = a.partial + ((at & 1) * (int64_t)a.groups + g) * a.parts * width;
+        float v[4] = {0.f, 0.f, 0.f, 0.f};
+        if (c < width)
+            for (int b = sub; b < a.parts; b += 256) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (b + 64 * i < a.parts) v[i] += from[(int64_t)(b + 64 * i) * width + c];
+            }
+        __syncthreads();                     // the last use of part is over
+        part[sub][col] = (v[0] + v[1]) + (v[2] + v[3]);
+        __syncthreads();
+        // a wave of the 16 takes one column
+        const float sum = wave_sum(part[lane][wave]);
+        if (lane == 0 && blockIdx.x * 16 + wave < width) to[g * width + blockIdx.x * 16 + wave] = sum;
+    }
+}
+
+// dweight and dbias of no rows
+__global__ __launch_bounds__(256) void k_layernorm_zero(float* dweight, float* dbias, int64_t n) {
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+        if (dweight) dweight[i] = 0.f;
+        if (dbias) dbias[i] = 0.f;
+    }
+}
+
+// lanes and steps of a row by its width
+#define PD_LAYERNORM_SHAPES(X) \
+    X(512, 64, 1)              \
+    X(1024, 64, 2)             \
+    X(2048, 64, 4)             \
+    X(4096, 256, 2)            \
+    X(8192, 256, 4)            \
+    X(16384, 1024, 2)          \
+    X(32768, 1024, 4)          \
+    X(65536, 1024, 8)
+
+template <typename T>
+void layernorm_t(const LayerNormArgs& a, hipStream_t s) {
+#define X(W, TPR, NV)                                                                                            \
+    if (a.d.width <= W) {                                                                                        \
+        constexpr int rows = TPR < 256 ? 256 / TPR : 1;                                                          \
+        hipLaunchKernelGGL((k_layernorm<T, TPR, NV>), dim3((unsigned)((a.d.rows + rows - 1) / rows)),            \
+                           dim3(TPR < 256 ? 256 : TPR), 0, s, a);                                                \
+        return;                                                                                                  \
+    }
+    PD_LAYERNORM_SHAPES(X)
+#undef X
+}
+
+// above this width dweight and dbias are summed by a pass of their own
+constexpr int64_t kFusedWidth = 8192;
+constexpr int64_t kMostBlocks = (int64_t)1 << 20;
+
+template <typename T>
+void layernorm_grad_t(const LayerNormGradArgs& a, hipStream_t s) {
+    const int64_t items = (int64_t)a.groups * a.parts;
+    const dim3 grid((unsigned)(items < kMostBlocks ? items : kMostBlocks));
+    const bool sums = a.dweight || a.dbias;
+    if (sums && a.d.width > kFusedWidth) {               // before dx, which may lie over dy
+        hipLaunchKernelGGL(k_layernorm_columns<T>, dim3((unsigned)((a.d.width + 255) / 256), (unsigned)(items < 16384 ? items : 16384)),
+                           dim3(256), 0, s, a);
+        PD_HIP(hipGetLastError());
+    }
+#define X(W, TPR, NV)                                                                                                 \
+    if (a.d.width <= W) {                                                                                             \
+        const dim3 block(TPR < 256 ? 256 : TPR);                                                                      \
+        if (sums && W <= kFusedWidth)                                                                                 \
+            hipLaunchKernelGGL((k_layernorm_grad<T, TPR, NV, W <= kFusedWidth>), grid, block, 0, s, a);               \
+        else                                                                                                          \
+            hipLaunchKernelGGL((k_layernorm_grad<T, TPR, NV, false>), grid, block, 0, s, a);                          \
+        return;                                                                                                       \
+    }
+    PD_LAYERNORM_SHAPES(X)
+#undef X
+}
+
+}  // namespace
+
+// A launch holds fewer than 2^32 threads: 2^21 rows (of up to 1024 lanes) at a time.
+constexpr int64_t kLaunchRows = (int64_t)1 << 21;
+
+void launch_layernorm(const LayerNormArgs& all, hipStream_t s) {
+    const int64_t elem = all.d.dtype == PD_F32 ? 4 : 2;
+    for (int64_t r0 = 0; r0 < all.d.rows; r0 += kLaunchRows) {
+        LayerNormArgs a = all;
+        a.d.rows = all.d.rows - r0 < kLaunchRows ? all.d.rows - r0 : kLaunchRows;
+        a.first = r0;
+        a.x = static_cast<const char*>(a.x) + r0 * a.d.x_stride * elem;
+        if (a.residual) a.residual = static_cast<const char*>(a.residual) + r0 * a.d.residual_stride * elem;
+        if (a.sum) a.sum = static_cast<char*>(a.sum) + r0 * a.d.sum_stride * elem;
+        a.y = static_cast<char*>(a.y) + r0 * a.d.y_stride * elem;
+        if (a.mean) a.mean += r0;
+        if (a.rstd) a.rstd += r0;
+        a.d.dtype == PD_F32 ? layernorm_t<float>(a, s) : layernorm_t<bf16>(a, s);
+        PD_HIP(hipGetLastError());
+    }
+}
+
+int layernorm_grad_parts(const pd_layernorm_desc& d) {
+    // all runs' parts together: two blocks a compute unit; never more than a run has rows for
+    const int64_t groups = d.rows ? d.rows / d.span : 1;
+    const int64_t per = d.width <= 2048 ? 4 : 1, need = (d.span + per - 1) / per, most = (2 * kCus + groups - 1) / groups;
+    return (int)(d.rows == 0 || need < 1 ? 1 : need < most ? need : most);
+}
+
+void launch_layernorm_grad(const LayerNormGradArgs& a, hipStream_t s) {
+    if (a.d.rows == 0) {
+        const int64_t n = (int64_t)a.groups * a.d.width;
+        hipLaunchKernelGGL(k_layernorm_zero, dim3((unsigned)((n + 255) / 256 < 4096 ? (n + 255) / 256 : 4096)), dim3(256), 0, s,
+                           a.dweight, a.dbias, n);
+        PD_HIP(hipGetLastError());
+        return;
+    }
+    a.d.dtype == PD_F32 ? layernorm_grad_t<float>(a, s) : layernorm_grad_t<bf16>(a, s);
+    PD_HIP(hipGetLastError());
+    if ((!a.dweight && !a.dbias) || a.parts == 1) return;
+    const int64_t rows = 2 * (int64_t)a.groups;
+    hipLaunchKernelGGL(k_layernorm_join, dim3((unsigned)((a.d.width + 15) / 16), (unsigned)(rows < 512 ? rows : 512)), dim3(1024), 0,
+                       s, a);
+    PD_HIP(hipGetLastError());
+}
+
+}  // namespace pd

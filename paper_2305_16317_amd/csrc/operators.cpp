@@ -94,6 +94,99 @@ void check_norm(const pd_rmsnorm_desc& d, bool backward) {
     require(g == 0 || (g >= 16 && g <= 512 && (g & (g - 1)) == 0), "group must be 0 or a power of two from 16 to 512");
 }
 
+// The desc as the kernels take it: runs of at least a row, which divide the rows.
+pd_layernorm_desc check_layernorm(const pd_layernorm_desc* p, bool backward) {
+    require(p != nullptr, "desc must not be NULL");
+    pd_layernorm_desc d = *p;
+    check_dtype(d.dtype);
+    require(d.rows >= 0 && d.rows <= (int64_t)1 << 31, "rows out of range");
+    require(d.width >= 1 && d.width <= 65536, "width must be in [1, 65536]");
+    require(d.eps >= 0.f && std::isfinite(d.eps), "eps must be finite and >= 0");
+    require(d.span >= 0 && (d.span == 0 || d.rows % d.span == 0), "span must be >= 0 and divide rows");
+    for (int64_t s : {d.x_stride, d.residual_stride, d.sum_stride, d.y_stride, d.weight_stride, d.bias_stride}) check_stride(s);
+    if (backward) require(d.rows <= 1 || d.x_stride >= d.width, "x_stride (of dx) must be >= width");
+    else require(d.rows <= 1 || d.y_stride >= d.width, "y_stride must be >= width");
+    if (d.span == 0) {
+        d.span = d.rows ? d.rows : 1;
+        d.weight_stride = d.bias_stride = 0;
+    }
+    return d;
+}
+// runs that have gradients: one of span 0 without rows
+int64_t layernorm_groups(const pd_layernorm_desc& given) { return given.span ? given.rows / given.span : 1; }
+
+// ------------------------------------------------------------------ rotary
+// What rotary calls have in common, and the desc as the kernels take it.
+pd_rotary_desc check_rotary(const pd_rotary_desc& given, const void* k) {
+    pd_rotary_desc d = given;
+    check_dtype(d.dtype);
+    require(d.layout == PD_ROTARY_HALF || d.layout == PD_ROTARY_INTERLEAVED,
+            "layout must be PD_ROTARY_HALF or PD_ROTARY_INTERLEAVED");
+    require(d.batch >= 0 && d.length >= 0, "batch and length must be >= 0");
+    if (!k) d.heads_k = 0;
+    require(d.heads_q >= 1 && d.heads_q <= 65536 && d.heads_k >= 0 && d.heads_k <= 65536, "heads out of range");
+    require(d.head_dim >= 2 && d.head_dim <= 1024, "head_dim must be in [2, 1024]");
+    require(d.rotary_dim >= 2 && d.rotary_dim <= d.head_dim && d.rotary_dim % 2 == 0,
+            "rotary_dim must be even and in [2, head_dim]");
+    require(d.position_stride >= 0, "position_stride must be >= 0");
+    for (int i = 0; i < 3; ++i)
+        for (int64_t s : {d.q_stride[i], d.k_stride[i], d.q_out_stride[i], d.k_out_stride[i]}) check_stride(s);
+    require(d.batch <= (int64_t)1 << 31 && d.length <= (int64_t)1 << 31, "batch or length out of range");
+    // a launch holds fewer than 2^32 threads (at least a unit of 8 values of 8 heads each)
+    const int64_t units = d.head_dim / 8 + 2, heads8 = ((int64_t)d.heads_q + d.heads_k + 7) / 8;
+    if (d.length && d.batch > ((int64_t)1 << 31) / (units * heads8) / d.length)
+        fail(PD_ERR_UNSUPPORTED, "so many tokens in one call are not implemented");
+    return d;
+}
+void check_rotary_memory(const pd_rotary_desc& d, const void* q, const void* k, const int32_t* positions, const float* table,
+                         void* q_out, void* k_out) {
+    require(q && positions && table && q_out && (!k || k_out), "NULL device pointer");
+    require(d.table_rows >= 1, "table_rows must be >= 1");
+    check_apart("q_out", d.q_out_stride, d.batch, d.length, d.heads_q, d.head_dim);
+    if (d.heads_k) check_apart("k_out", d.k_out_stride, d.batch, d.length, d.heads_k, d.head_dim);
+}
+// The axis of each pair.
+AxisMap axis_map(int axes, int order, const int32_t* sections, int rotary_dim) {
+    require(axes >= 1 && axes <= 4, "axes must be in [1, 4]");
+    require(order == PD_AXES_RUNS || order == PD_AXES_TURNS, "order must be PD_AXES_RUNS or PD_AXES_TURNS");
+    int left[4] = {0, 0, 0, 0};
+    int64_t sum = 0;
+    for (int a = 0; a < axes; ++a) {
+        require(sections[a] >= 0, "sections must be >= 0");
+        sum += left[a] = sections[a];
+    }
+    require(sum == rotary_dim / 2, "sections must add up to rotary_dim / 2");
+    AxisMap map{};
+    for (int k = 0, a = 0; k < rotary_dim / 2; ++k) {
+        while (left[a] == 0) a = (a + 1) % axes;
+        map.word[k >> 4] |= (uint32_t)a << (2 * (k & 15));
+        --left[a];
+        if (order == PD_AXES_TURNS) a = (a + 1) % axes;
+    }
+    return map;
+}
+
+// ------------------------------------------------------------------ gated product
+void check_gated(const pd_gated_desc& d) {
+    check_dtype(d.dtype);
+    require(d.rows >= 0, "rows must be >= 0");
+    require(d.width >= 1 && d.width <= 1 << 20 && d.hidden >= 1 && d.hidden <= 1 << 20, "width and hidden must be in [1, 2^20]");
+    require(d.activation >= PD_ACT_SILU && d.activation <= PD_ACT_RELU, "activation must be a PD_ACT_* kind");
+    require(d.weight_layout == PD_WEIGHTS_IN_OUT || d.weight_layout == PD_WEIGHTS_OUT_IN,
+            "weight_layout must be PD_WEIGHTS_IN_OUT or PD_WEIGHTS_OUT_IN");
+    for (int64_t s : {d.x_stride, d.w_gate_stride, d.w_up_stride, d.gate_stride, d.up_stride, d.h_stride, d.dh_stride, d.dx_stride,
+                      d.dw_gate_stride, d.dw_up_stride})
+        check_stride(s);
+    if (d.rows > (int64_t)1 << 24) fail(PD_ERR_UNSUPPORTED, "more than 2^24 rows are not implemented");
+    // a launch holds fewer than 2^32 threads, and a step's operands fewer than 2^40 elements
+    const int64_t tiles = ((int64_t)d.rows / 64 + 1) * (d.hidden / 64 + 1), tiles_x = ((int64_t)d.rows / 64 + 1) * (d.width / 64 + 1);
+    if (tiles > 1 << 22 || tiles_x > 1 << 22 || (int64_t)(d.width / 64 + 1) * (d.hidden / 64 + 1) > 1 << 22)
+        fail(PD_ERR_UNSUPPORTED, "products of more than 2^22 tiles of 64 x 64 are not implemented");
+}
+void check_rows_of(const char* what, const void* p, int64_t stride, int64_t rows, int64_t cols) {
+    require(!p || rows <= 1 || stride >= cols, std::string(what) + ": rows of an output share elements");
+}
+
 // ------------------------------------------------------------------ attention
 // The desc as the kernels take it: a window that hides nothing becomes 0, and
 // sinks count up to the keys there are.
@@ -202,29 +295,9 @@ extern "C" pd_status pd_rotary_apply(const pd_rotary_desc* desc, const void* q, 
                                      void* stream) {
     return guard([&] {
         require(desc != nullptr, "desc must not be NULL");
-        pd_rotary_desc d = *desc;
-        check_dtype(d.dtype);
-        require(d.layout == PD_ROTARY_HALF || d.layout == PD_ROTARY_INTERLEAVED,
-                "layout must be PD_ROTARY_HALF or PD_ROTARY_INTERLEAVED");
-        require(d.batch >= 0 && d.length >= 0, "batch and length must be >= 0");
-        if (!k) d.heads_k = 0;
-        require(d.heads_q >= 1 && d.heads_q <= 65536 && d.heads_k >= 0 && d.heads_k <= 65536, "heads out of range");
-        require(d.head_dim >= 2 && d.head_dim <= 1024, "head_dim must be in [2, 1024]");
-        require(d.rotary_dim >= 2 && d.rotary_dim <= d.head_dim && d.rotary_dim % 2 == 0,
-                "rotary_dim must be even and in [2, head_dim]");
-        require(d.position_stride >= 0, "position_stride must be >= 0");
-        for (int i = 0; i < 3; ++i)
-            for (int64_t s : {d.q_stride[i], d.k_stride[i], d.q_out_stride[i], d.k_out_stride[i]}) check_stride(s);
-        require(d.batch <= (int64_t)1 << 31 && d.length <= (int64_t)1 << 31, "batch or length out of range");
-        // a launch holds fewer than 2^32 threads (at least a unit of 8 values of 8 heads each)
-        const int64_t units = d.head_dim / 8 + 2, heads8 = ((int64_t)d.heads_q + d.heads_k + 7) / 8;
-        if (d.length && d.batch > ((int64_t)1 << 31) / (units * heads8) / d.length)
-            fail(PD_ERR_UNSUPPORTED, "so many tokens in one call are not implemented");
+        const pd_rotary_desc d = check_rotary(*desc, k);
         if (d.batch == 0 || d.length == 0) return;
-        require(q && positions && table && q_out && (!k || k_out), "NULL device pointer");
-        require(d.table_rows >= 1, "table_rows must be >= 1");
-        check_apart("q_out", d.q_out_stride, d.batch, d.length, d.heads_q, d.head_dim);
-        if (d.heads_k) check_apart("k_out", d.k_out_stride, d.batch, d.length, d.heads_k, d.head_dim);
+        check_rotary_memory(d, q, k, positions, table, q_out, k_out);
         require_gfx950();
         launch_rotary(RotaryArgs{d, q, k, positions, table, q_out, k_out}, static_cast<hipStream_t>(stream));
     });
@@ -287,5 +360,180 @@ extern "C" pd_status pd_attention_backward(const pd_attention_desc* desc, const 
         a.dout = dout, a.dq = dq, a.dk = dk, a.dv = dv;
         a.scratch = static_cast<float*>(scratch);
         launch_attention_grad(a, static_cast<hipStream_t>(stream));
+    });
+}
+
+extern "C" pd_status pd_layernorm_forward(const pd_layernorm_desc* desc, const void* x, const void* residual,
+                                          const float* weight, const float* bias, void* sum, void* y, float* mean,
+                                          float* rstd, void* stream) {
+    return guard([&] {
+        const pd_layernorm_desc d = check_layernorm(desc, false);
+        if (d.rows == 0) return;
+        require(x && y, "x and y must not be NULL");
+        require(!sum || d.rows <= 1 || d.sum_stride >= d.width, "sum_stride must be >= width");
+        require_gfx950();
+        launch_layernorm(LayerNormArgs{d, x, residual, weight, bias, sum, y, mean, rstd, 0}, static_cast<hipStream_t>(stream));
+    });
+}
+
+static int64_t layernorm_grad_scratch(const pd_layernorm_desc& d, int64_t groups) {
+    const int64_t parts = layernorm_grad_parts(d);
+    return parts == 1 ? 0 : 2 * groups * parts * d.width * (int64_t)sizeof(float);
+}
+
+extern "C" pd_status pd_layernorm_backward_scratch(const pd_layernorm_desc* desc, int64_t* bytes) {
+    return guard([&] {
+        require(bytes != nullptr, "bytes must not be NULL");
+        const pd_layernorm_desc d = check_layernorm(desc, true);
+        *bytes = layernorm_grad_scratch(d, layernorm_groups(*desc));
+    });
+}
+
+extern "C" pd_status pd_layernorm_backward(const pd_layernorm_desc* desc, const void* dy, const void* sum,
+                                           const float* weight, const float* mean, const float* rstd, const void* dsum,
+                                           void* dx, float* dweight, float* dbias, void* scratch, int64_t scratch_bytes,
+                                           void* stream) {
+    return guard([&] {
+        const pd_layernorm_desc d = check_layernorm(desc, true);
+        const int64_t groups = layernorm_groups(*desc);
+        if (groups == 0 || (d.rows == 0 && !dweight && !dbias)) return;
+        require(d.rows == 0 || (dy && sum && mean && rstd && dx), "dy, sum, mean, rstd and dx must not be NULL");
+        if (dweight || dbias) check_scratch(scratch, scratch_bytes, layernorm_grad_scratch(d, groups));
+        require_gfx950();
+        launch_layernorm_grad(LayerNormGradArgs{d, dy, sum, weight, mean, rstd, dsum, dx, dweight, dbias,
+                                                static_cast<float*>(scratch), groups, layernorm_grad_parts(d)},
+                              static_cast<hipStream_t>(stream));
+    });
+}
+
+extern "C" pd_status pd_rotary_axes_table(const pd_rotary_axes_table_desc* desc, int64_t first, int64_t rows, float* table,
+                                          void* stream) {
+    return guard([&] {
+        require(desc != nullptr, "desc must not be NULL");
+        const pd_rotary_axes_table_desc& d = *desc;
+        require(d.rotary_dim >= 2 && d.rotary_dim <= 1024 && d.rotary_dim % 2 == 0, "rotary_dim must be even and in [2, 1024]");
+        const AxisMap map = axis_map(d.axes, d.order, d.sections, d.rotary_dim);
+        for (int a = 0; a < d.axes; ++a) {
+            require(d.base[a] > 1.0 && std::isfinite(d.base[a]), "base must be finite and > 1");
+            require(std::isfinite(d.scale[a]), "scale must be finite");
+        }
+        require(first >= 0 && first <= (int64_t)1 << 40 && rows >= 0 && rows <= (int64_t)1 << 28, "first or rows out of range");
+        if (rows > ((int64_t)1 << 31) / (d.rotary_dim / 2))
+            fail(PD_ERR_UNSUPPORTED, "a table of more than 2^31 pairs is not implemented");
+        if (rows == 0) return;
+        require(table != nullptr, "table must not be NULL");
+        require_gfx950();
+        launch_rotary_axes_table(d, map, first, rows, table, static_cast<hipStream_t>(stream));
+    });
+}
+
+extern "C" pd_status pd_rotary_axes_apply(const pd_rotary_axes_desc* desc, const void* q, const void* k,
+                                          const int32_t* positions, const float* table, void* q_out, void* k_out,
+                                          void* stream) {
+    return guard([&] {
+        require(desc != nullptr, "desc must not be NULL");
+        const pd_rotary_desc d = check_rotary(desc->rotary, k);
+        const AxisMap map = axis_map(desc->axes, desc->order, desc->sections, d.rotary_dim);
+        for (int64_t s : desc->position_stride) check_stride(s);
+        if (d.batch == 0 || d.length == 0) return;
+        check_rotary_memory(d, q, k, positions, table, q_out, k_out);
+        require_gfx950();
+        launch_rotary_axes(RotaryAxesArgs{d, q, k, positions, table, q_out, k_out,
+                                          {desc->position_stride[0], desc->position_stride[1], desc->position_stride[2]}, map},
+                           static_cast<hipStream_t>(stream));
+    });
+}
+
+extern "C" pd_status pd_dropout_apply(const pd_dropout_desc* desc, const void* x, const void* residual,
+                                      const uint32_t* step_more, void* y, void* stream) {
+    return guard([&] {
+        require(desc != nullptr, "desc must not be NULL");
+        const pd_dropout_desc& d = *desc;
+        check_dtype(d.dtype);
+        require(d.rows >= 0 && d.rows <= (int64_t)1 << 40 && d.first_row >= 0 && d.first_row <= (int64_t)1 << 40, "rows out of range");
+        require(d.width >= 1 && d.width <= 0x7fffffff, "width must be in [1, 2^31 - 1]");
+        require(d.rows <= ((int64_t)1 << 46) / d.width, "rows x width out of range");
+        require(d.first_row + d.rows <= ((int64_t)1 << 60) / ((d.width + 7) / 8), "first_row out of range");
+        require(d.p >= 0.0 && d.p <= 1.0, "p must be in [0, 1]");
+        require(step_more || d.step != 0xffffffffu, "step must be below 2^32 - 1");
+        for (int64_t s : {d.x_stride, d.residual_stride, d.y_stride}) check_stride(s);
+        require(d.rows <= 1 || d.y_stride >= d.width, "y_stride must be >= width");
+        if (d.rows == 0) return;
+        require(x && y, "x and y must not be NULL");
+        require_gfx950();
+        DropoutArgs a{};
+        a.d = d;
+        a.x = x, a.residual = residual, a.step = step_more, a.y = y;
+        a.under = (uint32_t)std::floor(65536.0 * d.p + 0.5);
+        a.scale = a.under < 65536 ? (float)(65536.0 / (65536.0 - a.under)) : 0.f;
+        launch_dropout(a, static_cast<hipStream_t>(stream));
+    });
+}
+
+extern "C" pd_status pd_gated_forward_scratch(const pd_gated_desc* desc, int64_t* bytes) {
+    return guard([&] {
+        require(desc != nullptr && bytes != nullptr, "desc and bytes must not be NULL");
+        check_gated(*desc);
+        *bytes = gated_scratch_bytes(*desc);
+    });
+}
+
+extern "C" pd_status pd_gated_forward(const pd_gated_desc* desc, const void* x, const void* w_gate, const void* w_up,
+                                      void* gate, void* up, void* h, void* scratch, int64_t scratch_bytes, void* stream) {
+    return guard([&] {
+        require(desc != nullptr, "desc must not be NULL");
+        const pd_gated_desc& d = *desc;
+        check_gated(d);
+        if (d.rows == 0) return;
+        require(x && w_gate && w_up && h, "x, w_gate, w_up and h must not be NULL");
+        check_rows_of("h", h, d.h_stride, d.rows, d.hidden);
+        check_rows_of("gate", gate, d.gate_stride, d.rows, d.hidden);
+        check_rows_of("up", up, d.up_stride, d.rows, d.hidden);
+        check_scratch(scratch, scratch_bytes, gated_scratch_bytes(d));
+        require_gfx950();
+        GatedArgs a{};
+        a.d = d;
+        a.x = x, a.w_gate = w_gate, a.w_up = w_up;
+        a.gate = gate, a.up = up, a.h = h;
+        a.scratch = static_cast<char*>(scratch);
+        launch_gated(a, static_cast<hipStream_t>(stream));
+    });
+}
+
+extern "C" pd_status pd_gated_backward_scratch(const pd_gated_desc* desc, int64_t* bytes) {
+    return guard([&] {
+        require(desc != nullptr && bytes != nullptr, "desc and bytes must not be NULL");
+        check_gated(*desc);
+        *bytes = gated_grad_scratch_bytes(*desc);
+    });
+}
+
+extern "C" pd_status pd_gated_backward(const pd_gated_desc* desc, const void* x, const void* w_gate, const void* w_up,
+                                       const void* gate, const void* up, const void* dh, void* h, void* dx,
+                                       void* dw_gate, void* dw_up, void* scratch, int64_t scratch_bytes, void* stream) {
+    return guard([&] {
+        require(desc != nullptr, "desc must not be NULL");
+        const pd_gated_desc& d = *desc;
+        check_gated(d);
+        require(!dw_gate == !dw_up, "dw_gate and dw_up come together");
+        if (d.rows == 0 && !dw_gate) return;
+        if (!h && !dx && !dw_gate) return;
+        require(d.rows == 0 || (gate && up && dh), "gate, up and dh must not be NULL");
+        require(d.rows == 0 || !dx || (w_gate && w_up), "w_gate and w_up must not be NULL");
+        require(d.rows == 0 || !dw_gate || x, "x must not be NULL");
+        const bool in_out = d.weight_layout == PD_WEIGHTS_IN_OUT;
+        check_rows_of("h", h, d.h_stride, d.rows, d.hidden);
+        check_rows_of("dx", dx, d.dx_stride, d.rows, d.width);
+        check_rows_of("dw_gate", dw_gate, d.dw_gate_stride, in_out ? d.width : d.hidden, in_out ? d.hidden : d.width);
+        check_rows_of("dw_up", dw_up, d.dw_up_stride, in_out ? d.width : d.hidden, in_out ? d.hidden : d.width);
+        if (dx || dw_gate) check_scratch(scratch, scratch_bytes, gated_grad_scratch_bytes(d));
+        require_gfx950();
+        GatedArgs a{};
+        a.d = d;
+        a.x = x, a.w_gate = w_gate, a.w_up = w_up;
+        a.gate = const_cast<void*>(gate), a.up = const_cast<void*>(up), a.h = h;
+        a.dh = dh, a.dx = dx, a.dw_gate = dw_gate, a.dw_up = dw_up;
+        a.scratch = static_cast<char*>(scratch);
+        launch_gated_grad(a, static_cast<hipStream_t>(stream));
     });
 }

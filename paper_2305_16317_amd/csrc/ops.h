@@ -1,5 +1,5 @@
-// Shared by the transformer operators (norm.hip, rotary.hip, attention.hip,
-// attention_grad.hip) and their C entry points (operators.cpp).
+// Shared by the transformer operators (norm.hip, layernorm.hip, rotary.hip, dropout.hip,
+// gated.hip, attention.hip, attention_grad.hip) and their C entry points (operators.cpp).
 #pragma once
 
 #include "pd_internal.h"
@@ -85,7 +85,54 @@ struct NormGradArgs {
 int norm_grad_blocks(const pd_rmsnorm_desc& d);
 void launch_rmsnorm_grad(const NormGradArgs& a, hipStream_t s);
 
+// Compute units of an MI355X: how much scratch a call needs does not depend on a device.
+constexpr int kCus = 256;
+
+struct LayerNormArgs {
+    pd_layernorm_desc d;     // (span as the kernels take it: at least 1)
+    const void* x;
+    const void* residual;
+    const float* weight;     // or nullptr: ones
+    const float* bias;       // or nullptr: zeros
+    void* sum;
+    void* y;
+    float* mean;
+    float* rstd;
+    int64_t first;           // row that the launch begins at
+};
+void launch_layernorm(const LayerNormArgs& a, hipStream_t s);
+struct LayerNormGradArgs {
+    pd_layernorm_desc d;
+    const void* dy;
+    const void* sum;
+    const float* weight;
+    const float* mean;
+    const float* rstd;
+    const void* dsum;
+    void* dx;
+    float* dweight;
+    float* dbias;
+    float* partial;          // [2][groups][parts][width]; not used with one part
+    int64_t groups;
+    int parts;
+};
+int layernorm_grad_parts(const pd_layernorm_desc& d);
+void launch_layernorm_grad(const LayerNormGradArgs& a, hipStream_t s);
+
+struct DropoutArgs {
+    pd_dropout_desc d;
+    const void* x;
+    const void* residual;
+    const uint32_t* step;
+    void* y;
+    uint32_t under;          // a value is kept where its 16 bits are not under this
+    float scale;             // 65536 / (65536 - under)
+    int64_t first;           // row that the launch begins at, for the counters
+};
+void launch_dropout(const DropoutArgs& a, hipStream_t s);
+
 struct RotaryArgs {
+    static constexpr bool kAxes = false;
     pd_rotary_desc d;
     const void* q;
     const void* k;
@@ -95,6 +142,26 @@ struct RotaryArgs {
     void* k_out;
 };
 void launch_rotary(const RotaryArgs& a, hipStream_t s);
+// the axis of each pair, two bits a pair
+struct AxisMap {
+    uint32_t word[32];
+    __host__ __device__ int axis(int k) const { return (word[k >> 4] >> (2 * (k & 15))) & 3; }
+};
+struct RotaryAxesArgs {
+    static constexpr bool kAxes = true;
+    pd_rotary_desc d;
+    const void* q;
+    const void* k;
+    const int32_t* positions;
+    const float* table;
+    void* q_out;
+    void* k_out;
+    int64_t position_strides[3];   // batch, token, axis
+    AxisMap map;
+};
+void launch_rotary_axes(const RotaryAxesArgs& a, hipStream_t s);
+void launch_rotary_axes_table(const pd_rotary_axes_table_desc& d, const AxisMap& map, int64_t first, int64_t rows, float* table,
+                              hipStream_t s);
 void launch_rotary_table(const pd_rotary_table_desc& d, int64_t first, int64_t rows, float* table, hipStream_t s);
 
 struct AttentionArgs {
@@ -117,5 +184,25 @@ int64_t attention_scratch_bytes(const pd_attention_desc& d);
 void launch_attention(const AttentionArgs& a, hipStream_t s);
 int64_t attention_grad_scratch_bytes(const pd_attention_desc& d);
 void launch_attention_grad(const AttentionArgs& a, hipStream_t s);
+
+struct GatedArgs {
+    pd_gated_desc d;
+    const void* x;
+    const void* w_gate;
+    const void* w_up;
+    void* gate;              // forward: or nullptr
+    void* up;
+    void* h;                 // backward: or nullptr
+    // backward
+    const void* dh;
+    void* dx;                // or nullptr
+    void* dw_gate;           // or nullptr
+    void* dw_up;
+    char* scratch;
+};
+int64_t gated_scratch_bytes(const pd_gated_desc& d);
+void launch_gated(const GatedArgs& a, hipStream_t s);
+int64_t gated_grad_scratch_bytes(const pd_gated_desc& d);
+void launch_gated_grad(const GatedArgs& a, hipStream_t s);
 
 }  // namespace pd

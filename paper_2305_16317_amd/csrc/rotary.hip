@@ -2,6 +2,9 @@
 //
 //   pair k of a head at position p:  (a, b) -> (a c - b s, a s + b c),  (c, s) = table[p][k]
 //
+// With several axes a token has a position on each, and p is that of the axis which pair k
+// belongs to (AxisMap: two bits a pair).
+//
 // Bound by memory (each value read and written once; the table's row is shared
 // by a token's heads).  A lane holds the (cos, sin) of a unit's pairs in registers and
 // turns that unit in several heads.  A unit is eight pairs with halves (two runs of eight
@@ -39,10 +42,27 @@ __global__ __launch_bounds__(256) void k_rotary_table(const pd_rotary_table_desc
     table[2 * i + 1] = (float)(sn * d.magnitude);
 }
 
+// The table of several axes: pair k of axis a, the i-th of the axis's n, turns by
+// base_a^(-i / n) scale_a, or with `shared` by base_a^(-k / pairs) scale_a.
+__global__ __launch_bounds__(256) void k_rotary_axes_table(const pd_rotary_axes_table_desc d, const AxisMap map, int64_t first,
+                                                           int64_t rows, float* table) {
+    const int half = d.rotary_dim / 2;
+    const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (at >= rows * half) return;
+    const int k = (int)(at % half), a = map.axis(k);
+    int i = 0;
+    for (int j = 0; j < k; ++j) i += map.axis(j) == a;
+    const double part = d.shared ? (double)k / half : (double)i / d.sections[a];
+    double sn, cs;
+    sincos((double)(first + at / half) * (pow(d.base[a], -part) * d.scale[a]), &sn, &cs);
+    table[2 * at] = (float)cs;
+    table[2 * at + 1] = (float)sn;
+}
+
 // One lane: unit u of a token (pairs while u < pair_units, then values to copy) in the
 // heads hs, hs + lanes_h, ...; the heads of q, then of k.
-template <typename T, bool HALF>
-__global__ __launch_bounds__(256) void k_rotary(const RotaryArgs a, int units, int pair_units, int lanes_h, int64_t lanes) {
+template <typename T, bool HALF, class Args>
+__global__ __launch_bounds__(256) void k_rotary(const Args a, int units, int pair_units, int lanes_h, int64_t lanes) {
     constexpr int kPairs = HALF ? 8 : 4;
     const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (id >= lanes) return;
@@ -60,16 +80,35 @@ __global__ __launch_bounds__(256) void k_rotary(const RotaryArgs a, int units, i
         const int k0 = u * kPairs, pairs = min(half - k0, kPairs);
         e0 = HALF ? k0 : 2 * k0;
         n0 = HALF ? pairs : 2 * pairs;
-        int64_t pos = a.positions[b * a.d.position_stride + i];
-        pos = pos < 0 ? 0 : (pos >= a.d.table_rows ? a.d.table_rows - 1 : pos);
-        const float* t = a.table + (pos * half + k0) * 2;
+        const auto clamped = [&](int64_t pos) { return pos < 0 ? 0 : (pos >= a.d.table_rows ? a.d.table_rows - 1 : pos); };
+        const auto set = [&](int e, float c, float s) {
+            cs[e] = c;
+            sn[e] = a.d.backward ? -s : s;
+        };
+        const auto row = [&](int64_t pos) {                // the unit's pairs from one row of the table
+            const float* t = a.table + (clamped(pos) * half + k0) * 2;
 #pragma unroll
-        for (int r = 0; r < kPairs / 4; ++r) {
-            const f32x8 v = load8(t + 8 * r, 2 * pairs - 8 * r);
+            for (int r = 0; r < kPairs / 4; ++r) {
+                const f32x8 v = load8(t + 8 * r, 2 * pairs - 8 * r);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                cs[4 * r + e] = v[2 * e];
-                sn[4 * r + e] = a.d.backward ? -v[2 * e + 1] : v[2 * e + 1];
+                for (int e = 0; e < 4; ++e) set(4 * r + e, v[2 * e], v[2 * e + 1]);
+            }
+        };
+        if constexpr (!Args::kAxes) {
+            row(a.positions[b * a.d.position_stride + i]);
+        } else {
+            const int32_t* at = a.positions + b * a.position_strides[0] + i * a.position_strides[1];
+            const uint32_t axes = a.map.word[k0 >> 4] >> (2 * (k0 & 15)), mine = (1u << (2 * pairs)) - 1, one = axes & 3;
+            if (((axes ^ (one * 0x5555u)) & mine) == 0) {
+                row(at[one * a.position_strides[2]]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < kPairs; ++e) {
+                    const int64_t pos = clamped(at[((axes >> (2 * e)) & 3) * a.position_strides[2]]);
+                    const int k = e < pairs ? k0 + e : k0;
+                    const float* t = a.table + (pos * half + k) * 2;
+                    set(e, t[0], t[1]);
+                }
             }
         }
     } else {
@@ -111,8 +150,8 @@ __global__ __launch_bounds__(256) void k_rotary(const RotaryArgs a, int units, i
     }
 }
 
-template <typename T>
-void rotary_t(const RotaryArgs& a, hipStream_t s) {
+template <typename T, class Args>
+void rotary_t(const Args& a, hipStream_t s) {
     const pd_rotary_desc& d = a.d;
     const int pairs = d.layout == PD_ROTARY_HALF ? 8 : 4;
     const int pair_units = (d.rotary_dim / 2 + pairs - 1) / pairs, units = pair_units + (d.head_dim - d.rotary_dim + 7) / 8;
@@ -126,9 +165,9 @@ void rotary_t(const RotaryArgs& a, hipStream_t s) {
     const int64_t lanes = tokens * units * lanes_h;
     const dim3 grid((unsigned)((lanes + 255) / 256)), block(256);
     if (d.layout == PD_ROTARY_HALF)
-        hipLaunchKernelGGL((k_rotary<T, true>), grid, block, 0, s, a, units, pair_units, lanes_h, lanes);
+        hipLaunchKernelGGL((k_rotary<T, true, Args>), grid, block, 0, s, a, units, pair_units, lanes_h, lanes);
     else
-        hipLaunchKernelGGL((k_rotary<T, false>), grid, block, 0, s, a, units, pair_units, lanes_h, lanes);
+        hipLaunchKernelGGL((k_rotary<T, false, Args>), grid, block, 0, s, a, units, pair_units, lanes_h, lanes);
     PD_HIP(hipGetLastError());
 }
 
@@ -136,6 +175,17 @@ void rotary_t(const RotaryArgs& a, hipStream_t s) {
 
 void launch_rotary(const RotaryArgs& a, hipStream_t s) {
     a.d.dtype == PD_F32 ? rotary_t<float>(a, s) : rotary_t<bf16>(a, s);
+}
+
+void launch_rotary_axes(const RotaryAxesArgs& a, hipStream_t s) {
+    a.d.dtype == PD_F32 ? rotary_t<float>(a, s) : rotary_t<bf16>(a, s);
+}
+
+void launch_rotary_axes_table(const pd_rotary_axes_table_desc& d, const AxisMap& map, int64_t first, int64_t rows, float* table,
+                              hipStream_t s) {
+    const int64_t n = rows * (d.rotary_dim / 2);
+    hipLaunchKernelGGL(k_rotary_axes_table, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, d, map, first, rows, table);
+    PD_HIP(hipGetLastError());
 }
 
 void launch_rotary_table(const pd_rotary_table_desc& d, int64_t first, int64_t rows, float* table, hipStream_t s) {
