@@ -25,7 +25,7 @@ struct Product {
     const bf16* b1[kSegs];
     int64_t lda, ldb;
     int64_t a_group;                     // elements between the a of one group and the next
-    int segs, k, steps;                  // steps of 64 a segment
+    int segs, k, steps;                  // steps of the form's BK a segment
     int m, n;                            // rows, and columns of a half's matrix
     int apart;                           // the halves are two matrices (else neighbours in one)
     int tiles_m, tiles_n, groups, splits;
@@ -39,46 +39,100 @@ struct Product {
 };
 
 // ------------------------------------------------------------------ activations
-__device__ inline float sigmoid(float v) { return 1.f / (1.f + expf(-v)); }
-__device__ inline float activate(int act, float g) {
+// From the hardware's 2^x and 1/x (1 ulp each); with the math library's functions and
+// divisions the results' way out took longer than a block's products over 1024 values.
+// FINE (float32 results): e^x with what the product x log2 e leaves out, 2^-24 |x| of it.
+template <bool FINE>
+__device__ __forceinline__ float e_to(float x) {
+    const float t = x * kLog2e, e = exp2_fast(t);
+    if constexpr (!FINE) return e;
+    const float rest = fmaf(x, 1.92596299e-8f, fmaf(x, kLog2e, -t));       // log2 e = kLog2e + 1.926e-8
+    return fabsf(t) < 127.f ? fmaf(e, rest * kLn2, e) : e;                 // (else near 0, or infinity)
+}
+template <bool FINE>
+__device__ __forceinline__ float sigmoid(float x) {
+    return __builtin_amdgcn_rcpf(1.f + e_to<FINE>(-x));
+}
+// The normal distribution function: for x = |g| / sqrt 2, erfc x = e^(-x^2) t Q(t) with
+// t = 1 / (1 + 0.3 x); Q is fitted to e^(x^2) erfc(x) / t over 0 <= x <= 10 with relative errors
+// up to 2e-8 (past it the exponential is 0).
+template <bool FINE>
+__device__ __forceinline__ float normal_below(float g) {
+    const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(g), 0.212132034f, 1.f));
+    float q = -0.12952314f;
+    q = fmaf(q, t, 0.48556441f);
+    q = fmaf(q, t, -0.51228074f);
+    q = fmaf(q, t, 0.54772327f);
+    q = fmaf(q, t, -0.094653135f);
+    q = fmaf(q, t, 0.21492717f);
+    q = fmaf(q, t, 0.14833886f);
+    q = fmaf(q, t, 0.17071527f);
+    q = fmaf(q, t, 0.169188f);
+    const float tail = 0.5f * e_to<FINE>(-0.5f * g * g) * (q * t);
+    return g < 0.f ? tail : 1.f - tail;
+}
+// 2 sqrt(2/pi) (g + 0.044715 g^3), of which gelu's tanh form takes the sigmoid
+__device__ __forceinline__ float twice_inner(float g) { return 1.59576912f * fmaf(0.044715f * g * g, g, g); }
+// largest of g and 0, or NaN
+__device__ __forceinline__ float positive(float g) { return g > 0.f ? g : (g != g ? g : 0.f); }
+
+template <class V, class F>
+__device__ __forceinline__ V each(V g, F f) {
+#pragma unroll
+    for (int e = 0; e < (int)(sizeof(V) / 4); ++e) g[e] = f(g[e]);
+    return g;
+}
+template <bool FINE, class V>
+__device__ __forceinline__ V activate(int act, V g) {
     switch (act) {
-        case PD_ACT_SILU: return g / (1.f + expf(-g));
-        case PD_ACT_GELU: return 0.5f * g * (1.f + erff(g * 0.707106781f));
-        case PD_ACT_GELU_TANH: return 0.5f * g * (1.f + tanhf(0.797884561f * (g + 0.044715f * g * g * g)));
-        case PD_ACT_SIGMOID: return sigmoid(g);
-        default: return g > 0.f ? g : (g != g ? g : 0.f);
+        case PD_ACT_SILU: return each(g, [](float v) { return v * sigmoid<FINE>(v); });
+        case PD_ACT_GELU: return each(g, [](float v) { return v * normal_below<FINE>(v); });
+        case PD_ACT_GELU_TANH: return each(g, [](float v) { return v * sigmoid<FINE>(twice_inner(v)); });
+        case PD_ACT_SIGMOID: return each(g, [](float v) { return sigmoid<FINE>(v); });
+        default: return each(g, [](float v) { return positive(v); });
     }
 }
-// (act, its slope) at g
-__device__ inline void activate_grad(int act, float g, float& a, float& slope) {
+// act and its slope
+template <bool FINE>
+__device__ __forceinline__ void activate_grad(int act, f32x8 g, f32x8& a, f32x8& slope) {
     switch (act) {
-        case PD_ACT_SILU: {
-            const float s = sigmoid(g);
-            a = g * s;
-            slope = s * (1.f + g * (1.f - s));
+        case PD_ACT_SILU:
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float s = sigmoid<FINE>(g[e]);
+                a[e] = g[e] * s;
+                slope[e] = s * fmaf(g[e], 1.f - s, 1.f);
+            }
             return;
-        }
-        case PD_ACT_GELU: {
-            const float p = 0.5f * (1.f + erff(g * 0.707106781f));
-            a = g * p;
-            slope = p + g * expf(-0.5f * g * g) * 0.398942280f;
+        case PD_ACT_GELU:
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float p = normal_below<FINE>(g[e]), d = e_to<FINE>(-0.5f * g[e] * g[e]);
+                a[e] = g[e] * p;
+                slope[e] = d == 0.f ? p : fmaf(g[e], d * 0.398942280f, p);
+            }
             return;
-        }
-        case PD_ACT_GELU_TANH: {
-            const float t = tanhf(0.797884561f * (g + 0.044715f * g * g * g));
-            a = 0.5f * g * (1.f + t);
-            slope = 0.5f * (1.f + t) + 0.5f * g * (1.f - t * t) * 0.797884561f * (1.f + 0.134145f * g * g);
+        case PD_ACT_GELU_TANH:
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float s = sigmoid<FINE>(twice_inner(g[e])), d = s * (1.f - s);
+                a[e] = g[e] * s;
+                slope[e] = d == 0.f ? s : fmaf(g[e] * d, 1.59576912f * fmaf(0.134145f * g[e], g[e], 1.f), s);
+            }
             return;
-        }
-        case PD_ACT_SIGMOID: {
-            const float s = sigmoid(g);
-            a = s;
-            slope = s * (1.f - s);
+        case PD_ACT_SIGMOID:
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                a[e] = sigmoid<FINE>(g[e]);
+                slope[e] = a[e] * (1.f - a[e]);
+            }
             return;
-        }
         default:
-            a = g > 0.f ? g : (g != g ? g : 0.f);
-            slope = g > 0.f ? 1.f : (g != g ? g : 0.f);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                a[e] = positive(g[e]);
+                slope[e] = g[e] > 0.f ? 1.f : (g[e] != g[e] ? g[e] : 0.f);
+            }
     }
 }
 
@@ -96,18 +150,26 @@ __device__ __forceinline__ void copy16_from(const void* p, uint32_t lds) {
                  : "memory", "m0");
 }
 
-// A tile of ROWS rows of UNITS units of 16 bytes, copied by 256 threads in Tile's order.
-// ACROSS: its rows run along the sum, else its units do.
+// A tile of ROWS rows of UNITS units of 16 bytes, copied by 256 threads.  ACROSS: its rows
+// run along the sum, else its units do.  Units of row r are exchanged by swz(r), so that
+// what a cycle reads (16 rows at one unit; ACROSS: four rows at four neighbouring units)
+// lies in the 16 places of a 256-byte line, which 4, 2 or 1 rows share.
 template <int ROWS, int UNITS, bool ACROSS>
 struct Operand {
-    using Ti = Tile<bf16, UNITS * 8>;
+    static constexpr int kPitch = UNITS * 16;
+    static __device__ __forceinline__ int swz(int row) {
+        if constexpr (UNITS == 4) return (row >> 2) & 3;
+        else if constexpr (UNITS == 8) return ((row & 2) << 1) | ((row >> 2) & 3);
+        else return ((row & 3) << 2) | ((row >> 2) & 3);
+    }
+    static __device__ __forceinline__ int place(int row, int unit) { return row * kPitch + ((unit ^ swz(row)) << 4); }
     static constexpr int kCopies = ROWS * UNITS / 256, kBytes = ROWS * UNITS * 16;
     static_assert(ROWS * UNITS % 256 == 0, "whole copies");
     uint32_t off[kCopies];                 // from the tile's first element
     uint32_t to;
     static __device__ __forceinline__ int row_of(int i, int thread) { return (i * 256 + thread) / UNITS; }
     static __device__ __forceinline__ int unit_of(int i, int thread) {
-        return ((i * 256 + thread) % UNITS) ^ Ti::swz(row_of(i, thread));
+        return ((i * 256 + thread) % UNITS) ^ swz(row_of(i, thread));
     }
     // `left` rows (ACROSS: columns) of the matrix from the tile's first on; copies past
     // them repeat the last: what they meet is not stored
@@ -121,32 +183,27 @@ struct Operand {
         }
         to = __builtin_amdgcn_readfirstlane((thread & ~63) * 16);
     }
-    // the tile at `base`, of whose 64 steps `k` are left
-    __device__ __forceinline__ void copy(const bf16* base, const char* lds, int k, int thread) const {
-        const uint32_t at = __builtin_amdgcn_readfirstlane(lds_address(lds) + to);
-        if (k >= 64) {
-            const uint64_t from = uniform_address(base);
+    // copy i of the tile at `base` (from uniform_address) to `lds` (from lds_address)
+    __device__ __forceinline__ void copy(int i, uint64_t base, uint32_t lds) const { copy16(base, off[i], lds + to + i * 4096); }
+    // the whole tile, of whose values along the sum only `k` are left: zeros past them
+    __device__ __forceinline__ void copy_end(const bf16* base, uint32_t lds, int k, int thread) const {
 #pragma unroll
-            for (int i = 0; i < kCopies; ++i) copy16(from, off[i], at + i * 4096);
-        } else {
-#pragma unroll
-            for (int i = 0; i < kCopies; ++i) {
-                const bool real = ACROSS ? row_of(i, thread) < k : unit_of(i, thread) * 8 < k;
-                copy16_from(real ? reinterpret_cast<const char*>(base) + off[i] : reinterpret_cast<const char*>(kZeros), at + i * 4096);
-            }
+        for (int i = 0; i < kCopies; ++i) {
+            const bool real = ACROSS ? row_of(i, thread) < k : unit_of(i, thread) * 8 < k;
+            copy16_from(real ? reinterpret_cast<const char*>(base) + off[i] : reinterpret_cast<const char*>(kZeros), lds + to + i * 4096);
         }
     }
     // rows (ACROSS: columns) 32 t .. 32 t + 31 as a fragment, step c of 16: lane l has
     // row l % 32 and of the step the eight values from 8 (l / 32)
     static __device__ __forceinline__ bf16x8 read(const char* lds, int t, int c, int lane) {
         if constexpr (!ACROSS) {
-            return Ti::rows(lds, 32 * t, c, lane);
+            return *reinterpret_cast<const bf16x8*>(lds + place(32 * t + (lane & 31), 2 * c + (lane >> 5)));
         } else {
             const int i = lane & 15, row = 16 * c + 8 * (lane >> 5) + (i >> 2);
             const int unit = 4 * t + 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
             typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-            const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + Ti::at(row, unit) + 8 * (i & 1)));
-            const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + Ti::at(row + 4, unit) + 8 * (i & 1)));
+            const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + place(row, unit) + 8 * (i & 1)));
+            const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + place(row + 4, unit) + 8 * (i & 1)));
             typedef short s16x8 __attribute__((ext_vector_type(8)));
             return __builtin_bit_cast(bf16x8, s16x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]});
         }
@@ -156,137 +213,261 @@ struct Operand {
 // ------------------------------------------------------------------ the product
 enum Out { kGated, kStore, kPartial };
 
-// WM x 4/WM waves of 32 MT rows and in each half 16 NT columns.
-template <int MT, int NT, int WM, bool AC, bool BC, Out OUT, typename TO>
-__global__ __launch_bounds__(256) void k_product(const Product p) {
-    constexpr int WN = 4 / WM, BM = 32 * MT * WM, HT = NT / 2, HN = 32 * HT * WN;
-    using A = std::conditional_t<AC, Operand<64, BM / 8, true>, Operand<BM, 8, false>>;
-    using B = std::conditional_t<BC, Operand<64, HN / 8, true>, Operand<HN, 8, false>>;
-    constexpr int kBuffer = A::kBytes + 2 * B::kBytes;
-    __shared__ __attribute__((aligned(256))) char lds[2 * kBuffer];
+// Waits for all copies but the last n; then the barrier: LDS may be read where older copies
+// went, and written where it was read.
+template <int N>
+__device__ __forceinline__ void wait_copies_but() {
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
+// Of a transposed product's registers 8 p .. 8 p + 7, in bfloat16: lanes 0 .. 31 get the
+// eight neighbouring columns from 16 p on, lanes 32 .. 63 those from 16 p + 8 on.
+__device__ __forceinline__ bf16x8 eight_neighbours(const f32x16& v, int p) {
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    const f32x4 lo = {v[8 * p], v[8 * p + 1], v[8 * p + 2], v[8 * p + 3]}, hi = {v[8 * p + 4], v[8 * p + 5], v[8 * p + 6], v[8 * p + 7]};
+    const u32x2 a = __builtin_bit_cast(u32x2, __builtin_convertvector(lo, bf16x4));
+    const u32x2 b = __builtin_bit_cast(u32x2, __builtin_convertvector(hi, bf16x4));
+    const auto s = __builtin_amdgcn_permlane32_swap(a[0], b[0], false, false), t = __builtin_amdgcn_permlane32_swap(a[1], b[1], false, false);
+    return __builtin_bit_cast(bf16x8, u32x4{s[0], t[0], s[1], t[1]});
+}
+
+// WM x 4/WM waves of 32 MT rows and in each half 16 NT columns; BK values along the sum a
+// step, of which BUFS steps are in LDS or on the way.
+template <int MT, int NT, int WM, int BK, int BUFS>
+struct Form {
+    static constexpr int kMT = MT, kNT = NT, kWM = WM, kBK = BK, kBufs = BUFS;
+    static constexpr int BM = 32 * MT * WM, HN = 16 * NT * (4 / WM);
+    static constexpr int kBlocks = MT * NT >= 16 ? 1 : 2;        // a compute unit
+};
+template <class F, bool AC, bool BC, Out OUT, typename TO>
+__global__ __launch_bounds__(256, F::kBlocks) void k_product(const Product p) {
+    constexpr int MT = F::kMT, NT = F::kNT, WM = F::kWM, BK = F::kBK, BUFS = F::kBufs;
+    constexpr int WN = 4 / WM, BM = F::BM, HT = NT / 2, HN = F::HN, KS = BK / 16;
+    using A = std::conditional_t<AC, Operand<BK, BM / 8, true>, Operand<BM, BK / 8, false>>;
+    using B = std::conditional_t<BC, Operand<BK, HN / 8, true>, Operand<HN, BK / 8, false>>;
+    constexpr int kBuffer = A::kBytes + 2 * B::kBytes, kCopies = A::kCopies + 2 * B::kCopies;
+    constexpr int kCols = 32 * HT;                               // of a wave, in each half
+    __shared__ __attribute__((aligned(256))) char lds[BUFS * kBuffer];
     const int thread = threadIdx.x, lane = thread & 63, wave = __builtin_amdgcn_readfirstlane(thread >> 6);
     const int wm = wave / WN, wn = wave % WN;
-    // the block's tile: neighbours on a die share rows of a and columns of b
-    const int per = p.tiles_m * p.tiles_n;
-    int id = near_blocks(blockIdx.x, per * p.groups * p.splits);
-    const int z = id / (per * p.groups);
-    id -= z * per * p.groups;
-    const int group = id / per;
-    id -= group * per;
-    constexpr int kStrip = 4;
-    const int strip = id / (kStrip * p.tiles_n), in = id - strip * kStrip * p.tiles_n;
-    const int high = min(kStrip, p.tiles_m - strip * kStrip);
-    const int m0 = (strip * kStrip + in % high) * BM, tn = in / high;
-    const int n0 = tn * (p.apart ? HN : 2 * HN);                 // first column of the first half
-    const int n1 = p.apart ? n0 : n0 + HN;
-    // steps of this split
-    const int all = p.segs * p.steps, first = (int)((int64_t)all * z / p.splits), last = (int)((int64_t)all * (z + 1) / p.splits);
+    const uint32_t lds0 = lds_address(lds);
+    const int per = p.tiles_m * p.tiles_n, tiles = per * p.groups * p.splits;
+    // a tile of the block's: which split and group, its first row and columns, its steps
+    int z, group, m0, n0, n1, first, last;
+    // the next step to copy: its segment, where in it, its operands, where to
+    int fill_t, fill_s, fill_k, fill_at;
+    uint64_t ua, ub0, ub1;
+    const uint64_t step_a = (AC ? p.lda : 1) * (BK * 2), step_b = (BC ? p.ldb : 1) * (BK * 2);
+    bool two;
     A a;
     B b0, b1;
-    a.plan(p.lda, p.m - m0, thread);
-    b0.plan(p.ldb, p.n - n0, thread);
-    const bool two = n1 < p.n;                                   // (else the second half repeats the first)
-    b1.plan(p.ldb, two ? p.n - n1 : p.n - n0, thread);
-    const auto fill = [&](int t, char* to) {
-        const int s = t / p.steps, k0 = (t - s * p.steps) * 64, k = p.k - k0;
-        a.copy(p.a[s] + group * p.a_group + (AC ? (int64_t)k0 * p.lda + m0 : (int64_t)m0 * p.lda + k0), to, k, thread);
-        b0.copy(p.b0[s] + (BC ? (int64_t)k0 * p.ldb + n0 : (int64_t)n0 * p.ldb + k0), to + A::kBytes, k, thread);
-        const int n = two ? n1 : n0;
-        b1.copy(p.b1[s] + (BC ? (int64_t)k0 * p.ldb + n : (int64_t)n * p.ldb + k0), to + A::kBytes + B::kBytes, k, thread);
+    // neighbours on a die share rows of a and columns of b
+    const auto take = [&](int tile) {
+        int id = near_blocks(tile, tiles);
+        z = id / (per * p.groups);
+        id -= z * per * p.groups;
+        group = id / per;
+        id -= group * per;
+        constexpr int kStrip = 8;
+        const int strip = id / (kStrip * p.tiles_n), in = id - strip * kStrip * p.tiles_n;
+        const int high = min(kStrip, p.tiles_m - strip * kStrip);
+        m0 = (strip * kStrip + in % high) * BM;
+        n0 = in / high * (p.apart ? HN : 2 * HN);
+        n1 = p.apart ? n0 : n0 + HN;
+        const int all = p.segs * p.steps;
+        first = (int)((int64_t)all * z / p.splits);
+        last = (int)((int64_t)all * (z + 1) / p.splits);
+        a.plan(p.lda, p.m - m0, thread);
+        b0.plan(p.ldb, p.n - n0, thread);
+        two = n1 < p.n;                                          // (else the second half repeats the first)
+        b1.plan(p.ldb, two ? p.n - n1 : p.n - n0, thread);
+        fill_t = first;
+        fill_s = first / p.steps;
+        fill_k = (first - fill_s * p.steps) * BK;
+        fill_at = 0;
     };
-    f32x16 acc[MT][NT];
-#pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int j = 0; j < NT; ++j) acc[i][j] = f32x16{};
-    if (first < last) fill(first, lds);
-    wait_copies();
-    lds_barrier();
-    for (int t = first; t < last; ++t) {
-        const char* now = lds + ((t - first) & 1) * kBuffer;
-        if (t + 1 < last) fill(t + 1, lds + ((t - first + 1) & 1) * kBuffer);
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            bf16x8 fa[MT], fb[NT];
-#pragma unroll
-            for (int i = 0; i < MT; ++i) fa[i] = A::read(now, wm * MT + i, c, lane);
-#pragma unroll
-            for (int j = 0; j < NT; ++j) fb[j] = B::read(now + A::kBytes + (j / HT) * B::kBytes, wn * HT + j % HT, c, lane);
-#pragma unroll
-            for (int i = 0; i < MT; ++i)
-#pragma unroll
-                for (int j = 0; j < NT; ++j) acc[i][j] = mma(fa[i], fb[j], acc[i][j]);
+    // The operands' addresses stay in scalar registers from step to step: reading the segment's
+    // from memory for each took a tenth of a step.
+    const auto aim = [&] {
+        const int n = two ? n1 : n0;
+        ua = uniform_address(p.a[fill_s] + group * p.a_group + (AC ? (int64_t)fill_k * p.lda + m0 : (int64_t)m0 * p.lda + fill_k));
+        ub0 = uniform_address(p.b0[fill_s] + (BC ? (int64_t)fill_k * p.ldb + n0 : (int64_t)n0 * p.ldb + fill_k));
+        ub1 = uniform_address(p.b1[fill_s] + (BC ? (int64_t)fill_k * p.ldb + n : (int64_t)n * p.ldb + fill_k));
+    };
+    uint32_t to = 0;
+    // the next step's copies are done with
+    const auto advance = [&] {
+        ++fill_t;
+        fill_at = fill_at + 1 == BUFS ? 0 : fill_at + 1;
+        fill_k += BK;
+        ua += step_a, ub0 += step_b, ub1 += step_b;
+        if (fill_k >= p.steps * BK) {
+            fill_k = 0;
+            ++fill_s;
+            if (fill_t < last) aim();
         }
-        wait_copies();
-        lds_barrier();
-    }
-    // results, 32 rows of the wave at a time through LDS, so that a lane has eight neighbours
-    // of a row (in a product's result it has one column)
-    constexpr int kCols = 32 * HT, kPitch = 2 * kCols + 4;       // floats: both halves, and 4 against bank conflicts
-    static_assert(4 * 32 * kPitch * 4 <= 2 * kBuffer, "four waves' rows fit");
-    float* stage = reinterpret_cast<float*>(lds) + wave * 32 * kPitch;
-    const int unit = lane % (kCols / 8), sub = lane / (kCols / 8);
-    const int at0 = n0 + wn * kCols + 8 * unit, at1 = n1 + wn * kCols + 8 * unit;
-    const int left0 = p.n - at0, left1 = p.n - at1;
-#pragma unroll
-    for (int i = 0; i < MT; ++i) {
-#pragma unroll
-        for (int j = 0; j < NT; ++j)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) stage[tile_row(lane, r) * kPitch + 32 * j + (lane & 31)] = acc[i][j][r];
+    };
+    // begins a step's copies; true: copy(i) does them one by one, then advance() (else they are
+    // done here)
+    const auto begin = [&]() -> bool {
+        to = __builtin_amdgcn_readfirstlane(lds0 + fill_at * kBuffer);
+        const int k = p.k - fill_k;
+        if (k >= BK) return true;
+        a.copy_end(reinterpret_cast<const bf16*>(ua), to, k, thread);
+        b0.copy_end(reinterpret_cast<const bf16*>(ub0), to + A::kBytes, k, thread);
+        b1.copy_end(reinterpret_cast<const bf16*>(ub1), to + A::kBytes + B::kBytes, k, thread);
+        advance();
+        return false;
+    };
+    const auto copy = [&](int i) {
+        if (i < A::kCopies) a.copy(i, ua, to);
+        else if (i < A::kCopies + B::kCopies) b0.copy(i - A::kCopies, ub0, to + A::kBytes);
+        else b1.copy(i - A::kCopies - B::kCopies, ub1, to + A::kBytes + B::kBytes);
+    };
+    const auto fill_all = [&] {
+        aim();
 #pragma unroll 1
-        for (int r0 = sub; r0 < 32; r0 += 64 / (kCols / 8)) {
-            const int64_t row = m0 + (wm * MT + i) * 32 + r0;
-            if (row >= p.m) break;
-            const f32x4* from = reinterpret_cast<const f32x4*>(stage + r0 * kPitch + 8 * unit);
-            const f32x4 g0 = from[0], g1 = from[1], u0 = from[kCols / 4], u1 = from[kCols / 4 + 1];
-            const f32x8 v0 = {g0[0], g0[1], g0[2], g0[3], g1[0], g1[1], g1[2], g1[3]};
-            const f32x8 v1 = {u0[0], u0[1], u0[2], u0[3], u1[0], u1[1], u1[2], u1[3]};
-            if constexpr (OUT == kGated) {
-                if (left0 <= 0) break;
-                f32x8 h;
+        for (int i = 0; i < BUFS; ++i)
+            if (fill_t < last && begin()) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) h[e] = activate(p.act, v0[e]) * v1[e];
-                store8(static_cast<TO*>(p.c[0]) + row * p.ldc[0] + at0, left0, narrow<TO>(h));
-                if (p.gate) store8(static_cast<TO*>(p.gate) + row * p.ld_gate + at0, left0, narrow<TO>(v0));
-                if (p.up) store8(static_cast<TO*>(p.up) + row * p.ld_up + at0, left0, narrow<TO>(v1));
-            } else {
-                const int h0 = p.apart ? 0 : group, h1 = p.apart ? 1 : group;
-                TO *to0, *to1;
-                if constexpr (OUT == kStore) {
-                    to0 = static_cast<TO*>(p.c[h0]) + row * p.ldc[h0];
-                    to1 = static_cast<TO*>(p.c[h1]) + row * p.ldc[h1];
-                } else {
-                    const int64_t size = (int64_t)p.m * p.n, count = p.apart ? 2 : p.groups;
-                    to0 = p.partial + (z * count + h0) * size + row * p.n;
-                    to1 = p.partial + (z * count + h1) * size + row * p.n;
+                for (int j = 0; j < kCopies; ++j) copy(j);
+                advance();
+            }
+    };
+    take(blockIdx.x);
+    fill_all();
+    wait_copies();
+    for (int tile = blockIdx.x;;) {
+        // here the tile's first steps have come
+        lds_barrier();
+        f32x16 acc[MT][NT];
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) acc[i][j] = f32x16{};
+        bf16x8 fa[2][MT], fb[2][NT];
+        const auto read = [&](const char* from, int c, int to, int i) {      // fragment i of step c
+            if (i < MT) fa[to][i] = A::read(from, wm * MT + i, c, lane);
+            else fb[to][i - MT] = B::read(from + A::kBytes + ((i - MT) / HT) * B::kBytes, wn * HT + (i - MT) % HT, c, lane);
+        };
+#pragma unroll
+        for (int i = 0; i < MT + NT; ++i) read(lds, 0, 0, i);
+        int now = 0;
+#pragma unroll 1
+        for (int t = first; t < last; ++t) {
+            const char* here = lds + now * kBuffer;
+            now = now + 1 == BUFS ? 0 : now + 1;
+            const char* next = lds + now * kBuffer;
+#pragma unroll
+            for (int c = 0; c < KS; ++c) {
+                bool more = false;
+                if (c == KS - 1) {
+                    // this step's fragments are all in registers, its place is free; the next one's must be there
+                    if (t + BUFS <= last) wait_copies_but<(BUFS - 2) * kCopies>();
+                    else wait_copies();
+                    lds_barrier();
+                    if (fill_t < last) more = begin();
                 }
-                if (left0 > 0) store8(to0 + at0, left0, narrow<TO>(v0));
-                if (left1 > 0) store8(to1 + at1, left1, narrow<TO>(v1));
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int i = 0; i < MT * NT; ++i) {
+                    acc[i / NT][i % NT] = mma(fb[c & 1][i % NT], fa[c & 1][i / NT], acc[i / NT][i % NT]);
+                    // under the products: the next fragments, and the next copies
+                    if (i < MT + NT) read(c == KS - 1 ? next : here, c == KS - 1 ? 0 : c + 1, (c + 1) & 1, i);
+                    if (c == KS - 1 && i < kCopies && more) copy(i);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                if (c == KS - 1 && more) {
+#pragma unroll
+                    for (int i = MT * NT; i < kCopies; ++i) copy(i);
+                    advance();
+                }
+#pragma unroll
+                for (int i = MT * NT; i < MT + NT; ++i) read(c == KS - 1 ? next : here, c == KS - 1 ? 0 : c + 1, (c + 1) & 1, i);
             }
         }
+        lds_barrier();
+        // the next tile's first steps come while this one's results go
+        const int row0 = m0 + wm * MT * 32, at_z = z, at_group = group, at_n0 = n0 + wn * kCols, at_n1 = n1 + wn * kCols;
+        tile += gridDim.x;
+        const bool go_on = tile < tiles;
+        if (go_on) {
+            take(tile);
+            fill_all();
+        }
+        // results: the products are formed transposed, so lane l has row l % 32 and in registers
+        // 4 q .. 4 q + 3 columns 8 q + 4 (l / 32) ..; for bfloat16 halves of the wave exchange
+        // two such fours
+        constexpr int kSpan = sizeof(TO) == 2 ? 8 : 4;           // values a store: 16 bytes
+        const int lane_row = row0 + (lane & 31), lane_col = kSpan * (lane >> 5);
+        const auto emit = [&](const f32x16& v, int i, int j, TO* to, int64_t ld, int at) {
+            TO* mine = to + lane_row * ld + (at + lane_col) + 32 * i * ld + 32 * j;
+#pragma unroll
+            for (int s = 0; s < 16 / kSpan; ++s) {
+                const int left = p.n - at - lane_col - 32 * j - 2 * kSpan * s;
+                const bool real = lane_row + 32 * i < p.m && left > 0;
+                if constexpr (sizeof(TO) == 2) {
+                    const bf16x8 w = eight_neighbours(v, s);     // (all lanes)
+                    if (real) store8(mine + 2 * kSpan * s, left, w);
+                } else if (real) {
+                    store4(mine + 2 * kSpan * s, left, f32x4{v[4 * s], v[4 * s + 1], v[4 * s + 2], v[4 * s + 3]});
+                }
+            }
+        };
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+#pragma unroll
+            for (int j = 0; j < HT; ++j) {
+                const f32x16 v0 = acc[i][j], v1 = acc[i][j + HT];
+                if constexpr (OUT == kGated) {
+                    if (p.gate) emit(v0, i, j, static_cast<TO*>(p.gate), p.ld_gate, at_n0);
+                    if (p.up) emit(v1, i, j, static_cast<TO*>(p.up), p.ld_up, at_n0);
+                    emit(activate<sizeof(TO) == 4>(p.act, v0) * v1, i, j, static_cast<TO*>(p.c[0]), p.ldc[0], at_n0);
+                } else {
+                    const int h0 = p.apart ? 0 : at_group, h1 = p.apart ? 1 : at_group;
+                    if constexpr (OUT == kStore) {
+                        emit(v0, i, j, static_cast<TO*>(p.c[h0]), p.ldc[h0], at_n0);
+                        emit(v1, i, j, static_cast<TO*>(p.c[h1]), p.ldc[h1], at_n1);
+                    } else {
+                        const int64_t size = (int64_t)p.m * p.n, count = p.apart ? 2 : p.groups;
+                        emit(v0, i, j, p.partial + (at_z * count + h0) * size, p.n, at_n0);
+                        emit(v1, i, j, p.partial + (at_z * count + h1) * size, p.n, at_n1);
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);               // (one tile's results in registers at a time)
+            }
+            // (the copies have had time, the stores to come are not waited for)
+            if (i == (MT - 1) / 2) wait_copies();
+        }
+        if (!go_on) return;
     }
 }
 
-// The splits' sums together, in their order, and what comes after them.
+// The splits' sums together, in their order, and what comes after them: eight columns a
+// lane.
 template <bool GATED, typename TO>
 __global__ __launch_bounds__(256) void k_product_join(const Product p) {
+    const int per = (p.n + 7) / 8;
     const int64_t size = (int64_t)p.m * p.n, each = (p.apart ? 2 : p.groups) * size;
-    const int64_t count = GATED ? size : each;
+    const int64_t units = (int64_t)p.m * per, count = GATED ? units : (p.apart ? 2 : p.groups) * units;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < count; i += (int64_t)gridDim.x * 256) {
-        const int64_t matrix = i / size, in = i - matrix * size, row = in / p.n;
-        const int n = (int)(in - row * p.n);
-        float v0 = 0.f, v1 = 0.f;
+        const int64_t matrix = i / units, in = i - matrix * units, row = in / per;
+        const int at = (int)(in - row * per) * 8, n = p.n - at;
+        const float* from = p.partial + matrix * size + row * p.n + at;
+        f32x8 v0 = {}, v1 = {};
+#pragma unroll 4
         for (int z = 0; z < p.splits; ++z) {
-            v0 += p.partial[z * each + i];
-            if (GATED) v1 += p.partial[z * each + size + i];
+            v0 += load8(from + z * each, n);
+            if (GATED) v1 += load8(from + z * each + size, n);
         }
         if constexpr (GATED) {
-            static_cast<TO*>(p.c[0])[row * p.ldc[0] + n] = (TO)(activate(p.act, v0) * v1);
-            if (p.gate) static_cast<TO*>(p.gate)[row * p.ld_gate + n] = (TO)v0;
-            if (p.up) static_cast<TO*>(p.up)[row * p.ld_up + n] = (TO)v1;
+            const f32x8 h = activate<sizeof(TO) == 4>(p.act, v0) * v1;
+            store8(static_cast<TO*>(p.c[0]) + row * p.ldc[0] + at, n, narrow<TO>(h));
+            if (p.gate) store8(static_cast<TO*>(p.gate) + row * p.ld_gate + at, n, narrow<TO>(v0));
+            if (p.up) store8(static_cast<TO*>(p.up) + row * p.ld_up + at, n, narrow<TO>(v1));
         } else {
-            static_cast<TO*>(p.c[matrix])[row * p.ldc[matrix] + n] = (TO)v0;
+            store8(static_cast<TO*>(p.c[matrix]) + row * p.ldc[matrix] + at, n, narrow<TO>(v0));
         }
     }
 }
@@ -348,21 +529,16 @@ __global__ __launch_bounds__(256) void k_gated_slopes(const SlopeArgs a) {
     for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < units; u += (int64_t)gridDim.x * 256) {
         const int64_t row = u / (a.pitch / 8);
         const int c = (int)(u - row * (a.pitch / 8)) * 8, n = a.cols - c;
-        f32x8 dg = {}, du = {}, h = {};
+        f32x8 dg = {}, du = {};
         if (n > 0) {
             const f32x8 g = widen(load8(static_cast<const T*>(a.gate) + row * a.ld_gate + c, n));
             const f32x8 up = widen(load8(static_cast<const T*>(a.up) + row * a.ld_up + c, n));
             const f32x8 dh = widen(load8(static_cast<const T*>(a.dh) + row * a.ld_dh + c, n));
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                if (e >= n) continue;
-                float act, slope;
-                activate_grad(a.act, g[e], act, slope);
-                dg[e] = dh[e] * up[e] * slope;
-                du[e] = dh[e] * act;
-                h[e] = act * up[e];
-            }
-            if (a.h) store8(static_cast<T*>(a.h) + row * a.ld_h + c, n, narrow<T>(h));
+            f32x8 act, slope;
+            activate_grad<sizeof(T) == 4>(a.act, g, act, slope);
+            dg = dh * up * slope;            // (past the row's end dh and up are 0, slope is finite)
+            du = dh * act;
+            if (a.h) store8(static_cast<T*>(a.h) + row * a.ld_h + c, n, narrow<T>(act * up));
         }
         if (!a.dg) continue;
         bf16* to = a.dg + row * a.pitch + c;
@@ -420,28 +596,58 @@ void add_segments(Product& p, int dtype, const Matrix& a, const Matrix& b0, cons
     p.ldb = b0.ld;
 }
 
-// How a product is cut: the block's shape, and into how many sums.
-enum Shape { kLarge, kSmall, kFew };
+// How a product is cut: the block's form, and into how many sums.
+using Large = Form<4, 4, 2, 64, 2>;       // 256 x 256, one block a compute unit
+using Medium = Form<2, 4, 2, 32, 3>;      // 128 x 256, two blocks
+using Small = Form<2, 2, 2, 64, 2>;       // 128 x 128, two blocks
+using Few = Form<1, 2, 1, 64, 2>;         // 32 x 256, two blocks
+enum Shape { kLarge, kMedium, kSmall, kFew, kShapes };
+// What a round of blocks takes, in us: of a step of 64 and beside its steps; measured on
+// 36864 x 1024 x 4096 and 8192 x 4096 x 4096 (`alone`: of a step where a unit has one block).
+struct Cost {
+    int bm, hn, bk, slots;
+    double step, alone, fixed;
+};
+constexpr Cost kCost[kShapes] = {
+    {Large::BM, Large::HN, Large::kBK, kCus, 1.64, 1.64, 6.8},
+    {Medium::BM, Medium::HN, Medium::kBK, 2 * kCus, 1.75, 1.0, 5.5},
+    {Small::BM, Small::HN, Small::kBK, 2 * kCus, 0.95, 0.65, 3.4},
+    {Few::BM, Few::HN, Few::kBK, 2 * kCus, 0.6, 0.4, 3.0},
+};
 struct Cut {
     Shape shape;
-    int tiles_m, tiles_n, splits;
+    int tiles_m, tiles_n, splits, steps;
 };
-Cut cut(int64_t m, int64_t n, bool apart, int groups, int64_t steps, bool across) {
-    static const int bm[3] = {256, 128, 32}, hn[3] = {128, 64, 128};
-    Cut c{};
-    const auto tiles = [&](Shape s) {
-        c.shape = s;
-        c.tiles_m = (int)((m + bm[s] - 1) / bm[s]);
-        const int wide = apart ? hn[s] : 2 * hn[s];
+Cut cut(int64_t m, int64_t n, bool apart, int groups, int64_t k, int segs, bool across) {
+    Cut best{};
+    double least = 1e30;
+    for (int shape = 0; shape < kShapes; ++shape) {
+        if (shape == kFew ? across || m > 64 : m <= 32 && !across) continue;      // (`across`: a runs across the sum)
+        const Cost& f = kCost[shape];
+        Cut c{};
+        c.shape = (Shape)shape;
+        c.tiles_m = (int)((m + f.bm - 1) / f.bm);
+        const int wide = apart ? f.hn : 2 * f.hn;
         c.tiles_n = (int)((n + wide - 1) / wide);
-        return (int64_t)c.tiles_m * c.tiles_n * groups;
-    };
-    int64_t count;
-    if (m <= 32 && !across) count = tiles(kFew);        // (`across`: a runs across the sum)
-    else if ((count = tiles(kLarge)) < kCus) count = tiles(kSmall);
-    c.splits = 1;
-    while (count * c.splits * 2 <= 2 * kCus && steps / (c.splits * 2) >= 4) c.splits *= 2;
-    return c;
+        c.steps = (int)((k + f.bk - 1) / f.bk);
+        const int64_t tiles = (int64_t)c.tiles_m * c.tiles_n * groups;
+        const double steps = (double)c.steps * segs * f.bk / 64;
+        static const int kSplits[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32};
+        for (int s : kSplits) {
+            if (s > 1 && (steps / s < 4 || tiles * (s - 1) >= 4 * kCus)) break;
+            const int64_t blocks = tiles * s, rounds = blocks / f.slots, rest = blocks % f.slots;
+            double t = (double)rounds * (steps / s * f.step + f.fixed);
+            if (rest) t += steps / s * (rest <= kCus ? f.alone : f.step) + f.fixed;
+            // the sums go to memory and are read again
+            if (s > 1) t += 4 + 8e-6 * s * (double)m * (double)n * (apart ? 2 : groups) / 4;
+            if (t < least) {
+                least = t;
+                best = c;
+                best.splits = s;
+            }
+        }
+    }
+    return best;
 }
 int64_t partial_bytes(const Cut& c, int64_t m, int64_t n, bool apart, int groups) {
     return c.splits == 1 ? 0 : (int64_t)c.splits * groups * (apart ? 2 : 1) * m * n * 4;
@@ -449,24 +655,28 @@ int64_t partial_bytes(const Cut& c, int64_t m, int64_t n, bool apart, int groups
 
 template <bool AC, bool BC, Out OUT, typename TO>
 void launch_shape(const Product& p, Shape shape, hipStream_t s) {
-    const dim3 grid((unsigned)(p.tiles_m * p.tiles_n * p.groups * p.splits)), block(256);
+    // blocks that are on the chip together take tile after tile
+    const int tiles = p.tiles_m * p.tiles_n * p.groups * p.splits, most = kCost[shape].slots;
+    const dim3 grid((unsigned)(tiles < most ? tiles : most)), block(256);
     if (shape == kLarge)
-        hipLaunchKernelGGL((k_product<4, 4, 2, AC, BC, OUT, TO>), grid, block, 0, s, p);
+        hipLaunchKernelGGL((k_product<Large, AC, BC, OUT, TO>), grid, block, 0, s, p);
+    else if (shape == kMedium)
+        hipLaunchKernelGGL((k_product<Medium, AC, BC, OUT, TO>), grid, block, 0, s, p);
     else if (shape == kSmall)
-        hipLaunchKernelGGL((k_product<2, 2, 2, AC, BC, OUT, TO>), grid, block, 0, s, p);
+        hipLaunchKernelGGL((k_product<Small, AC, BC, OUT, TO>), grid, block, 0, s, p);
     else if constexpr (!AC)
-        hipLaunchKernelGGL((k_product<1, 2, 1, AC, BC, OUT, TO>), grid, block, 0, s, p);
+        hipLaunchKernelGGL((k_product<Few, AC, BC, OUT, TO>), grid, block, 0, s, p);
     PD_HIP(hipGetLastError());
 }
 template <bool AC, bool BC, bool GATED, typename TO>
 void launch_product(Product& p, float* partial, hipStream_t s) {
-    p.steps = (p.k + 63) / 64;
-    const Cut c = cut(p.m, p.n, p.apart, p.groups, (int64_t)p.steps * p.segs, AC);
+    const Cut c = cut(p.m, p.n, p.apart, p.groups, p.k, p.segs, AC);
+    p.steps = c.steps;
     p.tiles_m = c.tiles_m, p.tiles_n = c.tiles_n, p.splits = c.splits;
     p.partial = partial;
     if (c.splits == 1) return launch_shape<AC, BC, GATED ? kGated : kStore, TO>(p, c.shape, s);
     launch_shape<AC, BC, kPartial, float>(p, c.shape, s);
-    hipLaunchKernelGGL((k_product_join<GATED, TO>), dim3(blocks_for((int64_t)p.m * p.n * (GATED || !p.apart ? 1 : 2) * p.groups)),
+    hipLaunchKernelGGL((k_product_join<GATED, TO>), dim3(blocks_for((int64_t)p.m * ((p.n + 7) / 8) * (GATED || !p.apart ? 1 : 2) * p.groups)),
                        dim3(256), 0, s, p);
     PD_HIP(hipGetLastError());
 }
@@ -484,12 +694,12 @@ Layout layout(const pd_gated_desc& d, bool backward) {
         at += up_to(bytes, 256);
         return here;
     };
-    const int64_t segs = d.dtype == PD_F32 ? 6 : 1;
+    const int segs = d.dtype == PD_F32 ? 6 : 1;
     l.x = take(layout_bytes(d.dtype, d.rows, d.width));
     l.w = take(2 * (in_out ? layout_bytes(d.dtype, d.width, d.hidden) : layout_bytes(d.dtype, d.hidden, d.width)));
     int64_t partial = 0;
-    const auto more = [&](int64_t m, int64_t n, bool apart, int groups, int64_t k, int64_t s, bool across) {
-        const int64_t b = partial_bytes(cut(m, n, apart, groups, (k + 63) / 64 * s, across), m, n, apart, groups);
+    const auto more = [&](int64_t m, int64_t n, bool apart, int groups, int64_t k, int segs, bool across) {
+        const int64_t b = partial_bytes(cut(m, n, apart, groups, k, segs, across), m, n, apart, groups);
         partial = b > partial ? b : partial;
     };
     if (!backward) {
