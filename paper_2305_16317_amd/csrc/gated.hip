@@ -53,11 +53,11 @@ template <bool FINE>
 __device__ __forceinline__ float sigmoid(float x) {
     return __builtin_amdgcn_rcpf(1.f + e_to<FINE>(-x));
 }
-// The normal distribution function: for x = |g| / sqrt 2, erfc x = e^(-x^2) t Q(t) with
+// The normal distribution's part past |g|: for x = |g| / sqrt 2, erfc x = e^(-x^2) t Q(t) with
 // t = 1 / (1 + 0.3 x); Q is fitted to e^(x^2) erfc(x) / t over 0 <= x <= 10 with relative errors
 // up to 2e-8 (past it the exponential is 0).
 template <bool FINE>
-__device__ __forceinline__ float normal_below(float g) {
+__device__ __forceinline__ float normal_past(float g) {
     const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(g), 0.212132034f, 1.f));
     float q = -0.12952314f;
     q = fmaf(q, t, 0.48556441f);
@@ -68,8 +68,7 @@ __device__ __forceinline__ float normal_below(float g) {
     q = fmaf(q, t, 0.14833886f);
     q = fmaf(q, t, 0.17071527f);
     q = fmaf(q, t, 0.169188f);
-    const float tail = 0.5f * e_to<FINE>(-0.5f * g * g) * (q * t);
-    return g < 0.f ? tail : 1.f - tail;
+    return 0.5f * e_to<FINE>(-0.5f * g * g) * (q * t);
 }
 // 2 sqrt(2/pi) (g + 0.044715 g^3), of which gelu's tanh form takes the sigmoid
 __device__ __forceinline__ float twice_inner(float g) { return 1.59576912f * fmaf(0.044715f * g * g, g, g); }
@@ -86,7 +85,7 @@ template <bool FINE, class V>
 __device__ __forceinline__ V activate(int act, V g) {
     switch (act) {
         case PD_ACT_SILU: return each(g, [](float v) { return v * sigmoid<FINE>(v); });
-        case PD_ACT_GELU: return each(g, [](float v) { return v * normal_below<FINE>(v); });
+        case PD_ACT_GELU: return each(g, [](float v) { return fmaf(-fabsf(v), normal_past<FINE>(v), fmaxf(v, 0.f)); });
         case PD_ACT_GELU_TANH: return each(g, [](float v) { return v * sigmoid<FINE>(twice_inner(v)); });
         case PD_ACT_SIGMOID: return each(g, [](float v) { return sigmoid<FINE>(v); });
         default: return each(g, [](float v) { return positive(v); });
@@ -107,7 +106,7 @@ __device__ __forceinline__ void activate_grad(int act, f32x8 g, f32x8& a, f32x8&
         case PD_ACT_GELU:
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float p = normal_below<FINE>(g[e]), d = e_to<FINE>(-0.5f * g[e] * g[e]);
+                const float tail = normal_past<FINE>(g[e]), p = g[e] < 0.f ? tail : 1.f - tail, d = e_to<FINE>(-0.5f * g[e] * g[e]);
                 a[e] = g[e] * p;
                 slope[e] = d == 0.f ? p : fmaf(g[e], d * 0.398942280f, p);
             }
@@ -472,6 +471,140 @@ __global__ __launch_bounds__(256) void k_product_join(const Product p) {
     }
 }
 
+// ------------------------------------------------------------------ few rows
+// Up to 32 rows (a token of each of some sequences): bound by the weights, which are read
+// once.  A block takes 32 columns of gate and of up; each of its four waves takes every
+// fourth 128 bytes along the sum (64 values, or 32 in float32) through LDS of its own, three
+// such steps on the way, and the four join in LDS: one launch and no barrier before the end.
+// float32 runs on float32's own matrix instructions.
+// A step's tile of one operand: 4 KB, which a wave copies.  ACROSS: its rows run along the sum.
+template <typename T, bool ACROSS>
+struct FewTile {
+    static constexpr int E = 16 / (int)sizeof(T), KT = 8 * E;             // values a unit; of the sum a tile
+    static constexpr int UNITS = ACROSS ? 32 / E : 8;
+    using Ti = Operand<256, UNITS, ACROSS>;                                // (its order in LDS)
+    // `left`: rows (ACROSS: columns) from the tile's first on, repeated past the last; k: values
+    // of the sum, zeros past the last.  COPY: 16 bytes a lane past the registers.
+    template <bool COPY>
+    static __device__ __forceinline__ void fill(const T* base, int64_t stride, int left, int k, char* lds, int lane) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int at = i * 64 + lane;
+            int row = at / UNITS, unit = (at % UNITS) ^ Ti::swz(row);
+            if constexpr (COPY) {
+                const bool real = ACROSS ? row < k : unit * E < k;
+                if (ACROSS) unit = min(unit, (left + E - 1) / E - 1);
+                else row = min(row, left - 1);
+                copy16_from(real ? reinterpret_cast<const char*>(base + row * stride + unit * E) : reinterpret_cast<const char*>(kZeros),
+                            __builtin_amdgcn_readfirstlane(lds_address(lds) + i * 1024));
+            } else {
+                const int n = ACROSS ? (row < k ? left - unit * E : 0) : (row < left ? k - unit * E : 0);
+                T v[E];
+#pragma unroll
+                for (int e = 0; e < E; ++e) v[e] = e < n ? base[row * stride + unit * E + e] : (T)0.f;
+                typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+                u32x4 w;
+                __builtin_memcpy(&w, v, 16);
+                *reinterpret_cast<u32x4*>(lds + Ti::place(row, unit)) = w;
+            }
+        }
+    }
+    // step c of 16 as a fragment
+    static __device__ __forceinline__ Frag<T> read(const char* lds, int c, int lane) {
+        if constexpr (sizeof(T) == 2) {
+            return Ti::read(lds, 0, c, lane);
+        } else if constexpr (!ACROSS) {
+            const int row = lane & 31, unit = 4 * c + 2 * (lane >> 5);
+            const f32x4 a = *reinterpret_cast<const f32x4*>(lds + Ti::place(row, unit));
+            const f32x4 b = *reinterpret_cast<const f32x4*>(lds + Ti::place(row, unit + 1));
+            return f32x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+        } else {
+            f32x8 f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                f[e] = *reinterpret_cast<const float*>(lds + Ti::place(16 * c + 8 * (lane >> 5) + e, (lane & 31) >> 2) + 4 * (lane & 3));
+            return f;
+        }
+    }
+};
+struct FewArgs {
+    const void* x;
+    const void* w_gate;
+    const void* w_up;
+    void* h;
+    void* gate;
+    void* up;
+    int64_t ld_x, ld_gate_w, ld_up_w, ld_h, ld_gate, ld_up;
+    int rows, width, hidden, act;
+};
+template <typename T, bool ACROSS, bool COPY>
+__global__ __launch_bounds__(256) void k_gated_few(const FewArgs p) {
+    using X = FewTile<T, false>;
+    using W = FewTile<T, ACROSS>;
+    constexpr int kSlots = 3, kTile = 4096, kSlot = 3 * kTile, kCopies = 12, KT = X::KT;
+    __shared__ __attribute__((aligned(256))) char lds[4 * kSlots * kSlot];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    char* mine = lds + wave * kSlots * kSlot;
+    const int n0 = near_blocks(blockIdx.x, gridDim.x) * 32;
+    const int steps = (p.width + KT - 1) / KT, count = steps > wave ? (steps - wave + 3) / 4 : 0;     // this wave's
+    const auto fill = [&](int t) {
+        const int k0 = (wave + 4 * t) * KT, k = p.width - k0;
+        char* to = mine + t % kSlots * kSlot;
+        X::template fill<COPY>(static_cast<const T*>(p.x) + k0, p.ld_x, p.rows, k, to, lane);
+        const T* wg = static_cast<const T*>(p.w_gate) + (ACROSS ? k0 * p.ld_gate_w + n0 : n0 * p.ld_gate_w + k0);
+        const T* wu = static_cast<const T*>(p.w_up) + (ACROSS ? k0 * p.ld_up_w + n0 : n0 * p.ld_up_w + k0);
+        W::template fill<COPY>(wg, p.ld_gate_w, p.hidden - n0, k, to + kTile, lane);
+        W::template fill<COPY>(wu, p.ld_up_w, p.hidden - n0, k, to + 2 * kTile, lane);
+    };
+    f32x16 g = {}, u = {};
+#pragma unroll 1
+    for (int t = 0; t < kSlots && t < count; ++t) fill(t);
+#pragma unroll 1
+    for (int t = 0; t < count; ++t) {
+        if constexpr (COPY) {
+            if (t + 2 < count) wait_copies_but<2 * kCopies>();
+            else if (t + 1 < count) wait_copies_but<kCopies>();
+            else wait_copies();
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        const char* from = mine + t % kSlots * kSlot;
+#pragma unroll
+        for (int c = 0; c < KT / 16; ++c) {
+            const Frag<T> x = X::read(from, c, lane);
+            g = mma(W::read(from + kTile, c, lane), x, g);
+            u = mma(W::read(from + 2 * kTile, c, lane), x, u);
+        }
+        if (t + kSlots < count) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // the slot has been read
+            fill(t + kSlots);
+        }
+    }
+    // the four sums of [row][column], gate then up, 36 values apart
+    __syncthreads();
+    float* sums = reinterpret_cast<float*>(lds);
+    constexpr int kPitch = 36, kMatrix = 32 * kPitch;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        float* to = sums + wave * 2 * kMatrix + (lane & 31) * kPitch + 8 * q + 4 * (lane >> 5);
+        *reinterpret_cast<f32x4*>(to) = f32x4{g[4 * q], g[4 * q + 1], g[4 * q + 2], g[4 * q + 3]};
+        *reinterpret_cast<f32x4*>(to + kMatrix) = f32x4{u[4 * q], u[4 * q + 1], u[4 * q + 2], u[4 * q + 3]};
+    }
+    __syncthreads();
+    const int row = threadIdx.x >> 3, col = 4 * (threadIdx.x & 7), left = p.hidden - n0 - col;
+    if (row >= p.rows || left <= 0) return;
+    f32x4 vg = {}, vu = {};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        const float* from = sums + w * 2 * kMatrix + row * kPitch + col;
+        vg += *reinterpret_cast<const f32x4*>(from);
+        vu += *reinterpret_cast<const f32x4*>(from + kMatrix);
+    }
+    const f32x4 h = activate<sizeof(T) == 4>(p.act, vg) * vu;
+    store4(static_cast<T*>(p.h) + row * p.ld_h + n0 + col, left, h);
+    if (p.gate) store4(static_cast<T*>(p.gate) + row * p.ld_gate + n0 + col, left, vg);
+    if (p.up) store4(static_cast<T*>(p.up) + row * p.ld_up + n0 + col, left, vu);
+}
+
 // ------------------------------------------------------------------ layouts
 // A float32 in three parts, as split() makes them, but that values past the largest bfloat16
 // (3.39e38) keep a finite first part.
@@ -731,9 +864,31 @@ void weights(const GatedArgs& a, const Layout& l, Matrix& gate, Matrix& up, hipS
     up = laid_out(d.dtype, a.w_up, d.w_up_stride, rows, cols, a.scratch + l.w + layout_bytes(d.dtype, rows, cols), s, lie);
 }
 
+constexpr int64_t kFewRows = 32;
+template <typename T>
+void gated_few(const GatedArgs& a, hipStream_t s) {
+    const pd_gated_desc& d = a.d;
+    const bool in_out = d.weight_layout == PD_WEIGHTS_IN_OUT;
+    const int64_t wr = in_out ? d.width : d.hidden, wc = in_out ? d.hidden : d.width;
+    const auto whole = [](const void* p, int64_t stride, int64_t rows, int64_t cols) {
+        return (uintptr_t)p % 16 == 0 && cols * sizeof(T) % 16 == 0 && (rows == 1 || stride * sizeof(T) % 16 == 0);
+    };
+    const bool copy = whole(a.x, d.x_stride, d.rows, d.width) && whole(a.w_gate, d.w_gate_stride, wr, wc) &&
+                      whole(a.w_up, d.w_up_stride, wr, wc);
+    const FewArgs p{a.x, a.w_gate, a.w_up, a.h, a.gate, a.up, d.x_stride, d.w_gate_stride, d.w_up_stride, d.h_stride, d.gate_stride,
+                    d.up_stride, (int)d.rows, d.width, d.hidden, d.activation};
+    const dim3 grid((unsigned)((d.hidden + 31) / 32)), block(256);
+    if (in_out && copy) hipLaunchKernelGGL((k_gated_few<T, true, true>), grid, block, 0, s, p);
+    else if (in_out) hipLaunchKernelGGL((k_gated_few<T, true, false>), grid, block, 0, s, p);
+    else if (copy) hipLaunchKernelGGL((k_gated_few<T, false, true>), grid, block, 0, s, p);
+    else hipLaunchKernelGGL((k_gated_few<T, false, false>), grid, block, 0, s, p);
+    PD_HIP(hipGetLastError());
+}
+
 template <typename T>
 void gated_t(const GatedArgs& a, hipStream_t s) {
     const pd_gated_desc& d = a.d;
+    if (d.rows <= kFewRows) return gated_few<T>(a, s);
     const Layout l = layout(d, false);
     const Matrix x = inputs(a, l, s);
     Matrix wg, wu;
@@ -811,7 +966,7 @@ void gated_grad_t(const GatedArgs& a, hipStream_t s) {
 
 }  // namespace
 
-int64_t gated_scratch_bytes(const pd_gated_desc& d) { return d.rows ? layout(d, false).total : 0; }
+int64_t gated_scratch_bytes(const pd_gated_desc& d) { return d.rows > kFewRows ? layout(d, false).total : 0; }
 void launch_gated(const GatedArgs& a, hipStream_t s) { a.d.dtype == PD_F32 ? gated_t<float>(a, s) : gated_t<bf16>(a, s); }
 int64_t gated_grad_scratch_bytes(const pd_gated_desc& d) { return d.rows ? layout(d, true).total : 0; }
 void launch_gated_grad(const GatedArgs& a, hipStream_t s) { a.d.dtype == PD_F32 ? gated_grad_t<float>(a, s) : gated_grad_t<bf16>(a, s); }
