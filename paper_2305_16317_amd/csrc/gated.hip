@@ -158,7 +158,7 @@ struct Operand {
     static constexpr int kPitch = UNITS * 16;
     static __device__ __forceinline__ int swz(int row) {
         if constexpr (UNITS == 4) return (row >> 2) & 3;
-        else if constexpr (UNITS == 8) return ((row & 2) << 1) | ((row >> 2) & 3);
+        else if constexpr (UNITS % 16 == 8) return ((row & 2) << 1) | ((row >> 2) & 3);    // (neighbours half a line apart)
         else return ((row & 3) << 2) | ((row >> 2) & 3);
     }
     static __device__ __forceinline__ int place(int row, int unit) { return row * kPitch + ((unit ^ swz(row)) << 4); }
@@ -237,7 +237,7 @@ template <int MT, int NT, int WM, int BK, int BUFS>
 struct Form {
     static constexpr int kMT = MT, kNT = NT, kWM = WM, kBK = BK, kBufs = BUFS;
     static constexpr int BM = 32 * MT * WM, HN = 16 * NT * (4 / WM);
-    static constexpr int kBlocks = MT * NT >= 16 ? 1 : 2;        // a compute unit
+    static constexpr int kBlocks = MT * NT > 8 ? 1 : 2;        // a compute unit
 };
 template <class F, bool AC, bool BC, Out OUT, typename TO>
 __global__ __launch_bounds__(256, F::kBlocks) void k_product(const Product p) {
@@ -633,15 +633,26 @@ __device__ inline void store_parts(bf16* to, int64_t plane, f32x8 v) {
         *reinterpret_cast<bf16x8*>(to + 2 * plane) = s.l;
     }
 }
+struct LayOut {
+    const void* from;
+    int64_t stride, rows;
+    int cols, pitch;
+    bf16* to;
+};
+struct LayOuts {
+    LayOut m[3];
+    int64_t end[3];          // units of the matrices up to and with each
+};
 template <typename T>
-__global__ __launch_bounds__(256) void k_lay_out(const T* from, int64_t stride, int64_t rows, int cols, int pitch, bf16* to) {
-    const int64_t units = rows * (pitch / 8);
-    for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < units; u += (int64_t)gridDim.x * 256) {
-        const int64_t row = u / (pitch / 8);
-        const int c = (int)(u - row * (pitch / 8)) * 8;
+__global__ __launch_bounds__(256) void k_lay_out(const LayOuts a) {
+    for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < a.end[2]; u += (int64_t)gridDim.x * 256) {
+        const int which = u < a.end[0] ? 0 : u < a.end[1] ? 1 : 2;
+        const LayOut& m = a.m[which];
+        const int64_t in = u - (which ? a.end[which - 1] : 0), row = in / (m.pitch / 8);
+        const int c = (int)(in - row * (m.pitch / 8)) * 8;
         f32x8 v = {};
-        if (c < cols) v = widen(load8(from + row * stride + c, cols - c));
-        store_parts<T>(to + row * pitch + c, rows * pitch, v);
+        if (c < m.cols) v = widen(load8(static_cast<const T*>(m.from) + row * m.stride + c, m.cols - c));
+        store_parts<T>(m.to + row * m.pitch + c, m.rows * m.pitch, v);
     }
 }
 
@@ -704,18 +715,27 @@ int64_t layout_bytes(int dtype, int64_t rows, int64_t cols) { return rows * up_t
 bool as_it_lies(int dtype, const void* p, int64_t stride, int64_t rows, int64_t cols) {
     return dtype == PD_BF16 && (uintptr_t)p % 16 == 0 && cols % 8 == 0 && (rows == 1 || (stride % 8 == 0 && stride < (1 << 22)));
 }
-Matrix laid_out(int dtype, const void* p, int64_t stride, int64_t rows, int64_t cols, char* to, hipStream_t s, bool lies) {
-    if (lies) return Matrix{{static_cast<const bf16*>(p)}, rows == 1 ? cols : stride};
-    const int64_t pitch = up_to(cols, 64);
-    bf16* q = reinterpret_cast<bf16*>(to);
-    const dim3 grid(blocks_for(rows * pitch / 8)), block(256);
-    if (dtype == PD_F32)
-        hipLaunchKernelGGL(k_lay_out<float>, grid, block, 0, s, static_cast<const float*>(p), stride, rows, (int)cols, (int)pitch, q);
-    else
-        hipLaunchKernelGGL(k_lay_out<bf16>, grid, block, 0, s, static_cast<const bf16*>(p), stride, rows, (int)cols, (int)pitch, q);
-    PD_HIP(hipGetLastError());
-    return Matrix{{q, q + rows * pitch, q + 2 * rows * pitch}, pitch};
-}
+// Operands as products read them; those that do not lie so are laid out by one launch.
+struct Operands {
+    LayOuts todo{};
+    int count = 0;
+    Matrix add(int dtype, const void* p, int64_t stride, int64_t rows, int64_t cols, char* to, bool lies) {
+        if (lies) return Matrix{{static_cast<const bf16*>(p)}, rows == 1 ? cols : stride};
+        const int64_t pitch = up_to(cols, 64), units = rows * (pitch / 8);
+        bf16* q = reinterpret_cast<bf16*>(to);
+        todo.m[count] = LayOut{p, stride, rows, (int)cols, (int)pitch, q};
+        todo.end[count] = (count ? todo.end[count - 1] : 0) + units;
+        for (int i = ++count; i < 3; ++i) todo.end[i] = todo.end[count - 1];
+        return Matrix{{q, q + rows * pitch, q + 2 * rows * pitch}, pitch};
+    }
+    void run(int dtype, hipStream_t s) const {
+        if (!count) return;
+        const dim3 grid(blocks_for(todo.end[2])), block(256);
+        if (dtype == PD_F32) hipLaunchKernelGGL(k_lay_out<float>, grid, block, 0, s, todo);
+        else hipLaunchKernelGGL(k_lay_out<bf16>, grid, block, 0, s, todo);
+        PD_HIP(hipGetLastError());
+    }
+};
 // Appends the segments of a times (b0, b1) to p.
 void add_segments(Product& p, int dtype, const Matrix& a, const Matrix& b0, const Matrix& b1) {
     static const int pa[6] = {2, 0, 1, 1, 0, 0}, pb[6] = {0, 2, 1, 0, 1, 0};
@@ -731,10 +751,11 @@ void add_segments(Product& p, int dtype, const Matrix& a, const Matrix& b0, cons
 
 // How a product is cut: the block's form, and into how many sums.
 using Large = Form<4, 4, 2, 64, 2>;       // 256 x 256, one block a compute unit
+using Wide = Form<3, 4, 2, 64, 2>;        // 192 x 256, one
 using Medium = Form<2, 4, 2, 32, 3>;      // 128 x 256, two blocks
 using Small = Form<2, 2, 2, 64, 2>;       // 128 x 128, two blocks
 using Few = Form<1, 2, 1, 64, 2>;         // 32 x 256, two blocks
-enum Shape { kLarge, kMedium, kSmall, kFew, kShapes };
+enum Shape { kLarge, kWide, kMedium, kSmall, kFew, kShapes };
 // What a round of blocks takes, in us: of a step of 64 and beside its steps; measured on
 // 36864 x 1024 x 4096 and 8192 x 4096 x 4096 (`alone`: of a step where a unit has one block).
 struct Cost {
@@ -743,6 +764,7 @@ struct Cost {
 };
 constexpr Cost kCost[kShapes] = {
     {Large::BM, Large::HN, Large::kBK, kCus, 1.64, 1.64, 6.8},
+    {Wide::BM, Wide::HN, Wide::kBK, kCus, 1.35, 1.35, 6.3},
     {Medium::BM, Medium::HN, Medium::kBK, 2 * kCus, 1.75, 1.0, 5.5},
     {Small::BM, Small::HN, Small::kBK, 2 * kCus, 0.95, 0.65, 3.4},
     {Few::BM, Few::HN, Few::kBK, 2 * kCus, 0.6, 0.4, 3.0},
@@ -793,6 +815,8 @@ void launch_shape(const Product& p, Shape shape, hipStream_t s) {
     const dim3 grid((unsigned)(tiles < most ? tiles : most)), block(256);
     if (shape == kLarge)
         hipLaunchKernelGGL((k_product<Large, AC, BC, OUT, TO>), grid, block, 0, s, p);
+    else if (shape == kWide)
+        hipLaunchKernelGGL((k_product<Wide, AC, BC, OUT, TO>), grid, block, 0, s, p);
     else if (shape == kMedium)
         hipLaunchKernelGGL((k_product<Medium, AC, BC, OUT, TO>), grid, block, 0, s, p);
     else if (shape == kSmall)
@@ -848,20 +872,19 @@ Layout layout(const pd_gated_desc& d, bool backward) {
     return l;
 }
 
-Matrix inputs(const GatedArgs& a, const Layout& l, hipStream_t s) {
+Matrix inputs(const GatedArgs& a, const Layout& l, Operands& o) {
     const pd_gated_desc& d = a.d;
-    return laid_out(d.dtype, a.x, d.x_stride, d.rows, d.width, a.scratch + l.x, s,
-                    as_it_lies(d.dtype, a.x, d.x_stride, d.rows, d.width));
+    return o.add(d.dtype, a.x, d.x_stride, d.rows, d.width, a.scratch + l.x, as_it_lies(d.dtype, a.x, d.x_stride, d.rows, d.width));
 }
 // Both weights lie alike, as the kernel has one distance of rows for them.
-void weights(const GatedArgs& a, const Layout& l, Matrix& gate, Matrix& up, hipStream_t s) {
+void weights(const GatedArgs& a, const Layout& l, Matrix& gate, Matrix& up, Operands& o) {
     const pd_gated_desc& d = a.d;
     const bool in_out = d.weight_layout == PD_WEIGHTS_IN_OUT;
     const int64_t rows = in_out ? d.width : d.hidden, cols = in_out ? d.hidden : d.width;
     const bool lie = as_it_lies(d.dtype, a.w_gate, d.w_gate_stride, rows, cols) &&
                      as_it_lies(d.dtype, a.w_up, d.w_up_stride, rows, cols) && (rows == 1 || d.w_gate_stride == d.w_up_stride);
-    gate = laid_out(d.dtype, a.w_gate, d.w_gate_stride, rows, cols, a.scratch + l.w, s, lie);
-    up = laid_out(d.dtype, a.w_up, d.w_up_stride, rows, cols, a.scratch + l.w + layout_bytes(d.dtype, rows, cols), s, lie);
+    gate = o.add(d.dtype, a.w_gate, d.w_gate_stride, rows, cols, a.scratch + l.w, lie);
+    up = o.add(d.dtype, a.w_up, d.w_up_stride, rows, cols, a.scratch + l.w + layout_bytes(d.dtype, rows, cols), lie);
 }
 
 constexpr int64_t kFewRows = 32;
@@ -890,9 +913,11 @@ void gated_t(const GatedArgs& a, hipStream_t s) {
     const pd_gated_desc& d = a.d;
     if (d.rows <= kFewRows) return gated_few<T>(a, s);
     const Layout l = layout(d, false);
-    const Matrix x = inputs(a, l, s);
+    Operands o;
     Matrix wg, wu;
-    weights(a, l, wg, wu, s);
+    const Matrix x = inputs(a, l, o);
+    weights(a, l, wg, wu, o);
+    o.run(d.dtype, s);
     Product p{};
     add_segments(p, d.dtype, x, wg, wu);
     p.k = d.width, p.m = (int)d.rows, p.n = d.hidden;
@@ -933,9 +958,12 @@ void gated_grad_t(const GatedArgs& a, hipStream_t s) {
     PD_HIP(hipGetLastError());
     const Matrix dg{{g.dg, g.dg + plane, g.dg + 2 * plane}, pitch}, du{{g.dg + g.du, g.dg + g.du + plane, g.dg + g.du + 2 * plane}, pitch};
     float* partial = reinterpret_cast<float*>(a.scratch + l.partial);
+    Operands o;
+    Matrix x, wg, wu;
+    if (a.dx) weights(a, l, wg, wu, o);
+    if (a.dw_gate) x = inputs(a, l, o);
+    o.run(d.dtype, s);
     if (a.dx) {
-        Matrix wg, wu;
-        weights(a, l, wg, wu, s);
         Product p{};
         add_segments(p, d.dtype, dg, wg, wg);
         add_segments(p, d.dtype, du, wu, wu);
@@ -946,7 +974,6 @@ void gated_grad_t(const GatedArgs& a, hipStream_t s) {
         else launch_product<false, true, false, T>(p, partial, s);
     }
     if (a.dw_gate) {
-        const Matrix x = inputs(a, l, s);
         Product p{};
         if (in_out) {
             add_segments(p, d.dtype, x, dg, du);
