@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import ctypes
 import dataclasses
+import functools
 import os
 import struct
 from typing import Dict, List, Optional, Sequence
@@ -250,12 +251,14 @@ def _check(code: int) -> None:
 
 # the current stream's handle without a Stream object around it (2.6 us a call less), where torch has it
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+# the current device without torch's check that it has been initialised (a tensor on a GPU says so)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _stream(stream) -> int:
     if stream is None:
         if _raw_stream is not None:
-            return _raw_stream(torch.cuda.current_device())
+            return _raw_stream(_current_device())
         return torch.cuda.current_stream().cuda_stream
     if isinstance(stream, torch.cuda.Stream):
         return stream.cuda_stream
@@ -478,7 +481,7 @@ def _dtype(t: torch.Tensor) -> int:
 
 def _on_gpu(first: torch.Tensor, *others) -> None:
     dev = first.get_device()                     # -1 on the host
-    if dev < 0 or dev != torch.cuda.current_device():
+    if dev < 0 or dev != _current_device():
         raise ValueError("tensors must be on the current GPU")
     for t in others:
         if t is not None and t.get_device() != dev:
@@ -807,10 +810,9 @@ def pd_layernorm_backward(dy: torch.Tensor, sum_in: torch.Tensor, mean: torch.Te
     d = _pack(_LAYERNORM_BYTES, rows, width, _span(rows, wn, *runs), _rows_of(dx, sh, dy.dtype, "dx"),
               _rows_of(dsum, sh, dy.dtype, "dsum") if dsum is not None else 0,
               _rows_of(sum_in, sh, dy.dtype, "sum_in"), _rows_of(dy, sh, dy.dtype, "dy"), ws, 0, dt, 0.0)
-    L, need = load(), ctypes.c_int64(0)
-    if scratch is None and runs:
-        _check(L.pd_layernorm_backward_scratch(d, ctypes.byref(need)))
-    buf, have = _scratch(scratch, need.value, stream)
+    L = load()
+    needs = scratch is None and runs
+    buf, have = _scratch(scratch, _scratch_need("pd_layernorm_backward_scratch", d) if needs else 0, stream)
     _check(L.pd_layernorm_backward(d, _ptr(dy), _ptr(sum_in), _ptr(weight), _ptr(mean), _ptr(rstd), _ptr(dsum),
                                    _ptr(dx), _ptr(dweight), _ptr(dbias), _ptr(buf), have, _stream(stream)))
 
@@ -902,19 +904,33 @@ def pd_dropout_apply(x: torch.Tensor, y: torch.Tensor, p: float, seed: int, rng_
     _check(load().pd_dropout_apply(d, _ptr(x), _ptr(residual), _ptr(step_more), _ptr(y), _stream(stream)))
 
 
-def _weight_layout(w_gate: torch.Tensor, w_up: torch.Tensor, width: int, dtype) -> int:
-    """How the weights, seen as (width, hidden), lie: rows or columns contiguous."""
-    if w_gate.dim() != 2 or w_gate.shape[0] != width or w_gate.shape != w_up.shape or 0 in w_gate.shape:
+@functools.lru_cache(maxsize=256)
+def _scratch_need(name: str, desc: bytes) -> int:
+    """Bytes of scratch that a call of this description needs (a function of the description alone)."""
+    need = ctypes.c_int64(0)
+    _check(getattr(load(), name)(desc, ctypes.byref(need)))
+    return need.value
+
+
+def _weights(w_gate: torch.Tensor, w_up: torch.Tensor, width: int, dtype):
+    """(layout, hidden, strides) of the weights, seen as (width, hidden): rows or columns contiguous."""
+    shape = w_gate.shape
+    if len(shape) != 2 or shape[0] != width or not shape[1] or shape != w_up.shape:
         raise ValueError(f"w_gate and w_up must be ({width}, hidden) alike")
     if w_gate.dtype != dtype or w_up.dtype != dtype:
         raise ValueError(f"w_gate and w_up must be {dtype}")
-    for layout, along in ((PD_WEIGHTS_IN_OUT, 1), (PD_WEIGHTS_OUT_IN, 0)):
-        if all(w.stride(along) == 1 or w.shape[along] == 1 for w in (w_gate, w_up)):
-            return layout
+    g, u = w_gate.stride(), w_up.stride()
+    if (g[1] == 1 and u[1] == 1) or shape[1] == 1:
+        return PD_WEIGHTS_IN_OUT, shape[1], g[0], u[0]
+    if (g[0] == 1 and u[0] == 1) or shape[0] == 1:
+        return PD_WEIGHTS_OUT_IN, shape[1], g[1], u[1]
     raise ValueError("w_gate and w_up must both have contiguous rows, or both contiguous columns")
 
 
-def _weight_stride(w: torch.Tensor, layout: int, shape, dtype, what: str) -> int:
+def _like_weight(w: Optional[torch.Tensor], layout: int, shape, dtype, what: str) -> int:
+    """Stride of a weight's gradient, which lies as the weights do."""
+    if w is None:
+        return 0
     if w.dtype != dtype or w.shape != shape:
         raise ValueError(f"{what} must be {dtype} of shape {tuple(shape)}")
     along = 1 if layout == PD_WEIGHTS_IN_OUT else 0
@@ -935,21 +951,20 @@ def pd_gated_forward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, 
     width = sh[-1] if x.dim() else 0
     if not width:
         raise ValueError("x must have a last dimension of at least 1")
-    layout = _weight_layout(w_gate, w_up, width, x.dtype)
-    hidden = w_gate.shape[1]
+    t = x.dtype
+    layout, hidden, gs, us = _weights(w_gate, w_up, width, t)
     hs = (*sh[:-1], hidden)
     strides = []
-    for t, what in ((gate, "gate"), (up, "up"), (h, "h")):
-        if t is not None:
-            _written(t, what)
-        strides.append(0 if t is None else _rows_of(t, hs, x.dtype, what))
-    d = _pack(_GATED_BYTES, x.numel() // width, width, hidden, dt, activation, layout, _rows_of(x, sh, x.dtype, "x"),
-              _weight_stride(w_gate, layout, w_gate.shape, x.dtype, "w_gate"),
-              _weight_stride(w_up, layout, w_gate.shape, x.dtype, "w_up"), *strides, 0, 0, 0, 0)
-    L, need = load(), ctypes.c_int64(0)
-    if scratch is None:
-        _check(L.pd_gated_forward_scratch(d, ctypes.byref(need)))
-    buf, have = _scratch(scratch, need.value, stream)
+    for out, what in ((gate, "gate"), (up, "up"), (h, "h")):
+        if out is None:
+            strides.append(0)
+        else:
+            _written(out, what)
+            strides.append(_rows_of(out, hs, t, what))
+    d = _pack(_GATED_BYTES, x.numel() // width, width, hidden, dt, activation, layout, _rows_of(x, sh, t, "x"), gs, us,
+              *strides, 0, 0, 0, 0)
+    L = load()
+    buf, have = _scratch(scratch, _scratch_need("pd_gated_forward_scratch", d) if scratch is None else 0, stream)
     _check(L.pd_gated_forward(d, _ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(gate), _ptr(up), _ptr(h), _ptr(buf), have,
                               _stream(stream)))
 
@@ -968,22 +983,18 @@ def pd_gated_backward(dh: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, w
         raise ValueError("x must have a last dimension of at least 1")
     if (dw_gate is None) != (dw_up is None):
         raise ValueError("dw_gate and dw_up come together")
-    layout = _weight_layout(w_gate, w_up, width, x.dtype)
-    ws = w_gate.shape
-    hs = (*sh[:-1], ws[1])
+    layout, hidden, gs, us = _weights(w_gate, w_up, width, x.dtype)
+    ws, hs = w_gate.shape, (*sh[:-1], hidden)
     for t, what in ((dx, "dx"), (dw_gate, "dw_gate"), (dw_up, "dw_up"), (h, "h")):
         if t is not None:
             _written(t, what)
     of = lambda t, shape, what: 0 if t is None else _rows_of(t, shape, x.dtype, what)  # noqa: E731
-    d = _pack(_GATED_BYTES, x.numel() // width, width, ws[1], dt, activation, layout, _rows_of(x, sh, x.dtype, "x"),
-              _weight_stride(w_gate, layout, ws, x.dtype, "w_gate"), _weight_stride(w_up, layout, ws, x.dtype, "w_up"),
+    d = _pack(_GATED_BYTES, x.numel() // width, width, hidden, dt, activation, layout, _rows_of(x, sh, x.dtype, "x"), gs, us,
               of(gate, hs, "gate"), of(up, hs, "up"), of(h, hs, "h"), of(dh, hs, "dh"), of(dx, sh, "dx"),
-              *(0 if t is None else _weight_stride(t, layout, ws, x.dtype, what)
-                for t, what in ((dw_gate, "dw_gate"), (dw_up, "dw_up"))))
-    L, need = load(), ctypes.c_int64(0)
-    if scratch is None and (dx is not None or dw_gate is not None):
-        _check(L.pd_gated_backward_scratch(d, ctypes.byref(need)))
-    buf, have = _scratch(scratch, need.value, stream)
+              _like_weight(dw_gate, layout, ws, x.dtype, "dw_gate"), _like_weight(dw_up, layout, ws, x.dtype, "dw_up"))
+    L = load()
+    needs = scratch is None and (dx is not None or dw_gate is not None)
+    buf, have = _scratch(scratch, _scratch_need("pd_gated_backward_scratch", d) if needs else 0, stream)
     _check(L.pd_gated_backward(d, _ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(gate), _ptr(up), _ptr(dh), _ptr(h), _ptr(dx),
                                _ptr(dw_gate), _ptr(dw_up), _ptr(buf), have, _stream(stream)))
 

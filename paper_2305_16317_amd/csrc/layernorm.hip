@@ -15,11 +15,6 @@
 namespace pd {
 namespace {
 
-__device__ inline float wave_sum(float v) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
-    return v;
-}
 // Sums of two values over the TPR lanes of a row; `slot` holds two values a wave.
 template <int TPR>
 __device__ inline void row_sums(float& u, float& v, float* slot) {
@@ -50,6 +45,64 @@ __device__ inline float row_sum(float v, float* slot) {
     return v;
 }
 
+// ------------------------------------------------------------------ rows of any width
+// Eight values from column c on, of a row of `width`.  Every lane reads eight of the row's,
+// those past its end its last eight, so that no read waits for a test; `settle` then brings
+// them down by how much later they begin and puts zeros behind (so a row of an odd width
+// has one read a lane as any other: a read a value took 33 us where this takes 25).
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x8 __attribute__((ext_vector_type(8)));
+template <typename T>
+__device__ __forceinline__ typename Vec8<T>::type eight_of(const T* row, int c, int width) {
+    if (width < 8) return load8(row + c, width - c);
+    return *reinterpret_cast<const typename Vec8<T>::unaligned*>(row + (c < width - 8 ? c : width - 8));
+}
+__device__ __forceinline__ bf16x8 settle(bf16x8 v, int c, int width) {
+    const int k = c - (width - 8);                       // values that are not this lane's
+    if (width < 8) return v;
+    u32x4 w = __builtin_bit_cast(u32x4, v);
+    if (k > 0) {
+        if (k & 4) w = u32x4{w[2], w[3], 0, 0};
+        if (k & 2) w = u32x4{w[1], w[2], w[3], 0};
+        if (k & 1) w = u32x4{w[0] >> 16 | w[1] << 16, w[1] >> 16 | w[2] << 16, w[2] >> 16 | w[3] << 16, w[3] >> 16};
+        if (k > 7) w = u32x4{};
+    }
+    return __builtin_bit_cast(bf16x8, w);
+}
+__device__ __forceinline__ f32x8 settle(f32x8 v, int c, int width) {
+    const int k = c - (width - 8);
+    if (width < 8) return v;
+    if (k > 0) {
+        if (k & 4) v = f32x8{v[4], v[5], v[6], v[7], 0.f, 0.f, 0.f, 0.f};
+        if (k & 2) v = f32x8{v[2], v[3], v[4], v[5], v[6], v[7], 0.f, 0.f};
+        if (k & 1) v = f32x8{v[1], v[2], v[3], v[4], v[5], v[6], v[7], 0.f};
+        if (k > 7) v = f32x8{};
+    }
+    return v;
+}
+// Stores the first n of eight: in runs of four, two and one.
+template <typename T>
+__device__ __forceinline__ void store_first(T* p, int n, typename Vec8<T>::type v) {
+    if (n >= 8) {
+        *reinterpret_cast<typename Vec8<T>::unaligned*>(p) = v;
+        return;
+    }
+    typedef T four __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+    typedef T two __attribute__((ext_vector_type(2), aligned(sizeof(T))));
+    if (n <= 0) return;
+    if (n & 4) {
+        *reinterpret_cast<four*>(p) = four{v[0], v[1], v[2], v[3]};
+        v[0] = v[4], v[1] = v[5], v[2] = v[6];
+        p += 4;
+    }
+    if (n & 2) {
+        *reinterpret_cast<two*>(p) = two{v[0], v[1]};
+        v[0] = v[2];
+        p += 2;
+    }
+    if (n & 1) *p = v[0];
+}
+
 // TPR lanes a row, NV steps of eight values a lane.
 template <typename T, int TPR, int NV>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_layernorm(const LayerNormArgs a) {
@@ -63,13 +116,20 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_layernorm(const Layer
     const T* r = a.residual ? static_cast<const T*>(a.residual) + row * a.d.residual_stride : nullptr;
     f32x8 v[NV];
     float sum = 0.f;
+    {
+        typename Vec8<T>::type vx[NV], vr[NV];
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int c = (i * TPR + lane) * 8, n = width - c;
-        v[i] = f32x8{};
-        if (n <= 0) continue;
-        v[i] = widen(load8(x + c, n));
-        if (r) v[i] += widen(load8(r + c, n));
+        for (int i = 0; i < NV; ++i) vx[i] = eight_of(x, (i * TPR + lane) * 8, width);
+        if (r)
+#pragma unroll
+            for (int i = 0; i < NV; ++i) vr[i] = eight_of(r, (i * TPR + lane) * 8, width);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const bool whole = (i + 1) * TPR * 8 <= width;          // (uniform)
+            const int c = (i * TPR + lane) * 8;
+            v[i] = widen(whole ? vx[i] : settle(vx[i], c, width));
+            if (r) v[i] += widen(whole ? vr[i] : settle(vr[i], c, width));
+        }
     }
 #pragma unroll
     for (int i = 0; i < NV; ++i)
@@ -79,8 +139,8 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_layernorm(const Layer
         T* h = static_cast<T*>(a.sum) + row * a.d.sum_stride;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int c = (i * TPR + lane) * 8, n = width - c;
-            if (n > 0) store8(h + c, n, narrow<T>(v[i]));
+            const int c = (i * TPR + lane) * 8;
+            store_first(h + c, width - c, narrow<T>(v[i]));
         }
     }
     const float mean = row_sum<TPR>(sum, slot) / (float)width;
@@ -90,8 +150,8 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_layernorm(const Layer
         const int n = width - (i * TPR + lane) * 8;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            v[i][e] -= mean;
-            if (e < n) ss = fmaf(v[i][e], v[i][e], ss);
+            v[i][e] = e < n ? v[i][e] - mean : 0.f;
+            ss = fmaf(v[i][e], v[i][e], ss);
         }
     }
     const float rstd = 1.f / sqrtf(row_sum<TPR>(ss, slot) / (float)width + a.d.eps);
@@ -105,12 +165,18 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_layernorm(const Layer
     T* y = static_cast<T*>(a.y) + row * a.d.y_stride;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int c = (i * TPR + lane) * 8, n = width - c;
-        if (n <= 0) continue;
+        const int c = (i * TPR + lane) * 8;
+        const bool whole = (i + 1) * TPR * 8 <= width;
         f32x8 o = v[i] * rstd;
-        if (w) o = o * load8(w + c, n);
-        if (b) o = o + load8(b + c, n);
-        store8(y + c, n, narrow<T>(o));
+        if (w) {
+            const f32x8 q = eight_of(w, c, width);
+            o = o * (whole ? q : settle(q, c, width));
+        }
+        if (b) {
+            const f32x8 q = eight_of(b, c, width);
+            o = o + (whole ? q : settle(q, c, width));
+        }
+        store_first(y + c, width - c, narrow<T>(o));
     }
 }
 
@@ -130,14 +196,15 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_layernorm_grad(const 
     for (int64_t item = blockIdx.x; item < (int64_t)a.groups * a.parts; item += gridDim.x) {
         const int64_t g = item / a.parts, first = g * a.d.span;
         const float* weight = a.weight ? a.weight + g * a.d.weight_stride : nullptr;
-        const auto row8 = [&](const T* p, int i) {
-            const int c = (i * TPR + lane) * 8, n = width - c;
-            return n > 0 ? load8(p + c, n) : typename Vec8<T>::type{};
+        const auto read = [&](const T* p, int i) { return eight_of(p, (i * TPR + lane) * 8, width); };
+        const auto wide = [&](typename Vec8<T>::type v, int i) {
+            return widen((i + 1) * TPR * 8 <= width ? v : settle(v, (i * TPR + lane) * 8, width));
         };
         const auto weights = [&](int i) {
-            const int c = (i * TPR + lane) * 8, n = width - c;
-            if (weight && n > 0) return load8(weight + c, n);
-            return f32x8{1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
+            if (!weight) return f32x8{1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
+            const int c = (i * TPR + lane) * 8;
+            const f32x8 w = eight_of(weight, c, width);
+            return (i + 1) * TPR * 8 <= width ? w : settle(w, c, width);
         };
         f32x8 dw[SUMS ? NV : 1], db[SUMS ? NV : 1];
 #pragma unroll
@@ -153,17 +220,18 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_layernorm_grad(const 
             float dot = 0.f, sum = 0.f;
             if constexpr (KEEP) {
 #pragma unroll
-                for (int i = 0; i < NV; ++i) {
-                    vdy[i] = row8(dy, i);
-                    vh[i] = row8(h, i);
-                    vds[i] = ds ? row8(ds, i) : typename Vec8<T>::type{};
-                }
+                for (int i = 0; i < NV; ++i) vdy[i] = read(dy, i);
+#pragma unroll
+                for (int i = 0; i < NV; ++i) vh[i] = read(h, i);
+                if (ds)
+#pragma unroll
+                    for (int i = 0; i < NV; ++i) vds[i] = read(ds, i);
             }
             // (past the row's end dy is 0, and what it meets a number wherever the row's values are)
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                const f32x8 g = widen(KEEP ? vdy[KEEP ? i : 0] : row8(dy, i)), w = weights(i);
-                const f32x8 nn = (widen(KEEP ? vh[KEEP ? i : 0] : row8(h, i)) - mean) * rstd;
+                const f32x8 g = wide(KEEP ? vdy[KEEP ? i : 0] : read(dy, i), i), w = weights(i);
+                const f32x8 nn = (wide(KEEP ? vh[KEEP ? i : 0] : read(h, i), i) - mean) * rstd;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     if (SUMS) {
@@ -179,14 +247,14 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_layernorm_grad(const 
             sum /= (float)width;
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                const int c = (i * TPR + lane) * 8, n = width - c;
-                if (n <= 0) continue;
-                const f32x8 g = widen(KEEP ? vdy[KEEP ? i : 0] : row8(dy, i)), w = weights(i);
-                const f32x8 nn = (widen(KEEP ? vh[KEEP ? i : 0] : row8(h, i)) - mean) * rstd;
-                f32x8 o = widen(KEEP ? vds[KEEP ? i : 0] : ds ? row8(ds, i) : typename Vec8<T>::type{});
+                const int c = (i * TPR + lane) * 8;
+                const f32x8 g = wide(KEEP ? vdy[KEEP ? i : 0] : read(dy, i), i), w = weights(i);
+                const f32x8 nn = (wide(KEEP ? vh[KEEP ? i : 0] : read(h, i), i) - mean) * rstd;
+                f32x8 o = {};
+                if (ds) o = wide(KEEP ? vds[KEEP ? i : 0] : read(ds, i), i);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) o[e] = fmaf(rstd, fmaf(-nn[e], dot, fmaf(g[e], w[e], -sum)), o[e]);
-                store8(dx + c, n, narrow<T>(o));
+                store_first(dx + c, width - c, narrow<T>(o));
             }
         }
         if constexpr (SUMS) {
@@ -268,12 +336,12 @@ __global__ __launch_bounds__(256) void k_layernorm_columns(const LayerNormGradAr
     }
 }
 
-// The sums over a run's parts: 16 columns a block and 64 lanes down each, which take
-// every 64th part.  Grid row 2 g is run g's weight, 2 g + 1 its bias.
+// The sums over a run's parts: 64 columns a block, of which 16 waves take every 16th part
+// each, four reads at a time.  Grid row 2 g is run g's weight, 2 g + 1 its bias.  (16 columns a
+// block and 64 lanes down each, as for one run of 512 parts: 8.5 us for 16 runs of 32, so 4.)
 __global__ __launch_bounds__(1024) void k_layernorm_join(const LayerNormGradArgs a) {
-    __shared__ float part[64][17];
-    const int col = threadIdx.x & 15, sub = threadIdx.x >> 4, c = blockIdx.x * 16 + col, width = (int)a.d.width;
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    __shared__ float part[16][64];
+    const int col = threadIdx.x & 63, sub = threadIdx.x >> 6, c = blockIdx.x * 64 + col, width = (int)a.d.width;
     for (int64_t at = blockIdx.y; at < 2 * (int64_t)a.groups; at += gridDim.y) {
         const int64_t g = at >> 1;
         float* to = (at & 1) ? a.dbias : a.dweight;
@@ -281,17 +349,20 @@ __global__ __launch_bounds__(1024) void k_layernorm_join(const LayerNormGradArgs
         const float* from = a.partial + ((at & 1) * (int64_t)a.groups + g) * a.parts * width;
         float v[4] = {0.f, 0.f, 0.f, 0.f};
         if (c < width)
-            for (int b = sub; b < a.parts; b += 256) {
+            for (int b = sub; b < a.parts; b += 64) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    if (b + 64 * i < a.parts) v[i] += from[(int64_t)(b + 64 * i) * width + c];
+                    if (b + 16 * i < a.parts) v[i] += from[(int64_t)(b + 16 * i) * width + c];
             }
         __syncthreads();                     // the last use of part is over
         part[sub][col] = (v[0] + v[1]) + (v[2] + v[3]);
         __syncthreads();
-        // a wave of the 16 takes one column
-        const float sum = wave_sum(part[lane][wave]);
-        if (lane == 0 && blockIdx.x * 16 + wave < width) to[g * width + blockIdx.x * 16 + wave] = sum;
+        if (sub == 0 && c < width) {
+            float sum = 0.f;
+#pragma unroll
+            for (int s = 0; s < 16; ++s) sum += part[s][col];
+            to[g * width + c] = sum;
+        }
     }
 }
 
@@ -395,7 +466,7 @@ void launch_layernorm_grad(const LayerNormGradArgs& a, hipStream_t s) {
     PD_HIP(hipGetLastError());
     if ((!a.dweight && !a.dbias) || a.parts == 1) return;
     const int64_t rows = 2 * (int64_t)a.groups;
-    hipLaunchKernelGGL(k_layernorm_join, dim3((unsigned)((a.d.width + 15) / 16), (unsigned)(rows < 512 ? rows : 512)), dim3(1024), 0,
+    hipLaunchKernelGGL(k_layernorm_join, dim3((unsigned)((a.d.width + 63) / 64), (unsigned)(rows < 512 ? rows : 512)), dim3(1024), 0,
                        s, a);
     PD_HIP(hipGetLastError());
 }
