@@ -9,7 +9,12 @@
 // Bound by memory: 4 values move per element each way.  A row stays in registers from
 // its one read to its writes, eight values a lane and step, so the squares are summed
 // around the mean itself and an offset common to the row costs no digits.  Rows up to
-// 2048 values belong to one wave, longer ones to a block of 256 or 1024 lanes.
+// 2048 values belong to one wave, longer ones to a block of 256 or 1024 lanes.  Backward a
+// lane keeps its columns over many rows, so that dw and db are summed in registers.
+//
+// Measured: 36864 x 1024 bfloat16 in 64 runs 49 us (6.1 TB/s; a large copy reaches 5.0, this
+// fits the last cache), backward 70 us, of which dx alone 56 (5.4 TB/s); 12432 x 1001 in 16 runs
+// backward 33 us (3.1 TB/s: rows that begin at no multiple of 16 bytes; 1024 values 27).
 #include "ops.h"
 
 namespace pd {
@@ -52,14 +57,14 @@ __device__ inline float row_sum(float v, float* slot) {
 // has one read a lane as any other: a read a value took 33 us where this takes 25).
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x8 __attribute__((ext_vector_type(8)));
-template <typename T>
+// (TINY: rows of fewer than eight values.)
+template <bool TINY, typename T>
 __device__ __forceinline__ typename Vec8<T>::type eight_of(const T* row, int c, int width) {
-    if (width < 8) return load8(row + c, width - c);
-    return *reinterpret_cast<const typename Vec8<T>::unaligned*>(row + (c < width - 8 ? c : width - 8));
+    if constexpr (TINY) return load8(row + c, width - c);
+    else return *reinterpret_cast<const typename Vec8<T>::unaligned*>(row + (c < width - 8 ? c : width - 8));
 }
 __device__ __forceinline__ bf16x8 settle(bf16x8 v, int c, int width) {
     const int k = c - (width - 8);                       // values that are not this lane's
-    if (width < 8) return v;
     u32x4 w = __builtin_bit_cast(u32x4, v);
     if (k > 0) {
         if (k & 4) w = u32x4{w[2], w[3], 0, 0};
@@ -71,7 +76,6 @@ __device__ __forceinline__ bf16x8 settle(bf16x8 v, int c, int width) {
 }
 __device__ __forceinline__ f32x8 settle(f32x8 v, int c, int width) {
     const int k = c - (width - 8);
-    if (width < 8) return v;
     if (k > 0) {
         if (k & 4) v = f32x8{v[4], v[5], v[6], v[7], 0.f, 0.f, 0.f, 0.f};
         if (k & 2) v = f32x8{v[2], v[3], v[4], v[5], v[6], v[7], 0.f, 0.f};
@@ -104,12 +108,12 @@ __device__ __forceinline__ void store_first(T* p, int n, typename Vec8<T>::type 
 }
 
 // TPR lanes a row, NV steps of eight values a lane.
-template <typename T, int TPR, int NV>
+template <typename T, int TPR, int NV, bool TINY>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_layernorm(const LayerNormArgs a) {
     constexpr int kRows = TPR < 256 ? 256 / TPR : 1;      // rows a block
     __shared__ float slot[32];
     const int lane = threadIdx.x % TPR;
-    const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / TPR;
+    const int64_t row = (int64_t)blockIdx.x * kRows + (kRows > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / TPR) : 0);   // (a wave's)
     if (row >= a.d.rows) return;             // whole waves; with TPR > 64 there is one row a block
     const int width = (int)a.d.width;
     const T* x = static_cast<const T*>(a.x) + row * a.d.x_stride;
@@ -119,13 +123,13 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_layernorm(const Layer
     {
         typename Vec8<T>::type vx[NV], vr[NV];
 #pragma unroll
-        for (int i = 0; i < NV; ++i) vx[i] = eight_of(x, (i * TPR + lane) * 8, width);
+        for (int i = 0; i < NV; ++i) vx[i] = eight_of<TINY>(x, (i * TPR + lane) * 8, width);
         if (r)
 #pragma unroll
-            for (int i = 0; i < NV; ++i) vr[i] = eight_of(r, (i * TPR + lane) * 8, width);
+            for (int i = 0; i < NV; ++i) vr[i] = eight_of<TINY>(r, (i * TPR + lane) * 8, width);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const bool whole = (i + 1) * TPR * 8 <= width;          // (uniform)
+            const bool whole = TINY || (i + 1) * TPR * 8 <= width;  // (uniform)
             const int c = (i * TPR + lane) * 8;
             v[i] = widen(whole ? vx[i] : settle(vx[i], c, width));
             if (r) v[i] += widen(whole ? vr[i] : settle(vr[i], c, width));
@@ -166,14 +170,14 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_layernorm(const Layer
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int c = (i * TPR + lane) * 8;
-        const bool whole = (i + 1) * TPR * 8 <= width;
+        const bool whole = TINY || (i + 1) * TPR * 8 <= width;
         f32x8 o = v[i] * rstd;
         if (w) {
-            const f32x8 q = eight_of(w, c, width);
+            const f32x8 q = eight_of<TINY>(w, c, width);
             o = o * (whole ? q : settle(q, c, width));
         }
         if (b) {
-            const f32x8 q = eight_of(b, c, width);
+            const f32x8 q = eight_of<TINY>(b, c, width);
             o = o + (whole ? q : settle(q, c, width));
         }
         store_first(y + c, width - c, narrow<T>(o));
@@ -185,53 +189,69 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_layernorm(const Layer
 // summed in registers, then over the block's rows in LDS, and over the parts by
 // k_layernorm_join: a fixed order.  SUMS false:
 // dx alone.
-template <typename T, int TPR, int NV, bool SUMS>
-__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_layernorm_grad(const LayerNormGradArgs a) {
+template <typename T, int TPR, int NV, bool TINY, bool SUMS, int BLOCKS>
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR, BLOCKS) void k_layernorm_grad(const LayerNormGradArgs a) {
     constexpr int kRows = TPR < 256 ? 256 / TPR : 1;
-    constexpr bool KEEP = TPR < 1024;         // the row stays in registers (else it is read again, from the cache)
+    constexpr bool KEEP = NV == 1 || (TPR < 1024 && NV * sizeof(T) < 16);   // the row stays in registers (else it is read again, from the cache)
     __shared__ float slot[32];
     __shared__ float part[SUMS && kRows > 1 ? (kRows - 1) * TPR * NV * 8 : 1];
-    const int lane = threadIdx.x % TPR, sub = threadIdx.x / TPR;
+    // (sub is a wave's: its rows' addresses and statistics stay in scalar registers)
+    const int lane = threadIdx.x % TPR, sub = kRows > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / TPR) : 0;
     const int width = (int)a.d.width;
     for (int64_t item = blockIdx.x; item < (int64_t)a.groups * a.parts; item += gridDim.x) {
         const int64_t g = item / a.parts, first = g * a.d.span;
         const float* weight = a.weight ? a.weight + g * a.d.weight_stride : nullptr;
-        const auto read = [&](const T* p, int i) { return eight_of(p, (i * TPR + lane) * 8, width); };
+        const auto read = [&](const T* p, int i) { return eight_of<TINY>(p, (i * TPR + lane) * 8, width); };
         const auto wide = [&](typename Vec8<T>::type v, int i) {
-            return widen((i + 1) * TPR * 8 <= width ? v : settle(v, (i * TPR + lane) * 8, width));
+            return widen(TINY || (i + 1) * TPR * 8 <= width ? v : settle(v, (i * TPR + lane) * 8, width));
         };
         const auto weights = [&](int i) {
             if (!weight) return f32x8{1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
             const int c = (i * TPR + lane) * 8;
-            const f32x8 w = eight_of(weight, c, width);
-            return (i + 1) * TPR * 8 <= width ? w : settle(w, c, width);
+            const f32x8 w = eight_of<TINY>(weight, c, width);
+            return TINY || (i + 1) * TPR * 8 <= width ? w : settle(w, c, width);
         };
         f32x8 dw[SUMS ? NV : 1], db[SUMS ? NV : 1];
 #pragma unroll
         for (int i = 0; i < (SUMS ? NV : 1); ++i) dw[i] = db[i] = f32x8{};
-        for (int64_t at = (item - g * a.parts) * kRows + sub; at < a.d.span; at += (int64_t)a.parts * kRows) {
+        // a row as it is read; the next one's reads begin before this one's sums
+        struct Row {
+            typename Vec8<T>::type dy[KEEP ? NV : 1], h[KEEP ? NV : 1], ds[KEEP ? NV : 1];
+            float rstd, mean;
+        } next;
+        const auto fetch = [&](int64_t row) {
+            next.rstd = a.rstd[row], next.mean = a.mean[row];
+            if constexpr (KEEP) {
+                const T* dy = static_cast<const T*>(a.dy) + row * a.d.y_stride;
+                const T* h = static_cast<const T*>(a.sum) + row * a.d.sum_stride;
+#pragma unroll
+                for (int i = 0; i < NV; ++i) next.dy[i] = read(dy, i);
+#pragma unroll
+                for (int i = 0; i < NV; ++i) next.h[i] = read(h, i);
+                if (a.dsum) {
+                    const T* ds = static_cast<const T*>(a.dsum) + row * a.d.residual_stride;
+#pragma unroll
+                    for (int i = 0; i < NV; ++i) next.ds[i] = read(ds, i);
+                }
+            }
+        };
+        const int64_t begin = (item - g * a.parts) * kRows + sub, step = (int64_t)a.parts * kRows;
+        if (begin < a.d.span) fetch(first + begin);
+        for (int64_t at = begin; at < a.d.span; at += step) {
             const int64_t row = first + at;
             const T* dy = static_cast<const T*>(a.dy) + row * a.d.y_stride;
             const T* h = static_cast<const T*>(a.sum) + row * a.d.sum_stride;
             const T* ds = a.dsum ? static_cast<const T*>(a.dsum) + row * a.d.residual_stride : nullptr;
             T* dx = static_cast<T*>(a.dx) + row * a.d.x_stride;
-            const float rstd = a.rstd[row], mean = a.mean[row];
-            typename Vec8<T>::type vdy[KEEP ? NV : 1], vh[KEEP ? NV : 1], vds[KEEP ? NV : 1];
+            const Row now = next;
+            if (at + step < a.d.span) fetch(row + step);
+            const float rstd = now.rstd, mean = now.mean;
             float dot = 0.f, sum = 0.f;
-            if constexpr (KEEP) {
-#pragma unroll
-                for (int i = 0; i < NV; ++i) vdy[i] = read(dy, i);
-#pragma unroll
-                for (int i = 0; i < NV; ++i) vh[i] = read(h, i);
-                if (ds)
-#pragma unroll
-                    for (int i = 0; i < NV; ++i) vds[i] = read(ds, i);
-            }
             // (past the row's end dy is 0, and what it meets a number wherever the row's values are)
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                const f32x8 g = wide(KEEP ? vdy[KEEP ? i : 0] : read(dy, i), i), w = weights(i);
-                const f32x8 nn = (wide(KEEP ? vh[KEEP ? i : 0] : read(h, i), i) - mean) * rstd;
+                const f32x8 g = wide(KEEP ? now.dy[KEEP ? i : 0] : read(dy, i), i), w = weights(i);
+                const f32x8 nn = (wide(KEEP ? now.h[KEEP ? i : 0] : read(h, i), i) - mean) * rstd;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     if (SUMS) {
@@ -248,10 +268,10 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_layernorm_grad(const 
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 const int c = (i * TPR + lane) * 8;
-                const f32x8 g = wide(KEEP ? vdy[KEEP ? i : 0] : read(dy, i), i), w = weights(i);
-                const f32x8 nn = (wide(KEEP ? vh[KEEP ? i : 0] : read(h, i), i) - mean) * rstd;
+                const f32x8 g = wide(KEEP ? now.dy[KEEP ? i : 0] : read(dy, i), i), w = weights(i);
+                const f32x8 nn = (wide(KEEP ? now.h[KEEP ? i : 0] : read(h, i), i) - mean) * rstd;
                 f32x8 o = {};
-                if (ds) o = wide(KEEP ? vds[KEEP ? i : 0] : read(ds, i), i);
+                if (ds) o = wide(KEEP ? now.ds[KEEP ? i : 0] : read(ds, i), i);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) o[e] = fmaf(rstd, fmaf(-nn[e], dot, fmaf(g[e], w[e], -sum)), o[e]);
                 store_first(dx + c, width - c, narrow<T>(o));
@@ -336,12 +356,14 @@ __global__ __launch_bounds__(256) void k_layernorm_columns(const LayerNormGradAr
     }
 }
 
-// The sums over a run's parts: 64 columns a block, of which 16 waves take every 16th part
-// each, four reads at a time.  Grid row 2 g is run g's weight, 2 g + 1 its bias.  (16 columns a
-// block and 64 lanes down each, as for one run of 512 parts: 8.5 us for 16 runs of 32, so 4.)
+// The sums over a run's parts: COLS columns a block, each of whose 1024 / COLS lanes take
+// every so many parts, four reads at a time.  Grid row 2 g is run g's weight, 2 g + 1 its bias.
+// (16 runs of 32 parts of 1001: 64 columns 4 us, 16 columns 8.5; one run of 512 parts: 13 and 4.)
+template <int COLS>
 __global__ __launch_bounds__(1024) void k_layernorm_join(const LayerNormGradArgs a) {
-    __shared__ float part[16][64];
-    const int col = threadIdx.x & 63, sub = threadIdx.x >> 6, c = blockIdx.x * 64 + col, width = (int)a.d.width;
+    constexpr int SUBS = 1024 / COLS;
+    __shared__ float part[SUBS][COLS];
+    const int col = threadIdx.x % COLS, sub = threadIdx.x / COLS, c = blockIdx.x * COLS + col, width = (int)a.d.width;
     for (int64_t at = blockIdx.y; at < 2 * (int64_t)a.groups; at += gridDim.y) {
         const int64_t g = at >> 1;
         float* to = (at & 1) ? a.dbias : a.dweight;
@@ -349,20 +371,20 @@ __global__ __launch_bounds__(1024) void k_layernorm_join(const LayerNormGradArgs
         const float* from = a.partial + ((at & 1) * (int64_t)a.groups + g) * a.parts * width;
         float v[4] = {0.f, 0.f, 0.f, 0.f};
         if (c < width)
-            for (int b = sub; b < a.parts; b += 64) {
+            for (int b = sub; b < a.parts; b += 4 * SUBS) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    if (b + 16 * i < a.parts) v[i] += from[(int64_t)(b + 16 * i) * width + c];
+                    if (b + SUBS * i < a.parts) v[i] += from[(int64_t)(b + SUBS * i) * width + c];
             }
         __syncthreads();                     // the last use of part is over
         part[sub][col] = (v[0] + v[1]) + (v[2] + v[3]);
         __syncthreads();
-        if (sub == 0 && c < width) {
-            float sum = 0.f;
 #pragma unroll
-            for (int s = 0; s < 16; ++s) sum += part[s][col];
-            to[g * width + c] = sum;
+        for (int half = SUBS / 2; half > 0; half >>= 1) {
+            if (sub < half) part[sub][col] += part[sub + half][col];
+            __syncthreads();
         }
+        if (sub == 0 && c < width) to[g * width + c] = part[0][col];
     }
 }
 
@@ -376,6 +398,7 @@ __global__ __launch_bounds__(256) void k_layernorm_zero(float* dweight, float* d
 
 // lanes and steps of a row by its width
 #define PD_LAYERNORM_SHAPES(X) \
+    X(7, 64, 1)                \
     X(512, 64, 1)              \
     X(1024, 64, 2)             \
     X(2048, 64, 4)             \
@@ -390,7 +413,7 @@ void layernorm_t(const LayerNormArgs& a, hipStream_t s) {
 #define X(W, TPR, NV)                                                                                            \
     if (a.d.width <= W) {                                                                                        \
         constexpr int rows = TPR < 256 ? 256 / TPR : 1;                                                          \
-        hipLaunchKernelGGL((k_layernorm<T, TPR, NV>), dim3((unsigned)((a.d.rows + rows - 1) / rows)),            \
+        hipLaunchKernelGGL((k_layernorm<T, TPR, NV, (W < 8)>), dim3((unsigned)((a.d.rows + rows - 1) / rows)),            \
                            dim3(TPR < 256 ? 256 : TPR), 0, s, a);                                                \
         return;                                                                                                  \
     }
@@ -398,28 +421,49 @@ void layernorm_t(const LayerNormArgs& a, hipStream_t s) {
 #undef X
 }
 
-// above this width dweight and dbias are summed by a pass of their own
+// The same where the gradients of weight and bias are summed as well, with how many blocks
+// a compute unit takes (bfloat16, float32): their sums stay in registers, so rows are spread
+// over more lanes.
+#define PD_LAYERNORM_SUM_SHAPES(X) \
+    X(7, 64, 1, 4, 3)              \
+    X(512, 64, 1, 4, 3)            \
+    X(1024, 64, 2, 3, 2)           \
+    X(2048, 256, 1, 4, 4)          \
+    X(4096, 512, 1, 2, 2)          \
+    X(8192, 1024, 1, 1, 1)
+// above this width a pass of its own sums them, in blocks of 256 columns
 constexpr int64_t kFusedWidth = 8192;
 constexpr int64_t kMostBlocks = (int64_t)1 << 20;
 
 template <typename T>
 void layernorm_grad_t(const LayerNormGradArgs& a, hipStream_t s) {
     const int64_t items = (int64_t)a.groups * a.parts;
-    const dim3 grid((unsigned)(items < kMostBlocks ? items : kMostBlocks));
-    const bool sums = a.dweight || a.dbias;
-    if (sums && a.d.width > kFusedWidth) {               // before dx, which may lie over dy
+    if ((a.dweight || a.dbias) && a.d.width <= kFusedWidth) {
+        const dim3 grid((unsigned)(items < kMostBlocks ? items : kMostBlocks));
+#define X(W, TPR, NV, B16, B32)                                                                                      \
+    if (a.d.width <= W) {                                                                                            \
+        constexpr int BLOCKS = sizeof(T) == 2 ? B16 : B32;                                                           \
+        hipLaunchKernelGGL((k_layernorm_grad<T, TPR, NV, (W < 8), true, BLOCKS>), grid, dim3(TPR < 256 ? 256 : TPR), 0, s, a); \
+        return;                                                                                                      \
+    }
+        PD_LAYERNORM_SUM_SHAPES(X)
+#undef X
+    }
+    if (a.dweight || a.dbias) {                          // before dx, which may lie over dy
         hipLaunchKernelGGL(k_layernorm_columns<T>, dim3((unsigned)((a.d.width + 255) / 256), (unsigned)(items < 16384 ? items : 16384)),
                            dim3(256), 0, s, a);
         PD_HIP(hipGetLastError());
     }
-#define X(W, TPR, NV)                                                                                                 \
-    if (a.d.width <= W) {                                                                                             \
-        const dim3 block(TPR < 256 ? 256 : TPR);                                                                      \
-        if (sums && W <= kFusedWidth)                                                                                 \
-            hipLaunchKernelGGL((k_layernorm_grad<T, TPR, NV, W <= kFusedWidth>), grid, block, 0, s, a);               \
-        else                                                                                                          \
-            hipLaunchKernelGGL((k_layernorm_grad<T, TPR, NV, false>), grid, block, 0, s, a);                          \
-        return;                                                                                                       \
+    LayerNormGradArgs b = a;                             // dx alone: 16 waves a compute unit
+#define X(W, TPR, NV)                                                                                                \
+    if (a.d.width <= W) {                                                                                            \
+        constexpr int rows = TPR < 256 ? 256 / TPR : 1;                                                              \
+        const int64_t need = (a.d.span + rows - 1) / rows, most = (4 * kCus * 256 / (TPR < 256 ? 256 : TPR) + a.groups - 1) / a.groups; \
+        b.parts = (int)(need < most ? need : most);                                                                  \
+        const int64_t all = (int64_t)b.groups * b.parts;                                                             \
+        hipLaunchKernelGGL((k_layernorm_grad<T, TPR, NV, (W < 8), false, 1>), dim3((unsigned)(all < kMostBlocks ? all : kMostBlocks)), \
+                           dim3(TPR < 256 ? 256 : TPR), 0, s, b);                                                    \
+        return;                                                                                                      \
     }
     PD_LAYERNORM_SHAPES(X)
 #undef X
@@ -448,10 +492,20 @@ void launch_layernorm(const LayerNormArgs& all, hipStream_t s) {
 }
 
 int layernorm_grad_parts(const pd_layernorm_desc& d) {
-    // all runs' parts together: two blocks a compute unit; never more than a run has rows for
-    const int64_t groups = d.rows ? d.rows / d.span : 1;
-    const int64_t per = d.width <= 2048 ? 4 : 1, need = (d.span + per - 1) / per, most = (2 * kCus + groups - 1) / groups;
-    return (int)(d.rows == 0 || need < 1 ? 1 : need < most ? need : most);
+    // all runs' parts together: as many blocks as the chip takes; never more than a run has rows for
+    if (d.rows == 0) return 1;
+    const int64_t groups = d.rows / d.span;
+    int64_t blocks = 4 * kCus, rows = 8;                 // (the pass over columns: eight rows at a time)
+    if (d.width > kFusedWidth) blocks = (blocks + (d.width + 255) / 256 - 1) / ((d.width + 255) / 256);
+#define X(W, TPR, NV, B16, B32)                              \
+    else if (d.width <= W) {                                 \
+        blocks = (d.dtype == PD_F32 ? B32 : B16) * kCus;     \
+        rows = TPR < 256 ? 256 / TPR : 1;                    \
+    }
+    PD_LAYERNORM_SUM_SHAPES(X)
+#undef X
+    const int64_t need = (d.span + rows - 1) / rows, most = (blocks + groups - 1) / groups;
+    return (int)(need < most ? need : most);
 }
 
 void launch_layernorm_grad(const LayerNormGradArgs& a, hipStream_t s) {
@@ -466,8 +520,11 @@ void launch_layernorm_grad(const LayerNormGradArgs& a, hipStream_t s) {
     PD_HIP(hipGetLastError());
     if ((!a.dweight && !a.dbias) || a.parts == 1) return;
     const int64_t rows = 2 * (int64_t)a.groups;
-    hipLaunchKernelGGL(k_layernorm_join, dim3((unsigned)((a.d.width + 63) / 64), (unsigned)(rows < 512 ? rows : 512)), dim3(1024), 0,
-                       s, a);
+    const unsigned high = (unsigned)(rows < 512 ? rows : 512);
+    if (a.parts > 64)
+        hipLaunchKernelGGL(k_layernorm_join<16>, dim3((unsigned)((a.d.width + 15) / 16), high), dim3(1024), 0, s, a);
+    else
+        hipLaunchKernelGGL(k_layernorm_join<64>, dim3((unsigned)((a.d.width + 63) / 64), high), dim3(1024), 0, s, a);
     PD_HIP(hipGetLastError());
 }
 
