@@ -62,24 +62,40 @@ __global__ __launch_bounds__(256) void k_rotary_axes_table(const pd_rotary_axes_
 // One lane: unit u of a token (pairs while u < pair_units, then values to copy) in the
 // heads hs, hs + lanes_h, ...; the heads of q, then of k.
 template <typename T, bool HALF, class Args>
-__global__ __launch_bounds__(256) void k_rotary(const Args a, int units, int pair_units, int lanes_h, int64_t lanes) {
+__global__ __launch_bounds__(256) void k_rotary(const Args a, int units, int pair_units, int lanes_h, uint32_t lanes) {
     constexpr int kPairs = HALF ? 8 : 4;
-    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const uint32_t id = blockIdx.x * 256 + threadIdx.x;        // (fewer than 2^32 lanes)
     if (id >= lanes) return;
-    const int per_token = units * lanes_h;
-    const int64_t token = id / per_token;
+    const uint32_t per_token = units * lanes_h, token = id / per_token;
     const int rest = (int)(id - token * per_token);
     const int hs = rest / units, u = rest - hs * units;
-    const int64_t b = token / a.d.length, i = token - b * a.d.length;
+    int64_t b = 0, i = token;
+    if (a.d.batch > 1) b = token / (uint32_t)a.d.length, i = token - b * a.d.length;
     const int R = a.d.rotary_dim, half = R / 2;
     const bool turn = u < pair_units;
     // first element of the run (halves: and of the second), and how many of each count
-    int e0, n0;
+    const int k0 = u * kPairs, pairs = min(half - k0, kPairs);
+    const int e0 = !turn ? R + (u - pair_units) * 8 : HALF ? k0 : 2 * k0, n0 = !turn ? a.d.head_dim - e0 : HALF ? pairs : 2 * pairs;
+    const int heads = a.d.heads_q + a.d.heads_k;
+    // four heads' values at a time; the first four are on the way while the table is read
+    constexpr int kBatch = 4;
+    typename Vec8<T>::type p[kBatch], w[kBatch];
+    const auto fetch = [&](int first) {
+#pragma unroll
+        for (int c = 0; c < kBatch; ++c) {
+            const int h = first + c * lanes_h;
+            if (h >= heads) break;
+            const bool is_k = h >= a.d.heads_q;
+            const int hh = is_k ? h - a.d.heads_q : h;
+            const int64_t* st = is_k ? a.d.k_stride : a.d.q_stride;
+            const T* x = static_cast<const T*>(is_k ? a.k : a.q) + b * st[0] + i * st[1] + hh * st[2] + e0;
+            p[c] = load8(x, n0);
+            if (HALF && turn) w[c] = load8(x + half, n0);
+        }
+    };
+    fetch(hs);
     float cs[kPairs], sn[kPairs];
     if (turn) {
-        const int k0 = u * kPairs, pairs = min(half - k0, kPairs);
-        e0 = HALF ? k0 : 2 * k0;
-        n0 = HALF ? pairs : 2 * pairs;
         const auto clamped = [&](int64_t pos) { return pos < 0 ? 0 : (pos >= a.d.table_rows ? a.d.table_rows - 1 : pos); };
         const auto set = [&](int e, float c, float s) {
             cs[e] = c;
@@ -111,42 +127,41 @@ __global__ __launch_bounds__(256) void k_rotary(const Args a, int units, int pai
                 }
             }
         }
-    } else {
-        e0 = R + (u - pair_units) * 8;
-        n0 = a.d.head_dim - e0;
     }
-    const int heads = a.d.heads_q + a.d.heads_k;
-    for (int h = hs; h < heads; h += lanes_h) {
-        const bool is_k = h >= a.d.heads_q;
-        const int hh = is_k ? h - a.d.heads_q : h;
-        const int64_t* st = is_k ? a.d.k_stride : a.d.q_stride;
-        const int64_t* so = is_k ? a.d.k_out_stride : a.d.q_out_stride;
-        const T* x = static_cast<const T*>(is_k ? a.k : a.q) + b * st[0] + i * st[1] + hh * st[2] + e0;
-        T* y = static_cast<T*>(is_k ? a.k_out : a.q_out) + b * so[0] + i * so[1] + hh * so[2] + e0;
-        typename Vec8<T>::type p = load8(x, n0);
-        if (!turn) {
-            store8(y, n0, p);
-            continue;
-        }
-        const f32x8 v = widen(p);
-        f32x8 ra;
-        if constexpr (HALF) {
-            const f32x8 w = widen(load8(x + half, n0));
-            f32x8 rb;
+    for (int first = hs; first < heads; first += kBatch * lanes_h) {
+        if (first != hs) fetch(first);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                ra[e] = v[e] * cs[e] - w[e] * sn[e];
-                rb[e] = v[e] * sn[e] + w[e] * cs[e];
+        for (int c = 0; c < kBatch; ++c) {
+            const int h = first + c * lanes_h;
+            if (h >= heads) break;
+            const bool is_k = h >= a.d.heads_q;
+            const int hh = is_k ? h - a.d.heads_q : h;
+            const int64_t* so = is_k ? a.d.k_out_stride : a.d.q_out_stride;
+            T* y = static_cast<T*>(is_k ? a.k_out : a.q_out) + b * so[0] + i * so[1] + hh * so[2] + e0;
+            if (!turn) {
+                store8(y, n0, p[c]);
+                continue;
             }
-            store8(y + half, n0, narrow<T>(rb));
-        } else {
+            const f32x8 v = widen(p[c]);
+            f32x8 ra;
+            if constexpr (HALF) {
+                const f32x8 vw = widen(w[c]);
+                f32x8 rb;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                ra[2 * e] = v[2 * e] * cs[e] - v[2 * e + 1] * sn[e];
-                ra[2 * e + 1] = v[2 * e] * sn[e] + v[2 * e + 1] * cs[e];
+                for (int e = 0; e < 8; ++e) {
+                    ra[e] = v[e] * cs[e] - vw[e] * sn[e];
+                    rb[e] = v[e] * sn[e] + vw[e] * cs[e];
+                }
+                store8(y + half, n0, narrow<T>(rb));
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    ra[2 * e] = v[2 * e] * cs[e] - v[2 * e + 1] * sn[e];
+                    ra[2 * e + 1] = v[2 * e] * sn[e] + v[2 * e + 1] * cs[e];
+                }
             }
+            store8(y, n0, narrow<T>(ra));
         }
-        store8(y, n0, narrow<T>(ra));
     }
 }
 
@@ -165,9 +180,9 @@ void rotary_t(const Args& a, hipStream_t s) {
     const int64_t lanes = tokens * units * lanes_h;
     const dim3 grid((unsigned)((lanes + 255) / 256)), block(256);
     if (d.layout == PD_ROTARY_HALF)
-        hipLaunchKernelGGL((k_rotary<T, true, Args>), grid, block, 0, s, a, units, pair_units, lanes_h, lanes);
+        hipLaunchKernelGGL((k_rotary<T, true, Args>), grid, block, 0, s, a, units, pair_units, lanes_h, (uint32_t)lanes);
     else
-        hipLaunchKernelGGL((k_rotary<T, false, Args>), grid, block, 0, s, a, units, pair_units, lanes_h, lanes);
+        hipLaunchKernelGGL((k_rotary<T, false, Args>), grid, block, 0, s, a, units, pair_units, lanes_h, (uint32_t)lanes);
     PD_HIP(hipGetLastError());
 }
 
