@@ -811,6 +811,12 @@ def pd_layernorm_backward(dy: torch.Tensor, sum_in: torch.Tensor, mean: torch.Te
               _rows_of(dsum, sh, dy.dtype, "dsum") if dsum is not None else 0,
               _rows_of(sum_in, sh, dy.dtype, "sum_in"), _rows_of(dy, sh, dy.dtype, "dy"), ws, 0, dt, 0.0)
     L = load()
+    if not rows and runs and runs[0]:          # runs without rows: each one's gradients are 0
+        for i in range(runs[0]):
+            _check(L.pd_layernorm_backward(d, None, None, None, None, None, None, None,
+                                           *(None if t is None else t[i].data_ptr() for t in (dweight, dbias)),
+                                           None, 0, _stream(stream)))
+        return
     needs = scratch is None and runs
     buf, have = _scratch(scratch, _scratch_need("pd_layernorm_backward_scratch", d) if needs else 0, stream)
     _check(L.pd_layernorm_backward(d, _ptr(dy), _ptr(sum_in), _ptr(weight), _ptr(mean), _ptr(rstd), _ptr(dsum),

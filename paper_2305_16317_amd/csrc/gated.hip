@@ -85,7 +85,11 @@ template <bool FINE, class V>
 __device__ __forceinline__ V activate(int act, V g) {
     switch (act) {
         case PD_ACT_SILU: return each(g, [](float v) { return v * sigmoid<FINE>(v); });
-        case PD_ACT_GELU: return each(g, [](float v) { return fmaf(-fabsf(v), normal_past<FINE>(v), fmaxf(v, 0.f)); });
+        case PD_ACT_GELU:
+            return each(g, [](float v) {
+                const float tail = normal_past<FINE>(v);
+                return v * (v < 0.f ? tail : 1.f - tail);
+            });
         case PD_ACT_GELU_TANH: return each(g, [](float v) { return v * sigmoid<FINE>(twice_inner(v)); });
         case PD_ACT_SIGMOID: return each(g, [](float v) { return sigmoid<FINE>(v); });
         default: return each(g, [](float v) { return positive(v); });

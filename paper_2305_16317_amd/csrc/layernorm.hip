@@ -139,7 +139,8 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_layernorm(const Layer
     for (int i = 0; i < NV; ++i)
 #pragma unroll
         for (int e = 0; e < 8; ++e) sum += v[i][e];
-    if (a.sum) {
+    const float mean = row_sum<TPR>(sum, slot) / (float)width;
+    if (a.sum) {                             // (all of the row has been read: sum may lie over x or residual)
         T* h = static_cast<T*>(a.sum) + row * a.d.sum_stride;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
@@ -147,7 +148,6 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_layernorm(const Layer
             store_first(h + c, width - c, narrow<T>(v[i]));
         }
     }
-    const float mean = row_sum<TPR>(sum, slot) / (float)width;
     float ss = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
@@ -268,10 +268,18 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR, BLOCKS) void k_layernorm_gra
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 const int c = (i * TPR + lane) * 8;
-                const f32x8 g = wide(KEEP ? now.dy[KEEP ? i : 0] : read(dy, i), i), w = weights(i);
-                const f32x8 nn = (wide(KEEP ? now.h[KEEP ? i : 0] : read(h, i), i) - mean) * rstd;
-                f32x8 o = {};
-                if (ds) o = wide(KEEP ? now.ds[KEEP ? i : 0] : read(ds, i), i);
+                f32x8 g, nn, o = {};
+                if constexpr (KEEP) {
+                    g = wide(now.dy[i], i);
+                    nn = wide(now.h[i], i);
+                    if (ds) o = wide(now.ds[i], i);
+                } else {                     // (its own values alone: dx may lie over dy or dsum)
+                    g = widen(load8(dy + c, width - c));
+                    nn = widen(load8(h + c, width - c));
+                    if (ds) o = widen(load8(ds + c, width - c));
+                }
+                const f32x8 w = weights(i);
+                nn = (nn - mean) * rstd;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) o[e] = fmaf(rstd, fmaf(-nn[e], dot, fmaf(g[e], w[e], -sum)), o[e]);
                 store_first(dx + c, width - c, narrow<T>(o));

@@ -170,6 +170,9 @@ def test_layernorm_backward_of_no_rows_and_against_differences():
     dw, db = torch.full((40,), 7.0, device="cuda"), torch.full((40,), 7.0, device="cuda")
     pd.pd_layernorm_backward(z, z, none, none, torch.empty_like(z), dweight=dw, dbias=db)
     assert torch.all(dw == 0) and torch.all(db == 0)
+    dw = torch.full((3, 40), 7.0, device="cuda")
+    pd.pd_layernorm_backward(z, z, none, none, torch.empty_like(z), dweight=dw)        # runs without rows
+    assert torch.all(dw == 0)
     pd.pd_layernorm_forward(z, torch.empty_like(z))
     x, dy, w, d = (_rand(s, F32, 20 + i) for i, s in enumerate([(4, 50), (4, 50), (2, 50), (4, 50)]))
     y, h, mean, rstd, dx = torch.empty_like(x), torch.empty_like(x), *(torch.empty(4, device="cuda") for _ in range(2)), torch.empty_like(x)
@@ -178,6 +181,32 @@ def test_layernorm_backward_of_no_rows_and_against_differences():
     loss = lambda e: float(np.sum(ob.layernorm(_np(x) + e * _np(d), None, _np(w), None, 1e-6)[1] * _np(dy)))  # noqa: E731
     want = (loss(1e-5) - loss(-1e-5)) / 2e-5
     assert abs(float((dx.double() * d.double()).sum()) - want) <= 1e-5 * float(dx.norm() * d.norm())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("width", [515, 1027, 2049, 4099, 4610, 8195, 16387, 32770])
+def test_layernorm_in_place_at_odd_widths(width, dtype):
+    """Widths whose last values are read together with a neighbour's, in another wave or step."""
+    print(f"layernorm in place {width} {dtype}", flush=True)
+    rows = 300
+    x, r, w = _rand((rows, width), dtype, 31), _rand((rows, width), dtype, 32), _rand((3, width), F32, 33)
+    s, y, mean, rstd = ob.layernorm(_np(x), _np(r), _np(w), None, 1e-6)
+    y2, r2 = x.clone(), r.clone()
+    pd.pd_layernorm_forward(y2, y2, weight=w, residual=r2, sum_out=r2)
+    _close(y2, y, TOL[dtype])
+    _close(r2, s, TOL[dtype])
+    mean, rstd = (torch.from_numpy(v).float().cuda() for v in (mean, rstd))
+    h, dw, db = r2, torch.empty_like(w), torch.empty_like(w)
+    rx, rw, rb = ob.layernorm_grad(_np(x), _np(h), _np(w), _np(mean), _np(rstd), _np(r), 3)
+    for over in (0, 1):                                     # dx over dy, over dsum; with the sums and alone
+        dy, ds = x.clone(), r.clone()
+        pd.pd_layernorm_backward(dy, h, mean, rstd, (dy, ds)[over], weight=w, dweight=dw, dbias=db, dsum=ds)
+        _close((dy, ds)[over], rx, TOL[dtype])
+        _close(dw, rw, 5e-6)
+        _close(db, rb, 5e-6)
+        dy, ds = x.clone(), r.clone()
+        pd.pd_layernorm_backward(dy, h, mean, rstd, (dy, ds)[over], weight=w, dsum=ds)
+        _close((dy, ds)[over], rx, TOL[dtype])
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
@@ -480,6 +509,34 @@ def test_gated_of_many_tiles(M, D, F, layout):
     rx, rg, ru, _ = ob.gated_grad(*(_np(t) for t in (dh, x, wg, wu, g, u)), "silu")
     for got, ref in ((dx, rx), (dw[0], rg), (dw[1], ru)):
         _close(got, ref, TOL_GRAD[BF16])
+
+
+def test_gated_activations_of_infinite_gates():
+    """Through few rows, many rows and bfloat16: act(inf) = inf (the sigmoid: 1), and NaN stays."""
+    for dtype, rows in ((BF16, 4), (BF16, 300)):            # (float32 products give NaN for an infinity)
+        g = torch.tensor([float("inf"), NAN, 3.0], device="cuda").repeat(rows, 1).to(dtype)
+        x = torch.cat([g[:, :1], torch.ones_like(g[:, :1])], 1)
+        for act in ACTS:
+            for value, want in ((float("inf"), 1.0 if act == "sigmoid" else float("inf")), (NAN, NAN), (-200.0, 0.0)):
+                x[:, 0] = value
+                wg, wu = torch.tensor([[1.0], [0.0]], device="cuda", dtype=dtype), torch.tensor([[0.0], [1.0]], device="cuda", dtype=dtype)
+                x2 = x.clone()
+                h = torch.empty((rows, 1), device="cuda", dtype=dtype)
+                up = torch.empty_like(h)
+                pd.pd_gated_forward(x2, wg, wu, h, up=up, activation=ACTS[act])
+                if value == value and abs(value) != float("inf"):
+                    assert torch.all(h == want), (act, value)
+                else:                                       # 0 times the value is NaN in up, and so in h
+                    assert torch.isnan(up).all() and torch.isnan(h).all()
+        # the slopes' kernel alone: h from gate and up as stored
+        for act in ACTS:
+            gate = torch.tensor([[float("inf"), NAN, -200.0, 200.0]], device="cuda", dtype=dtype).repeat(rows, 2)
+            one, h = torch.ones_like(gate), torch.empty_like(gate)
+            w = torch.zeros((8, 8), device="cuda", dtype=dtype)
+            pd.pd_gated_backward(one, torch.zeros((rows, 8), device="cuda", dtype=dtype), w, w, gate, one, h=h, activation=ACTS[act])
+            top = 1.0 if act == "sigmoid" else float("inf")
+            assert torch.all(h[:, 0] == top) and torch.isnan(h[:, 1]).all() and torch.all(h[:, 2] == 0), act
+            assert torch.all(h[:, 3] == (1.0 if act == "sigmoid" else 200.0)), act
 
 
 @pytest.mark.parametrize("act", sorted(ACTS))
