@@ -880,13 +880,17 @@ Matrix inputs(const GatedArgs& a, const Layout& l, Operands& o) {
     const pd_gated_desc& d = a.d;
     return o.add(d.dtype, a.x, d.x_stride, d.rows, d.width, a.scratch + l.x, as_it_lies(d.dtype, a.x, d.x_stride, d.rows, d.width));
 }
-// Both weights lie alike, as the kernel has one distance of rows for them.
-void weights(const GatedArgs& a, const Layout& l, Matrix& gate, Matrix& up, Operands& o) {
+// Both weights lie alike, as the kernel has one distance of rows for them.  `along`: the
+// product reads them along the sum, 128 bytes of a row at a time; where these straddle the
+// memory's lines and there are many rows, laying them out pays (20000 x 1000 x 2664: 298 and
+// 266 us; 4608 rows 77 and 70; read across the sum 236 and 232).
+void weights(const GatedArgs& a, const Layout& l, bool along, Matrix& gate, Matrix& up, Operands& o) {
     const pd_gated_desc& d = a.d;
     const bool in_out = d.weight_layout == PD_WEIGHTS_IN_OUT;
     const int64_t rows = in_out ? d.width : d.hidden, cols = in_out ? d.hidden : d.width;
     const bool lie = as_it_lies(d.dtype, a.w_gate, d.w_gate_stride, rows, cols) &&
-                     as_it_lies(d.dtype, a.w_up, d.w_up_stride, rows, cols) && (rows == 1 || d.w_gate_stride == d.w_up_stride);
+                     as_it_lies(d.dtype, a.w_up, d.w_up_stride, rows, cols) && (rows == 1 || d.w_gate_stride == d.w_up_stride) &&
+                     !(along && d.rows >= 8192 && rows > 1 && d.w_gate_stride % 64);
     gate = o.add(d.dtype, a.w_gate, d.w_gate_stride, rows, cols, a.scratch + l.w, lie);
     up = o.add(d.dtype, a.w_up, d.w_up_stride, rows, cols, a.scratch + l.w + layout_bytes(d.dtype, rows, cols), lie);
 }
@@ -920,7 +924,7 @@ void gated_t(const GatedArgs& a, hipStream_t s) {
     Operands o;
     Matrix wg, wu;
     const Matrix x = inputs(a, l, o);
-    weights(a, l, wg, wu, o);
+    weights(a, l, d.weight_layout == PD_WEIGHTS_OUT_IN, wg, wu, o);
     o.run(d.dtype, s);
     Product p{};
     add_segments(p, d.dtype, x, wg, wu);
@@ -964,7 +968,7 @@ void gated_grad_t(const GatedArgs& a, hipStream_t s) {
     float* partial = reinterpret_cast<float*>(a.scratch + l.partial);
     Operands o;
     Matrix x, wg, wu;
-    if (a.dx) weights(a, l, wg, wu, o);
+    if (a.dx) weights(a, l, in_out, wg, wu, o);
     if (a.dw_gate) x = inputs(a, l, o);
     o.run(d.dtype, s);
     if (a.dx) {

@@ -495,7 +495,7 @@ def test_gated_backward(M, D, F, layout, dtype):
 
 
 @pytest.mark.parametrize("layout", [pd.PD_WEIGHTS_IN_OUT, pd.PD_WEIGHTS_OUT_IN])
-@pytest.mark.parametrize("M,D,F", [(4100, 136, 2056), (2304, 320, 1336), (8200, 72, 1000)])
+@pytest.mark.parametrize("M,D,F", [(4100, 136, 2056), (2304, 320, 1336), (8200, 72, 1000), (6200, 264, 1544), (1700, 200, 2731)])
 def test_gated_of_many_tiles(M, D, F, layout):
     """Enough tiles for the large blocks; the sums over many rows in parts."""
     x, dh = _rand((M, D), BF16, 80), _rand((M, F), BF16, 81)
