@@ -626,15 +626,15 @@ __device__ inline Split split_any(f32x8 x) {
 }
 // [rows][cols] as bfloat16 [rows][pitch], zeros past cols; float32: three parts, each a
 // matrix.
-template <typename T>
+template <int PARTS>
 __device__ inline void store_parts(bf16* to, int64_t plane, f32x8 v) {
-    if constexpr (sizeof(T) == 2) {
+    if constexpr (PARTS == 1) {
         *reinterpret_cast<bf16x8*>(to) = narrow<bf16>(v);
     } else {
         const Split s = split_any(v);
         *reinterpret_cast<bf16x8*>(to) = s.h;
         *reinterpret_cast<bf16x8*>(to + plane) = s.m;
-        *reinterpret_cast<bf16x8*>(to + 2 * plane) = s.l;
+        if constexpr (PARTS == 3) *reinterpret_cast<bf16x8*>(to + 2 * plane) = s.l;
     }
 }
 struct LayOut {
@@ -656,7 +656,7 @@ __global__ __launch_bounds__(256) void k_lay_out(const LayOuts a) {
         const int c = (int)(in - row * (m.pitch / 8)) * 8;
         f32x8 v = {};
         if (c < m.cols) v = widen(load8(static_cast<const T*>(m.from) + row * m.stride + c, m.cols - c));
-        store_parts<T>(m.to + row * m.pitch + c, m.rows * m.pitch, v);
+        store_parts<sizeof(T) == 4 ? 3 : 1>(m.to + row * m.pitch + c, m.rows * m.pitch, v);
     }
 }
 
@@ -671,7 +671,7 @@ struct SlopeArgs {
     bf16* dg;                // then du, after all parts of dg
     int64_t du;              // elements from dg to du
 };
-template <typename T>
+template <typename T, int PARTS>
 __global__ __launch_bounds__(256) void k_gated_slopes(const SlopeArgs a) {
     const int64_t units = a.rows * (a.pitch / 8);
     for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < units; u += (int64_t)gridDim.x * 256) {
@@ -690,8 +690,8 @@ __global__ __launch_bounds__(256) void k_gated_slopes(const SlopeArgs a) {
         }
         if (!a.dg) continue;
         bf16* to = a.dg + row * a.pitch + c;
-        store_parts<T>(to, a.rows * a.pitch, dg);
-        store_parts<T>(to + a.du, a.rows * a.pitch, du);
+        store_parts<PARTS>(to, a.rows * a.pitch, dg);
+        store_parts<PARTS>(to + a.du, a.rows * a.pitch, du);
     }
 }
 
@@ -713,8 +713,14 @@ struct Matrix {
     const bf16* part[3];
     int64_t ld;
 };
+constexpr int64_t kFewRows = 32;
 int parts_of(int dtype) { return dtype == PD_F32 ? 3 : 1; }
-int64_t layout_bytes(int dtype, int64_t rows, int64_t cols) { return rows * up_to(cols, 64) * 2 * parts_of(dtype); }
+// Parts of dg and du.  In bfloat16 one: their rounding adds as much to a gradient's error as its
+// own does, in the root mean square 1.41 times it together.  Few rows have few such roundings,
+// which a large one may rule (1.8 times was seen): they are kept in two, where the weights' bytes
+// and the launches make up the time.
+int slope_parts(const pd_gated_desc& d) { return d.dtype == PD_F32 ? 3 : d.rows <= kFewRows ? 2 : 1; }
+int64_t layout_bytes(int parts, int64_t rows, int64_t cols) { return rows * up_to(cols, 64) * 2 * parts; }
 // Copies of 16 bytes read the matrix as it lies.
 bool as_it_lies(int dtype, const void* p, int64_t stride, int64_t rows, int64_t cols) {
     return dtype == PD_BF16 && (uintptr_t)p % 16 == 0 && cols % 8 == 0 && (rows == 1 || (stride % 8 == 0 && stride < (1 << 22)));
@@ -740,10 +746,13 @@ struct Operands {
         PD_HIP(hipGetLastError());
     }
 };
-// Appends the segments of a times (b0, b1) to p.
-void add_segments(Product& p, int dtype, const Matrix& a, const Matrix& b0, const Matrix& b1) {
+// Appends the segments of a times (b0, b1) to p, small ones first: of the parts 0, 1, 2 of
+// each the pairs whose numbers add up to 2 at most.
+int segments(int parts_a, int parts_b) { return parts_a == 3 && parts_b == 3 ? 6 : parts_a * parts_b; }
+void add_segments(Product& p, const Matrix& a, int parts_a, const Matrix& b0, const Matrix& b1, int parts_b) {
     static const int pa[6] = {2, 0, 1, 1, 0, 0}, pb[6] = {0, 2, 1, 0, 1, 0};
-    for (int i = dtype == PD_F32 ? 0 : 5; i < 6; ++i) {
+    for (int i = 0; i < 6; ++i) {
+        if (pa[i] >= parts_a || pb[i] >= parts_b) continue;
         p.a[p.segs] = a.part[pa[i]];
         p.b0[p.segs] = b0.part[pb[i]];
         p.b1[p.segs] = b1.part[pb[i]];
@@ -855,9 +864,9 @@ Layout layout(const pd_gated_desc& d, bool backward) {
         at += up_to(bytes, 256);
         return here;
     };
-    const int segs = d.dtype == PD_F32 ? 6 : 1;
-    l.x = take(layout_bytes(d.dtype, d.rows, d.width));
-    l.w = take(2 * (in_out ? layout_bytes(d.dtype, d.width, d.hidden) : layout_bytes(d.dtype, d.hidden, d.width)));
+    const int parts = parts_of(d.dtype), slopes = slope_parts(d), segs = segments(backward ? slopes : parts, parts);
+    l.x = take(layout_bytes(parts, d.rows, d.width));
+    l.w = take(2 * (in_out ? layout_bytes(parts, d.width, d.hidden) : layout_bytes(parts, d.hidden, d.width)));
     int64_t partial = 0;
     const auto more = [&](int64_t m, int64_t n, bool apart, int groups, int64_t k, int segs, bool across) {
         const int64_t b = partial_bytes(cut(m, n, apart, groups, k, segs, across), m, n, apart, groups);
@@ -866,7 +875,7 @@ Layout layout(const pd_gated_desc& d, bool backward) {
     if (!backward) {
         more(d.rows, d.hidden, true, 1, d.width, segs, false);
     } else {
-        l.slopes = take(2 * layout_bytes(d.dtype, d.rows, d.hidden));
+        l.slopes = take(2 * layout_bytes(slopes, d.rows, d.hidden));
         more(d.rows, d.width, false, 1, d.hidden, 2 * segs, false);
         if (in_out) more(d.width, d.hidden, true, 1, d.rows, segs, true);
         else more(d.hidden, d.width, false, 2, d.rows, segs, true);
@@ -892,10 +901,9 @@ void weights(const GatedArgs& a, const Layout& l, bool along, Matrix& gate, Matr
                      as_it_lies(d.dtype, a.w_up, d.w_up_stride, rows, cols) && (rows == 1 || d.w_gate_stride == d.w_up_stride) &&
                      !(along && d.rows >= 8192 && rows > 1 && d.w_gate_stride % 64);
     gate = o.add(d.dtype, a.w_gate, d.w_gate_stride, rows, cols, a.scratch + l.w, lie);
-    up = o.add(d.dtype, a.w_up, d.w_up_stride, rows, cols, a.scratch + l.w + layout_bytes(d.dtype, rows, cols), lie);
+    up = o.add(d.dtype, a.w_up, d.w_up_stride, rows, cols, a.scratch + l.w + layout_bytes(parts_of(d.dtype), rows, cols), lie);
 }
 
-constexpr int64_t kFewRows = 32;
 template <typename T>
 void gated_few(const GatedArgs& a, hipStream_t s) {
     const pd_gated_desc& d = a.d;
@@ -927,7 +935,7 @@ void gated_t(const GatedArgs& a, hipStream_t s) {
     weights(a, l, d.weight_layout == PD_WEIGHTS_OUT_IN, wg, wu, o);
     o.run(d.dtype, s);
     Product p{};
-    add_segments(p, d.dtype, x, wg, wu);
+    add_segments(p, x, parts_of(d.dtype), wg, wu, parts_of(d.dtype));
     p.k = d.width, p.m = (int)d.rows, p.n = d.hidden;
     p.apart = 1, p.groups = 1;
     p.act = d.activation;
@@ -961,8 +969,12 @@ void gated_grad_t(const GatedArgs& a, hipStream_t s) {
     g.ld_gate = d.gate_stride, g.ld_up = d.up_stride, g.ld_dh = d.dh_stride, g.ld_h = d.h_stride;
     g.rows = d.rows, g.cols = d.hidden, g.pitch = (int)pitch, g.act = d.activation;
     g.dg = products ? reinterpret_cast<bf16*>(a.scratch + l.slopes) : nullptr;
-    g.du = parts_of(d.dtype) * plane;
-    hipLaunchKernelGGL(k_gated_slopes<T>, dim3(blocks_for(d.rows * pitch / 8)), dim3(256), 0, s, g);
+    const int parts = parts_of(d.dtype), slopes = slope_parts(d);
+    g.du = slopes * plane;
+    const dim3 grid(blocks_for(d.rows * pitch / 8)), block(256);
+    if (sizeof(T) == 4) hipLaunchKernelGGL((k_gated_slopes<T, 3>), grid, block, 0, s, g);
+    else if (slopes == 2) hipLaunchKernelGGL((k_gated_slopes<T, 2>), grid, block, 0, s, g);
+    else hipLaunchKernelGGL((k_gated_slopes<T, 1>), grid, block, 0, s, g);
     PD_HIP(hipGetLastError());
     const Matrix dg{{g.dg, g.dg + plane, g.dg + 2 * plane}, pitch}, du{{g.dg + g.du, g.dg + g.du + plane, g.dg + g.du + 2 * plane}, pitch};
     float* partial = reinterpret_cast<float*>(a.scratch + l.partial);
@@ -973,8 +985,8 @@ void gated_grad_t(const GatedArgs& a, hipStream_t s) {
     o.run(d.dtype, s);
     if (a.dx) {
         Product p{};
-        add_segments(p, d.dtype, dg, wg, wg);
-        add_segments(p, d.dtype, du, wu, wu);
+        add_segments(p, dg, slopes, wg, wg, parts);
+        add_segments(p, du, slopes, wu, wu, parts);
         p.k = d.hidden, p.m = (int)d.rows, p.n = d.width;
         p.apart = 0, p.groups = 1;
         p.c[0] = a.dx, p.ldc[0] = d.dx_stride;
@@ -984,11 +996,11 @@ void gated_grad_t(const GatedArgs& a, hipStream_t s) {
     if (a.dw_gate) {
         Product p{};
         if (in_out) {
-            add_segments(p, d.dtype, x, dg, du);
+            add_segments(p, x, parts, dg, du, slopes);
             p.m = d.width, p.n = d.hidden;
             p.apart = 1, p.groups = 1;
         } else {
-            add_segments(p, d.dtype, dg, x, x);
+            add_segments(p, dg, slopes, x, x, parts);
             p.m = d.hidden, p.n = d.width;
             p.apart = 0, p.groups = 2, p.a_group = g.du;
         }

@@ -5,8 +5,8 @@ largest of its value, the tensor's root mean square and its row's):
   float32   a norm's sums, a product's parts and its sum are 2^-24 each relative to their terms;
             with the activations' functions under 1e-6: 5e-6.
   bfloat16  a rounding is 2^-9 at most in the root mean square 1.7e-3 of the result: 4e-3; gradients
-            of the gated product round dgate and dup before their products (a sum's error is theirs
-            in the root mean square) and the result: 6e-3.
+            of the gated product of more than 32 rows round dgate and dup before their products (a
+            sum's error is theirs in the root mean square) and the result: 6e-3.
 """
 import numpy as np
 import pytest
@@ -483,7 +483,7 @@ def test_gated_backward(M, D, F, layout, dtype):
         pd.pd_gated_backward(dh, x, wg, wu, g, u, dx=dxb[:, 2:D + 2], dw_gate=dw[0], dw_up=dw[1], h=hb[:, :F], activation=ACTS[act])
         rx, rg, ru, rh = ob.gated_grad(*(_np(t) for t in (dh, x, wg, wu, g, u)), act)
         assert _untouched(dxb, 2, D, 9.0) and _untouched(hb, 0, F, 9.0)
-        tol = TOL_GRAD[dtype]
+        tol = TOL_GRAD[dtype] if M > 32 else TOL[dtype]     # (few rows keep dgate and dup in two parts)
         _close(dxb[:, 2:D + 2], rx, tol, "dx")
         _close(dw[0], rg, tol, "dw_gate")
         _close(dw[1], ru, tol, "dw_up")
