@@ -576,7 +576,8 @@ pd_status pd_dropout_apply(const pd_dropout_desc* desc, const void* x, const voi
  * keeps fewer) with products to 2^-24, as in attention; an infinity among them gives NaN.  In
  * PD_BF16 dgate and dup are rounded to bfloat16 as operands of the matrix cores (up to 32 rows
  * to twice its bits).  Sums are float32.  relu'(0) = 0.
- * 1 <= width, hidden <= 2^20; rows <= 2^24 (more: PD_ERR_UNSUPPORTED). */
+ * 1 <= width, hidden <= 2^20; more than 2^24 rows, or than 2^28 tiles of 64 x 64 in a product:
+ * PD_ERR_UNSUPPORTED. */
 #define PD_ACT_SILU 0
 #define PD_ACT_GELU 1
 #define PD_ACT_GELU_TANH 2

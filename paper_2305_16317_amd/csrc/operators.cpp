@@ -178,10 +178,10 @@ void check_gated(const pd_gated_desc& d) {
                       d.dw_gate_stride, d.dw_up_stride})
         check_stride(s);
     if (d.rows > (int64_t)1 << 24) fail(PD_ERR_UNSUPPORTED, "more than 2^24 rows are not implemented");
-    // a launch holds fewer than 2^32 threads, and a step's operands fewer than 2^40 elements
-    const int64_t tiles = ((int64_t)d.rows / 64 + 1) * (d.hidden / 64 + 1), tiles_x = ((int64_t)d.rows / 64 + 1) * (d.width / 64 + 1);
-    if (tiles > 1 << 22 || tiles_x > 1 << 22 || (int64_t)(d.width / 64 + 1) * (d.hidden / 64 + 1) > 1 << 22)
-        fail(PD_ERR_UNSUPPORTED, "products of more than 2^22 tiles of 64 x 64 are not implemented");
+    // tiles are counted in 32 bits
+    const int64_t m = d.rows / 64 + 1, n = d.hidden / 64 + 1, k = d.width / 64 + 1;
+    if (m * n > 1 << 28 || m * k > 1 << 28 || n * k > 1 << 28)
+        fail(PD_ERR_UNSUPPORTED, "products of more than 2^28 tiles of 64 x 64 are not implemented");
 }
 void check_rows_of(const char* what, const void* p, int64_t stride, int64_t rows, int64_t cols) {
     require(!p || rows <= 1 || stride >= cols, std::string(what) + ": rows of an output share elements");

@@ -209,7 +209,7 @@ def _gated(**kw):
     (dict(rows=-1), 1, "rows"), (dict(width=0), 1, "width"), (dict(hidden=0), 1, "hidden"), (dict(hidden=2**20 + 1), 1, "hidden"),
     (dict(dtype=2), 1, "dtype"), (dict(activation=5), 1, "activation"), (dict(activation=-1), 1, "activation"),
     (dict(weight_layout=2), 1, "weight_layout"), (dict(x_stride=-1), 1, "stride"), (dict(dw_up_stride=2**40), 1, "stride"),
-    (dict(rows=2**24 + 1), 5, "rows"), (dict(rows=2**24, hidden=2**12), 5, "tiles"), (dict(width=2**20, hidden=2**20), 5, "tiles")])
+    (dict(rows=2**24 + 1), 5, "rows"), (dict(rows=2**24, hidden=2**20), 5, "tiles"), (dict(width=2**20, hidden=2**20), 5, "tiles")])
 def test_gated_refusals(kw, code, msg):
     d = _gated(**kw)
     n = ctypes.c_int64()

@@ -713,3 +713,43 @@ def test_block_on_another_stream_and_in_graphs(n, dtype):
         assert all(torch.equal(a, b) for a, b in zip(outs, want)), i
         seen.append((outs[0] == res).flatten())
     assert not torch.equal(seen[0], seen[1])
+
+
+# ------------------------------------------------------------------ offsets past 32 bits
+def test_offsets_past_32_bits():
+    """Tensors of more than 2^31 values, of which the last rows hold numbers."""
+    rows, width = (1 << 21) + 40, 1032
+    x = torch.zeros((rows, width), device="cuda", dtype=BF16)
+    y = torch.empty_like(x)
+    x[-3:] = _rand((3, width), BF16, 150)
+    w = _rand((2, width), F32, 151)
+    pd.pd_layernorm_forward(x, y, weight=w, eps=1.0)
+    _close(y[-3:], ob.layernorm(_np(x[-3:]), None, _np(w[1]), None, 1.0)[1], TOL[BF16])
+    assert not y[:-3].any()
+    mean, rstd = torch.zeros(rows, device="cuda"), torch.ones(rows, device="cuda")
+    dw = torch.empty_like(w)
+    pd.pd_layernorm_backward(x, x, mean, rstd, y, weight=w, dweight=dw)
+    rx, rw, _ = ob.layernorm_grad(_np(x[-3:]), _np(x[-3:]), _np(w[1]), np.zeros(3), np.ones(3), None)
+    _close(y[-3:], rx, TOL[BF16])
+    _close(dw[1], rw, 5e-6)
+    assert not dw[0].any() and not y[:-3].any()
+    pd.pd_dropout_apply(x, y, 0.5, 7)
+    _close(y[-3:], ob.dropout(_np(x[-3:]), None, 0.5, ob.kept(3, width, 0.5, 7, 0, 0, rows - 3)), TOL[BF16])
+    del x, y
+    rows, F = 270000, 8192
+    x = torch.zeros((rows, 40), device="cuda", dtype=BF16)
+    x[-3:] = _rand((3, 40), BF16, 152)
+    wg, wu = _weights(40, F, BF16, 153, pd.PD_WEIGHTS_IN_OUT)
+    h, g, u = (torch.full((rows, F), 9.0, device="cuda", dtype=BF16) for _ in range(3))
+    pd.pd_gated_forward(x, wg, wu, h, gate=g, up=u)
+    rh, rg, ru = ob.gated(_np(x[-3:]), _np(wg), _np(wu), "silu")
+    for got, ref in ((h, rh), (g, rg), (u, ru)):
+        _close(got[-3:], ref, TOL[BF16])
+        assert not got[:-3].any()
+    dx, dw = torch.full_like(x, 9.0), [torch.empty_like(t) for t in (wg, wu)]
+    pd.pd_gated_backward(h, x, wg, wu, g, u, dx=dx, dw_gate=dw[0], dw_up=dw[1])
+    rx, rg, ru, _ = ob.gated_grad(*(_np(t) for t in (h[-3:], x[-3:], wg, wu, g[-3:], u[-3:])), "silu")
+    _close(dx[-3:], rx, TOL_GRAD[BF16])
+    assert not dx[:-3].any()
+    _close(dw[0], rg, TOL_GRAD[BF16])
+    _close(dw[1], ru, TOL_GRAD[BF16])
