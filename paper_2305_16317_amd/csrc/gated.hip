@@ -9,7 +9,7 @@
 // it (transposing LDS reads).  float32 operands are split into three bfloat16 parts first,
 // and the six products of parts that count are six segments of the sum, small ones first.
 // Operands that copies of 16 bytes cannot read (alignment, odd sizes) are laid out first.
-// Up to 32 rows forward go to a kernel of their own (k_gated_few).
+// Few rows forward (up to 64 or 128) go to a kernel of their own (k_gated_few).
 //
 // What bounds it: the matrix units (a 32 x 32 x 16 product takes 32 cycles, and a wave of
 // 128 x 128 results issues 64 of them a step), with one wave a SIMD that has to find everything
@@ -504,43 +504,75 @@ __global__ __launch_bounds__(256) void k_product_join(const Product p) {
 }
 
 // ------------------------------------------------------------------ few rows
-// Up to 32 rows (a token of each of some sequences): bound by the weights, which are read
-// once.  A block takes 32 columns of gate and of up; each of its four waves takes every
+// Few rows (a token of each of some sequences): bound by the weights, which are read once for
+// 32 rows.  A block takes 32 (or 16) columns of gate and of up; each of its four waves takes every
 // fourth 128 bytes along the sum (64 values, or 32 in float32) through LDS of its own, three
 // such steps on the way, and the four join in LDS: one launch and no barrier before the end.
-// (1 x 1024 x 4096 bfloat16: 5.9 us in the kernel, of which 3.4 are the weights' 16.8 MB; through
-// k_product with the sum in parts and their join 9.)
+// (1 x 1024 x 4096 bfloat16: 4.0 to 5.5 us in the kernel, of which 3.4 are the weights' 16.8 MB; through
+// k_product with the sum in parts and their join 9.  Odd sizes go through registers, two steps on the way:
+// 1 x 1001 x 2731 5.4 to 7.1.)
 // float32 runs on float32's own matrix instructions.
 // A step's tile of one operand: 4 KB, which a wave copies.  ACROSS: its rows run along the sum.
-template <typename T, bool ACROSS>
+// BOTH: half of the tile (rows; ACROSS: columns) is of a second matrix.
+template <typename T, bool ACROSS, bool BOTH = false>
 struct FewTile {
     static constexpr int E = 16 / (int)sizeof(T), KT = 8 * E;             // values a unit; of the sum a tile
     static constexpr int UNITS = ACROSS ? 32 / E : 8;
     using Ti = Operand<256, UNITS, ACROSS>;                                // (its order in LDS)
-    // `left`: rows (ACROSS: columns) from the tile's first on, repeated past the last; k: values
-    // of the sum, zeros past the last.  COPY: 16 bytes a lane past the registers.
-    template <bool COPY>
-    static __device__ __forceinline__ void fill(const T* base, int64_t stride, int left, int k, char* lds, int lane) {
+    // `left`: rows (ACROSS: columns) from the tile's first on; k: values of the sum, zeros past
+    // the last.  Here 16 bytes a lane past the registers, rows repeated past the last ..
+    static __device__ __forceinline__ bool second(int& row, int& unit) {
+        int& at = ACROSS ? unit : row;
+        constexpr int kHalf = ACROSS ? UNITS / 2 : 16;
+        if (!BOTH || at < kHalf) return false;
+        at -= kHalf;
+        return true;
+    }
+    static __device__ __forceinline__ void copy(const T* base, int64_t stride, const T* base2, int64_t stride2, int left, int k, char* lds, int lane) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int at = i * 64 + lane;
             int row = at / UNITS, unit = (at % UNITS) ^ Ti::swz(row);
-            if constexpr (COPY) {
-                const bool real = ACROSS ? row < k : unit * E < k;
-                if (ACROSS) unit = min(unit, (left + E - 1) / E - 1);
-                else row = min(row, left - 1);
-                copy16_from(real ? reinterpret_cast<const char*>(base + row * stride + unit * E) : reinterpret_cast<const char*>(kZeros),
-                            __builtin_amdgcn_readfirstlane(lds_address(lds) + i * 1024));
-            } else {
-                const int n = ACROSS ? (row < k ? left - unit * E : 0) : (row < left ? k - unit * E : 0);
-                T v[E];
+            const bool other = second(row, unit);
+            const bool real = ACROSS ? row < k : unit * E < k;
+            if (ACROSS) unit = min(unit, (left + E - 1) / E - 1);
+            else row = min(row, left - 1);
+            copy16_from(real ? reinterpret_cast<const char*>((other ? base2 + row * stride2 : base + row * stride) + unit * E) : reinterpret_cast<const char*>(kZeros),
+                        __builtin_amdgcn_readfirstlane(lds_address(lds) + i * 1024));
+        }
+    }
+    // .. and here through registers, from any alignment.  A unit past the end of a row reads the
+    // row's last E values (there are as many) and moves them down: a branch for each unit waited
+    // for each unit's load (8 x 2688 x 687 41 us).  put() has load()'s arguments.
+    typedef uint64_t Unit __attribute__((ext_vector_type(2)));
+    Unit v[4];
+    static __device__ __forceinline__ int start(int unit, int left, int k) { return min(unit * E, (ACROSS ? left : k) - E); }
+    __device__ __forceinline__ void load(const T* base, int64_t stride, const T* base2, int64_t stride2, int left, int k, int lane) {
+        typedef uint64_t Unit_u __attribute__((ext_vector_type(2), aligned(2)));
 #pragma unroll
-                for (int e = 0; e < E; ++e) v[e] = e < n ? base[row * stride + unit * E + e] : (T)0.f;
-                typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-                u32x4 w;
-                __builtin_memcpy(&w, v, 16);
-                *reinterpret_cast<u32x4*>(lds + Ti::place(row, unit)) = w;
+        for (int i = 0; i < 4; ++i) {
+            const int at = i * 64 + lane;
+            int row = at / UNITS, unit = (at % UNITS) ^ Ti::swz(row);
+            const bool other = second(row, unit);
+            row = min(row, (ACROSS ? k : left) - 1);
+            v[i] = *reinterpret_cast<const Unit_u*>((other ? base2 + row * stride2 : base + row * stride) + start(unit, left, k));
+        }
+    }
+    __device__ __forceinline__ void put(int left, int k, char* lds, int lane) const {
+        const bool whole = k >= KT && (!ACROSS || left >= (BOTH ? 16 : 32));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            Unit w = v[i];
+            if (!whole) {
+                const int at = i * 64 + lane;
+                int row = at / UNITS, unit = (at % UNITS) ^ Ti::swz(row);
+                second(row, unit);
+                const int off = (unit * E - start(unit, left, k)) * (int)sizeof(T) * 8;
+                const uint64_t low = off ? w[0] >> (off & 63) | (w[1] << 1) << (63 - (off & 63)) : w[0];
+                w = off >= 128 ? Unit{} : off >= 64 ? Unit{w[1] >> (off & 63), 0} : Unit{low, w[1] >> (off & 63)};
+                if (ACROSS && row >= k) w = Unit{};
             }
+            *reinterpret_cast<Unit*>(lds + i * 1024 + lane * 16) = w;
         }
     }
     // step c of 16 as a fragment
@@ -571,72 +603,108 @@ struct FewArgs {
     int64_t ld_x, ld_gate_w, ld_up_w, ld_h, ld_gate, ld_up;
     int rows, width, hidden, act;
 };
-template <typename T, bool ACROSS, bool COPY>
+template <typename T, bool ACROSS, bool COPY, int COLS>
 __global__ __launch_bounds__(256) void k_gated_few(const FewArgs p) {
+    constexpr bool BOTH = COLS == 16;
+    constexpr int kW = BOTH ? 1 : 2;                                       // tiles of weights
     using X = FewTile<T, false>;
-    using W = FewTile<T, ACROSS>;
-    constexpr int kSlots = 3, kTile = 4096, kSlot = 3 * kTile, kCopies = 12, KT = X::KT;
+    using W = FewTile<T, ACROSS, BOTH>;
+    constexpr int kSlots = COPY ? 3 : 1, kTile = 4096, kSlot = (1 + kW) * kTile, kCopies = 4 * (1 + kW), KT = X::KT;
     __shared__ __attribute__((aligned(256))) char lds[4 * kSlots * kSlot];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     char* mine = lds + wave * kSlots * kSlot;
-    const int n0 = near_blocks(blockIdx.x, gridDim.x) * 32;
+    // neighbours on a die: the same columns of other rows
+    const int high = (p.rows + 31) / 32, id = near_blocks(blockIdx.x, gridDim.x), n0 = id / high * COLS, m0 = id % high * 32;
+    const int rows = min(p.rows - m0, 32);
     const int steps = (p.width + KT - 1) / KT, count = steps > wave ? (steps - wave + 3) / 4 : 0;     // this wave's
-    const auto fill = [&](int t) {
-        const int k0 = (wave + 4 * t) * KT, k = p.width - k0;
-        char* to = mine + t % kSlots * kSlot;
-        X::template fill<COPY>(static_cast<const T*>(p.x) + k0, p.ld_x, p.rows, k, to, lane);
-        const T* wg = static_cast<const T*>(p.w_gate) + (ACROSS ? k0 * p.ld_gate_w + n0 : n0 * p.ld_gate_w + k0);
-        const T* wu = static_cast<const T*>(p.w_up) + (ACROSS ? k0 * p.ld_up_w + n0 : n0 * p.ld_up_w + k0);
-        W::template fill<COPY>(wg, p.ld_gate_w, p.hidden - n0, k, to + kTile, lane);
-        W::template fill<COPY>(wu, p.ld_up_w, p.hidden - n0, k, to + 2 * kTile, lane);
-    };
+    const T* x0 = static_cast<const T*>(p.x) + m0 * p.ld_x;
+    const auto of_gate = [&](int k0) { return static_cast<const T*>(p.w_gate) + (ACROSS ? k0 * p.ld_gate_w + n0 : n0 * p.ld_gate_w + k0); };
+    const auto of_up = [&](int k0) { return static_cast<const T*>(p.w_up) + (ACROSS ? k0 * p.ld_up_w + n0 : n0 * p.ld_up_w + k0); };
     f32x16 g = {}, u = {};
-#pragma unroll 1
-    for (int t = 0; t < kSlots && t < count; ++t) fill(t);
-#pragma unroll 1
-    for (int t = 0; t < count; ++t) {
-        if constexpr (COPY) {
-            if (t + 2 < count) wait_copies_but<2 * kCopies>();
-            else if (t + 1 < count) wait_copies_but<kCopies>();
-            else wait_copies();
-        }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        const char* from = mine + t % kSlots * kSlot;
+    const auto products = [&](const char* from) {
 #pragma unroll
         for (int c = 0; c < KT / 16; ++c) {
             const Frag<T> x = X::read(from, c, lane);
             g = mma(W::read(from + kTile, c, lane), x, g);
-            u = mma(W::read(from + 2 * kTile, c, lane), x, u);
+            if constexpr (!BOTH) u = mma(W::read(from + 2 * kTile, c, lane), x, u);
         }
-        if (t + kSlots < count) {
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // the slot has been read
-            fill(t + kSlots);
+    };
+    if constexpr (COPY) {
+        const auto fill = [&](int t) {
+            char* to = mine + t % kSlots * kSlot;
+            const int k0 = (wave + 4 * t) * KT, k = p.width - k0;
+            X::copy(x0 + k0, p.ld_x, nullptr, 0, rows, k, to, lane);
+            W::copy(of_gate(k0), p.ld_gate_w, of_up(k0), p.ld_up_w, p.hidden - n0, k, to + kTile, lane);
+            if constexpr (!BOTH) W::copy(of_up(k0), p.ld_up_w, nullptr, 0, p.hidden - n0, k, to + 2 * kTile, lane);
+        };
+#pragma unroll 1
+        for (int t = 0; t < kSlots && t < count; ++t) fill(t);
+#pragma unroll 1
+        for (int t = 0; t < count; ++t) {
+            if (t + 2 < count) wait_copies_but<2 * kCopies>();
+            else if (t + 1 < count) wait_copies_but<kCopies>();
+            else wait_copies();
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            products(mine + t % kSlots * kSlot);
+            if (t + kSlots < count) {
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the slot has been read
+                fill(t + kSlots);
+            }
+        }
+    } else {
+        // two steps on the way in registers; LDS serves a wave's requests in their order
+        X x[2];
+        W w[2][kW];
+        const auto load = [&](int t, int b) {
+            const int k0 = (wave + 4 * t) * KT, k = p.width - k0;
+            x[b].load(x0 + k0, p.ld_x, nullptr, 0, rows, k, lane);
+            w[b][0].load(of_gate(k0), p.ld_gate_w, of_up(k0), p.ld_up_w, p.hidden - n0, k, lane);
+            if constexpr (!BOTH) w[b][1].load(of_up(k0), p.ld_up_w, nullptr, 0, p.hidden - n0, k, lane);
+        };
+        if (count > 0) load(0, 0);
+        if (count > 1) load(1, 1);
+#pragma unroll 1
+        for (int t0 = 0; t0 < count; t0 += 2) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                const int t = t0 + b;
+                if (t >= count) break;
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                const int k = p.width - (wave + 4 * t) * KT;
+                x[b].put(rows, k, mine, lane);
+                w[b][0].put(p.hidden - n0, k, mine + kTile, lane);
+                if constexpr (!BOTH) w[b][1].put(p.hidden - n0, k, mine + 2 * kTile, lane);
+                if (t + 2 < count) load(t + 2, b);
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                products(mine);
+            }
         }
     }
-    // the four sums of [row][column], gate then up, 36 values apart
+    // the four sums of [row][column], gate then up (BOTH: side by side), 36 values apart
     __syncthreads();
     float* sums = reinterpret_cast<float*>(lds);
-    constexpr int kPitch = 36, kMatrix = 32 * kPitch;
+    constexpr int kPitch = 36, kMatrix = 32 * kPitch, kUp = BOTH ? 16 : kMatrix;
+    static_assert(sizeof(lds) >= 4 * kW * kMatrix * 4, "the sums' place");
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-        float* to = sums + wave * 2 * kMatrix + (lane & 31) * kPitch + 8 * q + 4 * (lane >> 5);
+        float* to = sums + wave * kW * kMatrix + (lane & 31) * kPitch + 8 * q + 4 * (lane >> 5);
         *reinterpret_cast<f32x4*>(to) = f32x4{g[4 * q], g[4 * q + 1], g[4 * q + 2], g[4 * q + 3]};
-        *reinterpret_cast<f32x4*>(to + kMatrix) = f32x4{u[4 * q], u[4 * q + 1], u[4 * q + 2], u[4 * q + 3]};
+        if constexpr (!BOTH) *reinterpret_cast<f32x4*>(to + kMatrix) = f32x4{u[4 * q], u[4 * q + 1], u[4 * q + 2], u[4 * q + 3]};
     }
     __syncthreads();
-    const int row = threadIdx.x >> 3, col = 4 * (threadIdx.x & 7), left = p.hidden - n0 - col;
-    if (row >= p.rows || left <= 0) return;
+    const int row = threadIdx.x / (COLS / 4), col = 4 * (threadIdx.x % (COLS / 4)), left = p.hidden - n0 - col;
+    if (row >= rows || left <= 0) return;
     f32x4 vg = {}, vu = {};
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-        const float* from = sums + w * 2 * kMatrix + row * kPitch + col;
+        const float* from = sums + w * kW * kMatrix + row * kPitch + col;
         vg += *reinterpret_cast<const f32x4*>(from);
-        vu += *reinterpret_cast<const f32x4*>(from + kMatrix);
+        vu += *reinterpret_cast<const f32x4*>(from + kUp);
     }
     const f32x4 h = activate<sizeof(T) == 4>(p.act, vg) * vu;
-    store4(static_cast<T*>(p.h) + row * p.ld_h + n0 + col, left, h);
-    if (p.gate) store4(static_cast<T*>(p.gate) + row * p.ld_gate + n0 + col, left, vg);
-    if (p.up) store4(static_cast<T*>(p.up) + row * p.ld_up + n0 + col, left, vu);
+    store4(static_cast<T*>(p.h) + (m0 + row) * p.ld_h + n0 + col, left, h);
+    if (p.gate) store4(static_cast<T*>(p.gate) + (m0 + row) * p.ld_gate + n0 + col, left, vg);
+    if (p.up) store4(static_cast<T*>(p.up) + (m0 + row) * p.ld_up + n0 + col, left, vu);
 }
 
 // ------------------------------------------------------------------ layouts
@@ -934,6 +1002,21 @@ void weights(const GatedArgs& a, const Layout& l, bool along, Matrix& gate, Matr
     up = o.add(d.dtype, a.w_up, d.w_up_stride, rows, cols, a.scratch + l.w + layout_bytes(parts_of(d.dtype), rows, cols), lie);
 }
 
+// Whether a forward pass is one of few rows.  us there and through the tiles, in bfloat16 and float32:
+// 64 x 1024 x 4096 6 and 12, 16 and 46; 128 rows 11 and 13, 28 and 47; 256 rows 20 and 14, 57 and 59;
+// 64 x 4096 x 16384 51 to 68 and 59 to 65, 190 and 575; 128 rows 97 to 135 and 58 to 66, 400 and 573.
+// 128 x 448 x 1792 4 and 9, 9 and 28.
+bool few(const pd_gated_desc& d) {
+    const bool small = d.dtype == PD_F32 || (int64_t)d.width * d.hidden <= 1 << 22;
+    return d.rows <= (small ? 128 : 64) && d.width >= 8 && d.hidden >= 8;
+}
+template <typename T, bool ACROSS, bool COPY>
+void launch_few(const FewArgs& p, bool half, int64_t high, hipStream_t s) {
+    const dim3 grid((unsigned)((half ? (p.hidden + 15) / 16 : (p.hidden + 31) / 32) * high)), block(256);
+    if (half) hipLaunchKernelGGL((k_gated_few<T, ACROSS, COPY, 16>), grid, block, 0, s, p);
+    else hipLaunchKernelGGL((k_gated_few<T, ACROSS, COPY, 32>), grid, block, 0, s, p);
+    PD_HIP(hipGetLastError());
+}
 template <typename T>
 void gated_few(const GatedArgs& a, hipStream_t s) {
     const pd_gated_desc& d = a.d;
@@ -946,18 +1029,20 @@ void gated_few(const GatedArgs& a, hipStream_t s) {
                       whole(a.w_up, d.w_up_stride, wr, wc);
     const FewArgs p{a.x, a.w_gate, a.w_up, a.h, a.gate, a.up, d.x_stride, d.w_gate_stride, d.w_up_stride, d.h_stride, d.gate_stride,
                     d.up_stride, (int)d.rows, d.width, d.hidden, d.activation};
-    const dim3 grid((unsigned)((d.hidden + 31) / 32)), block(256);
-    if (in_out && copy) hipLaunchKernelGGL((k_gated_few<T, true, true>), grid, block, 0, s, p);
-    else if (in_out) hipLaunchKernelGGL((k_gated_few<T, true, false>), grid, block, 0, s, p);
-    else if (copy) hipLaunchKernelGGL((k_gated_few<T, false, true>), grid, block, 0, s, p);
-    else hipLaunchKernelGGL((k_gated_few<T, false, false>), grid, block, 0, s, p);
-    PD_HIP(hipGetLastError());
+    const int64_t high = (d.rows + 31) / 32;
+    // 16 columns a block while these are no more than compute units (us, 32 and 16 columns: 1 x 1024 x 4096
+    // bfloat16 4.8 to 5.4 and 4.0 to 5.1, float32 12.9 to 14.5 and 8.6 to 10.4; 1 x 1024 x 8192 5.0 and 6.9, 15 and 17)
+    const bool half = ((int64_t)d.hidden + 15) / 16 * high <= kCus;
+    if (in_out && copy) launch_few<T, true, true>(p, half, high, s);
+    else if (in_out) launch_few<T, true, false>(p, half, high, s);
+    else if (copy) launch_few<T, false, true>(p, half, high, s);
+    else launch_few<T, false, false>(p, half, high, s);
 }
 
 template <typename T>
 void gated_t(const GatedArgs& a, hipStream_t s) {
     const pd_gated_desc& d = a.d;
-    if (d.rows <= kFewRows) return gated_few<T>(a, s);
+    if (few(d)) return gated_few<T>(a, s);
     const Layout l = layout(d, false);
     Operands o;
     Matrix wg, wu;
@@ -1043,7 +1128,7 @@ void gated_grad_t(const GatedArgs& a, hipStream_t s) {
 
 }  // namespace
 
-int64_t gated_scratch_bytes(const pd_gated_desc& d) { return d.rows > kFewRows ? layout(d, false).total : 0; }
+int64_t gated_scratch_bytes(const pd_gated_desc& d) { return few(d) ? 0 : layout(d, false).total; }
 void launch_gated(const GatedArgs& a, hipStream_t s) { a.d.dtype == PD_F32 ? gated_t<float>(a, s) : gated_t<bf16>(a, s); }
 int64_t gated_grad_scratch_bytes(const pd_gated_desc& d) { return d.rows ? layout(d, true).total : 0; }
 void launch_gated_grad(const GatedArgs& a, hipStream_t s) { a.d.dtype == PD_F32 ? gated_grad_t<float>(a, s) : gated_grad_t<bf16>(a, s); }

@@ -642,8 +642,8 @@ def test_gated_refuses_what_it_cannot_read():
         pd.pd_gated_forward(x, w, w, h, activation=5)
     none = torch.empty(0, device="cuda", dtype=torch.uint8)
     pd.pd_gated_forward(x, w, w, h, scratch=none)            # (few rows need none)
-    big = torch.zeros((40, 8), device="cuda")
-    for bad in (lambda: pd.pd_gated_forward(big, w, w, torch.zeros((40, 16), device="cuda"), scratch=none),
+    big = torch.zeros((140, 8), device="cuda")
+    for bad in (lambda: pd.pd_gated_forward(big, w, w, torch.zeros((140, 16), device="cuda"), scratch=none),
                 lambda: pd.pd_gated_backward(h, x, w, w, h, h, dx=x, scratch=none)):
         with pytest.raises(pd.PdError):
             bad()
@@ -713,6 +713,23 @@ def test_block_on_another_stream_and_in_graphs(n, dtype):
         assert all(torch.equal(a, b) for a, b in zip(outs, want)), i
         seen.append((outs[0] == res).flatten())
     assert not torch.equal(seen[0], seen[1])
+
+
+# ------------------------------------------------------------------ a few rows of any alignment
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("layout", [pd.PD_WEIGHTS_IN_OUT, pd.PD_WEIGHTS_OUT_IN])
+@pytest.mark.parametrize("M,D,F", [(1, 8, 8), (2, 9, 15), (33, 8, 687), (5, 133, 41), (64, 7, 40), (64, 300, 17), (65, 264, 520), (31, 1001, 303),
+                                   (128, 67, 1031), (100, 129, 1100), (3, 45, 4201), (17, 72, 4136), (129, 40, 72), (40, 8, 8)])
+def test_gated_few_rows_of_any_alignment(M, D, F, layout, dtype):
+    """The ends of rows inside a unit of 16 bytes, blocks of 32 and of 16 columns, several blocks of rows."""
+    print(f"gated few {M} x {D} x {F} {layout} {dtype}", flush=True)
+    for pad in (0, 5):
+        x, _ = _wide(M, D, dtype, 160, 0, pad)
+        wg, wu = _weights(D, F, dtype, 161, layout, pad)
+        h, g, u = _forward(x, wg, wu, "silu", dtype)
+        rh, rg, ru = ob.gated(_np(x), _np(wg), _np(wu), "silu")
+        for got, ref in ((h, rh), (g, rg), (u, ru)):
+            _close(got, ref, TOL[dtype])
 
 
 # ------------------------------------------------------------------ offsets past 32 bits
