@@ -1007,8 +1007,8 @@ void weights(const GatedArgs& a, const Layout& l, bool along, Matrix& gate, Matr
 // 64 x 4096 x 16384 51 to 68 and 59 to 65, 190 and 575; 128 rows 97 to 135 and 58 to 66, 400 and 573.
 // 128 x 448 x 1792 4 and 9, 9 and 28.
 bool few(const pd_gated_desc& d) {
-    const bool small = d.dtype == PD_F32 || (int64_t)d.width * d.hidden <= 1 << 22;
-    return d.rows <= (small ? 128 : 64) && d.width >= 8 && d.hidden >= 8;
+    const bool small = (int64_t)d.width * d.hidden <= 1 << 22;
+    return d.rows <= (d.dtype == PD_F32 ? 160 : small ? 128 : 64) && d.width >= 8 && d.hidden >= 8;
 }
 template <typename T, bool ACROSS, bool COPY>
 void launch_few(const FewArgs& p, bool half, int64_t high, hipStream_t s) {

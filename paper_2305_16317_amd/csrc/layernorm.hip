@@ -107,6 +107,14 @@ __device__ __forceinline__ void store_first(T* p, int n, typename Vec8<T>::type 
     if (n & 1) *p = v[0];
 }
 
+// 1 / sqrt(v), within a little more than half a unit of the last place: the rounded root's quotient,
+// and a Newton step from its exact residual (0 and infinity, whose residual is NaN, as they are).
+__device__ __forceinline__ float one_over_sqrt(float v) {
+    const float r = 1.f / sqrtf(v), t = v * r;
+    const float residual = fmaf(-t, r, 1.f) - fmaf(v, r, -t) * r, better = fmaf(0.5f * r, residual, r);
+    return better == better ? better : r;
+}
+
 // TPR lanes a row, NV steps of eight values a lane.
 template <typename T, int TPR, int NV, bool TINY>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_layernorm(const LayerNormArgs a) {
@@ -158,7 +166,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_layernorm(const Layer
             ss = fmaf(v[i][e], v[i][e], ss);
         }
     }
-    const float rstd = 1.f / sqrtf(row_sum<TPR>(ss, slot) / (float)width + a.d.eps);
+    const float rstd = one_over_sqrt(row_sum<TPR>(ss, slot) / (float)width + a.d.eps);
     if (lane == 0) {
         if (a.mean) a.mean[row] = mean;
         if (a.rstd) a.rstd[row] = rstd;

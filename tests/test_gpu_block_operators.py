@@ -642,8 +642,8 @@ def test_gated_refuses_what_it_cannot_read():
         pd.pd_gated_forward(x, w, w, h, activation=5)
     none = torch.empty(0, device="cuda", dtype=torch.uint8)
     pd.pd_gated_forward(x, w, w, h, scratch=none)            # (few rows need none)
-    big = torch.zeros((140, 8), device="cuda")
-    for bad in (lambda: pd.pd_gated_forward(big, w, w, torch.zeros((140, 16), device="cuda"), scratch=none),
+    big = torch.zeros((1000, 8), device="cuda")
+    for bad in (lambda: pd.pd_gated_forward(big, w, w, torch.zeros((1000, 16), device="cuda"), scratch=none),
                 lambda: pd.pd_gated_backward(h, x, w, w, h, h, dx=x, scratch=none)):
         with pytest.raises(pd.PdError):
             bad()
