@@ -508,9 +508,9 @@ __global__ __launch_bounds__(256) void k_product_join(const Product p) {
 // 32 rows.  A block takes 32 (or 16) columns of gate and of up; each of its four waves takes every
 // fourth 128 bytes along the sum (64 values, or 32 in float32) through LDS of its own, three
 // such steps on the way, and the four join in LDS: one launch and no barrier before the end.
-// (1 x 1024 x 4096 bfloat16: 4.0 to 5.5 us in the kernel, of which 3.4 are the weights' 16.8 MB; through
-// k_product with the sum in parts and their join 9.  Odd sizes go through registers, two steps on the way:
-// 1 x 1001 x 2731 5.4 to 7.1.)
+// (1 x 1024 x 4096 bfloat16: 4.0 to 5.5 us in the kernel, of which 3.4 are the weights' 16.8 MB at a large
+// copy's rate; through k_product with the sum in parts and their join 9.  Odd sizes go through registers,
+// two steps on the way: 1 x 1001 x 2731 5.3 to 7.1.)
 // float32 runs on float32's own matrix instructions.
 // A step's tile of one operand: 4 KB, which a wave copies.  ACROSS: its rows run along the sum.
 // BOTH: half of the tile (rows; ACROSS: columns) is of a second matrix.
@@ -1002,7 +1002,7 @@ void weights(const GatedArgs& a, const Layout& l, bool along, Matrix& gate, Matr
     up = o.add(d.dtype, a.w_up, d.w_up_stride, rows, cols, a.scratch + l.w + layout_bytes(parts_of(d.dtype), rows, cols), lie);
 }
 
-// Whether a forward pass is one of few rows.  us there and through the tiles, in bfloat16 and float32:
+// Whether a forward pass is one of few rows.  us there and through the tiles, in bfloat16 and float32 (137 x 3200 x 6400 155 and 196):
 // 64 x 1024 x 4096 6 and 12, 16 and 46; 128 rows 11 and 13, 28 and 47; 256 rows 20 and 14, 57 and 59;
 // 64 x 4096 x 16384 51 to 68 and 59 to 65, 190 and 575; 128 rows 97 to 135 and 58 to 66, 400 and 573.
 // 128 x 448 x 1792 4 and 9, 9 and 28.
@@ -1031,7 +1031,8 @@ void gated_few(const GatedArgs& a, hipStream_t s) {
                     d.up_stride, (int)d.rows, d.width, d.hidden, d.activation};
     const int64_t high = (d.rows + 31) / 32;
     // 16 columns a block while these are no more than compute units (us, 32 and 16 columns: 1 x 1024 x 4096
-    // bfloat16 4.8 to 5.4 and 4.0 to 5.1, float32 12.9 to 14.5 and 8.6 to 10.4; 1 x 1024 x 8192 5.0 and 6.9, 15 and 17)
+    // bfloat16 4.8 to 5.4 and 4.0 to 5.2, with weights from memory 7.2 to 9.5 and 6.0 to 8.1, float32 12.6 to 14.5
+    // and 8.3 to 10.4; 1 x 1024 x 8192 5.0 and 6.9, 15 and 17)
     const bool half = ((int64_t)d.hidden + 15) / 16 * high <= kCus;
     if (in_out && copy) launch_few<T, true, true>(p, half, high, s);
     else if (in_out) launch_few<T, true, false>(p, half, high, s);

@@ -184,7 +184,7 @@ void check_gated(const pd_gated_desc& d) {
         fail(PD_ERR_UNSUPPORTED, "products of more than 2^28 tiles of 64 x 64 are not implemented");
 }
 void check_rows_of(const char* what, const void* p, int64_t stride, int64_t rows, int64_t cols) {
-    require(!p || rows <= 1 || stride >= cols, std::string(what) + ": rows of an output share elements");
+    if (p && rows > 1 && stride < cols) fail(PD_ERR_INVALID_ARG, std::string(what) + ": rows of an output share elements");
 }
 
 // ------------------------------------------------------------------ attention
