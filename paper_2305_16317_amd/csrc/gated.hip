@@ -722,17 +722,38 @@ __device__ inline Split split_any(f32x8 x) {
     s.l = narrow<bf16>(r - widen(s.m));
     return s;
 }
+// A float32 in two bfloat16 parts, to 2^-16 of it, for products with operands of one part.  The first
+// is rounded towards 0 and the second is never 0 (but for 0, and values under 2^-96): where the other
+// operand is infinite, both parts give infinities of one sign.
+struct Halves {
+    bf16x8 h, m;
+};
+__device__ inline Halves split_in_two(f32x8 x) {
+    f32x8 h, m;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float v = x[e];
+        h[e] = fabsf(v) < INFINITY ? __uint_as_float(__float_as_uint(v) & 0xffff0000u) : copysignf(1.f, v);
+        const float rest = v - h[e];         // (exact; infinity and NaN stay in it)
+        m[e] = rest != 0.f ? rest : v * 0x1p-30f;
+    }
+    return Halves{narrow<bf16>(h), narrow<bf16>(m)};
+}
 // [rows][cols] as bfloat16 [rows][pitch], zeros past cols; float32: three parts, each a
 // matrix.
 template <int PARTS>
 __device__ inline void store_parts(bf16* to, int64_t plane, f32x8 v) {
     if constexpr (PARTS == 1) {
         *reinterpret_cast<bf16x8*>(to) = narrow<bf16>(v);
+    } else if constexpr (PARTS == 2) {
+        const Halves s = split_in_two(v);
+        *reinterpret_cast<bf16x8*>(to) = s.h;
+        *reinterpret_cast<bf16x8*>(to + plane) = s.m;
     } else {
         const Split s = split_any(v);
         *reinterpret_cast<bf16x8*>(to) = s.h;
         *reinterpret_cast<bf16x8*>(to + plane) = s.m;
-        if constexpr (PARTS == 3) *reinterpret_cast<bf16x8*>(to + 2 * plane) = s.l;
+        *reinterpret_cast<bf16x8*>(to + 2 * plane) = s.l;
     }
 }
 struct LayOut {

@@ -1,0 +1,71 @@
+"""The gated product's values where they are easily lost: infinities, gelu's tail, the rounding of its gradients.
+
+Compared with the formulas in float64 (`oracle/block.py`); the tolerances are derived where they stand."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2305_16317_amd as pd
+from oracle import block as ob
+
+pytestmark = pytest.mark.gpu
+F32, BF16 = torch.float32, torch.bfloat16
+INF = float("inf")
+ACTS = {"silu": pd.PD_ACT_SILU, "gelu": pd.PD_ACT_GELU, "gelu_tanh": pd.PD_ACT_GELU_TANH, "sigmoid": pd.PD_ACT_SIGMOID,
+        "relu": pd.PD_ACT_RELU}
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    pd.load()
+
+
+def _np(t):
+    return t.detach().double().cpu().numpy()
+
+
+def _rand(shape, dtype, seed, scale=1.0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return (torch.randn(shape, device="cuda", generator=g) * scale).to(dtype)
+
+
+def _weight(D, F, dtype, seed, layout):
+    w = _rand((D, F), dtype, seed, D ** -0.5)
+    return w if layout == pd.PD_WEIGHTS_IN_OUT else w.t().contiguous().t()
+
+
+def _same(got, ref, tol, what):
+    """Infinities and NaN where the formula has them; the rest within tol in the root mean square."""
+    got = _np(got)
+    assert np.array_equal(np.isnan(got), np.isnan(ref)), (what, "NaN", np.isnan(got).sum(), np.isnan(ref).sum())
+    far = np.isinf(ref)
+    assert np.array_equal(got[far], ref[far]) and not np.isinf(got[~far]).any(), what
+    fine = np.isfinite(ref)
+    assert np.linalg.norm(got[fine] - ref[fine]) <= tol * np.linalg.norm(ref[fine]), what
+
+
+def _infinite_gradients(M, layout, dtype, tol):
+    """One infinity at a time: in x, in a weight of each half, in dh, in up."""
+    D, F = 72, 100
+    for act in ("silu", "relu"):
+        for where in ("x", "w_gate", "w_up", "dh", "up"):
+            a = dict(dh=_rand((M, F), dtype, 1), x=_rand((M, D), dtype, 2), w_gate=_weight(D, F, dtype, 3, layout),
+                     w_up=_weight(D, F, dtype, 4, layout), gate=_rand((M, F), dtype, 5), up=_rand((M, F), dtype, 6))
+            a[where][1, 7] = -INF
+            dx, dw = torch.empty_like(a["x"]), [torch.empty_like(a[n]) for n in ("w_gate", "w_up")]
+            pd.pd_gated_backward(*a.values(), dx=dx, dw_gate=dw[0], dw_up=dw[1], activation=ACTS[act])
+            with np.errstate(invalid="ignore"):
+                rx, rg, ru, _ = ob.gated_grad(*(_np(t) for t in a.values()), act)
+            assert not all(np.isfinite(r).all() for r in (rx, rg, ru))
+            for got, ref, what in ((dx, rx, "dx"), (dw[0], rg, "dw_gate"), (dw[1], ru, "dw_up")):
+                _same(got, ref, tol, (act, where, what))
+
+
+@pytest.mark.parametrize("layout", [pd.PD_WEIGHTS_IN_OUT, pd.PD_WEIGHTS_OUT_IN])
+@pytest.mark.parametrize("M", [2, 20, 32, 33, 300])
+def test_gradients_of_infinite_values_bfloat16(M, layout):
+    """An infinite x or weight meets both parts of dgate and dup: neither is 0 or of the other sign.  (Two roundings, of
+    at most 2^-8 / sqrt 3 in the root mean square each: 4e-3.)"""
+    _infinite_gradients(M, layout, BF16, 4e-3)
