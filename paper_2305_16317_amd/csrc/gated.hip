@@ -832,13 +832,11 @@ struct Matrix {
     const bf16* part[3];
     int64_t ld;
 };
-constexpr int64_t kFewRows = 32;
-int parts_of(int dtype) { return dtype == PD_F32 ? 3 : 1; }
-// Parts of dg and du.  In bfloat16 one: their rounding adds as much to a gradient's error as its
-// own does, in the root mean square 1.41 times it together.  Few rows have few such roundings,
-// which a large one may rule (1.8 times was seen): they are kept in two, where the weights' bytes
-// and the launches make up the time.
-int slope_parts(const pd_gated_desc& d) { return d.dtype == PD_F32 ? 3 : d.rows <= kFewRows ? 2 : 1; }
+constexpr int parts_of(int dtype) { return dtype == PD_F32 ? 3 : 1; }
+// Parts of dg and du.  In bfloat16 two: one would add as much to a gradient's error as the
+// rounding of the result does (1.41 times it together, with few rows up to 1.8 times), for half
+// of the products.
+constexpr int slope_parts(int dtype) { return dtype == PD_F32 ? 3 : 2; }
 int64_t layout_bytes(int parts, int64_t rows, int64_t cols) { return rows * up_to(cols, 64) * 2 * parts; }
 // Copies of 16 bytes read the matrix as it lies.
 bool as_it_lies(int dtype, const void* p, int64_t stride, int64_t rows, int64_t cols) {
@@ -983,7 +981,7 @@ Layout layout(const pd_gated_desc& d, bool backward) {
         at += up_to(bytes, 256);
         return here;
     };
-    const int parts = parts_of(d.dtype), slopes = slope_parts(d), segs = segments(backward ? slopes : parts, parts);
+    const int parts = parts_of(d.dtype), slopes = slope_parts(d.dtype), segs = segments(backward ? slopes : parts, parts);
     l.x = take(layout_bytes(parts, d.rows, d.width));
     l.w = take(2 * (in_out ? layout_bytes(parts, d.width, d.hidden) : layout_bytes(parts, d.hidden, d.width)));
     int64_t partial = 0;
@@ -1106,12 +1104,10 @@ void gated_grad_t(const GatedArgs& a, hipStream_t s) {
     g.ld_gate = d.gate_stride, g.ld_up = d.up_stride, g.ld_dh = d.dh_stride, g.ld_h = d.h_stride;
     g.rows = d.rows, g.cols = d.hidden, g.pitch = (int)pitch, g.act = d.activation;
     g.dg = products ? reinterpret_cast<bf16*>(a.scratch + l.slopes) : nullptr;
-    const int parts = parts_of(d.dtype), slopes = slope_parts(d);
+    constexpr int kType = sizeof(T) == 4 ? PD_F32 : PD_BF16, parts = parts_of(kType), slopes = slope_parts(kType);
     g.du = slopes * plane;
     const dim3 grid(blocks_for(d.rows * pitch / 8)), block(256);
-    if (sizeof(T) == 4) hipLaunchKernelGGL((k_gated_slopes<T, 3>), grid, block, 0, s, g);
-    else if (slopes == 2) hipLaunchKernelGGL((k_gated_slopes<T, 2>), grid, block, 0, s, g);
-    else hipLaunchKernelGGL((k_gated_slopes<T, 1>), grid, block, 0, s, g);
+    hipLaunchKernelGGL((k_gated_slopes<T, slopes>), grid, block, 0, s, g);
     PD_HIP(hipGetLastError());
     const Matrix dg{{g.dg, g.dg + plane, g.dg + 2 * plane}, pitch}, du{{g.dg + g.du, g.dg + g.du + plane, g.dg + g.du + 2 * plane}, pitch};
     float* partial = reinterpret_cast<float*>(a.scratch + l.partial);

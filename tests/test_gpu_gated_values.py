@@ -69,3 +69,24 @@ def test_gradients_of_infinite_values_bfloat16(M, layout):
     """An infinite x or weight meets both parts of dgate and dup: neither is 0 or of the other sign.  (Two roundings, of
     at most 2^-8 / sqrt 3 in the root mean square each: 4e-3.)"""
     _infinite_gradients(M, layout, BF16, 4e-3)
+
+
+# ------------------------------------------------------------------ the gradients' rounding
+@pytest.mark.parametrize("layout", [pd.PD_WEIGHTS_IN_OUT, pd.PD_WEIGHTS_OUT_IN])
+@pytest.mark.parametrize("M,D,F", [(5, 72, 100), (40, 72, 100), (129, 200, 333), (700, 1024, 264), (2304, 320, 1336)])
+def test_gradients_bfloat16_are_rounded_once(M, D, F, layout):
+    """dgate and dup are operands to 2^-16, and act and its slope to 1e-5: a gradient's sum is off by at most 2.5e-5 of
+    its terms' root mean square.  It then rounds to another value than the formula's with a probability of that over a
+    step (2^-7 of the value at most), and is a step off: sqrt(2.5e-5 2^-7) = 4.4e-4 in the root mean square at most, where
+    operands rounded to bfloat16 give 1.6e-3 to 2.3e-3."""
+    dh, x, g, u = _rand((M, F), BF16, 20), _rand((M, D), BF16, 21), _rand((M, F), BF16, 22), _rand((M, F), BF16, 23)
+    wg, wu = _weight(D, F, BF16, 24, layout), _weight(D, F, BF16, 25, layout)
+    for act in ("silu", "gelu"):
+        dx, dw = torch.empty_like(x), [torch.empty_like(t) for t in (wg, wu)]
+        pd.pd_gated_backward(dh, x, wg, wu, g, u, dx=dx, dw_gate=dw[0], dw_up=dw[1], activation=ACTS[act])
+        refs = ob.gated_grad(*(_np(t) for t in (dh, x, wg, wu, g, u)), act)
+        for got, ref, what in ((dx, refs[0], "dx"), (dw[0], refs[1], "dw_gate"), (dw[1], refs[2], "dw_up")):
+            once = _np(torch.from_numpy(ref).to(BF16))
+            off = np.linalg.norm(_np(got) - once) / np.linalg.norm(once)
+            print(M, D, F, act, what, off, flush=True)
+            assert off <= 4.4e-4, (act, what, off)
