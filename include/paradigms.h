@@ -573,8 +573,8 @@ pd_status pd_dropout_apply(const pd_dropout_desc* desc, const void* x, const voi
  * dw_gate and dw_up in the weights' layout and type (zeros where there are no rows).  dx, the
  * pair dw_gate and dw_up, and h (act(gate) up, formed again) may be NULL: not formed.
  * In PD_F32 operands are the sums of three bfloat16 parts (24 bits; a value under 2^-110
- * keeps fewer) with products to 2^-24, as in attention; an infinity among them gives NaN (forward
- * passes of few rows multiply in float32).  In PD_BF16 dgate and dup are operands of two bfloat16
+ * keeps fewer) with products to 2^-24, as in attention (forward passes of few rows multiply in
+ * float32); an infinity among them gives what the formula gives.  In PD_BF16 dgate and dup are operands of two bfloat16
  * parts (to 2^-16), so that a gradient is rounded once.  Sums are float32.  relu'(0) = 0.
  * 1 <= width, hidden <= 2^20; more than 2^24 rows, or than 2^28 tiles of 64 x 64 in a product:
  * PD_ERR_UNSUPPORTED. */

@@ -709,17 +709,27 @@ __global__ __launch_bounds__(256) void k_gated_few(const FewArgs p) {
 
 // ------------------------------------------------------------------ layouts
 // A float32 in three parts, as split() makes them, but that values past the largest bfloat16
-// (3.39e38) keep a finite first part.
+// (3.39e38) keep a finite first part, and an infinity is (1, 0, infinity) with its sign: its last part
+// meets the other operand's first alone, which is 0 or has the other sign only where that operand does.
 constexpr float kMostBf16 = 3.38953139e38f;
 __device__ inline Split split_any(f32x8 x) {
-    f32x8 y;
+    f32x8 y, r;
+    bool infinite[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) y[e] = fminf(fmaxf(x[e], -kMostBf16), kMostBf16);
+    for (int e = 0; e < 8; ++e) {
+        infinite[e] = fabsf(x[e]) == INFINITY;
+        y[e] = infinite[e] ? copysignf(1.f, x[e]) : fminf(fmaxf(x[e], -kMostBf16), kMostBf16);
+    }
     Split s;
     s.h = narrow<bf16>(y);
-    const f32x8 r = x - widen(s.h);          // (NaN stays in it)
+    const f32x8 h = widen(s.h);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r[e] = infinite[e] ? 0.f : x[e] - h[e];      // (NaN stays in it)
     s.m = narrow<bf16>(r);
-    s.l = narrow<bf16>(r - widen(s.m));
+    const f32x8 m = widen(s.m);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r[e] = infinite[e] ? x[e] : r[e] - m[e];
+    s.l = narrow<bf16>(r);
     return s;
 }
 // A float32 in two bfloat16 parts, to 2^-16 of it, for products with operands of one part.  The first

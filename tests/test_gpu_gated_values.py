@@ -90,3 +90,32 @@ def test_gradients_bfloat16_are_rounded_once(M, D, F, layout):
             off = np.linalg.norm(_np(got) - once) / np.linalg.norm(once)
             print(M, D, F, act, what, off, flush=True)
             assert off <= 4.4e-4, (act, what, off)
+
+
+# ------------------------------------------------------------------ infinities in float32
+@pytest.mark.parametrize("layout", [pd.PD_WEIGHTS_IN_OUT, pd.PD_WEIGHTS_OUT_IN])
+@pytest.mark.parametrize("M", [2, 33, 161, 300])
+def test_gradients_of_infinite_values_float32(M, layout):
+    """(Sums of some hundred terms in float32: 5e-6.)"""
+    _infinite_gradients(M, layout, F32, 5e-6)
+
+
+@pytest.mark.parametrize("layout", [pd.PD_WEIGHTS_IN_OUT, pd.PD_WEIGHTS_OUT_IN])
+@pytest.mark.parametrize("dtype,M", [(F32, 2), (F32, 160), (F32, 161), (F32, 700), (BF16, 2), (BF16, 300)])
+def test_forward_of_infinite_values(dtype, M, layout):
+    """The formula's infinities and NaN whatever the number of rows: one in x, one in a weight, and one in each."""
+    D, F = 72, 100
+    for act in ACTS:
+        for where in ((1,), (2,), (1, 2)):
+            x, w = _rand((M, D), dtype, 10), [_weight(D, F, dtype, 11 + i, layout) for i in range(2)]
+            if 1 in where:
+                x[1, 7] = INF
+            if 2 in where:
+                w[0][7, 5] = -INF
+                w[1][9, 60] = INF
+            h, g, u = (torch.empty((M, F), device="cuda", dtype=dtype) for _ in range(3))
+            pd.pd_gated_forward(x, *w, h, gate=g, up=u, activation=ACTS[act])
+            with np.errstate(invalid="ignore", over="ignore"):
+                refs = ob.gated(_np(x), _np(w[0]), _np(w[1]), act)
+            for got, ref, what in zip((h, g, u), refs, ("h", "gate", "up")):
+                _same(got, ref, 4e-3 if dtype == BF16 else 5e-6, (act, where, what))
