@@ -1,6 +1,8 @@
 """The gated product's values where they are easily lost: infinities, gelu's tail, the rounding of its gradients.
 
 Compared with the formulas in float64 (`oracle/block.py`); the tolerances are derived where they stand."""
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -119,3 +121,48 @@ def test_forward_of_infinite_values(dtype, M, layout):
                 refs = ob.gated(_np(x), _np(w[0]), _np(w[1]), act)
             for got, ref, what in zip((h, g, u), refs, ("h", "gate", "up")):
                 _same(got, ref, 4e-3 if dtype == BF16 else 5e-6, (act, where, what))
+
+
+# ------------------------------------------------------------------ gelu's tail
+def _tail_error():
+    """Relative error of tail = e^(-g^2/2) t Q(t) in float32: t's two roundings (2^-24, 2^-23) times 3.8, the most that
+    t Q(t) follows t by (d log / d log at t = 1); Q's fit 2.2e-8 and its sum 2^-23; the exponential's 2^-23 and four products and sums of 2^-24."""
+    return 3.8 * (2.0**-24 + 2.0**-23) + 2.2e-8 + 2.0**-23 + 2.0**-23 + 4 * 2.0**-24
+
+
+@pytest.mark.parametrize("dtype,rows,width", [(F32, 100, 8), (F32, 4001, 2), (BF16, 50, 8), (BF16, 4001, 2)])
+def test_gelu_of_negative_gates_is_relative_to_itself(dtype, rows, width):
+    """Gates from -12 to 0 through few rows and the tiles, up 1: the tail alone is left of the value.  bfloat16 adds its
+    rounding (2^-8), its shorter fit (9e-6), and the exponent's rounding (up to 72 2^-23)."""
+    g = torch.linspace(-12, -0.01, rows, device="cuda").to(dtype)[:, None]
+    x = torch.zeros((rows, width), device="cuda", dtype=dtype)
+    x[:, :1], x[:, 1] = g, 1.0
+    w = torch.zeros((2, width, 8), device="cuda", dtype=dtype)
+    w[0, 0], w[1, 1] = 1.0, 1.0
+    h = torch.empty((rows, 8), device="cuda", dtype=dtype)
+    pd.pd_gated_forward(x, w[0], w[1], h, activation=pd.PD_ACT_GELU)
+    # (the formula's 1 + erf loses the tail's digits: erfc has them)
+    gn = _np(g)
+    ref = gn * 0.5 * np.vectorize(math.erfc)(-gn / math.sqrt(2))
+    tol = 2.0**-8 + 1e-5 + 72 * 2.0**-23 if dtype == BF16 else _tail_error() + 2.0**-24
+    off = np.abs(_np(h) - ref) / np.abs(ref)
+    print(dtype, rows, off.max(), flush=True)
+    assert off.max() <= tol
+
+
+def test_gelu_slope_of_negative_gates_is_relative_to_itself():
+    """Gates from -12 to -2, where the slope is g phi(g) and the tail, of which the second is at most a quarter: their
+    errors are 5/3 of themselves in the difference."""
+    g = torch.linspace(-12, -2, 4001, device="cuda")[:, None].contiguous()
+    w = torch.zeros((2, 8, 1), device="cuda")
+    w[0, 0], w[1, 1] = 1.0, 1.0
+    x, one, dx = torch.zeros((4001, 8), device="cuda"), torch.ones_like(g), torch.empty((4001, 8), device="cuda")
+    pd.pd_gated_backward(one, x, w[0], w[1], g, one, dx=dx, activation=pd.PD_ACT_GELU)
+    gn = _np(g)
+    tail = 0.5 * np.vectorize(math.erfc)(-gn / math.sqrt(2))
+    ref = tail + gn * np.exp(-0.5 * gn * gn) / math.sqrt(2 * math.pi)
+    off = np.abs(_np(dx)[:, :1] - ref) / np.abs(ref)
+    print(off.max(), flush=True)
+    assert off.max() <= 5 / 3 * _tail_error() + 2.0**-23        # (and dx's three products in parts)
+    off = np.abs(_np(dx)[:, 1:2] - gn * tail) / np.abs(gn * tail)
+    assert off.max() <= _tail_error() + 2.0**-23
