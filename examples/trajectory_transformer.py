@@ -56,9 +56,10 @@ class Rotary(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dq, dk):
         positions, table = ctx.saved_tensors
-        dq, dk = dq.contiguous(), dk.contiguous()
-        pd.pd_rotary_apply(dq, dk, positions, table, dq, dk, backward=True)
-        return dq, dk, None, None
+        dq, dk = dq.contiguous(), dk.contiguous()       # (not to be written: they may be another consumer's too)
+        to_q, to_k = torch.empty_like(dq), torch.empty_like(dk)
+        pd.pd_rotary_apply(dq, dk, positions, table, to_q, to_k, backward=True)
+        return to_q, to_k, None, None
 
 
 class Attend(torch.autograd.Function):
