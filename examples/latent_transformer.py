@@ -69,17 +69,17 @@ class Add(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, residual, p, seed, site, step):
         ctx.how = (p, seed, site)
-        ctx.step = step
+        ctx.save_for_backward(step.clone())            # (the caller's may be counted up before the gradient)
         y = torch.empty_like(residual)
         pd.pd_dropout_apply(x.contiguous(), y, p, seed, rng_stream=site, step_more=step, residual=residual.contiguous())
         return y
 
     @staticmethod
     def backward(ctx, dy):
-        p, seed, site = ctx.how
+        (p, seed, site), (step,) = ctx.how, ctx.saved_tensors
         dy = dy.contiguous()
         dx = torch.empty_like(dy)
-        pd.pd_dropout_apply(dy, dx, p, seed, rng_stream=site, step_more=ctx.step)
+        pd.pd_dropout_apply(dy, dx, p, seed, rng_stream=site, step_more=step)
         return dx, dy, None, None, None, None
 
 

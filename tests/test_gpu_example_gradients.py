@@ -51,3 +51,18 @@ def test_rotary_leaves_the_gradients_that_reach_it(which, latent, trajectory):
     # linear in q and k: <dq, q> is <gq, q2>, in float32 sums of 576 terms
     for x, y, g in ((q, q2, gq), (k, k2, gk)):
         assert abs(float((x.grad * x).sum() - (g * y).sum())) <= 1e-5 * float(g.norm() * y.norm())
+
+
+def test_dropout_gradient_has_its_own_forward_passes_mask(latent):
+    """The step may be counted up between a forward pass and its gradient, as where gradients are accumulated."""
+    x, res = _rand((2, 30, 64), 10).requires_grad_(), _rand((2, 30, 64), 11)
+    step = torch.zeros(1, device="cuda", dtype=torch.int32)
+    ys = []
+    for _ in range(2):
+        ys.append(latent.Add.apply(x, res, 0.5, 3, 1, step))
+        step += 1
+    masks = [(y != res).detach() for y in ys]              # (no kept x is 0, or too small to see)
+    assert not torch.equal(*masks)
+    for y, m in zip(ys, masks):
+        dx, = torch.autograd.grad(y, x, torch.ones_like(y))
+        assert torch.equal(dx, 2.0 * m)                    # (p = 1/2: kept values are doubled)
