@@ -576,6 +576,9 @@ pd_status pd_dropout_apply(const pd_dropout_desc* desc, const void* x, const voi
  * keeps fewer) with products to 2^-24, as in attention (forward passes of few rows multiply in
  * float32); an infinity among them gives what the formula gives.  In PD_BF16 dgate and dup are operands of two bfloat16
  * parts (to 2^-16), so that a gradient is rounded once.  Sums are float32.  relu'(0) = 0.
+ * aligned, not 0: x, w_gate and w_up begin at multiples of 16 bytes (else PD_ERR_INVALID_ARG).  The
+ * scratch then has no room for those that are read where they are: in PD_BF16 with rows of a multiple
+ * of 8 values, a multiple of 8 values apart, most are.
  * 1 <= width, hidden <= 2^20; more than 2^24 rows, or than 2^28 tiles of 64 x 64 in a product:
  * PD_ERR_UNSUPPORTED. */
 #define PD_ACT_SILU 0
@@ -589,6 +592,7 @@ typedef struct pd_gated_desc {
     int64_t rows;
     int32_t width, hidden;
     int32_t dtype, activation, weight_layout;
+    int32_t aligned;
     int64_t x_stride, w_gate_stride, w_up_stride, gate_stride, up_stride, h_stride;   /* from row to row */
     int64_t dh_stride, dx_stride, dw_gate_stride, dw_up_stride;                       /* backward only */
 } pd_gated_desc;

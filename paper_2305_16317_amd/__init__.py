@@ -164,7 +164,7 @@ class _DropoutDesc(ctypes.Structure):
 class _GatedDesc(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int64), ("width", ctypes.c_int32), ("hidden", ctypes.c_int32),
                 ("dtype", ctypes.c_int32), ("activation", ctypes.c_int32),
-                ("weight_layout", ctypes.c_int32), ("x_stride", ctypes.c_int64),
+                ("weight_layout", ctypes.c_int32), ("aligned", ctypes.c_int32), ("x_stride", ctypes.c_int64),
                 ("w_gate_stride", ctypes.c_int64), ("w_up_stride", ctypes.c_int64),
                 ("gate_stride", ctypes.c_int64), ("up_stride", ctypes.c_int64),
                 ("h_stride", ctypes.c_int64), ("dh_stride", ctypes.c_int64),
@@ -179,7 +179,7 @@ _ATTENTION_BYTES = struct.Struct("10if24q")
 _LAYERNORM_BYTES = struct.Struct("9qif")
 _ROTARY_AXES_BYTES = struct.Struct("2q7i14q6i3q")
 _DROPOUT_BYTES = struct.Struct("6qQd2Ii4x")
-_GATED_BYTES = struct.Struct("q5i10q")
+_GATED_BYTES = struct.Struct("q6i10q")
 
 _LIB: Optional[ctypes.CDLL] = None
 
@@ -933,6 +933,14 @@ def _weights(w_gate: torch.Tensor, w_up: torch.Tensor, width: int, dtype):
     raise ValueError("w_gate and w_up must both have contiguous rows, or both contiguous columns")
 
 
+def _whole_units(*tensors: torch.Tensor) -> bool:
+    """Whether all begin at multiples of 16 bytes (torch's own allocations do)."""
+    at = 0
+    for t in tensors:
+        at |= t.data_ptr()
+    return at % 16 == 0
+
+
 def _like_weight(w: Optional[torch.Tensor], layout: int, shape, dtype, what: str) -> int:
     """Stride of a weight's gradient, which lies as the weights do."""
     if w is None:
@@ -967,8 +975,8 @@ def pd_gated_forward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, 
         else:
             _written(out, what)
             strides.append(_rows_of(out, hs, t, what))
-    d = _pack(_GATED_BYTES, x.numel() // width, width, hidden, dt, activation, layout, _rows_of(x, sh, t, "x"), gs, us,
-              *strides, 0, 0, 0, 0)
+    d = _pack(_GATED_BYTES, x.numel() // width, width, hidden, dt, activation, layout, _whole_units(x, w_gate, w_up),
+              _rows_of(x, sh, t, "x"), gs, us, *strides, 0, 0, 0, 0)
     L = load()
     buf, have = _scratch(scratch, _scratch_need("pd_gated_forward_scratch", d) if scratch is None else 0, stream)
     _check(L.pd_gated_forward(d, _ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(gate), _ptr(up), _ptr(h), _ptr(buf), have,
@@ -995,7 +1003,8 @@ def pd_gated_backward(dh: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, w
         if t is not None:
             _written(t, what)
     of = lambda t, shape, what: 0 if t is None else _rows_of(t, shape, x.dtype, what)  # noqa: E731
-    d = _pack(_GATED_BYTES, x.numel() // width, width, hidden, dt, activation, layout, _rows_of(x, sh, x.dtype, "x"), gs, us,
+    d = _pack(_GATED_BYTES, x.numel() // width, width, hidden, dt, activation, layout, _whole_units(x, w_gate, w_up),
+              _rows_of(x, sh, x.dtype, "x"), gs, us,
               of(gate, hs, "gate"), of(up, hs, "up"), of(h, hs, "h"), of(dh, hs, "dh"), of(dx, sh, "dx"),
               _like_weight(dw_gate, layout, ws, x.dtype, "dw_gate"), _like_weight(dw_up, layout, ws, x.dtype, "dw_up"))
     L = load()

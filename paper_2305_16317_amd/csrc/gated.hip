@@ -856,9 +856,21 @@ constexpr int parts_of(int dtype) { return dtype == PD_F32 ? 3 : 1; }
 // of the products.
 constexpr int slope_parts(int dtype) { return dtype == PD_F32 ? 3 : 2; }
 int64_t layout_bytes(int parts, int64_t rows, int64_t cols) { return rows * up_to(cols, 64) * 2 * parts; }
-// Copies of 16 bytes read the matrix as it lies.
-bool as_it_lies(int dtype, const void* p, int64_t stride, int64_t rows, int64_t cols) {
-    return dtype == PD_BF16 && (uintptr_t)p % 16 == 0 && cols % 8 == 0 && (rows == 1 || (stride % 8 == 0 && stride < (1 << 22)));
+// Copies of 16 bytes read the matrix as it lies, if it begins at a multiple of them.
+bool as_it_lies(int dtype, int64_t stride, int64_t rows, int64_t cols) {
+    return dtype == PD_BF16 && cols % 8 == 0 && (rows == 1 || (stride % 8 == 0 && stride < (1 << 22)));
+}
+bool whole_units(const void* p) { return (uintptr_t)p % 16 == 0; }
+bool inputs_lie(const pd_gated_desc& d) { return as_it_lies(d.dtype, d.x_stride, d.rows, d.width); }
+// Both weights lie alike, as the kernel has one distance of rows for them.  `along`: the
+// product reads them along the sum, 128 bytes of a row at a time; where these straddle the
+// memory's lines and there are many rows, laying them out pays (20000 x 1000 x 2664: 298 and
+// 266 us; 4608 rows 77 and 70; read across the sum 236 and 232).
+bool weights_lie(const pd_gated_desc& d, bool along) {
+    const bool in_out = d.weight_layout == PD_WEIGHTS_IN_OUT;
+    const int64_t rows = in_out ? d.width : d.hidden, cols = in_out ? d.hidden : d.width;
+    return as_it_lies(d.dtype, d.w_gate_stride, rows, cols) && as_it_lies(d.dtype, d.w_up_stride, rows, cols) &&
+           (rows == 1 || d.w_gate_stride == d.w_up_stride) && !(along && d.rows >= 8192 && rows > 1 && d.w_gate_stride % 64);
 }
 // Operands as products read them; those that do not lie so are laid out by one launch.
 struct Operands {
@@ -1000,8 +1012,10 @@ Layout layout(const pd_gated_desc& d, bool backward) {
         return here;
     };
     const int parts = parts_of(d.dtype), slopes = slope_parts(d.dtype), segs = segments(backward ? slopes : parts, parts);
-    l.x = take(layout_bytes(parts, d.rows, d.width));
-    l.w = take(2 * (in_out ? layout_bytes(parts, d.width, d.hidden) : layout_bytes(parts, d.hidden, d.width)));
+    // (no room for operands that are read where they are)
+    if (!(d.aligned && inputs_lie(d))) l.x = take(layout_bytes(parts, d.rows, d.width));
+    if (!(d.aligned && weights_lie(d, backward == in_out)))
+        l.w = take(2 * (in_out ? layout_bytes(parts, d.width, d.hidden) : layout_bytes(parts, d.hidden, d.width)));
     int64_t partial = 0;
     const auto more = [&](int64_t m, int64_t n, bool apart, int groups, int64_t k, int segs, bool across) {
         const int64_t b = partial_bytes(cut(m, n, apart, groups, k, segs, across), m, n, apart, groups);
@@ -1022,19 +1036,13 @@ Layout layout(const pd_gated_desc& d, bool backward) {
 
 Matrix inputs(const GatedArgs& a, const Layout& l, Operands& o) {
     const pd_gated_desc& d = a.d;
-    return o.add(d.dtype, a.x, d.x_stride, d.rows, d.width, a.scratch + l.x, as_it_lies(d.dtype, a.x, d.x_stride, d.rows, d.width));
+    return o.add(d.dtype, a.x, d.x_stride, d.rows, d.width, a.scratch + l.x, inputs_lie(d) && whole_units(a.x));
 }
-// Both weights lie alike, as the kernel has one distance of rows for them.  `along`: the
-// product reads them along the sum, 128 bytes of a row at a time; where these straddle the
-// memory's lines and there are many rows, laying them out pays (20000 x 1000 x 2664: 298 and
-// 266 us; 4608 rows 77 and 70; read across the sum 236 and 232).
 void weights(const GatedArgs& a, const Layout& l, bool along, Matrix& gate, Matrix& up, Operands& o) {
     const pd_gated_desc& d = a.d;
     const bool in_out = d.weight_layout == PD_WEIGHTS_IN_OUT;
     const int64_t rows = in_out ? d.width : d.hidden, cols = in_out ? d.hidden : d.width;
-    const bool lie = as_it_lies(d.dtype, a.w_gate, d.w_gate_stride, rows, cols) &&
-                     as_it_lies(d.dtype, a.w_up, d.w_up_stride, rows, cols) && (rows == 1 || d.w_gate_stride == d.w_up_stride) &&
-                     !(along && d.rows >= 8192 && rows > 1 && d.w_gate_stride % 64);
+    const bool lie = weights_lie(d, along) && whole_units(a.w_gate) && whole_units(a.w_up);
     gate = o.add(d.dtype, a.w_gate, d.w_gate_stride, rows, cols, a.scratch + l.w, lie);
     up = o.add(d.dtype, a.w_up, d.w_up_stride, rows, cols, a.scratch + l.w + layout_bytes(parts_of(d.dtype), rows, cols), lie);
 }

@@ -183,6 +183,11 @@ void check_gated(const pd_gated_desc& d) {
     if (m * n > 1 << 28 || m * k > 1 << 28 || n * k > 1 << 28)
         fail(PD_ERR_UNSUPPORTED, "products of more than 2^28 tiles of 64 x 64 are not implemented");
 }
+void check_alignment(const pd_gated_desc& d, const void* x, const void* w_gate, const void* w_up) {
+    if (!d.aligned) return;
+    for (const void* p : {x, w_gate, w_up})
+        require((uintptr_t)p % 16 == 0, "x, w_gate and w_up do not all begin at multiples of 16 bytes, as aligned says");
+}
 void check_rows_of(const char* what, const void* p, int64_t stride, int64_t rows, int64_t cols) {
     if (p && rows > 1 && stride < cols) fail(PD_ERR_INVALID_ARG, std::string(what) + ": rows of an output share elements");
 }
@@ -486,6 +491,7 @@ extern "C" pd_status pd_gated_forward(const pd_gated_desc* desc, const void* x, 
         check_gated(d);
         if (d.rows == 0) return;
         require(x && w_gate && w_up && h, "x, w_gate, w_up and h must not be NULL");
+        check_alignment(d, x, w_gate, w_up);
         check_rows_of("h", h, d.h_stride, d.rows, d.hidden);
         check_rows_of("gate", gate, d.gate_stride, d.rows, d.hidden);
         check_rows_of("up", up, d.up_stride, d.rows, d.hidden);
@@ -521,6 +527,7 @@ extern "C" pd_status pd_gated_backward(const pd_gated_desc* desc, const void* x,
         require(d.rows == 0 || (gate && up && dh), "gate, up and dh must not be NULL");
         require(d.rows == 0 || !dx || (w_gate && w_up), "w_gate and w_up must not be NULL");
         require(d.rows == 0 || !dw_gate || x, "x must not be NULL");
+        check_alignment(d, x, w_gate, w_up);
         const bool in_out = d.weight_layout == PD_WEIGHTS_IN_OUT;
         check_rows_of("h", h, d.h_stride, d.rows, d.hidden);
         check_rows_of("dx", dx, d.dx_stride, d.rows, d.width);

@@ -166,3 +166,38 @@ def test_gelu_slope_of_negative_gates_is_relative_to_itself():
     assert off.max() <= 5 / 3 * _tail_error() + 2.0**-23        # (and dx's three products in parts)
     off = np.abs(_np(dx)[:, 1:2] - gn * tail) / np.abs(gn * tail)
     assert off.max() <= _tail_error() + 2.0**-23
+
+
+# ------------------------------------------------------------------ operands read where they are, or laid out
+@pytest.mark.parametrize("layout", [pd.PD_WEIGHTS_IN_OUT, pd.PD_WEIGHTS_OUT_IN])
+@pytest.mark.parametrize("shift", [0, 1, 4, 8])
+@pytest.mark.parametrize("which", ["x", "w_gate", "w_up"])
+def test_operands_that_begin_anywhere(which, shift, layout):
+    """Rows a multiple of 16 bytes apart, the first of which begins `shift` values after one: through the tiles, forward
+    and backward, with the scratch that the binding makes."""
+    M, D, F = 300, 128, 264
+    def at(shape, seed, name, scale=1.0):
+        n = shape[0] * (shape[1] + 8)
+        buf = torch.full((n + 16,), float("nan"), device="cuda", dtype=BF16)
+        v = buf[shift if name == which else 0:][:n].view(shape[0], shape[1] + 8)[:, :shape[1]]
+        return v.copy_(_rand(shape, BF16, seed, scale))
+    x = at((M, D), 30, "x")
+    wg, wu = (at((F, D), 31 + i, n, D ** -0.5).t() if layout else at((D, F), 31 + i, n, D ** -0.5) for i, n in enumerate(("w_gate", "w_up")))
+    dh = _rand((M, F), BF16, 33)
+    h, g, u = (torch.empty((M, F), device="cuda", dtype=BF16) for _ in range(3))
+    pd.pd_gated_forward(x, wg, wu, h, gate=g, up=u)
+    for got, ref in zip((h, g, u), ob.gated(_np(x), _np(wg), _np(wu), "silu")):
+        _same(got, ref, 4e-3, "forward")
+    dx, dw = torch.empty((M, D), device="cuda", dtype=BF16), [torch.empty_strided(w.shape, (F, 1) if not layout else (1, D), device="cuda", dtype=BF16) for w in (wg, wu)]
+    pd.pd_gated_backward(dh, x, wg, wu, g, u, dx=dx, dw_gate=dw[0], dw_up=dw[1])
+    for got, ref in zip((dx, *dw), ob.gated_grad(*(_np(t) for t in (dh, x, wg, wu, g, u)), "silu")):
+        _same(got, ref, 4e-3, "backward")
+
+
+def test_forward_of_aligned_operands_takes_no_memory():
+    x, w, h = _rand((4096, 1024), BF16, 40), [_rand((1024, 2736), BF16, 41 + i) for i in range(2)], torch.empty((4096, 2736), device="cuda", dtype=BF16)
+    torch.cuda.synchronize()
+    torch.cuda.reset_peak_memory_stats()
+    before = torch.cuda.memory_allocated()
+    pd.pd_gated_forward(x, *w, h)
+    assert torch.cuda.max_memory_allocated() == before
