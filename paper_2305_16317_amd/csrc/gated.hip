@@ -998,6 +998,15 @@ void launch_product(Product& p, float* partial, hipStream_t s) {
     PD_HIP(hipGetLastError());
 }
 
+// A call's products: f(rows, columns, apart, groups, sum, segments, across) of each.
+template <class F>
+void each_product(const pd_gated_desc& d, bool backward, F f) {
+    const int parts = parts_of(d.dtype), segs = segments(backward ? slope_parts(d.dtype) : parts, parts);
+    if (!backward) return f(d.rows, d.hidden, true, 1, d.width, segs, false);
+    f(d.rows, d.width, false, 1, d.hidden, 2 * segs, false);
+    if (d.weight_layout == PD_WEIGHTS_IN_OUT) f(d.width, d.hidden, true, 1, d.rows, segs, true);
+    else f(d.hidden, d.width, false, 2, d.rows, segs, true);
+}
 // Scratch of a call: operands laid out, then the products' partial sums.
 struct Layout {
     int64_t x, w, slopes, partial, total;    // bytes, each at a multiple of 256
@@ -1011,24 +1020,17 @@ Layout layout(const pd_gated_desc& d, bool backward) {
         at += up_to(bytes, 256);
         return here;
     };
-    const int parts = parts_of(d.dtype), slopes = slope_parts(d.dtype), segs = segments(backward ? slopes : parts, parts);
+    const int parts = parts_of(d.dtype);
     // (no room for operands that are read where they are)
     if (!(d.aligned && inputs_lie(d))) l.x = take(layout_bytes(parts, d.rows, d.width));
     if (!(d.aligned && weights_lie(d, backward == in_out)))
         l.w = take(2 * (in_out ? layout_bytes(parts, d.width, d.hidden) : layout_bytes(parts, d.hidden, d.width)));
+    if (backward) l.slopes = take(2 * layout_bytes(slope_parts(d.dtype), d.rows, d.hidden));
     int64_t partial = 0;
-    const auto more = [&](int64_t m, int64_t n, bool apart, int groups, int64_t k, int segs, bool across) {
+    each_product(d, backward, [&](int64_t m, int64_t n, bool apart, int groups, int64_t k, int segs, bool across) {
         const int64_t b = partial_bytes(cut(m, n, apart, groups, k, segs, across), m, n, apart, groups);
         partial = b > partial ? b : partial;
-    };
-    if (!backward) {
-        more(d.rows, d.hidden, true, 1, d.width, segs, false);
-    } else {
-        l.slopes = take(2 * layout_bytes(slopes, d.rows, d.hidden));
-        more(d.rows, d.width, false, 1, d.hidden, 2 * segs, false);
-        if (in_out) more(d.width, d.hidden, true, 1, d.rows, segs, true);
-        else more(d.hidden, d.width, false, 2, d.rows, segs, true);
-    }
+    });
     l.partial = take(partial);
     l.total = at;
     return l;
@@ -1174,6 +1176,17 @@ void gated_grad_t(const GatedArgs& a, hipStream_t s) {
 
 int64_t gated_scratch_bytes(const pd_gated_desc& d) { return few(d) ? 0 : layout(d, false).total; }
 void launch_gated(const GatedArgs& a, hipStream_t s) { a.d.dtype == PD_F32 ? gated_t<float>(a, s) : gated_t<bf16>(a, s); }
+int gated_forms(const pd_gated_desc& d, bool backward, int* out) {
+    if (d.rows == 0 || (!backward && few(d))) return 0;
+    int count = 0;
+    each_product(d, backward, [&](int64_t m, int64_t n, bool apart, int groups, int64_t k, int segs, bool across) {
+        const Cut c = cut(m, n, apart, groups, k, segs, across);
+        const int values[4] = {c.shape, c.splits, c.tiles_m * c.tiles_n * groups * c.splits, kCost[c.shape].slots};
+        for (int v : values) *out++ = v;
+        ++count;
+    });
+    return count;
+}
 int64_t gated_grad_scratch_bytes(const pd_gated_desc& d) { return d.rows ? layout(d, true).total : 0; }
 void launch_gated_grad(const GatedArgs& a, hipStream_t s) { a.d.dtype == PD_F32 ? gated_grad_t<float>(a, s) : gated_grad_t<bf16>(a, s); }
 

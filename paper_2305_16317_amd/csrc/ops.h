@@ -203,6 +203,9 @@ struct GatedArgs {
 int64_t gated_scratch_bytes(const pd_gated_desc& d);
 void launch_gated(const GatedArgs& a, hipStream_t s);
 int64_t gated_grad_scratch_bytes(const pd_gated_desc& d);
+// How a call's products are cut, four numbers each: the form (256, 192, 128 by 256, 128 by 128, 32 by 256), parts of
+// the sum, tiles, blocks at once; returns how many products there are.  For tests, which reach all of them.
+int gated_forms(const pd_gated_desc& d, bool backward, int* out);
 void launch_gated_grad(const GatedArgs& a, hipStream_t s);
 
 }  // namespace pd
