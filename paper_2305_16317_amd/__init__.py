@@ -933,14 +933,6 @@ def _weights(w_gate: torch.Tensor, w_up: torch.Tensor, width: int, dtype):
     raise ValueError("w_gate and w_up must both have contiguous rows, or both contiguous columns")
 
 
-def _whole_units(*tensors: torch.Tensor) -> bool:
-    """Whether all begin at multiples of 16 bytes (torch's own allocations do)."""
-    at = 0
-    for t in tensors:
-        at |= t.data_ptr()
-    return at % 16 == 0
-
-
 def _like_weight(w: Optional[torch.Tensor], layout: int, shape, dtype, what: str) -> int:
     """Stride of a weight's gradient, which lies as the weights do."""
     if w is None:
@@ -975,11 +967,12 @@ def pd_gated_forward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, 
         else:
             _written(out, what)
             strides.append(_rows_of(out, hs, t, what))
-    d = _pack(_GATED_BYTES, x.numel() // width, width, hidden, dt, activation, layout, _whole_units(x, w_gate, w_up),
+    px, pg, pu = x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr()
+    d = _pack(_GATED_BYTES, x.numel() // width, width, hidden, dt, activation, layout, (px | pg | pu) % 16 == 0,
               _rows_of(x, sh, t, "x"), gs, us, *strides, 0, 0, 0, 0)
     L = load()
     buf, have = _scratch(scratch, _scratch_need("pd_gated_forward_scratch", d) if scratch is None else 0, stream)
-    _check(L.pd_gated_forward(d, _ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(gate), _ptr(up), _ptr(h), _ptr(buf), have,
+    _check(L.pd_gated_forward(d, px, pg, pu, _ptr(gate), _ptr(up), _ptr(h), _ptr(buf), have,
                               _stream(stream)))
 
 
@@ -1003,14 +996,15 @@ def pd_gated_backward(dh: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, w
         if t is not None:
             _written(t, what)
     of = lambda t, shape, what: 0 if t is None else _rows_of(t, shape, x.dtype, what)  # noqa: E731
-    d = _pack(_GATED_BYTES, x.numel() // width, width, hidden, dt, activation, layout, _whole_units(x, w_gate, w_up),
+    px, pg, pu = x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr()
+    d = _pack(_GATED_BYTES, x.numel() // width, width, hidden, dt, activation, layout, (px | pg | pu) % 16 == 0,
               _rows_of(x, sh, x.dtype, "x"), gs, us,
               of(gate, hs, "gate"), of(up, hs, "up"), of(h, hs, "h"), of(dh, hs, "dh"), of(dx, sh, "dx"),
               _like_weight(dw_gate, layout, ws, x.dtype, "dw_gate"), _like_weight(dw_up, layout, ws, x.dtype, "dw_up"))
     L = load()
     needs = scratch is None and (dx is not None or dw_gate is not None)
     buf, have = _scratch(scratch, _scratch_need("pd_gated_backward_scratch", d) if needs else 0, stream)
-    _check(L.pd_gated_backward(d, _ptr(x), _ptr(w_gate), _ptr(w_up), _ptr(gate), _ptr(up), _ptr(dh), _ptr(h), _ptr(dx),
+    _check(L.pd_gated_backward(d, px, pg, pu, _ptr(gate), _ptr(up), _ptr(dh), _ptr(h), _ptr(dx),
                                _ptr(dw_gate), _ptr(dw_up), _ptr(buf), have, _stream(stream)))
 
 
