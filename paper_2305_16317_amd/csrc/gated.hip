@@ -7,7 +7,8 @@
 // and twice HN columns, the two halves being gate and up, or neighbours of one matrix.
 // Operands are read as they lie, along the sum (units of a row are fragments) or across
 // it (transposing LDS reads).  float32 operands are split into three bfloat16 parts first,
-// and the six products of parts that count are six segments of the sum, small ones first.
+// and the six products of parts that count are six segments of the sum, small ones first;
+// dg and du of bfloat16 are two parts, and their products two segments.
 // Operands that copies of 16 bytes cannot read (alignment, odd sizes) are laid out first.
 // Few rows forward (up to 64 or 128) go to a kernel of their own (k_gated_few).
 //
@@ -23,8 +24,8 @@
 // library product reaches 1228), where a tile has 64 steps; 36864 x 1024 x 4096 580 us (1065;
 // the library's product of x with both weights side by side, without the rest, 552), where it
 // has 16 and results take a quarter of a tile; with gelu 630.  Matrix units busy 44% of the
-// cycles there, vector units 29, no bank conflicts.  Gradients of 9216 x 1024 x 2736 273 us (758),
-// of which dgate and dup 39 (6.4 TB/s); float32 4096 x 1024 x 2736 272 us (169; the library's
+// cycles there, vector units 29, no bank conflicts.  Gradients of 9216 x 1024 x 2736 534 to 556 us
+// (372 to 387, and twice that executed, as dgate and dup have two parts), of which dgate and dup 55 (6.4 TB/s); float32 4096 x 1024 x 2736 272 us (169; the library's
 // float32 products 154).
 #include "attention_tile.h"
 
@@ -853,7 +854,7 @@ struct Matrix {
 constexpr int parts_of(int dtype) { return dtype == PD_F32 ? 3 : 1; }
 // Parts of dg and du.  In bfloat16 two: one would add as much to a gradient's error as the
 // rounding of the result does (1.41 times it together, with few rows up to 1.8 times), for half
-// of the products.
+// of the products (9216 x 1024 x 2736: 282 and 534 us).
 constexpr int slope_parts(int dtype) { return dtype == PD_F32 ? 3 : 2; }
 int64_t layout_bytes(int parts, int64_t rows, int64_t cols) { return rows * up_to(cols, 64) * 2 * parts; }
 // Copies of 16 bytes read the matrix as it lies, if it begins at a multiple of them.

@@ -13,7 +13,7 @@
 // launch.
 //
 // Measured: 16381 tokens of 32 + 8 heads of 128 bfloat16 values, 96 of them turned, pairs
-// side by side, 73 us (4.7 TB/s; a large copy reaches 4.8 to 5.0); 16384 tokens of a video's
+// side by side, 70 to 72 us (4.7 TB/s; a large copy reaches 4.8 to 5.0); 16384 tokens of a video's
 // three axes in turn, 32 + 8 heads of 128, 70 us (4.8 TB/s; with one head's values at a time,
 // read after the table, 86).
 #include "ops.h"
