@@ -574,8 +574,9 @@ pd_status pd_dropout_apply(const pd_dropout_desc* desc, const void* x, const voi
  * pair dw_gate and dw_up, and h (act(gate) up, formed again) may be NULL: not formed.
  * In PD_F32 operands are the sums of three bfloat16 parts (24 bits; a value under 2^-110
  * keeps fewer) with products to 2^-24, as in attention (forward passes of few rows multiply in
- * float32); an infinity among them gives what the formula gives.  In PD_BF16 dgate and dup are operands of two bfloat16
- * parts (to 2^-16), so that a gradient is rounded once.  Sums are float32.  relu'(0) = 0.
+ * float32); an infinity among them gives what the formula gives.  In PD_BF16 dgate and dup are
+ * operands of two bfloat16 parts (to 2^-16), so that a gradient is rounded once.  Sums are float32.
+ * relu'(0) = 0.
  * aligned, not 0: x, w_gate and w_up begin at multiples of 16 bytes (else PD_ERR_INVALID_ARG).  The
  * scratch then has no room for those that are read where they are: in PD_BF16 with rows of a multiple
  * of 8 values, a multiple of 8 values apart, most are.
